@@ -24,6 +24,8 @@ SYMBOLS = (
     "optorch_seq_step_encoded", "optorch_seq_predict_encoded", "optorch_seq_plan_info", "optorch_seq_step_static", "optorch_seq_debug_unit_output",
     "optorch_encoded_words", "optorch_encode", "optorch_decode", "optorch_decode_normalized", "optorch_encode_lossless",
     "optorch_decode_lossless", "optorch_dataflow_last_error",
+    "optorch_linear_workspace", "optorch_linear_forward", "optorch_linear_backward", "optorch_ortho_create", "optorch_ortho_query",
+    "optorch_ortho_bind", "optorch_orthogonalize", "optorch_muon_update", "optorch_ortho_destroy", "optorch_matrix_last_error",
 )
 
 KERNEL_CLASSES = ("cast_in", "conv_fwd", "conv_dgrad", "conv_wgrad", "bn_stats", "bn_apply", "bn_bwd", "pool", "head",
@@ -44,6 +46,31 @@ class optorch_seq_config_t(C.Structure):
         ("loss_scale_init", C.c_float), ("scale_growth", C.c_float), ("scale_backoff", C.c_float),
         ("growth_interval", C.c_int32), ("storage_mode", C.c_int32),
     ]
+
+
+class optorch_linear_t(C.Structure):
+    _fields_ = [("precision", C.c_int32), ("activation", C.c_int32), ("rows", C.c_int64), ("in_features", C.c_int32),
+                ("out_features", C.c_int32)]
+    for _n in ("x", "w", "bias", "residual", "y", "z", "dy", "dx", "dw"):
+        _fields_.append((_n, C.c_void_p))
+        if _n != "bias":
+            _fields_.append(({"residual": "ldr"}.get(_n, "ld" + _n), C.c_int64))
+    _fields_ += [("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("hip_stream", C.c_void_p)]
+
+
+class optorch_matrix_t(C.Structure):
+    _fields_ = [("offset", C.c_int64), ("rows", C.c_int32), ("cols", C.c_int32), ("ld", C.c_int64)]
+
+
+class optorch_ortho_config_t(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("coefficients", C.POINTER(C.c_float)), ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class optorch_muon_t(C.Structure):
+    _fields_ = [("g_precision", C.c_int32), ("g", C.c_void_p), ("w", C.c_void_p), ("v", C.c_void_p),
+                ("w16_precision", C.c_int32), ("w16", C.c_void_p), ("lr", C.c_float), ("momentum", C.c_float),
+                ("weight_decay", C.c_float), ("grad_scale", C.c_float), ("nesterov", C.c_int32), ("scale_mode", C.c_int32),
+                ("skipped", C.c_void_p)]
 
 
 _lib = None
@@ -100,6 +127,27 @@ def load_library() -> C.CDLL:
     lib.optorch_decode_lossless.restype = C.c_int
     lib.optorch_dataflow_last_error.argtypes = []
     lib.optorch_dataflow_last_error.restype = C.c_char_p
+    L = C.POINTER(optorch_linear_t)
+    lib.optorch_linear_workspace.argtypes = [L, C.c_int32]
+    lib.optorch_linear_workspace.restype = C.c_int64
+    lib.optorch_linear_forward.argtypes = [L]
+    lib.optorch_linear_forward.restype = C.c_int
+    lib.optorch_linear_backward.argtypes = [L]
+    lib.optorch_linear_backward.restype = C.c_int
+    lib.optorch_ortho_create.argtypes = [C.POINTER(optorch_matrix_t), C.c_int32, C.POINTER(optorch_ortho_config_t), C.POINTER(H)]
+    lib.optorch_ortho_create.restype = C.c_int
+    lib.optorch_ortho_query.argtypes = [H, C.POINTER(C.c_uint64), C.POINTER(C.c_int64)]
+    lib.optorch_ortho_query.restype = C.c_int
+    lib.optorch_ortho_bind.argtypes = [H, C.c_void_p, C.c_uint64]
+    lib.optorch_ortho_bind.restype = C.c_int
+    lib.optorch_orthogonalize.argtypes = [H, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+    lib.optorch_orthogonalize.restype = C.c_int
+    lib.optorch_muon_update.argtypes = [H, C.POINTER(optorch_muon_t), C.c_void_p]
+    lib.optorch_muon_update.restype = C.c_int
+    lib.optorch_ortho_destroy.argtypes = [H]
+    lib.optorch_ortho_destroy.restype = None
+    lib.optorch_matrix_last_error.argtypes = []
+    lib.optorch_matrix_last_error.restype = C.c_char_p
     lib.optorch_seq_predict.argtypes = [H, C.c_void_p, C.c_void_p]
     lib.optorch_seq_predict.restype = C.c_int
     lib.optorch_seq_running_stats.argtypes = [H, C.c_void_p, C.c_uint64, C.POINTER(C.c_uint64), C.c_int32]
@@ -474,3 +522,247 @@ def decode_lossless(a, o, batch: int, n_pos: int, z: int):
     out = torch.empty((batch, n_pos), dtype=torch.uint8, device=a.device)
     _df_check(load_library().optorch_decode_lossless(a.data_ptr(), o.data_ptr(), batch, n_pos, z, out.data_ptr(), _stream(torch)))
     return out
+
+
+# ---- matrix operators (optorch_matrix.h): tensors and workspaces allocated through torch, kernels on torch's current stream ----
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+SCALE_MODES = {"none": 0, "aspect": 1, "rms": 2}
+_PRECISION = {}  # torch dtype -> optorch_precision_t, filled on first use (torch is imported lazily)
+
+
+def _precision(dtype) -> int:
+    if not _PRECISION:
+        import torch
+        _PRECISION.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    try:
+        return _PRECISION[dtype]
+    except KeyError:
+        raise TypeError("expected a float32, bfloat16 or float16 tensor, got %s" % dtype) from None
+
+
+def _mat_fail(rc: int):
+    raise OptorchError(rc, (load_library().optorch_matrix_last_error() or b"").decode())
+
+
+def _check_matrix(name, t, rows, cols, like):
+    """A rows x cols matrix of like's type and device whose rows lie one behind the other (any distance)."""
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError("%s: expected a %d x %d matrix, got %s" % (name, rows, cols, tuple(t.shape)))
+    if t.dtype != like.dtype or t.device != like.device:
+        raise TypeError("%s: expected %s on %s, got %s on %s" % (name, like.dtype, like.device, t.dtype, t.device))
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("%s: the elements of a row must lie next to each other" % name)
+
+
+def _ld(t):
+    """Distance of a matrix' rows.  (One row or none: torch's stride says nothing.)"""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _check_vector(name, t, n, like):
+    import torch
+    if t.dtype != torch.float32 or t.device != like.device:
+        raise TypeError("%s: expected float32 on %s, got %s on %s" % (name, like.device, t.dtype, t.device))
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: expected %d contiguous values" % (name, n))
+
+
+def _linear_args(x, activation, rows, cin, cout):
+    if activation not in ACTIVATIONS:
+        raise ValueError("activation must be one of %s" % ", ".join(sorted(ACTIVATIONS)))
+    if not x.is_cuda:
+        raise ValueError("the operands must be on the GPU")
+    a = optorch_linear_t()
+    a.precision, a.activation = _precision(x.dtype), ACTIVATIONS[activation]
+    a.rows, a.in_features, a.out_features = rows, cin, cout
+    return a
+
+
+def _linear_call(lib, fn, a, backward, device):
+    import torch
+    with torch.cuda.device(device):
+        n = lib.optorch_linear_workspace(C.byref(a), backward)
+        if n < 0:
+            _mat_fail(n)
+        if n:
+            ws = torch.empty(n, dtype=torch.uint8, device=device)  # (torch aligns allocations to 512 bytes)
+            a.workspace, a.workspace_bytes = ws.data_ptr(), n
+        a.hip_stream = torch.cuda.current_stream(device).cuda_stream
+        rc = fn(C.byref(a))
+    if rc != OK:
+        _mat_fail(rc)
+
+
+def linear_forward(x, w, bias=None, *, residual=None, activation="none", save_pre=False, out=None):
+    """y = activation(x w^T + bias) + residual: x [rows, in] and w [out, in] in fp32, bf16 or fp16, bias float32 [out],
+    residual [rows, out].  save_pre: also returns z = x w^T + bias, which `linear_backward` reads."""
+    import torch
+    rows, cin = x.shape
+    cout = w.shape[0]
+    a = _linear_args(x, activation, rows, cin, cout)
+    _check_matrix("x", x, rows, cin, x)
+    _check_matrix("w", w, cout, cin, x)
+    a.x, a.ldx, a.w, a.ldw = x.data_ptr(), _ld(x), w.data_ptr(), _ld(w)
+    if bias is not None:
+        _check_vector("bias", bias, cout, x)
+        a.bias = bias.data_ptr()
+    if residual is not None:
+        _check_matrix("residual", residual, rows, cout, x)
+        a.residual, a.ldr = residual.data_ptr(), _ld(residual)
+    if out is None:
+        out = torch.empty((rows, cout), dtype=x.dtype, device=x.device)
+    else:
+        _check_matrix("out", out, rows, cout, x)
+    a.y, a.ldy = out.data_ptr(), _ld(out)
+    z = None
+    if save_pre:
+        z = torch.empty((rows, cout), dtype=x.dtype, device=x.device)
+        a.z, a.ldz = z.data_ptr(), cout
+    lib = load_library()
+    _linear_call(lib, lib.optorch_linear_forward, a, 0, x.device)
+    return (out, z) if save_pre else out
+
+
+def linear_backward(dy, x, w, z=None, *, activation="none", need=("dx", "dw", "dbias")):
+    """The gradients (dx, dw, dbias) of `linear_forward` from dy [rows, out] and what forward was given and saved; those not
+    in `need` are not computed and come back as None.  dbias is float32, the others have x's type."""
+    import torch
+    rows, cin = x.shape
+    cout = w.shape[0]
+    if not need or not set(need) <= {"dx", "dw", "dbias"}:
+        raise ValueError("need must name some of dx, dw, dbias")
+    a = _linear_args(x, activation, rows, cin, cout)
+    _check_matrix("x", x, rows, cin, x)
+    _check_matrix("w", w, cout, cin, x)
+    _check_matrix("dy", dy, rows, cout, x)
+    a.x, a.ldx, a.w, a.ldw, a.dy, a.lddy = x.data_ptr(), _ld(x), w.data_ptr(), _ld(w), dy.data_ptr(), _ld(dy)
+    if activation != "none":
+        if z is None:
+            raise ValueError("z (linear_forward's save_pre) is needed for the slope of %s" % activation)
+        _check_matrix("z", z, rows, cout, x)
+        a.z, a.ldz = z.data_ptr(), _ld(z)
+    dx = dw = dbias = None
+    if "dx" in need:
+        dx = torch.empty((rows, cin), dtype=x.dtype, device=x.device)
+        a.dx, a.lddx = dx.data_ptr(), cin
+    if "dw" in need:
+        dw = torch.empty((cout, cin), dtype=x.dtype, device=x.device)
+        a.dw, a.lddw = dw.data_ptr(), cin
+    if "dbias" in need:
+        dbias = torch.empty(cout, dtype=torch.float32, device=x.device)
+        a.dbias = dbias.data_ptr()
+    lib = load_library()
+    _linear_call(lib, lib.optorch_linear_backward, a, 1, x.device)
+    return dx, dw, dbias
+
+
+class OrthoPlan:
+    """optorch_ortho_create + optorch_ortho_query: the host-side plan for a list of matrices, no device needed.
+
+    matrices: (rows, cols) each, one behind the other in a flat vector, or (offset, rows, cols, ld) for other places.
+    coefficients: (a, b, c) for every step, or one such triple per step."""
+
+    def __init__(self, matrices, *, steps: int = 5, coefficients=None, eps: float = 1e-7):
+        self.lib = load_library()
+        self.handle = C.c_void_p()
+        arr = (optorch_matrix_t * max(1, len(matrices)))()
+        at = 0
+        for i, m in enumerate(matrices):
+            if len(m) == 2:
+                m = (at, m[0], m[1], m[1])
+            arr[i] = optorch_matrix_t(*[int(v) for v in m])
+            at = m[0] + (m[1] - 1) * m[3] + m[2]
+        cfg = optorch_ortho_config_t()
+        cfg.steps, cfg.eps = steps, eps
+        if coefficients is not None:
+            co = list(coefficients)
+            co = [float(v) for c in co for v in c] if hasattr(co[0], "__len__") else [float(v) for v in co] * steps
+            if len(co) != 3 * steps:
+                raise ValueError("expected %d coefficients, got %d" % (3 * steps, len(co)))
+            cfg.coefficients = C.cast((C.c_float * len(co))(*co), C.POINTER(C.c_float))
+        rc = self.lib.optorch_ortho_create(arr, len(matrices), C.byref(cfg), C.byref(self.handle))
+        if rc != OK:
+            self.handle = C.c_void_p()
+            _mat_fail(rc)
+        wb, span = C.c_uint64(), C.c_int64()
+        self._check(self.lib.optorch_ortho_query(self.handle, C.byref(wb), C.byref(span)))
+        self.workspace_bytes, self.span = wb.value, span.value
+
+    def _check(self, rc: int):
+        if rc != OK:
+            _mat_fail(rc)
+
+    def close(self):
+        if getattr(self, "handle", None) and self.handle.value:
+            self.lib.optorch_ortho_destroy(self.handle)
+            self.handle = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Orthogonalizer(OrthoPlan):
+    """A bound plan: workspace allocated through torch, calls on torch's current stream.  Calls of one object share the
+    workspace: on different streams they have to be ordered by the caller."""
+
+    def __init__(self, matrices, *, device="cuda:0", **kw):
+        import torch
+        super().__init__(matrices, **kw)
+        self.torch = torch
+        self.device = torch.device(device)
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU visible: the matrix operators only run on the HIP path")
+        with torch.cuda.device(self.device):
+            self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+            # (the memory may have been another stream's until now)
+            torch.cuda.current_stream(self.device).synchronize()
+            self._check(self.lib.optorch_ortho_bind(self.handle, self.workspace.data_ptr(), self.workspace_bytes))
+
+    def _flat(self, name, t, dtypes=None):
+        if not t.is_cuda or t.device.index != (self.device.index or 0):
+            raise TypeError("%s: expected a tensor on %s" % (name, self.device))
+        if not t.is_contiguous() or t.numel() < self.span:
+            raise ValueError("%s: expected at least %d contiguous elements" % (name, self.span))
+        p = _precision(t.dtype)
+        if dtypes is not None and p not in dtypes:
+            raise TypeError("%s: unexpected type %s" % (name, t.dtype))
+        return p
+
+    def _stream(self):
+        return self.torch.cuda.current_stream(self.device).cuda_stream
+
+    def orthogonalize(self, g, out=None):
+        """Newton-Schulz steps on every matrix of the flat tensor g, into out (g's type by default)."""
+        if out is None:
+            out = self.torch.empty_like(g)
+        gp, op = self._flat("g", g), self._flat("out", out)
+        with self.torch.cuda.device(self.device):
+            self._check(self.lib.optorch_orthogonalize(self.handle, gp, g.data_ptr(), op, out.data_ptr(), self._stream()))
+        return out
+
+    def muon_update(self, w, v, g, *, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale="aspect", grad_scale=1.0,
+                    weights16=None, skipped=None):
+        """One update of all matrices in place (optorch_muon_update): float32 weights w and momentum v, gradients g, all flat;
+        weights16: a bf16 or fp16 copy of w that is refreshed; skipped: cuda int32 tensor of one element, set to 1 if the
+        update was skipped because of a gradient that is not finite, else 0."""
+        a = optorch_muon_t()
+        a.g_precision = self._flat("g", g)
+        self._flat("w", w, (0,))
+        self._flat("v", v, (0,))
+        a.g, a.w, a.v = g.data_ptr(), w.data_ptr(), v.data_ptr()
+        if weights16 is not None:
+            a.w16_precision, a.w16 = self._flat("weights16", weights16, (1, 2)), weights16.data_ptr()
+        if scale not in SCALE_MODES:
+            raise ValueError("scale must be one of %s" % ", ".join(sorted(SCALE_MODES)))
+        a.lr, a.momentum, a.weight_decay, a.grad_scale = lr, momentum, weight_decay, grad_scale
+        a.nesterov, a.scale_mode = int(nesterov), SCALE_MODES[scale]
+        if skipped is not None:
+            if skipped.dtype != self.torch.int32 or skipped.numel() != 1 or not skipped.is_cuda:
+                raise TypeError("skipped: expected one int32 on the GPU")
+            a.skipped = skipped.data_ptr()
+        with self.torch.cuda.device(self.device):
+            self._check(self.lib.optorch_muon_update(self.handle, C.byref(a), self._stream()))

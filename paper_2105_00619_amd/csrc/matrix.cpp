@@ -1,0 +1,104 @@
+// C ABI of the matrix operators (optorch_matrix.h): argument checks, then the kernels of k_linear.hip and k_ortho.hip on the
+// caller's stream.  Nothing here allocates on the device; only optorch_ortho_bind synchronises.
+#include <hip/hip_runtime.h>
+
+#include <string>
+
+#include "matrix.h"
+
+using namespace oseq;
+
+static thread_local std::string g_mat_error;
+
+int oseq_mat_err(int code, const std::string& m);
+int oseq_mat_err(int code, const std::string& m) {
+  try { g_mat_error = m; } catch (...) {}
+  return code;
+}
+
+// every entry runs inside this: no C++ exception (host memory running out) leaves the library
+template <class F> static auto guarded(F&& f) -> decltype(f()) {
+  try { return f(); } catch (...) { return oseq_mat_err(OPTORCH_E_INVALID, "out of host memory"); }
+}
+
+static int mat_launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return oseq_mat_err(OPTORCH_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
+  return OPTORCH_OK;
+}
+
+extern "C" const char* optorch_matrix_last_error(void) { return g_mat_error.c_str(); }
+
+static bool precision_ok(int32_t p) { return p == OPTORCH_FP32 || p == OPTORCH_BF16 || p == OPTORCH_FP16; }
+static int bytes_of(int32_t p) { return p == OPTORCH_FP32 ? 4 : 2; }
+
+// ---- linear layers -----------------------------------------------------------------------------------------------------
+
+static constexpr int64_t kMaxFeatures = (1 << 22) - 8;  // offsets inside a tile are 32-bit
+
+static int linear_check(const optorch_linear_t* a, bool backward) {
+  if (!a) return oseq_mat_err(OPTORCH_E_INVALID, "null arguments");
+  if (!precision_ok(a->precision)) return oseq_mat_err(OPTORCH_E_INVALID, "unknown precision");
+  if (a->activation < OPTORCH_ACT_NONE || a->activation > OPTORCH_ACT_SILU) return oseq_mat_err(OPTORCH_E_INVALID, "unknown activation");
+  if (a->rows < 0 || a->rows > 0x7fffff00) return oseq_mat_err(OPTORCH_E_INVALID, "rows must be 0 .. 2^31 - 256");
+  if (a->in_features < 1 || a->out_features < 1 || a->in_features > kMaxFeatures || a->out_features > kMaxFeatures)
+    return oseq_mat_err(OPTORCH_E_INVALID, "in_features and out_features must be 1 .. 2^22 - 8");
+  const int esize = bytes_of(a->precision);
+  // a matrix that is used: present, its rows apart, its elements aligned
+  auto matrix = [&](const void* p, int64_t ld, int32_t cols, const char* name) {
+    if (!p) return oseq_mat_err(OPTORCH_E_INVALID, std::string("null ") + name);
+    if (ld < cols || ld > kMaxFeatures) return oseq_mat_err(OPTORCH_E_INVALID, std::string("leading dimension of ") + name + " must be its columns .. 2^22 - 8");
+    if ((uintptr_t)p % esize) return oseq_mat_err(OPTORCH_E_INVALID, std::string(name) + " is not aligned to its elements");
+    return (int)OPTORCH_OK;
+  };
+  auto vector = [&](const float* p, const char* name) {
+    return (uintptr_t)p % 4 ? oseq_mat_err(OPTORCH_E_INVALID, std::string(name) + " is not aligned to its elements") : (int)OPTORCH_OK;
+  };
+  int rc = OPTORCH_OK;
+  const int32_t in = a->in_features, out = a->out_features;
+  const bool some = a->rows > 0;  // (an empty batch has no matrices of its own)
+  if (!backward) {
+    if (some && rc == OPTORCH_OK) rc = matrix(a->x, a->ldx, in, "x");
+    if (rc == OPTORCH_OK) rc = matrix(a->w, a->ldw, in, "w");
+    if (some && rc == OPTORCH_OK) rc = matrix(a->y, a->ldy, out, "y");
+    if (some && rc == OPTORCH_OK && a->residual) rc = matrix(a->residual, a->ldr, out, "residual");
+    if (some && rc == OPTORCH_OK && a->z) rc = matrix(a->z, a->ldz, out, "z");
+    if (rc == OPTORCH_OK) rc = vector(a->bias, "bias");
+    return rc;
+  }
+  if (!a->dx && !a->dw && !a->dbias) return oseq_mat_err(OPTORCH_E_INVALID, "no gradient asked for");
+  if (some && rc == OPTORCH_OK) rc = matrix(a->dy, a->lddy, out, "dy");
+  if (some && rc == OPTORCH_OK && a->activation != OPTORCH_ACT_NONE) rc = matrix(a->z, a->ldz, out, "z");
+  if (some && rc == OPTORCH_OK && a->dw) rc = matrix(a->x, a->ldx, in, "x");
+  if (rc == OPTORCH_OK && a->dw) rc = matrix(a->dw, a->lddw, in, "dw");
+  if (some && rc == OPTORCH_OK && a->dx) rc = matrix(a->w, a->ldw, in, "w");
+  if (some && rc == OPTORCH_OK && a->dx) rc = matrix(a->dx, a->lddx, in, "dx");
+  if (rc == OPTORCH_OK) rc = vector(a->dbias, "dbias");
+  return rc;
+}
+
+extern "C" int64_t optorch_linear_workspace(const optorch_linear_t* a, int32_t backward) {
+  return guarded([&]() -> int64_t {
+    const int rc = linear_check(a, backward != 0);
+    if (rc != OPTORCH_OK) return rc;
+    return a->rows ? (int64_t)plan_linear(*a, backward != 0).bytes : 0;
+  });
+}
+
+static int linear_run(const optorch_linear_t* a, bool backward) {
+  const int rc = linear_check(a, backward);
+  if (rc != OPTORCH_OK) return rc;
+  LinearPlan p = {};
+  if (a->rows) {
+    p = plan_linear(*a, backward);
+    if (p.bytes && !a->workspace) return oseq_mat_err(OPTORCH_E_INVALID, "null workspace");
+    if (p.bytes > a->workspace_bytes) return oseq_mat_err(OPTORCH_E_BUDGET, "workspace too small: " + std::to_string(p.bytes) + " bytes are needed");
+    if (p.bytes && (uintptr_t)a->workspace % 256) return oseq_mat_err(OPTORCH_E_INVALID, "workspace must be 256-byte aligned");
+  }
+  if (!backward && a->rows) launch_linear_forward(*a, p);
+  if (backward) launch_linear_backward(*a, p);
+  return mat_launched(backward ? "linear_backward" : "linear_forward");
+}
+
+extern "C" int optorch_linear_forward(const optorch_linear_t* a) { return guarded([&] { return linear_run(a, false); }); }
+extern "C" int optorch_linear_backward(const optorch_linear_t* a) { return guarded([&] { return linear_run(a, true); }); }
