@@ -65,7 +65,9 @@ __device__ __forceinline__ void planes_of(float x, bf16_t (&p)[3]) {
   p[2] = (bf16_t)(x - (float)p[1]);
 }
 
-template <int PL, class T> __device__ __forceinline__ void store_planes8(T* p, int64_t plane, const float (&v)[8]) {
+// eight neighbouring columns from c on, laid out as the products want them (mat_core.h)
+template <int PL, class T> __device__ __forceinline__ void store_planes8(T* row, int c, const float (&v)[8]) {
+  T* p = row + place_of<PL>(c);
   if (PL == 1) {
     store_f32<T, 8>(p, v);
   } else {
@@ -78,21 +80,21 @@ template <int PL, class T> __device__ __forceinline__ void store_planes8(T* p, i
       for (int k = 0; k < 3; ++k) q[k].v[e] = t[k];
     }
 #pragma unroll
-    for (int k = 0; k < 3; ++k) *reinterpret_cast<Vec<bf16_t, 8>*>(p + k * plane) = q[k];
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<Vec<bf16_t, 8>*>(p + k * 16) = q[k];
   }
 }
 
-// S: type in memory; T: type of the planes.  Columns are filled up to a multiple of eight with zeros.
+// S: type in memory; T: type of the planes.  Columns are filled up to whole blocks (block_of) with zeros.
 template <class S, class T, int PL>
 __global__ void __launch_bounds__(256) pack_kernel(const S* __restrict__ src, int64_t ld, int64_t rows, int cols, bool wide, T* __restrict__ dst) {
-  const int c8 = (cols + 7) / 8;
+  const int c8 = (cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
   const int64_t n = rows * c8;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / c8;
     const int c = (int)(i - r * c8) * 8;
     float v[8];
     load8<S>(src + r * ld + c, min(8, cols - c), wide, v);
-    store_planes8<PL, T>(dst + i * 8, n * 8, v);
+    store_planes8<PL, T>(dst + r * c8 * (8 * span_of(PL)), c, v);
   }
 }
 
@@ -101,18 +103,18 @@ struct DzArgs {
   const void* dy; int64_t lddy; const void* z; int64_t ldz;
   int64_t rows; int cols, rows_per_block;
   bool wide_dy, wide_z, write;
-  void* dz;       // planes of rows x up8(cols)
+  void* dz;       // laid out as the products want it
   float* sums;    // [row blocks][cols], or null
 };
 template <class S, class T, int PL, int ACT>
 __global__ void __launch_bounds__(256) dz_kernel(DzArgs a) {
   __shared__ float part[8][256 + 8];
   const int cg = threadIdx.x & 31, rl = threadIdx.x >> 5, c = blockIdx.x * 256 + cg * 8;
-  const int cols8 = (a.cols + 7) & ~7;
+  const int padded = (a.cols + block_of(PL) - 1) / block_of(PL) * block_of(PL);
   const int64_t r0 = (int64_t)blockIdx.y * a.rows_per_block, r1 = min(a.rows, r0 + a.rows_per_block);
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const int n = min(8, a.cols - c);
-  if (n > 0)
+  if (c < padded)
     for (int64_t r = r0 + rl; r < r1; r += 8) {
       float v[8], z[8];
       load8<S>((const S*)a.dy + r * a.lddy + c, n, a.wide_dy, v);
@@ -126,7 +128,7 @@ __global__ void __launch_bounds__(256) dz_kernel(DzArgs a) {
         if (e >= n) v[e] = 0.f;
         sum[e] += v[e];
       }
-      if (a.write) store_planes8<PL, T>((T*)a.dz + r * cols8 + c, a.rows * cols8, v);
+      if (a.write) store_planes8<PL, T>((T*)a.dz + r * padded * span_of(PL), c, v);
     }
   if (!a.sums) return;
 #pragma unroll
@@ -160,11 +162,10 @@ __global__ void __launch_bounds__(256) dbias_kernel(const float* __restrict__ su
 
 // ---- the products ------------------------------------------------------------------------------------------------------
 struct ProductArgs {
-  const void* a; int64_t a_plane; int lda;  // planes of the operands, mat_core.h
-  const void* b; int64_t b_plane; int ldb;
-  Planes planes;
+  const void* a; int lda;  // the operands, mat_core.h
+  const void* b; int ldb;
   int64_t M;
-  int N, K;           // K: up to the operands' zero padding where they are along it
+  int N, K;
   int tiles_m, tiles_n, parts, k_part;
   float* partial;     // parts > 1: [parts][M][up8(N)] sums
   // what becomes of a sum
@@ -196,11 +197,11 @@ __device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int co
   store8<O>((O*)a.out + row * a.ldo + col, n, a.wide_out, v);
 }
 
-// The value at (r, k) of an operand of planes
-template <bool R> __device__ __forceinline__ float value_of(const bf16_t* p, int64_t plane, int64_t ld, int64_t r, int64_t k) {
-  p += R ? k * ld + r : r * ld + k;
+// The value at (r, k) of an operand of three planes
+template <bool R> __device__ __forceinline__ float value_of(const bf16_t* p, int64_t ld, int64_t r, int64_t k) {
+  p += R ? k * ld + place_of<3>(r) : r * ld + place_of<3>(k);
   const float hi = (float)p[0];
-  return fabsf(hi) <= 3.4028235e38f ? (hi + (float)p[plane]) + (float)p[2 * plane] : hi;
+  return fabsf(hi) <= 3.4028235e38f ? (hi + (float)p[16]) + (float)p[32] : hi;
 }
 
 // An infinity among the operands makes sums of planes NaN (infinity times a plane of zero): such a sum is made again, one product
@@ -209,7 +210,7 @@ template <bool AR, bool BR>
 __device__ __forceinline__ float sum_again(const ProductArgs& a, int64_t m, int n, int k0, int k1) {
   float s = 0.f;
   for (int k = k0; k < k1; ++k)
-    s = fmaf(value_of<AR>((const bf16_t*)a.a, a.a_plane, a.lda, m, k), value_of<BR>((const bf16_t*)a.b, a.b_plane, a.ldb, n, k), s);
+    s = fmaf(value_of<AR>((const bf16_t*)a.a, a.lda, m, k), value_of<BR>((const bf16_t*)a.b, a.ldb, n, k), s);
   return s;
 }
 
@@ -217,7 +218,8 @@ __device__ __forceinline__ float sum_again(const ProductArgs& a, int64_t m, int 
 template <class O, class T, int W, bool AR, bool BR, int ACT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
 product_kernel(ProductArgs a) {
-  typedef Tile<T, W, W, AR, BR> G;
+  constexpr int PL = sizeof(O) == 4 ? 3 : 1;
+  typedef Tile<T, PL, W, AR, BR> G;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   // neighbouring tiles on one XCD: each of the eight takes a run of them, eight rows of tiles at a time
   const int total = a.tiles_m * a.tiles_n * a.parts;
@@ -226,17 +228,17 @@ product_kernel(ProductArgs a) {
   const int tiles = a.tiles_m * a.tiles_n, part = id / tiles, t = id - part * tiles;
   const int band = t / (8 * a.tiles_n), rows_in = min(8, a.tiles_m - band * 8), u = t - band * 8 * a.tiles_n;
   const int tn = u / rows_in, tm = band * 8 + u - tn * rows_in;
-  const int64_t m0 = (int64_t)tm * G::BM;
-  const int n0 = tn * G::BN;
-  const int rows = (int)min<int64_t>(G::BM, a.M - m0), cols = min(G::BN, a.N - n0);
+  const int64_t m0 = (int64_t)tm * G::EDGE;
+  const int n0 = tn * G::EDGE;
+  const int rows = (int)min<int64_t>(G::EDGE, a.M - m0), cols = min(G::EDGE, a.N - n0);
   const int k0 = part * a.k_part, k1 = min(a.K, k0 + a.k_part);
   Operand<T> oa, ob;
-  oa.base = (const T*)a.a + (AR ? (int64_t)k0 * a.lda + m0 : m0 * a.lda + k0);
-  oa.plane = a.a_plane; oa.ld = a.lda; oa.rows = rows;
-  ob.base = (const T*)a.b + (BR ? (int64_t)k0 * a.ldb + n0 : (int64_t)n0 * a.ldb + k0);
-  ob.plane = a.b_plane; ob.ld = a.ldb; ob.rows = cols;
+  oa.base = (const T*)a.a + (AR ? (int64_t)k0 * a.lda + place_of<PL>(m0) : m0 * a.lda + place_of<PL>(k0));
+  oa.ld = a.lda; oa.rows = rows;
+  ob.base = (const T*)a.b + (BR ? (int64_t)k0 * a.ldb + place_of<PL>(n0) : (int64_t)n0 * a.ldb + place_of<PL>(k0));
+  ob.ld = a.ldb; ob.rows = cols;
   typename G::Acc acc;
-  G::product(smem, oa, ob, a.planes, k1 - k0, acc);
+  G::product(smem, oa, ob, k1 - k0, acc);
   const int n8 = (a.N + 7) & ~7;
   auto emit = [&](int r, int c, float (&v)[8], int n) {
     if (a.parts > 1) store_f32<float, 8>(a.partial + ((int64_t)part * a.M + m0 + r) * n8 + n0 + c, v);
@@ -296,7 +298,8 @@ template <class T> __global__ void __launch_bounds__(256) clear_kernel(T* p, int
 int grid_of(int64_t n) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, 4096)); }
 
 template <class O, class T, int W, bool AR, bool BR, int ACT> void run_product_w(hipStream_t st, ProductArgs& a) {
-  typedef Tile<T, W, W, AR, BR> G;
+  constexpr int PL = sizeof(O) == 4 ? 3 : 1;
+  typedef Tile<T, PL, W, AR, BR> G;
   const int per = (a.tiles_m * a.tiles_n * a.parts + 7) / 8;
   auto k = product_kernel<O, T, W, AR, BR, ACT>;
   // (more LDS than a launch gets unasked; set again on every launch: which devices know it is not ours to remember)
@@ -308,7 +311,7 @@ template <class O, class T, int W, bool AR, bool BR, int ACT> void run_product_w
 template <class O, class T, bool AR, bool BR, int ACT> void run_product(hipStream_t st, ProductArgs& a, const ProductShape& s) {
   const int b = 2 * s.wave;
   a.tiles_m = ceil_div(a.M, b); a.tiles_n = ceil_div(a.N, b);
-  a.k_part = (int)(((int64_t)ceil_div(a.K, BK) + s.parts - 1) / s.parts) * BK;
+  a.k_part = (int)(((int64_t)ceil_div(a.K, 64) + s.parts - 1) / s.parts) * 64;
   a.parts = ceil_div(a.K, a.k_part);
   if (s.wave == 128) run_product_w<O, T, 128, AR, BR, ACT>(st, a);
   else if (s.wave == 64) run_product_w<O, T, 64, AR, BR, ACT>(st, a);
@@ -325,7 +328,7 @@ bool direct(const void* p, int64_t ld, int cols) { return aligned16(p) && ld % 8
 // do not.
 ProductShape shape_of(int64_t M, int64_t N, int64_t K) {
   auto tiles = [&](int w) { return (int64_t)ceil_div(M, 2 * w) * ceil_div(N, 2 * w); };
-  const int64_t steps = (K + BK - 1) / BK;
+  const int64_t steps = (K + 63) / 64;
   if (tiles(128) >= 224) return {128, 1};
   if (tiles(64) >= 224) return {64, 1};
   const int w = tiles(32) > 512 ? 64 : 32;
@@ -356,20 +359,21 @@ template <class S, class T, int PL, int ACT> void run_dz(hipStream_t st, const o
     OSEQ_LAUNCH(dbias_kernel, dim3(ceil_div(d.cols, 16)), dim3(256), 0, st, (const float*)d.sums, p.sum_blocks, d.cols, a.dbias);
 }
 
-struct Where { const void* p; int64_t plane; int ld; };
+struct Where { const void* p; int ld; };
+// places of a row of n columns laid out anew
+template <int PL> int row_of(int n) { return (n + block_of(PL) - 1) / block_of(PL) * block_of(PL) * span_of(PL); }
 
 template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, const LinearPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
-  const int64_t k8 = up8(a.in_features);
-  Where x{a.x, 0, (int)a.ldx}, w{a.w, 0, (int)a.ldw};
-  if (p.pack_x) { pack<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x); x = {ws + p.off_x, a.rows * k8, (int)k8}; }
-  if (p.pack_w) { pack<S, T, PL>(st, a.w, a.ldw, a.out_features, a.in_features, ws + p.off_w); w = {ws + p.off_w, a.out_features * k8, (int)k8}; }
+  const int row = row_of<PL>(a.in_features);
+  Where x{a.x, (int)a.ldx}, w{a.w, (int)a.ldw};
+  if (p.pack_x) { pack<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x); x = {ws + p.off_x, row}; }
+  if (p.pack_w) { pack<S, T, PL>(st, a.w, a.ldw, a.out_features, a.in_features, ws + p.off_w); w = {ws + p.off_w, row}; }
   ProductArgs g = {};
-  g.a = x.p; g.a_plane = x.plane; g.lda = x.ld;
-  g.b = w.p; g.b_plane = w.plane; g.ldb = w.ld;
-  g.planes = Planes::of(PL);
-  g.M = a.rows; g.N = a.out_features; g.K = (int)k8;
+  g.a = x.p; g.lda = x.ld;
+  g.b = w.p; g.ldb = w.ld;
+  g.M = a.rows; g.N = a.out_features; g.K = (int)up8(a.in_features);  // (up to the zeros behind a row)
   g.partial = (float*)(ws + p.off_parts);
   g.bias = a.bias;
   g.residual = a.residual; g.ldr = a.ldr; g.wide_r = a.residual && wide(a.residual, a.ldr, sizeof(S));
@@ -386,29 +390,28 @@ template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, c
 template <class S, class T, int PL> void backward_of(const optorch_linear_t& a, const LinearPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
-  const int64_t in8 = up8(a.in_features), out8 = up8(a.out_features);
+  const int row = row_of<PL>(a.in_features);
   if (p.make_dz || a.dbias) switch (a.activation) {
     case OPTORCH_ACT_NONE: run_dz<S, T, PL, OPTORCH_ACT_NONE>(st, a, p); break;
     case OPTORCH_ACT_RELU: run_dz<S, T, PL, OPTORCH_ACT_RELU>(st, a, p); break;
     case OPTORCH_ACT_GELU: run_dz<S, T, PL, OPTORCH_ACT_GELU>(st, a, p); break;
     default: run_dz<S, T, PL, OPTORCH_ACT_SILU>(st, a, p);
   }
-  Where dz{a.dy, 0, (int)a.lddy}, x{a.x, 0, (int)a.ldx}, w{a.w, 0, (int)a.ldw};
-  if (p.make_dz) dz = {ws + p.off_dz, a.rows * out8, (int)out8};
-  if (p.pack_x) { pack<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x); x = {ws + p.off_x, a.rows * in8, (int)in8}; }
-  if (p.pack_w) { pack<S, T, PL>(st, a.w, a.ldw, a.out_features, a.in_features, ws + p.off_w); w = {ws + p.off_w, a.out_features * in8, (int)in8}; }
+  Where dz{a.dy, (int)a.lddy}, x{a.x, (int)a.ldx}, w{a.w, (int)a.ldw};
+  if (p.make_dz) dz = {ws + p.off_dz, row_of<PL>(a.out_features)};
+  if (p.pack_x) { pack<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x); x = {ws + p.off_x, row}; }
+  if (p.pack_w) { pack<S, T, PL>(st, a.w, a.ldw, a.out_features, a.in_features, ws + p.off_w); w = {ws + p.off_w, row}; }
   ProductArgs g = {};
-  g.planes = Planes::of(PL);
-  g.a = dz.p; g.a_plane = dz.plane; g.lda = dz.ld;
+  g.a = dz.p; g.lda = dz.ld;
   g.partial = (float*)(ws + p.off_parts);
   if (a.dx) {
-    g.b = w.p; g.b_plane = w.plane; g.ldb = w.ld;
+    g.b = w.p; g.ldb = w.ld;
     g.M = a.rows; g.N = a.in_features; g.K = a.out_features;
     g.out = a.dx; g.ldo = a.lddx; g.wide_out = wide(a.dx, a.lddx, sizeof(S));
     run_product<S, T, false, true, -1>(st, g, p.dx);
   }
   if (a.dw) {
-    g.b = x.p; g.b_plane = x.plane; g.ldb = x.ld;
+    g.b = x.p; g.ldb = x.ld;
     g.M = a.out_features; g.N = a.in_features; g.K = (int)a.rows;
     g.out = a.dw; g.ldo = a.lddw; g.wide_out = wide(a.dw, a.lddw, sizeof(S));
     run_product<S, T, true, true, -1>(st, g, p.dw);
@@ -426,17 +429,17 @@ template <class S> void clear(const optorch_linear_t& a) {
 LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
   LinearPlan p = {};
   const bool f32 = a.precision == OPTORCH_FP32;
-  p.planes = f32 ? 3 : 1;
-  const int64_t in8 = up8(a.in_features), out8 = up8(a.out_features);
+  const uint64_t in_row = 2 * (uint64_t)(f32 ? row_of<3>(a.in_features) : row_of<1>(a.in_features));
+  const uint64_t out_row = 2 * (uint64_t)(f32 ? row_of<3>(a.out_features) : row_of<1>(a.out_features));
   const bool need_x = !backward || a.dw, need_w = !backward || a.dx;
   p.pack_x = need_x && (f32 || !direct(a.x, a.ldx, a.in_features));
   p.pack_w = need_w && (f32 || !direct(a.w, a.ldw, a.in_features));
   p.make_dz = backward && (a.dx || a.dw) && (f32 || a.activation != OPTORCH_ACT_NONE || !direct(a.dy, a.lddy, a.out_features));
   uint64_t o = 0;
   auto take = [&](uint64_t n) { const uint64_t at = o; o = up256(o + n); return at; };
-  if (p.pack_x) p.off_x = take((uint64_t)a.rows * in8 * 2 * p.planes);
-  if (p.pack_w) p.off_w = take((uint64_t)a.out_features * in8 * 2 * p.planes);
-  if (p.make_dz) p.off_dz = take((uint64_t)a.rows * out8 * 2 * p.planes);
+  if (p.pack_x) p.off_x = take((uint64_t)a.rows * in_row);
+  if (p.pack_w) p.off_w = take((uint64_t)a.out_features * in_row);
+  if (p.make_dz) p.off_dz = take((uint64_t)a.rows * out_row);
   uint64_t parts = 0;
   auto product = [&](ProductShape& s, int64_t M, int64_t N, int64_t K) {
     s = shape_of(M, N, K * (f32 ? 6 : 1));

@@ -23,16 +23,19 @@ __device__ __forceinline__ void split8(const float (&v)[8], Vec<f16_t, 8>& hi, V
   for (int e = 0; e < 8; ++e) l[e] = v[e] - (float)hi.v[e];
   lo = round_vec<f16_t, 8>(l);
 }
-__device__ __forceinline__ void store_planes(f16_t* p, int64_t plane, const float (&v)[8]) {
+// eight neighbouring columns from c on of a row in two planes (mat_core.h)
+__device__ __forceinline__ void store_planes(f16_t* row, int c, const float (&v)[8]) {
   Vec<f16_t, 8> hi, lo;
   split8(v, hi, lo);
+  f16_t* p = row + place_of<2>(c);
   *reinterpret_cast<Vec<f16_t, 8>*>(p) = hi;
-  *reinterpret_cast<Vec<f16_t, 8>*>(p + plane) = lo;
+  *reinterpret_cast<Vec<f16_t, 8>*>(p + 32) = lo;
 }
-__device__ __forceinline__ void load_planes(const f16_t* p, int64_t plane, float (&v)[8]) {
+__device__ __forceinline__ void load_planes(const f16_t* row, int c, float (&v)[8]) {
+  const f16_t* p = row + place_of<2>(c);
   float l[8];
   load_f32<f16_t, 8>(p, v);
-  load_f32<f16_t, 8>(p + plane, l);
+  load_f32<f16_t, 8>(p + 32, l);
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] += l[e];
 }
@@ -127,7 +130,6 @@ __global__ void __launch_bounds__(256) planes_kernel(OrthoTables t, Source s, in
   const int c8 = m.cp / 8, last = min(c.first + ORTHO_GROUPS, m.rp * c8);
   const double scale = t.scale[c.mat];
   f16_t* x = (f16_t*)(t.ws + m.x[0]);
-  const int64_t plane = (int64_t)m.rp * m.cp;
   for (int g = c.first + threadIdx.x; g < last; g += 256) {
     const int r = g / c8, col = (g - r * c8) * 8, n = r < m.rows ? min(8, m.cols - col) : 0;
     float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, vn[8];
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(256) planes_kernel(OrthoTables t, Source s, in
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[e] = e < n ? (float)((double)u[e] * scale) : 0.f;
     }
-    store_planes(x + (int64_t)g * 8, plane, u);
+    store_planes(x + (int64_t)r * 2 * m.cp, col, u);
   }
 }
 
@@ -149,35 +151,34 @@ __device__ __forceinline__ f16_t* chain_at(const OrthoTables& t, const OrthoMat&
 
 // dst = alpha * sum + beta * extra + diag * identity at eight neighbouring places of a symmetric matrix's planes
 __device__ __forceinline__ void chain_store(const OrthoTables& t, const OrthoMat& m, const OrthoOp& op, int r, int c, float (&v)[8]) {
-  const int64_t at = (int64_t)r * m.mp + c, plane = (int64_t)m.mp * m.mp;
+  const int64_t row = (int64_t)r * 2 * m.mp;
   float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (op.extra >= 0) load_planes(chain_at(t, m, op.extra) + at, plane, x);
+  if (op.extra >= 0) load_planes(chain_at(t, m, op.extra) + row, c, x);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     v[e] = __fmaf_rn(op.alpha, v[e], op.beta * x[e]);
     if (r == c + e) v[e] += op.diag;
   }
-  store_planes(chain_at(t, m, op.dst) + at, plane, v);
+  store_planes(chain_at(t, m, op.dst) + row, c, v);
 }
 
 template <int W, bool TALL>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
 gram_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoOp op) {
-  typedef Tile<f16_t, W, W, TALL, TALL> G;
+  typedef Tile<f16_t, 2, W, TALL, TALL> G;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const OrthoWork w = works[blockIdx.x];
   const OrthoMat& m = t.mats[w.mat];
   const f16_t* x = (const f16_t*)(t.ws + m.x[src]);
-  const int ld = m.cp, r0 = w.tm * G::BM, c0 = w.tn * G::BN;
-  const int64_t plane = (int64_t)m.rp * m.cp;
-  const int rows = min(G::BM, m.mp - r0), cols = min(G::BN, m.mp - c0);
-  Operand<f16_t> a{x + (TALL ? (int64_t)w.k0 * ld + r0 : (int64_t)r0 * ld + w.k0), plane, ld, rows};
-  Operand<f16_t> b{x + (TALL ? (int64_t)w.k0 * ld + c0 : (int64_t)c0 * ld + w.k0), plane, ld, cols};
+  const int ld = 2 * m.cp, r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
+  const int rows = min(G::EDGE, m.mp - r0), cols = min(G::EDGE, m.mp - c0);
+  Operand<f16_t> a{x + (TALL ? (int64_t)w.k0 * ld + 2 * r0 : (int64_t)r0 * ld + 2 * w.k0), ld, rows};
+  Operand<f16_t> b{x + (TALL ? (int64_t)w.k0 * ld + 2 * c0 : (int64_t)c0 * ld + 2 * w.k0), ld, cols};
   typename G::Acc acc;
-  G::product(smem, a, b, Planes::of(2), w.k1 - w.k0, acc);
+  G::product(smem, a, b, w.k1 - w.k0, acc);
   if (w.slot >= 0) {
-    float* s = t.slots + (int64_t)w.slot * (G::BM * G::BN);
-    G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { store_f32<float, 8>(s + r * G::BN + c, v); },
+    float* s = t.slots + (int64_t)w.slot * (G::EDGE * G::EDGE);
+    G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { store_f32<float, 8>(s + r * G::EDGE + c, v); },
            [](int, int, float (&)[8], int) {}, false);
   } else {
     G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { chain_store(t, m, op, r0 + r, c0 + c, v); },
@@ -222,19 +223,18 @@ __global__ void __launch_bounds__(256) gram_join_kernel(OrthoTables t, const Ort
 template <int W>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
 chain_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int n, OrthoOp op0, OrthoOp op1) {
-  typedef Tile<f16_t, W, W, false, false> G;
+  typedef Tile<f16_t, 2, W, false, false> G;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const bool second = (int)blockIdx.x >= n;
   const OrthoWork w = works[second ? blockIdx.x - n : blockIdx.x];
   const OrthoOp op = second ? op1 : op0;
   const OrthoMat& m = t.mats[w.mat];
-  const int ld = m.mp, r0 = w.tm * G::BM, c0 = w.tn * G::BN;
-  const int64_t plane = (int64_t)ld * ld;
-  const int rows = min(G::BM, ld - r0), cols = min(G::BN, ld - c0);
-  Operand<f16_t> a{chain_at(t, m, op.a) + (int64_t)r0 * ld, plane, ld, rows};
-  Operand<f16_t> b{chain_at(t, m, op.b) + (int64_t)c0 * ld, plane, ld, cols};
+  const int ld = 2 * m.mp, r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
+  const int rows = min(G::EDGE, m.mp - r0), cols = min(G::EDGE, m.mp - c0);
+  Operand<f16_t> a{chain_at(t, m, op.a) + (int64_t)r0 * ld, ld, rows};
+  Operand<f16_t> b{chain_at(t, m, op.b) + (int64_t)c0 * ld, ld, cols};
   typename G::Acc acc;
-  G::product(smem, a, b, Planes::of(2), ld, acc);
+  G::product(smem, a, b, m.mp, acc);
   G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { chain_store(t, m, op, r0 + r, c0 + c, v); },
          [&](int c, int r, float (&v)[8], int) { chain_store(t, m, op, c0 + c, r0 + r, v); }, w.tm != w.tn);
 }
@@ -250,26 +250,25 @@ enum { TO_PLANES = -1 };  // else the precision of o, or 3: muon
 template <int W, bool TALL, int OUT>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
 apply_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoOp op, Target out) {
-  typedef Tile<f16_t, W, W, false, !TALL> G;
+  typedef Tile<f16_t, 2, W, false, !TALL> G;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   if (OUT == 3 && t.skip[0]) return;
   const OrthoWork w = works[blockIdx.x];
   const OrthoMat& m = t.mats[w.mat];
   const f16_t* x = (const f16_t*)(t.ws + m.x[src]);
   const f16_t* q = chain_at(t, m, op.a);
-  const int r0 = w.tm * G::BM, c0 = w.tn * G::BN;
-  const int64_t xp = (int64_t)m.rp * m.cp, qp = (int64_t)m.mp * m.mp;
-  const int rows = min(G::BM, m.rp - r0), cols = min(G::BN, m.cp - c0);
+  const int r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
+  const int rows = min(G::EDGE, m.rp - r0), cols = min(G::EDGE, m.cp - c0);
   Operand<f16_t> a, b;
   if (TALL) {
-    a = {x + (int64_t)r0 * m.cp, xp, m.cp, rows};
-    b = {q + (int64_t)c0 * m.mp, qp, m.mp, cols};
+    a = {x + (int64_t)r0 * 2 * m.cp, 2 * m.cp, rows};
+    b = {q + (int64_t)c0 * 2 * m.mp, 2 * m.mp, cols};
   } else {
-    a = {q + (int64_t)r0 * m.mp, qp, m.mp, rows};
-    b = {x + c0, xp, m.cp, cols};
+    a = {q + (int64_t)r0 * 2 * m.mp, 2 * m.mp, rows};
+    b = {x + 2 * c0, 2 * m.cp, cols};
   }
   typename G::Acc acc;
-  G::product(smem, a, b, Planes::of(2), m.mp, acc);
+  G::product(smem, a, b, m.mp, acc);
   const int real_cols = m.cols;
   float lr = 0.f;
   if (OUT == 3) {
@@ -283,7 +282,7 @@ apply_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoO
 #pragma unroll
            for (int e = 0; e < 8; ++e) v[e] *= op.alpha;
            if (OUT == TO_PLANES) {
-             store_planes((f16_t*)(t.ws + m.x[src ^ 1]) + (int64_t)r * m.cp + c, xp, v);
+             store_planes((f16_t*)(t.ws + m.x[src ^ 1]) + (int64_t)r * 2 * m.cp, c, v);
              return;
            }
            const int n = min(8, real_cols - c);
@@ -312,7 +311,7 @@ template <class K> void allow_lds(K k, size_t lds) {
 }
 
 template <int W, bool TALL> void run_gram(hipStream_t st, const OrthoTables& t, const OrthoWork* w, int n, const OrthoLaunch& l) {
-  const size_t lds = Tile<f16_t, W, W, TALL, TALL>::LDS;
+  const size_t lds = Tile<f16_t, 2, W, TALL, TALL>::LDS;
   allow_lds(gram_kernel<W, TALL>, lds);
   OSEQ_LAUNCH((gram_kernel<W, TALL>), dim3(n), dim3(256), lds, st, t, w, l.src, l.op[0]);
 }
@@ -323,12 +322,12 @@ template <bool TALL> void run_gram_of(int w, hipStream_t st, const OrthoTables& 
   else run_gram<32, TALL>(st, t, ws, n, l);
 }
 template <int W> void run_chain(hipStream_t st, const OrthoTables& t, const OrthoWork* w, int n, const OrthoLaunch& l) {
-  const size_t lds = Tile<f16_t, W, W, false, false>::LDS;
+  const size_t lds = Tile<f16_t, 2, W, false, false>::LDS;
   allow_lds(chain_kernel<W>, lds);
   OSEQ_LAUNCH(chain_kernel<W>, dim3(n * l.ops), dim3(256), lds, st, t, w, n, l.op[0], l.op[1]);
 }
 template <int W, bool TALL, int OUT> void run_apply(hipStream_t st, const OrthoTables& t, const OrthoWork* w, int n, const OrthoLaunch& l, const Target& o) {
-  const size_t lds = Tile<f16_t, W, W, false, !TALL>::LDS;
+  const size_t lds = Tile<f16_t, 2, W, false, !TALL>::LDS;
   allow_lds(apply_kernel<W, TALL, OUT>, lds);
   OSEQ_LAUNCH((apply_kernel<W, TALL, OUT>), dim3(n), dim3(256), lds, st, t, w, l.src, l.op[0], o);
 }

@@ -1,18 +1,29 @@
 // Matrix products on the 16-bit matrix cores: C[m][n] = sum over k of A(m, k) * B(n, k), one tile of C per block.
 //
-// Either operand lies in memory along the reduction ("K": element (r, k) at r * ld + k) or across it ("R": at k * ld + r), so
-// one kernel body serves a layer (K, K), its data gradient (K, R) and its weight gradient (R, R).  A product may be a sum of
-// several products of planes (fp32 values as two or three 16-bit planes): the planes of a pair are one longer reduction.
+// Either operand lies in memory along the reduction ("K": rows of k) or across it ("R": rows of one k each), so one kernel body
+// serves a layer (K, K), its data gradient (K, R) and its weight gradient (R, R).
 //
-// Four wavefronts in two rows and two columns, each with WM x WN of the block's 2 WM x 2 WN; 64 values of k a stage, two stages in
-// LDS, filled by loads that write LDS themselves.  A stage is loaded while the one before it is used.  With 128 x 128 a wavefront
-// reads 32 KB from LDS for 64 MFMAs of 32 cycles, four of them 1024 of the 2048 cycles of a stage and the stage's writes 512; with
-// 64 x 64 it would be 1024 of 512 + 512: tiles that large pay as soon as there is one for every CU.
+// Values of more bits than 16 are two or three 16-bit planes, and their products the sum of several products of planes (the
+// largest ones; mat::Steps).  The planes of neighbouring columns lie together, so that what is loaded once serves all products:
+//   one plane      columns as they are
+//   two planes     32 columns of plane 0, the same 32 of plane 1; ...
+//   three planes   16 columns of plane 0, of plane 1, of plane 2, 16 unused; ...
+// "Places" below are positions in a row so laid out.  64 places of an operand along k are a slot: four groups of 16, each group one
+// plane of 16 values of k.  (Planes apart in memory, one product of planes after the other, take half as many loads again with two
+// planes and twice as many with three.)
 //
-// LDS, K: rows of 128 bytes, the 16-byte piece c of row r at c ^ (r & 7), so that the eight lanes a cycle serves (consecutive
-// rows, one piece) touch all banks once.  R: rows of one k, 32-byte units u of 16 values at u ^ f(k): the transposing read takes
-// four consecutive k of two units at once.  The loads write LDS in lane order, so each lane fetches the piece that belongs there.
+// Four wavefronts in two rows and two columns, each with W x W of the block's 2 W x 2 W.  Slots are a ring in LDS, A and B in turn,
+// filled by loads that write LDS themselves.  While the products of two slots are made, the loads of the two that were used up
+// before go out, evenly: with 256 x 256 and one plane the address unit takes 1024 of the 2048 cycles of a tile step for them, the reads
+// of LDS 512 and its writes 512.
+//
+// LDS, K: rows of 128 bytes, the 16-byte piece c of row r at c ^ (r / 2 & 7), so that sixteen consecutive rows, one piece of each,
+// touch all 64 banks once (c ^ (r & 7), right for 32 banks, cost half as many cycles again).  R: rows of one k, 32-byte units u of 16
+// values at u ^ fold(k): the transposing read takes four consecutive k of two blocks of rows at once.  The loads write LDS in lane
+// order, so each lane fetches the piece that belongs there.
 #pragma once
+#include <utility>
+
 #include "dev_common.h"
 
 namespace oseq {
@@ -31,32 +42,22 @@ template <> struct Op<f16_t> {
   __device__ static __forceinline__ v16f mma(V a, V b, v16f c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 };
 
-// One operand of a tile: `base` is its element (first row of the tile, k = 0) in plane 0, `rows` how many of the tile's rows
-// exist (at least 1; R: in memory there are as many as the next multiple of 8).  ld is a multiple of 8 and base 16-byte aligned.
-// K: the reduction's length is a multiple of 8.
+// Places that a column takes, columns that are laid out together, and where plane p of column c is
+constexpr int span_of(int planes) { return planes == 3 ? 4 : planes; }
+constexpr int block_of(int planes) { return planes == 1 ? 8 : planes == 2 ? 32 : 16; }
+template <int PL> __host__ __device__ constexpr int64_t place_of(int64_t c, int p = 0) {
+  return PL == 1 ? c : PL == 2 ? (c >> 5) * 64 + p * 32 + (c & 31) : (c >> 4) * 64 + p * 16 + (c & 15);
+}
+
+// One operand of a tile: `base` is its first place (first row of the tile, k = 0), ld the places from one row of memory to the next
+// (a multiple of 8; base 16-byte aligned), `rows` how many of the tile's rows exist (at least 1).  Memory holds whole blocks of columns
+// (block_of; one plane: of eight).
 template <class T> struct Operand {
   const T* base;
-  int64_t plane;  // elements from one plane to the next
   int ld, rows;
 };
 
-// The planes that are multiplied, in the order given: product s takes plane a(s) of A and b(s) of B
-struct Planes {
-  uint32_t a = 0, b = 0;  // two bits each
-  int n = 1;
-  __host__ __device__ void add(int i, int j) { a |= (uint32_t)i << (2 * n); b |= (uint32_t)j << (2 * n); ++n; }
-  // values in `planes` planes: every product whose planes' indices add up to less than `planes`, the small ones first
-  __host__ __device__ static Planes of(int planes) {
-    Planes p;
-    if (planes == 1) return p;
-    p.n = 0;
-    for (int s = planes - 1; s >= 0; --s)
-      for (int i = 0; i <= s; ++i) p.add(i, s - i);
-    return p;
-  }
-};
-
-constexpr int BK = 64;
+constexpr int SLOT_K = 64;                 // places of a slot along k (R: values of k and their planes)
 constexpr uint32_t OUTSIDE = 0x80000000u;  // a buffer offset beyond every buffer: reads as zero
 
 __device__ __forceinline__ v4i buffer_of(const void* p) {
@@ -74,168 +75,235 @@ __device__ __forceinline__ void load_to_lds(const v4i& buf, uint32_t off, uint32
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(buf));
 }
 
-// The loads of one operand: B rows of a tile, 64 of k
-template <class T, int B, bool R>
-struct Stage {
-  static constexpr int BYTES = B * BK * 2, NLD = BYTES / 4096;  // loads per thread
-  static constexpr int KROWS = R ? 512 / B : 0;                 // R: rows of k that a wavefront's load covers
-  static constexpr int UNITS = B / 16;
-  __device__ static __forceinline__ int fold(int k) { return UNITS >= 8 ? (k & 3) * 2 : UNITS >= 4 ? (k & 1) * 2 : 0; }
+// The loads and reads of one operand: B rows of a tile
+template <class T, int PL, int B, bool R>
+struct Feed {
+  static constexpr int BYTES = B * SLOT_K * 2, NLD = BYTES / 4096;  // of a slot; loads per thread
+  static constexpr int SPAN = span_of(PL);
+  static constexpr int PITCH = B * SPAN;          // R: places of a row of k
+  static constexpr int KROWS = R ? 512 / PITCH : 0;  // R: rows of k that a wavefront's load covers (or 0: half a row)
+  static constexpr int KS = R ? SLOT_K / SPAN : SLOT_K;  // what a slot takes of the reduction: values of k (R) or places
+  static constexpr int UNITS = PITCH / 16;
+  __device__ static __forceinline__ int fold(int k) { return PL == 3 ? (k & 3) : UNITS >= 8 ? (k & 3) * 2 : UNITS >= 4 ? (k & 1) * 2 : 0; }
 
   uint32_t off[NLD];
-  int kfirst;  // the k of this thread's piece within a stage (R: of its first load)
+  int kfirst;  // the k (or place) of this thread's piece within a slot, in its first load
   const T* next;
   int64_t step;
+  v4i buf;
+  int left;  // of the reduction from the next slot on; what lies beyond is filled with zeros
 
-  __device__ __forceinline__ void init(const Operand<T>& o, int wave, int lane) {
+  __device__ __forceinline__ void init(const Operand<T>& o, int K, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < NLD; ++i) {
       const int j = wave * NLD + i;
       if (R) {
-        const int k = j * KROWS + lane / (B / 8), slot = lane % (B / 8);
-        int r = ((slot >> 1) ^ fold(k)) * 16 + (slot & 1) * 8;
-        r = min(r, (o.rows - 1) & ~7);
-        off[i] = ((uint32_t)k * (uint32_t)o.ld + (uint32_t)r) * 2u;
+        const int e = j * 512 + lane * 8, k = e / PITCH, slot = (e % PITCH) / 8;
+        const int unit = (slot >> 1) ^ fold(k);
+        const int v = min(unit * 16 + (slot & 1) * 8, ((o.rows * SPAN - 1) | (PL == 1 ? 7 : 63)) - 7);
+        off[i] = ((uint32_t)k * (uint32_t)o.ld + (uint32_t)v) * 2u | (PL == 3 && unit % 4 == 3 ? OUTSIDE : 0u);
         if (i == 0) kfirst = k;
       } else {
-        const int r = min(j * 8 + (lane >> 3), o.rows - 1), c = (lane & 7) ^ (lane >> 3);
-        off[i] = ((uint32_t)r * (uint32_t)o.ld + (uint32_t)c * 8u) * 2u;
-        kfirst = c * 8;
+        const int r = j * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
+        off[i] = ((uint32_t)min(r, o.rows - 1) * (uint32_t)o.ld + (uint32_t)c * 8u) * 2u | (PL == 3 && c >= 6 ? OUTSIDE : 0u);
+        if (i == 0) kfirst = c * 8;
       }
     }
-    step = R ? (int64_t)BK * o.ld : BK;
+    next = o.base;
+    buf = buffer_of(next);
+    step = R ? (int64_t)KS * o.ld : KS;
+    left = K;
   }
-  // `left` values of k exist from the stage's first on
-  __device__ __forceinline__ void load(int i, const v4i& buf, int left, uint32_t lds, int wave) const {
-    const uint32_t out = (R ? kfirst + i * KROWS : kfirst) < left ? 0u : OUTSIDE;
-    load_to_lds(buf, off[i] | out, lds + (uint32_t)(wave * NLD + i) * 1024u);
-  }
-  // the MFMA operand of rows [32 * block, + 32) of the wavefront's rows from `first` on, k in [16 * ks, + 16)
-  typedef typename Op<T>::V V;
-  __device__ static __forceinline__ V read(const unsigned char* st, int row, int ks, int lane) {
-    if (R) {
-      const int g = lane >> 4, i16 = lane & 15;
-      const int k = ks * 16 + (g >> 1) * 8 + (i16 >> 2);
-      const int unit = (row >> 4) + (g & 1);
-      const unsigned char* p = st + k * (B * 2) + ((unit ^ fold(k)) * 32 + (i16 & 3) * 8);
-      return lds_tr_read8<V>(reinterpret_cast<const T*>(p), reinterpret_cast<const T*>(p + 4 * (B * 2)));
+  __device__ __forceinline__ void load(int i, uint32_t lds, int wave) const {
+    uint32_t o = off[i];
+    if (PL == 1) {  // (planes are laid out to whole slots along k)
+      const int k = R ? kfirst + i * 512 / PITCH : kfirst ^ ((i & 1) * 32);  // (K: a load further, eight rows, the piece's bit 2 changes)
+      o |= k < left ? 0u : OUTSIDE;
+    } else if (R) {
+      const int k = kfirst + i * 512 / PITCH;
+      o |= k < left ? 0u : OUTSIDE;
+    } else {
+      o |= left > 0 ? 0u : OUTSIDE;
     }
-    const int r = row + (lane & 31), c = (ks * 2 + (lane >> 5)) ^ (r & 7);
+    load_to_lds(buf, o, lds + (uint32_t)(wave * NLD + i) * 1024u);
+  }
+  __device__ __forceinline__ void advance() {
+    left -= KS;
+    next += step;
+    buf = buffer_of(next);
+  }
+  // the MFMA operand of group g, rows [row, row + 32) of the tile
+  typedef typename Op<T>::V V;
+  __device__ static __forceinline__ V read(const unsigned char* st, int row, int g, int lane) {
+    if (R) {
+      const int kk = PL == 1 ? g : PL == 2 ? (g & 1) : 0, plane = PL == 1 ? 0 : PL == 2 ? (g >> 1) : g;
+      const int q = lane >> 4, i16 = lane & 15;
+      const int k = kk * 16 + (q >> 1) * 8 + (i16 >> 2);
+      const int b = (row >> 4) + (q & 1);  // block of 16 rows
+      const int unit = PL == 1 ? b : PL == 2 ? (b >> 1) * 4 + plane * 2 + (b & 1) : b * 4 + plane;
+      const unsigned char* p = st + k * (PITCH * 2) + ((unit ^ fold(k)) * 32 + (i16 & 3) * 8);
+      return lds_tr_read8<V>(reinterpret_cast<const T*>(p), reinterpret_cast<const T*>(p + 4 * (PITCH * 2)));
+    }
+    const int r = row + (lane & 31), c = (g * 2 + (lane >> 5)) ^ ((r >> 1) & 7);
     return *reinterpret_cast<const V*>(st + r * 128 + c * 16);
   }
 };
 
-template <class T, int WM, int WN, bool AR, bool BR>
+// The products of two slots: step s multiplies group a(s) of A with group b(s) of B.  Every group is read into registers once;
+// `reads` says which ones step s reads behind its MFMAs (bits 0-3: groups of A, 4-7: of B), from the steps HAND on those of the next
+// two slots: a group is read again one step after its last use or later, and a step or more before its next one.  At HAND
+// every group of the two slots has been read, and they change hands.
+template <int PL> struct Steps;
+template <> struct Steps<1> {
+  static constexpr int N = 4, HAND = 2, FIRST = 0x77;
+  static constexpr int a(int s) { return s; }
+  static constexpr int b(int s) { return s; }
+  static constexpr int reads(int s) { return s == 0 ? 0x88 : s == 1 ? 0 : s == 2 ? 0x11 : 0x66; }
+};
+template <> struct Steps<2> {  // (0: hi of k 0-15, 1: hi of 16-31, 2, 3: lo)  hi lo + lo hi + hi hi of each
+  static constexpr int N = 6, HAND = 3, FIRST = 0x55;
+  static constexpr int a(int s) { return s == 0 ? 0 : s == 1 ? 2 : s == 2 ? 0 : s == 3 ? 1 : s == 4 ? 3 : 1; }
+  static constexpr int b(int s) { return s == 0 ? 2 : s == 1 ? 0 : s == 2 ? 0 : s == 3 ? 3 : s == 4 ? 1 : 1; }
+  static constexpr int reads(int s) { return s == 0 ? 0x82 : s == 1 ? 0x28 : s == 3 ? 0x41 : s == 4 ? 0x14 : 0; }
+};
+template <> struct Steps<3> {  // every product of planes whose indices add up to at most two
+  static constexpr int N = 6, HAND = 3, FIRST = 0x22;
+  static constexpr int a(int s) { return s == 0 ? 1 : s == 1 ? 1 : s == 5 ? 2 : 0; }
+  static constexpr int b(int s) { return s == 0 ? 1 : s == 1 ? 0 : s == 2 ? 1 : s == 3 ? 0 : s == 4 ? 2 : 0; }
+  static constexpr int reads(int s) { return s == 0 ? 0x55 : s == 3 ? 0x22 : 0; }
+};
+
+// f(0), f(1), ... f(N - 1), each with its number as a constant (the compiler gives up on unrolling what is below)
+template <class F, int... I> __device__ __forceinline__ void each_of(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F> __device__ __forceinline__ void each(F&& f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+// the group of the read number `i` of a step that reads the groups of `set`, mi blocks of rows each
+constexpr int group_of(int set, int i, int mi) {
+  for (int g = 0; g < 8; ++g)
+    if (set >> g & 1) {
+      if (i < mi) return g;
+      i -= mi;
+    }
+  return 0;
+}
+
+constexpr int ring_slots(int w) { return w == 128 ? 5 : w == 64 ? 8 : 16; }
+
+template <class T, int PL, int W, bool AR, bool BR>
 struct Tile {
-  static constexpr int BM = 2 * WM, BN = 2 * WN, MI = WM / 32, NI = WN / 32;
-  typedef Stage<T, BM, AR> SA;
-  typedef Stage<T, BN, BR> SB;
-  static constexpr int STAGE = SA::BYTES + SB::BYTES, LDS = 2 * STAGE;
-  static constexpr int EPITCH = WN + 4;  // floats of a row on its way out
+  static constexpr int RING = ring_slots(W), EDGE = 2 * W, MI = W / 32;
+  typedef Feed<T, PL, EDGE, AR> FA;
+  typedef Feed<T, PL, EDGE, BR> FB;
+  typedef Steps<PL> S;
+  static constexpr int SLOT = FA::BYTES, LDS = RING * SLOT;
+  static constexpr int EPITCH = W + 4;  // floats of a row on its way out
   static_assert(4 * 32 * EPITCH * 4 <= LDS, "the epilogue's rows do not fit");
   typedef typename Op<T>::V V;
-  typedef v16f Acc[MI][NI];
+  typedef v16f Acc[MI][MI];
 
-  // the sum over k in [0, K) of every plane pair
-  __device__ static __forceinline__ void product(unsigned char* smem, const Operand<T>& a, const Operand<T>& b, const Planes& pl, int K,
-                                                 Acc& acc) {
+  // the sum over k in [0, K)
+  __device__ static __forceinline__ void product(unsigned char* smem, const Operand<T>& a, const Operand<T>& b, int K, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    SA sa; SB sb;
-    sa.init(a, wave, lane);
-    sb.init(b, wave, lane);
+    FA fda;
+    FB fdb;
+    // what a slot takes: values of k where the operand lies across it, places where along
+    const int kv = PL == 1 ? K : (K + block_of(PL) - 1) / block_of(PL) * SLOT_K;
+    fda.init(a, AR ? K : kv, wave, lane);
+    fdb.init(b, BR ? K : kv, wave, lane);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    const int per = (K + BK - 1) / BK, total = per * pl.n;
-    int s = 0, left = K;  // of the next stage to load
-    const T* pa = a.base + (int64_t)(pl.a & 3) * a.plane;
-    const T* pb = b.base + (int64_t)(pl.b & 3) * b.plane;
-    v4i ba, bb;
-    auto begin = [&]() { ba = buffer_of(pa); bb = buffer_of(pb); };
-    auto advance = [&]() {
-      left -= BK;
-      pa += sa.step; pb += sb.step;
-      if (left <= 0) {
-        ++s;
-        left = K;
-        pa = a.base + (int64_t)((pl.a >> (2 * s)) & 3) * a.plane;
-        pb = b.base + (int64_t)((pl.b >> (2 * s)) & 3) * b.plane;
-      }
+    const int total = (kv + SLOT_K - 1) / SLOT_K;
+    constexpr int NLD = FA::NLD, MFMAS = MI * MI, PLACES = S::N * MFMAS;
+    // Load n of the sequence A, B, A, B, ... goes to slot n mod RING; from the hand-over of tile step t - 1 to that of t, loads
+    // 2 t + RING - 2 and the next go out
+    constexpr bool B_FIRST = RING % 2 != 0;
+    auto load_place = [&](auto place, uint32_t first, uint32_t second) {
+      each<2 * NLD>([&](auto n) {
+        if constexpr (n * PLACES / (2 * NLD) == place) {
+          constexpr int i = n % NLD;
+          constexpr bool of_b = (n < NLD) == B_FIRST;
+          const uint32_t lds = lds0 + (n < NLD ? first : second);
+          if constexpr (of_b) fdb.load(i, lds, wave); else fda.load(i, lds, wave);
+          if constexpr (i == NLD - 1) { if constexpr (of_b) fdb.advance(); else fda.advance(); }
+        }
+      });
     };
-    auto load_piece = [&](int i, uint32_t lds) {
-      if (i < SA::NLD) sa.load(i, ba, left, lds, wave);
-      else sb.load(i - SA::NLD, bb, left, lds + SA::BYTES, wave);
-    };
-    constexpr int NLD = SA::NLD + SB::NLD;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
+      for (int j = 0; j < MI; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    begin();
 #pragma unroll
-    for (int i = 0; i < NLD; ++i) load_piece(i, lds0);
-    advance();
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    for (int n = 0; n < RING - 2; ++n) {
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        if (n % 2) fdb.load(i, lds0 + n * SLOT, wave); else fda.load(i, lds0 + n * SLOT, wave);
+      }
+      if (n % 2) fdb.advance(); else fda.advance();
+    }
+    // every read of the two slots is done and the next two have arrived (younger loads may be on their way): the barrier hands all
+    // four over
+    constexpr int FLYING = (RING - 4) * NLD;
+    auto hand_over = [&]() {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLYING) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    hand_over();
+    auto after = [](int slot, int by) { slot += by * SLOT; return slot >= RING * SLOT ? slot - RING * SLOT : slot; };
+    int at = 0;  // the slot of A, in bytes; B's is the next one
+    // operands of the MFMAs, by group; read number i of a step's set
+    V fa[4][MI], fb[4][MI];
+    auto read_of = [&](auto set, auto i, const unsigned char* sa, const unsigned char* sb) {
+      constexpr int g = group_of(set, i, MI), r = i % MI;
+      if constexpr (g < 4) fa[g][r] = FA::read(sa, wm * W + r * 32, g, lane);
+      else fb[g - 4][r] = FB::read(sb, wn * W + r * 32, g - 4, lane);
+    };
+    each<(S::N - S::HAND) * MFMAS>([&](auto n) { load_place(n, (RING - 2) * SLOT, (RING - 1) * SLOT); });
+    each<__builtin_popcount(S::FIRST) * MI>([&](auto i) { read_of(std::integral_constant<int, S::FIRST>{}, i, smem, smem + SLOT); });
+    for (int t = 0; t < total; ++t) {
+      const unsigned char *sa = smem + at, *sb = smem + after(at, 1), *na = smem + after(at, 2), *nb = smem + after(after(at, 2), 1);
+      const int free0 = after(at, RING - 2), free1 = after(at, RING - 1);
+      // Nothing is moved across the bars between MFMAs, or the compiler reads each operand right before its use.
+      each<S::N>([&](auto s) {
+        if constexpr (s == S::HAND) hand_over();
+        __builtin_amdgcn_sched_barrier(0);
+        constexpr int set = S::reads(s), count = __builtin_popcount(set) * MI, per = (count + MFMAS - 1) / MFMAS;
+        each<MFMAS>([&](auto n) {
+          acc[n / MI][n % MI] = Op<T>::mma(fa[S::a(s)][n / MI], fb[S::b(s)][n % MI], acc[n / MI][n % MI]);
+          __builtin_amdgcn_sched_barrier(0);
+          each<per>([&](auto j) {  // (of the last tile step: what is read is not used)
+            constexpr int i = n * per + j;
+            if constexpr (i < count)
+              read_of(std::integral_constant<int, set>{}, std::integral_constant<int, i>{}, s < S::HAND ? sa : na, s < S::HAND ? sb : nb);
+          });
+          if constexpr (s < S::HAND) load_place(std::integral_constant<int, (s + S::N - S::HAND) * MFMAS + n>{}, free0, free1);
+          else load_place(std::integral_constant<int, (s - S::HAND) * MFMAS + n>{}, at, after(at, 1));
+          __builtin_amdgcn_sched_barrier(0);
+        });
+      });
+      at = after(at, 2);
+    }
+    // (the epilogue writes LDS: what was loaded past the end has to be there first)
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    if (total > 1) {
-      begin();
-#pragma unroll
-      for (int i = 0; i < NLD; ++i) load_piece(i, lds0 + STAGE);
-      advance();
-    }
-    V fa[2][MI], fb[2][NI];
-    const unsigned char* cur = smem;
-    auto read = [&](int buf, const unsigned char* st, int ks) {
-#pragma unroll
-      for (int i = 0; i < MI; ++i) fa[buf][i] = SA::read(st, wm * WM + i * 32, ks, lane);
-#pragma unroll
-      for (int j = 0; j < NI; ++j) fb[buf][j] = SB::read(st + SA::BYTES, wn * WN + j * 32, ks, lane);
-    };
-    read(0, cur, 0);
-    for (int t = 0; t < total; ++t) {
-      const unsigned char* other = smem + (cur == smem ? STAGE : 0);
-      const uint32_t cur_lds = lds0 + (cur == smem ? 0 : STAGE);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        const int buf = ks & 1;
-        if (ks < 3) {
-          read(buf ^ 1, cur, ks + 1);
-        } else {
-          // every read of this stage is done and the next stage has arrived: the barrier hands both over
-          asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-          __builtin_amdgcn_s_barrier();
-          asm volatile("" ::: "memory");
-          if (t + 2 < total) {
-            begin();
-#pragma unroll
-            for (int i = 0; i < NLD; ++i) load_piece(i, cur_lds);
-            advance();
-          }
-          if (t + 1 < total) read(buf ^ 1, other, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-          for (int j = 0; j < NI; ++j) acc[i][j] = Op<T>::mma(fa[buf][i], fb[buf][j], acc[i][j]);
-      }
-      cur = other;
-    }
   }
 
   // the place in the tile of a thread's eight values number `idx` on their way out
-  static constexpr int LPR = WN / 8, RPP = 64 / LPR, PASSES = 32 / RPP;  // lanes per row, rows per pass
+  static constexpr int LPR = W / 8, RPP = 64 / LPR, PASSES = 32 / RPP;  // lanes per row, rows per pass
   __device__ static __forceinline__ void place(int idx, int& r, int& c) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    r = (wave >> 1) * WM + idx / PASSES * 32 + idx % PASSES * RPP + lane / LPR;
-    c = (wave & 1) * WN + lane % LPR * 8;
+    r = (wave >> 1) * W + idx / PASSES * 32 + idx % PASSES * RPP + lane / LPR;
+    c = (wave & 1) * W + lane % LPR * 8;
   }
 
   // f(idx, row, column, values, n) for eight neighbouring columns at a time, n of them inside: row < rows, column < cols, both from
   // the tile's corner.  A wavefront takes 32 rows at a time through its own part of LDS, so that memory sees whole rows.
-  // ft, where given: the same for the transposed tile, f(column, row, ...) with eight neighbouring rows.
+  // ft, where `transposed`: the same for the transposed tile, f(column, row, ...) with eight neighbouring rows.
   template <class F, class FT>
   __device__ static __forceinline__ void out(unsigned char* smem, const Acc& acc, int rows, int cols, F&& f, FT&& ft, bool transposed) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -243,9 +311,9 @@ struct Tile {
     float* area = reinterpret_cast<float*>(smem) + wave * (32 * EPITCH);
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
-      const int r0 = wm * WM + i * 32, c0 = wn * WN;
+      const int r0 = wm * W + i * 32, c0 = wn * W;
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
+      for (int j = 0; j < MI; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) area[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * EPITCH + j * 32 + (lane & 31)] = acc[i][j][e];
       asm volatile("" ::: "memory");
@@ -259,7 +327,7 @@ struct Tile {
       }
       if (transposed) {
 #pragma unroll 1
-        for (int p = 0; p < WN / 16; ++p) {
+        for (int p = 0; p < W / 16; ++p) {
           const int c = p * 16 + (lane & 15), r = (lane >> 4) * 8;
           float v[8];
 #pragma unroll

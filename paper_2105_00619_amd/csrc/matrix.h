@@ -18,7 +18,6 @@ struct ProductShape { int wave, parts; };
 
 // What a linear layer's call does with its workspace: where each piece begins, and how the products run
 struct LinearPlan {
-  int planes;                       // 16-bit planes of a value: 1, or 3 for fp32
   bool pack_x, pack_w, pack_dy, make_dz;  // operands that are laid out anew (fp32, or not aligned for 16-byte loads)
   uint64_t off_x, off_w, off_dz, off_sums, off_parts, bytes;
   int sum_blocks;                   // blocks of rows whose dbias sums are kept apart
@@ -30,8 +29,8 @@ void launch_linear_backward(const optorch_linear_t& a, const LinearPlan& p);
 
 // ---- orthogonalised updates: what the host plans and the kernels read ----
 
-// One matrix of the list.  X, its iterate, is kept as it lies in memory (rows x cols), padded with zeros to multiples of eight
-// as two fp16 planes; everything else is m x m, m the shorter side.
+// One matrix of the list.  X, its iterate, is kept as it lies in memory (rows x cols), padded with zeros to multiples of 32,
+// in two fp16 planes (mat_core.h); everything else is m x m, m the shorter side.
 struct OrthoMat {
   int64_t offset, ld;      // in the caller's flat vectors
   int32_t rows, cols, rp, cp, mp, tall;  // rp, cp, mp: padded rows, columns, shorter side; tall: rows > cols

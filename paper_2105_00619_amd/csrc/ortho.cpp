@@ -120,6 +120,7 @@ bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
   return true;
 }
 
+int up32(int n) { return (n + 31) & ~31; }
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int64_t tiles_of(int64_t m, int64_t n, int w) { return (int64_t)cdiv(m, 2 * w) * cdiv(n, 2 * w); }
 
@@ -233,7 +234,7 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
     const optorch_matrix_t& s = matrices[i];
     OrthoMat m = {};
     m.offset = s.offset; m.ld = s.ld; m.rows = s.rows; m.cols = s.cols;
-    m.rp = (int)up8(s.rows); m.cp = (int)up8(s.cols); m.mp = std::min(m.rp, m.cp);
+    m.rp = up32(s.rows); m.cp = up32(s.cols); m.mp = std::min(m.rp, m.cp);
     m.tall = m.rp > m.cp;
     m.chunk0 = (int)p.chunks.size();
     const int64_t groups = (int64_t)m.rp * (m.cp / 8);
