@@ -78,21 +78,38 @@ __device__ __forceinline__ void source8(const Source& s, int64_t at, int n, floa
   }
 }
 
+// f(place in the flat vectors, n, row of X, column) for groups of eight neighbouring columns of a piece, n of them inside (0: none);
+// a tall matrix' groups run along its own columns: row and column of the transposed group's first value
+template <class F> __device__ __forceinline__ void groups_of(const OrthoChunk& c, const OrthoMat& m, F&& f) {
+  if (m.tall) {
+    const int col = c.first + (threadIdx.x & 15) * 8;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int r = c.row + k * 16 + (threadIdx.x >> 4);
+      f(m.offset + r * m.ld + col, r < m.rows ? min(8, m.cols - col) : 0, col, r);
+    }
+  } else {
+    const int c8 = m.n / 8, last = min(c.first + ORTHO_GROUPS, m.m * c8);
+    for (int g = c.first + threadIdx.x; g < last; g += 256) {
+      const int r = g / c8, col = (g - r * c8) * 8;
+      f(m.offset + r * m.ld + col, r < m.rows ? min(8, m.cols - col) : 0, r, col);
+    }
+  }
+}
+
 template <class G, bool MUON>
 __global__ void __launch_bounds__(256) norms_kernel(OrthoTables t, Source s) {
   __shared__ double part[4];
   const OrthoChunk c = t.chunks[blockIdx.x];
-  const OrthoMat& m = t.mats[c.mat];
-  const int c8 = m.cp / 8, last = min(c.first + ORTHO_GROUPS, m.rows * c8);
   double sum = 0.;
-  for (int g = c.first + threadIdx.x; g < last; g += 256) {
-    const int r = g / c8, col = (g - r * c8) * 8;
+  groups_of(c, t.mats[c.mat], [&](int64_t at, int n, int, int) {
+    if (n <= 0) return;
     float u[8], vn[8];
-    source8<G, MUON>(s, m.offset + r * m.ld + col, min(8, m.cols - col), u, vn);
+    source8<G, MUON>(s, at, n, u, vn);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (col + e < m.cols) sum = fma((double)u[e], (double)u[e], sum);
-  }
+      if (e < n) sum = fma((double)u[e], (double)u[e], sum);
+  });
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
@@ -100,13 +117,17 @@ __global__ void __launch_bounds__(256) norms_kernel(OrthoTables t, Source s) {
   if (threadIdx.x == 0) t.partial[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__global__ void __launch_bounds__(64) scales_kernel(OrthoTables t, float eps, double times) {
+__global__ void __launch_bounds__(256) scales_kernel(OrthoTables t, float eps, double times) {
+  __shared__ double part[4];
   const OrthoMat& m = t.mats[blockIdx.x];
   double sum = 0.;
-  for (int i = threadIdx.x; i < m.chunks; i += 64) sum += t.partial[m.chunk0 + i];
+  for (int i = threadIdx.x; i < m.chunks; i += 256) sum += t.partial[m.chunk0 + i];
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
+  __syncthreads();
   if (threadIdx.x == 0) {
+    sum = (part[0] + part[1]) + (part[2] + part[3]);
     const double norm = sqrt(sum);
     t.scale[blockIdx.x] = times / (norm < (double)eps ? (double)eps : norm);  // (NaN stays NaN)
     t.bad[blockIdx.x] = sum <= 1.7976931348623157e308 ? 0 : 1;
@@ -115,6 +136,7 @@ __global__ void __launch_bounds__(64) scales_kernel(OrthoTables t, float eps, do
 
 template <class G, bool MUON>
 __global__ void __launch_bounds__(256) planes_kernel(OrthoTables t, Source s, int32_t* skipped) {
+  __shared__ float turn[128][65];  // a tall matrix' piece on its way to its transposed place
   const OrthoChunk c = t.chunks[blockIdx.x];
   const OrthoMat& m = t.mats[c.mat];
   bool skip = false;
@@ -127,31 +149,43 @@ __global__ void __launch_bounds__(256) planes_kernel(OrthoTables t, Source s, in
       if (skipped) *skipped = skip;
     }
   }
-  const int c8 = m.cp / 8, last = min(c.first + ORTHO_GROUPS, m.rp * c8);
   const double scale = t.scale[c.mat];
   f16_t* x = (f16_t*)(t.ws + m.x[0]);
-  for (int g = c.first + threadIdx.x; g < last; g += 256) {
-    const int r = g / c8, col = (g - r * c8) * 8, n = r < m.rows ? min(8, m.cols - col) : 0;
+  groups_of(c, m, [&](int64_t at, int n, int r, int col) {
     float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, vn[8];
     if (n > 0) {
-      const int64_t at = m.offset + r * m.ld + col;
       source8<G, MUON>(s, at, n, u, vn);
       if (MUON && !skip) put8(s.v + at, n, vn);
 #pragma unroll
       for (int e = 0; e < 8; ++e) u[e] = e < n ? (float)((double)u[e] * scale) : 0.f;
     }
-    store_planes(x + (int64_t)r * 2 * m.cp, col, u);
+    if (m.tall) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) turn[r - c.first + e][col - c.row] = u[e];
+    } else {
+      store_planes(x + (int64_t)r * 2 * m.n, col, u);
+    }
+  });
+  if (!m.tall) return;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int g = threadIdx.x + k * 256, r = g >> 3, col = (g & 7) * 8;
+    float u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = turn[r][col + e];
+    if (c.first + r < m.m && c.row + col < m.n) store_planes(x + (int64_t)(c.first + r) * 2 * m.n, c.row + col, u);
   }
 }
 
 // ---- the products ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ f16_t* chain_at(const OrthoTables& t, const OrthoMat& m, int buf) {
-  return (f16_t*)(t.ws + m.chain) + (int64_t)buf * 2 * m.mp * m.mp;
+  return (f16_t*)(t.ws + m.chain) + (int64_t)buf * 2 * m.m * m.m;
 }
 
 // dst = alpha * sum + beta * extra + diag * identity at eight neighbouring places of a symmetric matrix's planes
 __device__ __forceinline__ void chain_store(const OrthoTables& t, const OrthoMat& m, const OrthoOp& op, int r, int c, float (&v)[8]) {
-  const int64_t row = (int64_t)r * 2 * m.mp;
+  const int64_t row = (int64_t)r * 2 * m.m;
   float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (op.extra >= 0) load_planes(chain_at(t, m, op.extra) + row, c, x);
 #pragma unroll
@@ -162,22 +196,13 @@ __device__ __forceinline__ void chain_store(const OrthoTables& t, const OrthoMat
   store_planes(chain_at(t, m, op.dst) + row, c, v);
 }
 
-template <int W, bool TALL>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
-gram_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoOp op) {
-  typedef Tile<f16_t, 2, W, TALL, TALL> G;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-  const OrthoWork w = works[blockIdx.x];
-  const OrthoMat& m = t.mats[w.mat];
-  const f16_t* x = (const f16_t*)(t.ws + m.x[src]);
-  const int ld = 2 * m.cp, r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
-  const int rows = min(G::EDGE, m.mp - r0), cols = min(G::EDGE, m.mp - c0);
-  Operand<f16_t> a{x + (TALL ? (int64_t)w.k0 * ld + 2 * r0 : (int64_t)r0 * ld + 2 * w.k0), ld, rows};
-  Operand<f16_t> b{x + (TALL ? (int64_t)w.k0 * ld + 2 * c0 : (int64_t)c0 * ld + 2 * w.k0), ld, cols};
-  typename G::Acc acc;
-  G::product(smem, a, b, w.k1 - w.k0, acc);
+// a finished tile of a symmetric matrix, or a part of its sum
+template <class G>
+__device__ __forceinline__ void symmetric_out(unsigned char* smem, const OrthoTables& t, const OrthoMat& m, const OrthoWork& w, const OrthoOp& op,
+                                              int slot0, int rows, int cols, const typename G::Acc& acc) {
+  const int r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
   if (w.slot >= 0) {
-    float* s = t.slots + (int64_t)w.slot * (G::EDGE * G::EDGE);
+    float* s = t.slots + (int64_t)(slot0 + w.slot) * (G::EDGE * G::EDGE);
     G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { store_f32<float, 8>(s + r * G::EDGE + c, v); },
            [](int, int, float (&)[8], int) {}, false);
   } else {
@@ -186,57 +211,78 @@ gram_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoOp
   }
 }
 
-// The parts of a tile of X X^T, added in order: a block has 32 x 32 values
-__global__ void __launch_bounds__(256) gram_join_kernel(OrthoTables t, const OrthoJoin* __restrict__ joins, int edge, OrthoOp op) {
+#define ORTHO_BOUNDS(W) __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
+
+// X X^T
+template <int W>
+__global__ void ORTHO_BOUNDS(W) gram_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoOp op) {
+  typedef Tile<f16_t, 2, W, false, false> G;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const OrthoWork w = works[blockIdx.x];
+  if (w.mat < 0) return;
+  const OrthoMat& m = t.mats[w.mat];
+  const f16_t* x = (const f16_t*)(t.ws + m.x[src]) + 2 * w.k0;
+  const int ld = 2 * m.n, r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
+  const int rows = min(G::EDGE, m.m - r0), cols = min(G::EDGE, m.m - c0);
+  typename G::Acc acc;
+  G::product(smem, Operand<f16_t>{x + (int64_t)r0 * ld, ld, rows}, Operand<f16_t>{x + (int64_t)c0 * ld, ld, cols}, w.k1 - w.k0, acc);
+  symmetric_out<G>(smem, t, m, w, op, 0, rows, cols, acc);
+}
+
+// The parts of a tile's sum, added in order: a block has 32 x 32 values.  The second half of the blocks: of the second operation.
+__global__ void __launch_bounds__(256) join_kernel(OrthoTables t, const OrthoJoin* __restrict__ joins, int njoins, int slots, int edge,
+                                                   OrthoOp op0, OrthoOp op1) {
   __shared__ float area[32][33];
-  const int per = edge / 32, sub = blockIdx.x % (per * per);
-  const OrthoJoin j = joins[blockIdx.x / (per * per)];
+  const int per = edge / 32, sub = blockIdx.x % (per * per), tile = blockIdx.x / (per * per);
+  const bool second = tile >= njoins;
+  const OrthoOp op = second ? op1 : op0;
+  const OrthoJoin j = joins[second ? tile - njoins : tile];
   const OrthoMat& m = t.mats[j.mat];
   const int sr = sub / per * 32, sc = sub % per * 32, r0 = j.tm * edge + sr, c0 = j.tn * edge + sc;
-  if (r0 >= m.mp || c0 >= m.mp) return;
-  for (int i = threadIdx.x; i < 1024; i += 256) {
-    const int r = i >> 5, c = i & 31;
-    const float* s = t.slots + (int64_t)j.slot * edge * edge + (sr + r) * edge + sc + c;
-    float v = 0.f;
-    if (r0 + r < m.mp && c0 + c < m.mp)
-      for (int p = 0; p < j.parts; ++p) v += s[(int64_t)p * edge * edge];
-    area[r][c] = v;
+  if (r0 >= m.m || c0 >= m.m) return;
+  const int q = threadIdx.x & 127, lr = q >> 2, lc = (q & 3) * 8, half = threadIdx.x >> 7;
+  {
+    const int r = threadIdx.x >> 3, c = (threadIdx.x & 7) * 4;
+    const float* s = t.slots + (int64_t)(j.slot + (second ? slots : 0)) * edge * edge + (sr + r) * edge + sc + c;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < j.parts; ++p) {
+      float x[4];
+      load_f32<float, 4>(s + (int64_t)p * edge * edge, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) area[r][c + e] = v[e];
   }
   __syncthreads();
-  const int half = threadIdx.x >> 7, q = threadIdx.x & 127, r = q >> 2, c = (q & 3) * 8;
   float v[8];
   if (half == 0) {
-    if (r0 + r < m.mp && c0 + c < m.mp) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = area[r][c + e];
-      chain_store(t, m, op, r0 + r, c0 + c, v);
-    }
+    for (int e = 0; e < 8; ++e) v[e] = area[lr][lc + e];
+    chain_store(t, m, op, r0 + lr, c0 + lc, v);
   } else if (j.tm != j.tn) {
-    if (c0 + r < m.mp && r0 + c < m.mp) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = area[c + e][r];
-      chain_store(t, m, op, c0 + r, r0 + c, v);
-    }
+    for (int e = 0; e < 8; ++e) v[e] = area[lc + e][lr];
+    chain_store(t, m, op, c0 + lr, r0 + lc, v);
   }
 }
 
+// products of the m x m matrices; the second half of the blocks: the second operation
 template <int W>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
-chain_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int n, OrthoOp op0, OrthoOp op1) {
+__global__ void ORTHO_BOUNDS(W) chain_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int n, int slots, OrthoOp op0, OrthoOp op1) {
   typedef Tile<f16_t, 2, W, false, false> G;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const bool second = (int)blockIdx.x >= n;
   const OrthoWork w = works[second ? blockIdx.x - n : blockIdx.x];
+  if (w.mat < 0) return;
   const OrthoOp op = second ? op1 : op0;
   const OrthoMat& m = t.mats[w.mat];
-  const int ld = 2 * m.mp, r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
-  const int rows = min(G::EDGE, m.mp - r0), cols = min(G::EDGE, m.mp - c0);
-  Operand<f16_t> a{chain_at(t, m, op.a) + (int64_t)r0 * ld, ld, rows};
-  Operand<f16_t> b{chain_at(t, m, op.b) + (int64_t)c0 * ld, ld, cols};
+  const int ld = 2 * m.m, r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
+  const int rows = min(G::EDGE, m.m - r0), cols = min(G::EDGE, m.m - c0);
   typename G::Acc acc;
-  G::product(smem, a, b, m.mp, acc);
-  G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { chain_store(t, m, op, r0 + r, c0 + c, v); },
-         [&](int c, int r, float (&v)[8], int) { chain_store(t, m, op, c0 + c, r0 + r, v); }, w.tm != w.tn);
+  G::product(smem, Operand<f16_t>{chain_at(t, m, op.a) + (int64_t)r0 * ld + 2 * w.k0, ld, rows},
+             Operand<f16_t>{chain_at(t, m, op.b) + (int64_t)c0 * ld + 2 * w.k0, ld, cols}, w.k1 - w.k0, acc);
+  symmetric_out<G>(smem, t, m, w, op, second ? slots : 0, rows, cols, acc);
 }
 
 struct Target {
@@ -246,108 +292,78 @@ struct Target {
 };
 enum { TO_PLANES = -1 };  // else the precision of o, or 3: muon
 
-// OUT: TO_PLANES, the precision of o, or 3 (weights)
-template <int W, bool TALL, int OUT>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
-apply_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoOp op, Target out) {
-  typedef Tile<f16_t, 2, W, false, !TALL> G;
+// Q X.  OUT: TO_PLANES, the precision of o, or 3 (weights)
+template <int W, int OUT>
+__global__ void ORTHO_BOUNDS(W) apply_kernel(OrthoTables t, const OrthoWork* __restrict__ works, int src, OrthoOp op, Target out) {
+  typedef Tile<f16_t, 2, W, false, true> G;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   if (OUT == 3 && t.skip[0]) return;
   const OrthoWork w = works[blockIdx.x];
+  if (w.mat < 0) return;
   const OrthoMat& m = t.mats[w.mat];
-  const f16_t* x = (const f16_t*)(t.ws + m.x[src]);
-  const f16_t* q = chain_at(t, m, op.a);
   const int r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
-  const int rows = min(G::EDGE, m.rp - r0), cols = min(G::EDGE, m.cp - c0);
-  Operand<f16_t> a, b;
-  if (TALL) {
-    a = {x + (int64_t)r0 * 2 * m.cp, 2 * m.cp, rows};
-    b = {q + (int64_t)c0 * 2 * m.mp, 2 * m.mp, cols};
-  } else {
-    a = {q + (int64_t)r0 * 2 * m.mp, 2 * m.mp, rows};
-    b = {x + 2 * c0, 2 * m.cp, cols};
-  }
+  const int rows = min(G::EDGE, m.m - r0), cols = min(G::EDGE, m.n - c0);
   typename G::Acc acc;
-  G::product(smem, a, b, m.mp, acc);
-  const int real_cols = m.cols;
+  G::product(smem, Operand<f16_t>{chain_at(t, m, op.a) + (int64_t)r0 * 2 * m.m, 2 * m.m, rows},
+             Operand<f16_t>{(const f16_t*)(t.ws + m.x[src]) + 2 * c0, 2 * m.n, cols}, m.m, acc);
   float lr = 0.f;
   if (OUT == 3) {
     const double ratio = out.scale_mode == OPTORCH_SCALE_ASPECT ? fmax(1., (double)m.rows / m.cols)
                          : out.scale_mode == OPTORCH_SCALE_RMS ? 0.04 * max(m.rows, m.cols) : 1.;
     lr = (float)(out.lr * sqrt(ratio));
   }
+  // eight neighbouring columns of the caller's matrix
+  auto give = [&](int r, int c, float (&v)[8]) {
+    const int n = min(8, m.cols - c);
+    if (r >= m.rows || n <= 0) return;
+    const int64_t at = m.offset + r * m.ld + c;
+    if (OUT == OPTORCH_FP32) put8((float*)out.o + at, n, v);
+    if (OUT == OPTORCH_BF16) put8((bf16_t*)out.o + at, n, v);
+    if (OUT == OPTORCH_FP16) put8((f16_t*)out.o + at, n, v);
+    if (OUT == 3) {
+      float w0[8];
+      get8((const float*)out.w + at, n, w0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn(-lr, v[e], w0[e] * out.keep);
+      put8(out.w + at, n, v);
+      if (out.w16) {
+        if (out.w16_bf16) put8((bf16_t*)out.w16 + at, n, v);
+        else put8((f16_t*)out.w16 + at, n, v);
+      }
+    }
+  };
+  const bool turned = OUT != TO_PLANES && m.tall;
   G::out(smem, acc, rows, cols,
          [&](int, int r, int c, float (&v)[8], int) {
-           r += r0; c += c0;
+           if (turned) return;
 #pragma unroll
            for (int e = 0; e < 8; ++e) v[e] *= op.alpha;
-           if (OUT == TO_PLANES) {
-             store_planes((f16_t*)(t.ws + m.x[src ^ 1]) + (int64_t)r * 2 * m.cp, c, v);
-             return;
-           }
-           const int n = min(8, real_cols - c);
-           if (r >= m.rows || n <= 0) return;
-           const int64_t at = m.offset + r * m.ld + c;
-           if (OUT == OPTORCH_FP32) put8((float*)out.o + at, n, v);
-           if (OUT == OPTORCH_BF16) put8((bf16_t*)out.o + at, n, v);
-           if (OUT == OPTORCH_FP16) put8((f16_t*)out.o + at, n, v);
-           if (OUT == 3) {
-             float w0[8];
-             get8((const float*)out.w + at, n, w0);
-#pragma unroll
-             for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn(-lr, v[e], w0[e] * out.keep);
-             put8(out.w + at, n, v);
-             if (out.w16) {
-               if (out.w16_bf16) put8((bf16_t*)out.w16 + at, n, v);
-               else put8((f16_t*)out.w16 + at, n, v);
-             }
-           }
+           if (OUT == TO_PLANES) store_planes((f16_t*)(t.ws + m.x[src ^ 1]) + (int64_t)(r0 + r) * 2 * m.n, c0 + c, v);
+           else give(r0 + r, c0 + c, v);
          },
-         [](int, int, float (&)[8], int) {}, false);
+         [&](int c, int r, float (&v)[8], int) {
+#pragma unroll
+           for (int e = 0; e < 8; ++e) v[e] *= op.alpha;
+           give(c0 + c, r0 + r, v);
+         },
+         turned);
 }
 
-template <class K> void allow_lds(K k, size_t lds) {
+template <class K, class... A> void run(K k, int n, size_t lds, hipStream_t st, A... a) {
   if (lds > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+  OSEQ_LAUNCH(k, dim3(n), dim3(256), lds, st, a...);
 }
+template <int W> constexpr size_t lds_of() { return Tile<f16_t, 2, W, false, false>::LDS; }
 
-template <int W, bool TALL> void run_gram(hipStream_t st, const OrthoTables& t, const OrthoWork* w, int n, const OrthoLaunch& l) {
-  const size_t lds = Tile<f16_t, 2, W, TALL, TALL>::LDS;
-  allow_lds(gram_kernel<W, TALL>, lds);
-  OSEQ_LAUNCH((gram_kernel<W, TALL>), dim3(n), dim3(256), lds, st, t, w, l.src, l.op[0]);
-}
-template <bool TALL> void run_gram_of(int w, hipStream_t st, const OrthoTables& t, const OrthoWork* ws, int n, const OrthoLaunch& l) {
-  if (!n) return;
-  if (w == 128) run_gram<128, TALL>(st, t, ws, n, l);
-  else if (w == 64) run_gram<64, TALL>(st, t, ws, n, l);
-  else run_gram<32, TALL>(st, t, ws, n, l);
-}
-template <int W> void run_chain(hipStream_t st, const OrthoTables& t, const OrthoWork* w, int n, const OrthoLaunch& l) {
-  const size_t lds = Tile<f16_t, 2, W, false, false>::LDS;
-  allow_lds(chain_kernel<W>, lds);
-  OSEQ_LAUNCH(chain_kernel<W>, dim3(n * l.ops), dim3(256), lds, st, t, w, n, l.op[0], l.op[1]);
-}
-template <int W, bool TALL, int OUT> void run_apply(hipStream_t st, const OrthoTables& t, const OrthoWork* w, int n, const OrthoLaunch& l, const Target& o) {
-  const size_t lds = Tile<f16_t, 2, W, false, !TALL>::LDS;
-  allow_lds(apply_kernel<W, TALL, OUT>, lds);
-  OSEQ_LAUNCH((apply_kernel<W, TALL, OUT>), dim3(n), dim3(256), lds, st, t, w, l.src, l.op[0], o);
-}
-template <bool TALL, int OUT> void run_apply_w(int w, hipStream_t st, const OrthoTables& t, const OrthoWork* ws, int n, const OrthoLaunch& l, const Target& o) {
-  if (w == 128) run_apply<128, TALL, OUT>(st, t, ws, n, l, o);
-  else if (w == 64) run_apply<64, TALL, OUT>(st, t, ws, n, l, o);
-  else run_apply<32, TALL, OUT>(st, t, ws, n, l, o);
-}
-template <bool TALL> void run_apply_of(int w, hipStream_t st, const OrthoTables& t, const OrthoWork* ws, int n, const OrthoLaunch& l, const OrthoRun& r, const Target& o) {
-  if (!n) return;
-  if (!l.last) run_apply_w<TALL, TO_PLANES>(w, st, t, ws, n, l, o);
-  else if (r.muon) run_apply_w<TALL, 3>(w, st, t, ws, n, l, o);
-  else if (r.o_precision == OPTORCH_FP32) run_apply_w<TALL, OPTORCH_FP32>(w, st, t, ws, n, l, o);
-  else if (r.o_precision == OPTORCH_BF16) run_apply_w<TALL, OPTORCH_BF16>(w, st, t, ws, n, l, o);
-  else run_apply_w<TALL, OPTORCH_FP16>(w, st, t, ws, n, l, o);
+template <int OUT> void run_apply(hipStream_t st, const OrthoTables& t, const OrthoList& l, const OrthoWork* w, const OrthoLaunch& c, const Target& o) {
+  if (l.w == 128) run(apply_kernel<128, OUT>, l.n, lds_of<128>(), st, t, w, c.src, c.op[0], o);
+  else if (l.w == 64) run(apply_kernel<64, OUT>, l.n, lds_of<64>(), st, t, w, c.src, c.op[0], o);
+  else run(apply_kernel<32, OUT>, l.n, lds_of<32>(), st, t, w, c.src, c.op[0], o);
 }
 
 template <class G, bool MUON> void run_elements(hipStream_t st, const OrthoTables& t, const OrthoPlanHost& p, const Source& s, int32_t* skipped) {
   OSEQ_LAUNCH((norms_kernel<G, MUON>), dim3(t.nchunks), dim3(256), 0, st, t, s);
-  OSEQ_LAUNCH(scales_kernel, dim3(t.nmat), dim3(64), 0, st, t, p.eps, (double)p.first_scale);
+  OSEQ_LAUNCH(scales_kernel, dim3(t.nmat), dim3(256), 0, st, t, p.eps, (double)p.first_scale);
   OSEQ_LAUNCH((planes_kernel<G, MUON>), dim3(t.nchunks), dim3(256), 0, st, t, s, skipped);
 }
 
@@ -381,22 +397,34 @@ void launch_ortho(hipStream_t st, const OrthoPlanHost& p, char* ws, const OrthoR
     o.keep = (float)(1.0 - (double)r.m.lr * r.m.weight_decay); o.lr = r.m.lr; o.scale_mode = r.m.scale_mode;
   }
   const OrthoWork* works = (const OrthoWork*)(ws + p.off_works);
-  for (const OrthoLaunch& l : p.launches) {
-    if (l.kind == OL_GRAM) {
-      run_gram_of<false>(p.w_gram, st, t, works + p.gram[0].off, p.gram[0].n, l);
-      run_gram_of<true>(p.w_gram, st, t, works + p.gram[1].off, p.gram[1].n, l);
-      if (!p.joins.empty()) {
-        const int edge = 2 * p.w_gram, per = edge / 32;
-        OSEQ_LAUNCH(gram_join_kernel, dim3((int)p.joins.size() * per * per), dim3(256), 0, st, t, (const OrthoJoin*)(ws + p.off_joins), edge, l.op[0]);
-      }
-    } else if (l.kind == OL_CHAIN) {
-      const OrthoWork* w = works + p.chain.off;
-      if (p.w_chain == 128) run_chain<128>(st, t, w, p.chain.n, l);
-      else if (p.w_chain == 64) run_chain<64>(st, t, w, p.chain.n, l);
-      else run_chain<32>(st, t, w, p.chain.n, l);
+  const OrthoJoin* joins = (const OrthoJoin*)(ws + p.off_joins);
+  auto join = [&](const OrthoList& l, const OrthoLaunch& c) {
+    if (!l.joins) return;
+    const int edge = 2 * l.w, per = edge / 32;
+    run(join_kernel, l.joins * c.ops * per * per, 0, st, t, joins + l.join0, l.joins, l.slots, edge, c.op[0], c.op[1]);
+  };
+  // what is stored in fp32 as it is takes the more exact steps
+  for (const OrthoLaunch& c : p.launches[!r.muon && r.o_precision == OPTORCH_FP32]) {
+    if (c.kind == OL_GRAM) {
+      const OrthoWork* w = works + p.gram.work0;
+      if (p.gram.w == 128) run(gram_kernel<128>, p.gram.n, lds_of<128>(), st, t, w, c.src, c.op[0]);
+      else if (p.gram.w == 64) run(gram_kernel<64>, p.gram.n, lds_of<64>(), st, t, w, c.src, c.op[0]);
+      else run(gram_kernel<32>, p.gram.n, lds_of<32>(), st, t, w, c.src, c.op[0]);
+      join(p.gram, c);
+    } else if (c.kind == OL_CHAIN) {
+      const OrthoList& l = p.chain;
+      const OrthoWork* w = works + l.work0;
+      if (l.w == 128) run(chain_kernel<128>, l.n * c.ops, lds_of<128>(), st, t, w, l.n, l.slots, c.op[0], c.op[1]);
+      else if (l.w == 64) run(chain_kernel<64>, l.n * c.ops, lds_of<64>(), st, t, w, l.n, l.slots, c.op[0], c.op[1]);
+      else run(chain_kernel<32>, l.n * c.ops, lds_of<32>(), st, t, w, l.n, l.slots, c.op[0], c.op[1]);
+      join(l, c);
     } else {
-      run_apply_of<false>(p.w_apply, st, t, works + p.apply[0].off, p.apply[0].n, l, r, o);
-      run_apply_of<true>(p.w_apply, st, t, works + p.apply[1].off, p.apply[1].n, l, r, o);
+      const OrthoWork* w = works + p.apply.work0;
+      if (!c.last) run_apply<TO_PLANES>(st, t, p.apply, w, c, o);
+      else if (r.muon) run_apply<3>(st, t, p.apply, w, c, o);
+      else if (r.o_precision == OPTORCH_FP32) run_apply<OPTORCH_FP32>(st, t, p.apply, w, c, o);
+      else if (r.o_precision == OPTORCH_BF16) run_apply<OPTORCH_BF16>(st, t, p.apply, w, c, o);
+      else run_apply<OPTORCH_FP16>(st, t, p.apply, w, c, o);
     }
   }
 }

@@ -29,28 +29,34 @@ void launch_linear_backward(const optorch_linear_t& a, const LinearPlan& p);
 
 // ---- orthogonalised updates: what the host plans and the kernels read ----
 
-// One matrix of the list.  X, its iterate, is kept as it lies in memory (rows x cols), padded with zeros to multiples of 32,
-// in two fp16 planes (mat_core.h); everything else is m x m, m the shorter side.
+// One matrix of the list.  X, its iterate, has the shorter side as rows (tall matrices are transposed on the way in and out),
+// padded with zeros to multiples of 32, in two fp16 planes (mat_core.h); everything else is m x m, m the shorter side.
 struct OrthoMat {
   int64_t offset, ld;      // in the caller's flat vectors
-  int32_t rows, cols, rp, cp, mp, tall;  // rp, cp, mp: padded rows, columns, shorter side; tall: rows > cols
+  int32_t rows, cols, m, n;  // m, n: padded shorter and longer side
+  int32_t tall, chunk0, chunks, unused;  // rows > cols; its pieces in the passes over all elements
   uint64_t x[2], chain;    // bytes into the workspace: the iterate (two buffers), the m x m buffers
-  int32_t chunk0, chunks;  // its pieces in the passes over all elements
 };
 enum { OB_A = 0, OB_P, OB_C, OB_Q0, OB_Q1, OB_COUNT };
 
-struct OrthoChunk { int32_t mat, first; };  // 8192 values: groups of eight from `first` on
-constexpr int ORTHO_GROUPS = 1024;          // groups of a chunk
+// A piece of a matrix: 8192 places of X, as 1024 groups of eight (first: of the groups, row by row), or of a tall one 128 columns from
+// `first` on of 64 rows from `row` on
+struct OrthoChunk { int32_t mat, first, row; };
+constexpr int ORTHO_GROUPS = 1024;
 
-// one block's tile of a product
-struct OrthoWork { int32_t mat, tm, tn, k0, k1, slot; };  // slot >= 0: a part of the sum, kept apart
+// one block's tile of a product (mat < 0: nothing); slot >= 0: a part of the sum, kept apart
+struct OrthoWork { int32_t mat, tm, tn, k0, k1, slot; };
 // a tile whose sum is in `parts` slots from `slot` on
 struct OrthoJoin { int32_t mat, tm, tn, slot, parts; };
 
 // dst = alpha * (a b) + beta * extra + diag * identity, all of it in planes (extra < 0: none)
 struct OrthoOp { int32_t a, b, dst, extra; float alpha, beta, diag; };
 
-struct OrthoList { uint64_t off; int32_t n; };  // OrthoWork entries at off in the workspace
+// the blocks of one kind of product, in launch order, with wavefront tiles of w
+struct OrthoList {
+  int w = 32, n = 0, joins = 0, slots = 0;
+  uint64_t work0 = 0, join0 = 0;
+};
 
 enum { OL_GRAM = 0, OL_CHAIN, OL_APPLY };
 struct OrthoLaunch {
@@ -71,14 +77,12 @@ struct OrthoPlanHost {
   std::vector<OrthoChunk> chunks;
   std::vector<OrthoWork> works;   // all lists, one behind the other
   std::vector<OrthoJoin> joins;
-  OrthoList gram[2] = {}, chain = {}, apply[2] = {};  // [0] wide, [1] tall; off: index into works
-  int w_gram = 32, w_chain = 32, w_apply = 32;        // wavefront tiles
-  std::vector<OrthoLaunch> launches;
+  OrthoList gram, chain, apply;
+  std::vector<OrthoLaunch> launches[2];  // [1]: for results of fp32
   float eps = 1e-7f, first_scale = 1.f;  // first_scale: power of two of the first iterate's planes
   int64_t span = 0;
   uint64_t off_mats = 0, off_chunks = 0, off_works = 0, off_joins = 0, off_partial = 0, off_scale = 0, off_bad = 0, off_slots = 0,
            bytes = 0;
-  int slots = 0;
 };
 
 struct OrthoRun {  // one call

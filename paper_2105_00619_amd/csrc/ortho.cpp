@@ -5,8 +5,8 @@
 // Q X at the end touch the long side of X; all other products are m x m and symmetric, so that half of their tiles are made.  For
 // m = n that costs what the steps on X cost (20 m^3 for five steps), for n = 4 m 38 m^3 instead of 65.  But an error of A grows by
 // a^2 a step in the directions of small singular values, and rounding errors of A are not small against those: after five
-// steps on A the result is off by up to 3e-4.  So after three steps X is made and A from it again: 1e-6 to 2e-5, what the
-// steps on X give in fp32.
+// steps on A the result is off by up to 3e-4.  So after three steps X is made and A from it again: 1e-6 to 2e-5, up to twice what the
+// steps on X give in fp32; after two where the result of more steps is stored in fp32: no more than theirs (47 m^3 for n = 4 m).
 //
 // The operands are pairs of fp16 planes (hi + lo, 22 bits and a sign), times a power of two for each kind of matrix, since
 // the bounds of all of them are known (host: from the polynomials): three products of 16-bit matrix cores for one, with an error
@@ -17,6 +17,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <new>
 #include <string>
 
@@ -37,10 +38,10 @@ namespace {
 // beyond 2^12 (the low plane of a value of 2^-12 then still has all its bits)
 float plane_scale(double bound) { return (float)std::exp2(std::min(12.0, std::floor(std::log2(16384.0 / std::max(bound, 1e-3))))); }
 
-constexpr int RESTART = 3;  // steps on A between two iterates
+constexpr int RESTART[2] = {3, 2};  // steps on A between two iterates; [1]: for results of fp32
 
 // The launches and their scales.  Returns false where the steps let a singular value grow too far.
-bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
+bool plan_steps(OrthoPlanHost& p, std::vector<OrthoLaunch>& launches, int restart, int steps, const float* co) {
   constexpr int GRID = 4096;
   std::vector<double> l(GRID + 1), q(GRID + 1);
   for (int i = 0; i <= GRID; ++i) l[i] = (double)i / GRID;  // squares of singular values; sampled, the bounds have a margin
@@ -50,13 +51,13 @@ bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
   p.first_scale = plane_scale(1.0);
   float sx = p.first_scale;
   for (int s = 0; s < steps;) {
-    const int e = std::min(steps, s + RESTART);
+    const int e = std::min(steps, s + restart);
     const double amax = top([&](int i) { return l[i]; });
     float sa = plane_scale(amax), sq = 1.f;
     OrthoLaunch g = {};
     g.kind = OL_GRAM; g.src = src; g.ops = 1;
     g.op[0] = OrthoOp{0, 0, OB_A, -1, sa / (sx * sx), 0.f, 0.f};
-    p.launches.push_back(g);
+    launches.push_back(g);
     int qbuf = OB_Q0;
     std::fill(q.begin(), q.end(), 1.0);
     for (int k = s; k < e; ++k) {
@@ -68,7 +69,7 @@ bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
       OrthoLaunch lp = {};
       lp.kind = OL_CHAIN; lp.ops = 1;
       lp.op[0] = OrthoOp{OB_A, OB_A, pbuf, OB_A, (float)(sp * c / (sa * sa)), (float)(sp * b / sa), (float)(sp * a)};
-      p.launches.push_back(lp);
+      launches.push_back(lp);
       for (int i = 0; i <= GRID; ++i) q[i] *= poly(i);
       const float sq_new = plane_scale(top([&](int i) { return q[i]; }));
       OrthoLaunch ln = {};
@@ -85,11 +86,11 @@ bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
         } else {
           sq = sp;
         }
-        p.launches.push_back(ln);
+        launches.push_back(ln);
         OrthoLaunch la = {};
         la.kind = OL_CHAIN; la.ops = 1;
         la.op[0] = OrthoOp{OB_C, pbuf, OB_A, -1, sa_new / (sc * sp), 0.f, 0.f};
-        p.launches.push_back(la);
+        launches.push_back(la);
         sa = sa_new;
       } else {
         for (int i = 0; i <= GRID; ++i) { const double t = poly(i); l[i] *= t * t; }
@@ -97,7 +98,7 @@ bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
           ln.op[ln.ops++] = OrthoOp{OB_P, qbuf, qbuf ^ OB_Q0 ^ OB_Q1, -1, sq_new / (sp * sq), 0.f, 0.f};
           qbuf ^= OB_Q0 ^ OB_Q1;
           sq = sq_new;
-          p.launches.push_back(ln);
+          launches.push_back(ln);
         } else {
           sq = sp;
         }
@@ -109,7 +110,7 @@ bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
     x.kind = OL_APPLY; x.src = src; x.ops = 1; x.last = e == steps;
     const float sx_new = plane_scale(xmax);
     x.op[0] = OrthoOp{qbuf, 0, 0, -1, x.last ? 1.f / (sq * sx) : sx_new / (sq * sx), 0.f, 0.f};
-    p.launches.push_back(x);
+    launches.push_back(x);
     sx = sx_new;
     src ^= 1;
     s = e;
@@ -122,65 +123,113 @@ bool plan_steps(OrthoPlanHost& p, int steps, const float* co) {
 
 int up32(int n) { return (n + 31) & ~31; }
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-int64_t tiles_of(int64_t m, int64_t n, int w) { return (int64_t)cdiv(m, 2 * w) * cdiv(n, 2 * w); }
 
-// the largest tiles that give the CUs work
-template <class F> int tile_for(F&& count) {
-  for (int w : {128, 64})
-    if (count(w) >= 256) return w;
-  return 32;
+// ---- which block makes what ----------------------------------------------------------------------------------------------
+// What a launch is estimated to take, in us, from the time of a tile step (64 places of two operands, one block to a CU) and of a
+// block's beginning and end.  Measured on products of 2048 and 4096 rows.
+double step_us(int w) { return w == 128 ? 2.4 : w == 64 ? 0.65 : 0.28; }
+double block_us(int w) { return w == 128 ? 8.0 : w == 64 ? 5.0 : 4.0; }
+constexpr int CUS = 256, XCDS = 8;
+
+struct Tiles { int mat, count, steps; };  // tiles of one matrix, each of so many steps
+
+// blocks are taken by the CU that is free first, the longest ones first
+double launch_us(const std::vector<Tiles>& list, int w, int most) {
+  std::vector<std::pair<double, int64_t>> blocks;
+  double join = 0;
+  for (const Tiles& t : list) {
+    const int parts = cdiv(t.steps, most);
+    blocks.push_back({cdiv(t.steps, parts) * step_us(w) + block_us(w), (int64_t)t.count * parts});
+    if (parts > 1) join += (double)t.count * parts * (2 * w) * (2 * w) * 8 / 3e6;  // written and read again
+  }
+  std::sort(blocks.begin(), blocks.end(), [](auto& a, auto& b) { return a.first > b.first; });
+  std::vector<double> cu(CUS, 0.);  // a heap, the earliest on top
+  for (auto& b : blocks) {
+    if (b.second > 64 * CUS) {  // (many alike: a whole round for every CU, as often as it goes)
+      const int64_t rounds = b.second / CUS - 1;
+      for (double& c : cu) c += rounds * b.first;
+      b.second -= rounds * CUS;
+    }
+    for (int64_t i = 0; i < b.second; ++i) {
+      std::pop_heap(cu.begin(), cu.end(), std::greater<>());
+      cu.back() += b.first;
+      std::push_heap(cu.begin(), cu.end(), std::greater<>());
+    }
+  }
+  return *std::max_element(cu.begin(), cu.end()) + (join > 0 ? join + 5.0 : 0.0);
 }
 
-void plan_works(OrthoPlanHost& p) {
-  auto tri = [](int64_t t) { return t * (t + 1) / 2; };
-  auto chain_tiles = [&](int w) { int64_t n = 0; for (const OrthoMat& m : p.mats) n += tri(cdiv(m.mp, 2 * w)); return n; };
-  p.w_chain = tile_for(chain_tiles);
-  p.w_apply = tile_for([&](int w) { int64_t n = 0; for (const OrthoMat& m : p.mats) n += tiles_of(m.rp, m.cp, w); return n; });
-  p.w_gram = tile_for(chain_tiles);
-  // longest sums first
-  std::vector<int> order(p.mats.size());
-  for (size_t i = 0; i < order.size(); ++i) order[i] = (int)i;
-  auto list = [&](OrthoList& l, auto&& add) {
-    l.off = p.works.size();
-    for (int i : order) add(i, p.mats[i]);
-    l.n = (int)(p.works.size() - l.off);
-  };
-  auto by = [&](auto key) { std::stable_sort(order.begin(), order.end(), [&](int i, int j) { return key(p.mats[i]) > key(p.mats[j]); }); };
-  by([](const OrthoMat& m) { return m.mp; });
-  list(p.chain, [&](int i, const OrthoMat& m) {
-    const int t = cdiv(m.mp, 2 * p.w_chain);
-    for (int a = 0; a < t; ++a)
-      for (int b = 0; b <= a; ++b) p.works.push_back(OrthoWork{i, a, b, 0, m.mp, -1});
-  });
-  for (int tall = 0; tall < 2; ++tall)
-    list(p.apply[tall], [&](int i, const OrthoMat& m) {
-      if (m.tall != tall) return;
-      const int tm = cdiv(m.rp, 2 * p.w_apply), tn = cdiv(m.cp, 2 * p.w_apply);
-      // (bands of eight rows of tiles: neighbours share operands)
-      for (int band = 0; band < tm; band += 8)
-        for (int b = 0; b < tn; ++b)
-          for (int a = band; a < std::min(tm, band + 8); ++a) p.works.push_back(OrthoWork{i, a, b, 0, m.mp, -1});
-    });
-  // X X^T: the long sums are cut where there are few tiles
-  by([](const OrthoMat& m) { return std::max(m.rp, m.cp); });
-  int64_t steps = 0;
-  for (const OrthoMat& m : p.mats) steps += tri(cdiv(m.mp, 2 * p.w_gram)) * cdiv(std::max(m.rp, m.cp), 64);
-  const int64_t share = std::max<int64_t>(4, (steps + 511) / 512);  // 64-deep steps a block should have
-  for (int tall = 0; tall < 2; ++tall)
-    list(p.gram[tall], [&](int i, const OrthoMat& m) {
-      if (m.tall != tall) return;
-      const int K = std::max(m.rp, m.cp), ks = cdiv(K, 64), t = cdiv(m.mp, 2 * p.w_gram);
-      int parts = (int)std::min<int64_t>(32, std::max<int64_t>(1, (ks + share / 2) / share));
-      const int per = cdiv(ks, parts) * 64;
-      parts = cdiv(K, per);
-      for (int a = 0; a < t; ++a)
-        for (int b = 0; b <= a; ++b) {
-          if (parts > 1) p.joins.push_back(OrthoJoin{i, a, b, p.slots, parts});
-          for (int s = 0; s < parts; ++s)
-            p.works.push_back(OrthoWork{i, a, b, s * per, std::min(K, (s + 1) * per), parts > 1 ? p.slots + s : -1});
-          if (parts > 1) p.slots += parts;
-        }
-    });
+int64_t triangle(int64_t t) { return t * (t + 1) / 2; }
+
+// The blocks of a product: its tiles (all of rows x cols, or the lower triangle), sums longer than `most` steps cut.
+// Tiles are taken in squares of four by four, so that neighbours share operands, and neighbours go to one XCD: each has its own L2.
+void add_list(OrthoPlanHost& p, OrthoList& l, bool lower, int w, int most, bool along_n) {
+  l.w = w;
+  l.work0 = p.works.size();
+  l.join0 = p.joins.size();
+  struct Unit { std::vector<OrthoWork> works; double cost = 0; int steps = 0; };
+  std::vector<Unit> units;
+  for (size_t i = 0; i < p.mats.size(); ++i) {
+    const OrthoMat& m = p.mats[i];
+    const int e = 2 * w, tm = cdiv(m.m, e), tn = lower ? tm : cdiv(m.n, e), K = along_n ? m.n : m.m, steps = cdiv(K, 32);
+    int parts = cdiv(steps, most);
+    const int per = cdiv(steps, parts) * 32;
+    parts = cdiv(K, per);
+    const int64_t all = (lower ? triangle(tm) : (int64_t)tm * tn) * parts;
+    const int unit = (int)std::max<int64_t>(1, std::min<int64_t>(32, cdiv(all, XCDS)));
+    Unit u;
+    auto flush = [&]() { if (!u.works.empty()) units.push_back(std::move(u)); u = Unit(); };
+    for (int a4 = 0; a4 < tm; a4 += 4)
+      for (int b4 = 0; b4 < (lower ? a4 + 1 : tn); b4 += 4)
+        for (int a = a4; a < std::min(tm, a4 + 4); ++a)
+          for (int b = b4; b < std::min(lower ? a + 1 : tn, b4 + 4); ++b) {
+            if (parts > 1) p.joins.push_back(OrthoJoin{(int)i, a, b, l.slots, parts});
+            for (int s = 0; s < parts; ++s) {
+              u.works.push_back(OrthoWork{(int)i, a, b, s * per, std::min(K, (s + 1) * per), parts > 1 ? l.slots + s : -1});
+              u.steps = per / 32;
+              u.cost += u.steps * step_us(w) + block_us(w);
+              if ((int)u.works.size() >= unit) flush();
+            }
+            if (parts > 1) l.slots += parts;
+          }
+    flush();
+  }
+  l.joins = (int)(p.joins.size() - l.join0);
+  // the longest sums first, each unit to the XCD with the least to do
+  std::stable_sort(units.begin(), units.end(), [](const Unit& a, const Unit& b) { return a.steps > b.steps; });
+  std::vector<OrthoWork> bin[XCDS];
+  double load[XCDS] = {};
+  for (const Unit& u : units) {
+    const int x = (int)(std::min_element(load, load + XCDS) - load);
+    bin[x].insert(bin[x].end(), u.works.begin(), u.works.end());
+    load[x] += u.cost;
+  }
+  size_t most_in = 0;
+  for (const auto& b : bin) most_in = std::max(most_in, b.size());
+  // block i runs on XCD i % 8
+  for (size_t i = 0; i < most_in; ++i)
+    for (const auto& b : bin) p.works.push_back(i < b.size() ? b[i] : OrthoWork{-1, 0, 0, 0, 0, -1});
+  l.n = (int)(p.works.size() - l.work0);
+}
+
+void plan_list(OrthoPlanHost& p, OrthoList& l, bool lower, bool along_n, bool cut) {
+  int best_w = 32, best_most = 1 << 20;
+  double best = 1e300;
+  for (int w : {128, 64, 32}) {
+    std::vector<Tiles> tiles;
+    for (size_t i = 0; i < p.mats.size(); ++i) {
+      const OrthoMat& m = p.mats[i];
+      const int tm = cdiv(m.m, 2 * w);
+      const int64_t count = lower ? triangle(tm) : (int64_t)tm * cdiv(m.n, 2 * w);
+      tiles.push_back(Tiles{(int)i, (int)std::min<int64_t>(count, 1 << 30), cdiv(along_n ? m.n : m.m, 32)});
+    }
+    for (int most : {1 << 20, 128, 96, 64, 48, 32, 24, 16, 8}) {
+      if (most < (1 << 20) && !cut) continue;
+      const double us = launch_us(tiles, w, most);
+      if (us < best) { best = us; best_w = w; best_most = most; }
+    }
+  }
+  add_list(p, l, lower, best_w, best_most, along_n);
 }
 
 }  // namespace
@@ -228,22 +277,29 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
   OrthoPlanHost& p = h->p;
   p.eps = cfg->eps > 0 ? cfg->eps : 1e-7f;
   p.span = span;
-  if (!plan_steps(p, steps, co.data()))
+  if (!plan_steps(p, p.launches[0], RESTART[0], steps, co.data()) || !plan_steps(p, p.launches[1], RESTART[steps > RESTART[0]], steps, co.data()))
     return oseq_mat_err(OPTORCH_E_INVALID, "the coefficients let a singular value grow beyond 64");
   for (int i = 0; i < n; ++i) {
     const optorch_matrix_t& s = matrices[i];
     OrthoMat m = {};
     m.offset = s.offset; m.ld = s.ld; m.rows = s.rows; m.cols = s.cols;
-    m.rp = up32(s.rows); m.cp = up32(s.cols); m.mp = std::min(m.rp, m.cp);
-    m.tall = m.rp > m.cp;
+    m.tall = s.rows > s.cols;
+    m.m = up32(std::min(s.rows, s.cols)); m.n = up32(std::max(s.rows, s.cols));
     m.chunk0 = (int)p.chunks.size();
-    const int64_t groups = (int64_t)m.rp * (m.cp / 8);
+    const int64_t groups = (int64_t)m.m * (m.n / 8);
     if (groups > 0x7fff0000) return oseq_mat_err(OPTORCH_E_INVALID, "matrix " + std::to_string(i) + " has too many elements");
-    for (int64_t g = 0; g < groups; g += ORTHO_GROUPS) p.chunks.push_back(OrthoChunk{i, (int32_t)g});
+    if (m.tall) {
+      for (int r = 0; r < m.n; r += 64)
+        for (int c = 0; c < m.m; c += 128) p.chunks.push_back(OrthoChunk{i, c, r});
+    } else {
+      for (int64_t g = 0; g < groups; g += ORTHO_GROUPS) p.chunks.push_back(OrthoChunk{i, (int32_t)g, 0});
+    }
     m.chunks = (int)p.chunks.size() - m.chunk0;
     p.mats.push_back(m);
   }
-  plan_works(p);
+  plan_list(p, p.gram, true, true, true);
+  plan_list(p, p.chain, true, false, true);
+  plan_list(p, p.apply, false, false, false);
   uint64_t o = 0;
   auto take = [&](uint64_t bytes) { const uint64_t at = o; o = up256(o + bytes); return at; };
   p.off_mats = take(p.mats.size() * sizeof(OrthoMat));
@@ -253,12 +309,12 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
   p.off_partial = take(p.chunks.size() * 8);
   p.off_scale = take(p.mats.size() * 8);
   p.off_bad = take(p.mats.size() * 4 + 4);
-  p.off_slots = take((uint64_t)p.slots * (2 * p.w_gram) * (2 * p.w_gram) * 4);
-  const bool two = steps > RESTART;
+  p.off_slots = take(std::max((uint64_t)p.gram.slots * p.gram.w * p.gram.w, 2 * (uint64_t)p.chain.slots * p.chain.w * p.chain.w) * 16);
+  const bool two = steps > RESTART[0];
   for (OrthoMat& m : p.mats) {
-    m.x[0] = take((uint64_t)m.rp * m.cp * 4);
-    m.x[1] = two ? take((uint64_t)m.rp * m.cp * 4) : m.x[0];
-    m.chain = take((uint64_t)OB_COUNT * m.mp * m.mp * 4);
+    m.x[0] = take((uint64_t)m.m * m.n * 4);
+    m.x[1] = two ? take((uint64_t)m.m * m.n * 4) : m.x[0];
+    m.chain = take((uint64_t)OB_COUNT * m.m * m.m * 4);
   }
   p.bytes = o;
   drop.h = nullptr;
