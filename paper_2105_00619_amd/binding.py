@@ -49,13 +49,14 @@ class optorch_seq_config_t(C.Structure):
 
 
 class optorch_linear_t(C.Structure):
-    _fields_ = [("precision", C.c_int32), ("activation", C.c_int32), ("rows", C.c_int64), ("in_features", C.c_int32),
-                ("out_features", C.c_int32)]
-    for _n in ("x", "w", "bias", "residual", "y", "z", "dy", "dx", "dw"):
-        _fields_.append((_n, C.c_void_p))
-        if _n != "bias":
-            _fields_.append(({"residual": "ldr"}.get(_n, "ld" + _n), C.c_int64))
-    _fields_ += [("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("hip_stream", C.c_void_p)]
+    _fields_ = [
+        ("precision", C.c_int32), ("activation", C.c_int32), ("rows", C.c_int64), ("in_features", C.c_int32),
+        ("out_features", C.c_int32), ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64),
+        ("bias", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64),
+        ("z", C.c_void_p), ("ldz", C.c_int64), ("dy", C.c_void_p), ("lddy", C.c_int64), ("dx", C.c_void_p),
+        ("lddx", C.c_int64), ("dw", C.c_void_p), ("lddw", C.c_int64), ("dbias", C.c_void_p), ("workspace", C.c_void_p),
+        ("workspace_bytes", C.c_uint64), ("hip_stream", C.c_void_p),
+    ]
 
 
 class optorch_matrix_t(C.Structure):
@@ -579,17 +580,18 @@ def _linear_args(x, activation, rows, cin, cout):
     return a
 
 
-def _linear_call(lib, fn, a, backward, device):
-    import torch
-    with torch.cuda.device(device):
-        n = lib.optorch_linear_workspace(C.byref(a), backward)
-        if n < 0:
-            _mat_fail(n)
-        if n:
-            ws = torch.empty(n, dtype=torch.uint8, device=device)  # (torch aligns allocations to 512 bytes)
-            a.workspace, a.workspace_bytes = ws.data_ptr(), n
-        a.hip_stream = torch.cuda.current_stream(device).cuda_stream
-        rc = fn(C.byref(a))
+def _linear_call(torch, lib, fn, a, backward, device):
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _linear_call(torch, lib, fn, a, backward, device)
+    n = lib.optorch_linear_workspace(C.byref(a), backward)
+    if n < 0:
+        _mat_fail(n)
+    if n:
+        ws = torch.empty(n, dtype=torch.uint8, device=device)  # (torch aligns allocations to 512 bytes)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), n
+    a.hip_stream = torch.cuda.current_stream().cuda_stream
+    rc = fn(C.byref(a))
     if rc != OK:
         _mat_fail(rc)
 
@@ -620,7 +622,7 @@ def linear_forward(x, w, bias=None, *, residual=None, activation="none", save_pr
         z = torch.empty((rows, cout), dtype=x.dtype, device=x.device)
         a.z, a.ldz = z.data_ptr(), cout
     lib = load_library()
-    _linear_call(lib, lib.optorch_linear_forward, a, 0, x.device)
+    _linear_call(torch, lib, lib.optorch_linear_forward, a, 0, x.device)
     return (out, z) if save_pre else out
 
 
@@ -653,7 +655,7 @@ def linear_backward(dy, x, w, z=None, *, activation="none", need=("dx", "dw", "d
         dbias = torch.empty(cout, dtype=torch.float32, device=x.device)
         a.dbias = dbias.data_ptr()
     lib = load_library()
-    _linear_call(lib, lib.optorch_linear_backward, a, 1, x.device)
+    _linear_call(torch, lib, lib.optorch_linear_backward, a, 1, x.device)
     return dx, dw, dbias
 
 

@@ -14,40 +14,63 @@ namespace {
 
 using namespace mat;
 
-constexpr float INV_SQRT2 = 0.70710678118654752f, INV_SQRT_2PI = 0.39894228040143268f;
+// Phi(z) = (1 + erf(z / sqrt 2)) / 2 by Abramowitz and Stegun 7.1.26 (to 1e-7: three times the rounding of a result of 1), and e =
+// exp(-z^2 / 2), which the density has too.  (The library's erfcf takes three times as long: 8192 x 8192 outputs 150 us, 60.)
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float x = fabsf(z) * 0.70710678118654752f;
+  const float t = __builtin_amdgcn_rcpf(__fmaf_rn(0.3275911f, x, 1.f));
+  e = __builtin_amdgcn_exp2f(x * x * -1.4426950408889634f);
+  float p = __fmaf_rn(1.061405429f, t, -1.453152027f);
+  p = __fmaf_rn(p, t, 1.421413741f);
+  p = __fmaf_rn(p, t, -0.284496736f);
+  p = __fmaf_rn(p, t, 0.254829592f);
+  p = p * t * (0.5f * e);  // Phi(-|z|)
+  return z < 0.f ? p : 1.f - p;
+}
+__device__ __forceinline__ float logistic(float z) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f));
+}
 
 template <int ACT> __device__ __forceinline__ float act(float z) {
   if (ACT == OPTORCH_ACT_RELU) return z > 0.f ? z : (z != z ? z : 0.f);
-  if (ACT == OPTORCH_ACT_GELU) return 0.5f * z * erfcf(-z * INV_SQRT2);
-  if (ACT == OPTORCH_ACT_SILU) return z / (1.f + expf(-z));
+  if (ACT == OPTORCH_ACT_GELU) { float e; return z * normal_cdf(z, e); }
+  if (ACT == OPTORCH_ACT_SILU) return z * logistic(z);
   return z;
 }
 
 template <int ACT> __device__ __forceinline__ float act_slope(float z) {
   if (ACT == OPTORCH_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-  if (ACT == OPTORCH_ACT_GELU) return 0.5f * erfcf(-z * INV_SQRT2) + z * expf(-0.5f * z * z) * INV_SQRT_2PI;
+  if (ACT == OPTORCH_ACT_GELU) {
+    float e;
+    const float c = normal_cdf(z, e);
+    return __fmaf_rn(z * 0.39894228040143268f, e, c);
+  }
   if (ACT == OPTORCH_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
+    const float s = logistic(z);
     return s * (1.f + z * (1.f - s));
   }
   return 1.f;
 }
 
-// Eight neighbouring values, n of them inside; `wide`: their addresses are 16-byte aligned whenever n is 8
-template <class T> __device__ __forceinline__ void load8(const T* p, int n, bool wide, float (&v)[8]) {
-  if (wide && n == 8) {
-    load_f32<T, 8>(p, v);
+// Eight (or four) neighbouring values, n of them inside, at any address (the memory system takes accesses off their alignment; value by
+// value 20011 rows of 514 took 34 us, so 20)
+template <class T, int V> struct Loose { T v[V]; } __attribute__((packed, aligned(alignof(T))));
+template <class T, int V> __device__ __forceinline__ void load8(const T* p, int n, float (&v)[V]) {
+  if (n == V) {
+    const Loose<T, V> t = *reinterpret_cast<const Loose<T, V>*>(p);
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = to_f32(t.v[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(p[e]) : 0.f;
+    for (int e = 0; e < V; ++e) v[e] = e < n ? to_f32(p[e]) : 0.f;
   }
 }
-template <class T> __device__ __forceinline__ void store8(T* p, int n, bool wide, const float (&v)[8]) {
-  if (wide && n == 8) {
-    store_f32<T, 8>(p, v);
+template <class T, int V> __device__ __forceinline__ void store8(T* p, int n, const float (&v)[V]) {
+  if (n == V) {
+    *reinterpret_cast<Loose<T, V>*>(p) = __builtin_bit_cast(Loose<T, V>, round_vec<T, V>(v));
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
+    for (int e = 0; e < V; ++e)
       if (e < n) p[e] = from_f32<T>(v[e]);
   }
 }
@@ -86,14 +109,14 @@ template <int PL, class T> __device__ __forceinline__ void store_planes8(T* row,
 
 // S: type in memory; T: type of the planes.  Columns are filled up to whole blocks (block_of) with zeros.
 template <class S, class T, int PL>
-__global__ void __launch_bounds__(256) pack_kernel(const S* __restrict__ src, int64_t ld, int64_t rows, int cols, bool wide, T* __restrict__ dst) {
+__global__ void __launch_bounds__(256) pack_kernel(const S* __restrict__ src, int64_t ld, int64_t rows, int cols, T* __restrict__ dst) {
   const int c8 = (cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
   const int64_t n = rows * c8;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / c8;
     const int c = (int)(i - r * c8) * 8;
     float v[8];
-    load8<S>(src + r * ld + c, min(8, cols - c), wide, v);
+    load8<S>(src + r * ld + c, min(8, cols - c), v);
     store_planes8<PL, T>(dst + r * c8 * (8 * span_of(PL)), c, v);
   }
 }
@@ -102,7 +125,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const S* __restrict__ src, in
 struct DzArgs {
   const void* dy; int64_t lddy; const void* z; int64_t ldz;
   int64_t rows; int cols, rows_per_block;
-  bool wide_dy, wide_z, write;
+  bool write;
   void* dz;       // laid out as the products want it
   float* sums;    // [row blocks][cols], or null
 };
@@ -117,9 +140,9 @@ __global__ void __launch_bounds__(256) dz_kernel(DzArgs a) {
   if (c < padded)
     for (int64_t r = r0 + rl; r < r1; r += 8) {
       float v[8], z[8];
-      load8<S>((const S*)a.dy + r * a.lddy + c, n, a.wide_dy, v);
+      load8<S>((const S*)a.dy + r * a.lddy + c, n, v);
       if (ACT != OPTORCH_ACT_NONE) {
-        load8<S>((const S*)a.z + r * a.ldz + c, n, a.wide_z, z);
+        load8<S>((const S*)a.z + r * a.ldz + c, n, z);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT>(z[e]);
       }
@@ -148,8 +171,16 @@ __global__ void __launch_bounds__(256) dbias_kernel(const float* __restrict__ su
   __shared__ float part[16][17];
   const int cl = threadIdx.x & 15, t = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
   float s = 0.f;
-  if (c < cols)
-    for (int b = t; b < blocks; b += 16) s += sums[(int64_t)b * cols + c];
+  if (c < cols) {
+    float q[4] = {0.f, 0.f, 0.f, 0.f};  // (four loads on their way)
+    int b = t;
+    for (; b + 48 < blocks; b += 64) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) q[e] += sums[(int64_t)(b + 16 * e) * cols + c];
+    }
+    for (; b < blocks; b += 16) q[0] += sums[(int64_t)b * cols + c];
+    s = (q[0] + q[1]) + (q[2] + q[3]);
+  }
   part[t][cl] = s;
   __syncthreads();
   if (t == 0 && c < cols) {
@@ -173,28 +204,27 @@ struct ProductArgs {
   const void* residual; int64_t ldr;
   void* out; int64_t ldo;   // y, dx or dw
   void* z; int64_t ldz;     // or null
-  bool wide_out, wide_z, wide_r;
 };
 
 // bias, activation and skip connection of eight neighbouring sums; ACT < 0: the sums alone
-template <class O, int ACT>
-__device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int col, float (&v)[8], int n) {
+template <class O, int ACT, int V>
+__device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int col, float (&v)[V], int n) {
   if (ACT >= 0) {
     if (a.bias) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += e < n ? a.bias[col + e] : 0.f;
+      for (int e = 0; e < V; ++e) v[e] += e < n ? a.bias[col + e] : 0.f;
     }
-    if (a.z) store8<O>((O*)a.z + row * a.ldz + col, n, a.wide_z, v);
+    if (a.z) store8<O>((O*)a.z + row * a.ldz + col, n, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act<ACT>(v[e]);
+    for (int e = 0; e < V; ++e) v[e] = act<ACT>(v[e]);
     if (a.residual) {
-      float r[8];
-      load8<O>((const O*)a.residual + row * a.ldr + col, n, a.wide_r, r);
+      float r[V];
+      load8<O>((const O*)a.residual + row * a.ldr + col, n, r);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] += r[e];
+      for (int e = 0; e < V; ++e) v[e] += r[e];
     }
   }
-  store8<O>((O*)a.out + row * a.ldo + col, n, a.wide_out, v);
+  store8<O>((O*)a.out + row * a.ldo + col, n, v);
 }
 
 // The value at (r, k) of an operand of three planes
@@ -290,6 +320,117 @@ __global__ void __launch_bounds__(256) join_kernel(ProductArgs a) {
   }
 }
 
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+// Up to 64 samples: the weights are what is read, once, straight into the operands of 16 x 16 MFMAs.  A block has 16 outputs of all
+// samples, its wavefronts (4 to 16) share the reduction and add up through LDS.  1 x 4096 -> 16384 in bf16, 134 MB: 30 us (4.4 TB/s);
+// as tiles of 64 x 64 with the reduction in four parts 38.
+struct SkinnyArgs {
+  ProductArgs p;       // a: x, b: w as they lie in memory; tiles and parts unused
+  int k_wave;          // what a wavefront takes of the reduction, a multiple of 32
+};
+
+typedef __attribute__((ext_vector_type(4))) float v4f;
+__device__ __forceinline__ v4f mma16(Op<bf16_t>::V a, Op<bf16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v4f mma16(Op<f16_t>::V a, Op<f16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// eight values of a row from k on (up to the row's end, zeros behind it) as loaded; WIDE: all or none of them exist
+template <class S> struct Raw8 { Chunk c[sizeof(S) / 2]; };
+template <class S, bool WIDE> __device__ __forceinline__ Raw8<S> raw8(const S* row, int k, int end) {
+  Raw8<S> r;
+  if (WIDE) {
+    r = __builtin_bit_cast(Raw8<S>, *reinterpret_cast<const Loose<S, 8>*>(row + min(k, end - 8)));
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(S) / 2; ++i)
+      if (k >= end) r.c[i] = zero_chunk();
+  } else {
+    Vec<S, 8> v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.v[e] = k + e < end ? row[k + e] : from_f32<S>(0.f);
+    r = __builtin_bit_cast(Raw8<S>, v);
+  }
+  return r;
+}
+// ... as MFMA operands
+template <class S, class T> __device__ __forceinline__ void planes8(const Raw8<S>& r, typename Op<T>::V (&p)[sizeof(S) == 4 ? 3 : 1]) {
+  if constexpr (sizeof(S) == 2) {
+    p[0] = __builtin_bit_cast(typename Op<T>::V, r.c[0]);
+  } else {
+    const Vec<float, 8> v = __builtin_bit_cast(Vec<float, 8>, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      bf16_t t[3];
+      planes_of(v.v[e], t);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) p[k][e] = t[k];
+    }
+  }
+}
+
+// S: type in memory; T: of the planes; MB: blocks of 16 samples
+template <class S, class T, int MB, bool WIDE, int ACT>
+__global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
+  constexpr int PL = sizeof(S) == 4 ? 3 : 1, U = PL == 3 ? (MB == 4 ? 1 : 2) : !WIDE ? 1 : MB == 4 ? 4 : 8;
+  typedef typename Op<T>::V V;
+  extern __shared__ float red[];  // [wavefront][MB][256]
+  const ProductArgs& a = g.p;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int n0 = blockIdx.x * 16, r16 = lane & 15, kc = (lane >> 4) * 8;
+  const int k0 = wave * g.k_wave, k1 = min(a.K, k0 + g.k_wave);
+  const S* w = (const S*)a.b + (int64_t)min(n0 + r16, a.N - 1) * a.ldb;
+  const S* x[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) x[m] = (const S*)a.a + min<int64_t>(m * 16 + r16, a.M - 1) * a.lda;
+  v4f acc[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int k = k0; k < k1; k += 32 * U) {
+    Raw8<S> rw[U], rx[U][MB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) rw[u] = raw8<S, WIDE>(w, k + u * 32 + kc, k1);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < MB; ++m) rx[u][m] = raw8<S, WIDE>(x[m], k + u * 32 + kc, k1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      V pw[PL], px[PL];
+      planes8<S, T>(rw[u], pw);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) {
+        planes8<S, T>(rx[u][m], px);
+#pragma unroll
+        for (int i = PL - 1; i >= 0; --i)
+#pragma unroll
+          for (int j = PL - 1 - i; j >= 0; --j) acc[m] = mma16(pw[i], px[j], acc[m]);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MB; ++m) *reinterpret_cast<v4f*>(red + ((wave * MB + m) * 64 + lane) * 4) = acc[m];
+  __syncthreads();
+  // a thread has four neighbouring outputs of a sample
+  for (int i = threadIdx.x; i < MB * 64; i += blockDim.x) {
+    const int row = (i >> 6) * 16 + (i & 15), col = n0 + ((i & 63) >> 4) * 4, n = min(4, a.N - col);
+    if (row >= a.M || n <= 0) continue;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int q = 0; q < waves; ++q) {
+      const v4f t = *reinterpret_cast<const v4f*>(red + (q * MB * 64 + i) * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += t[e];
+    }
+    if constexpr (PL == 3) {
+      for (int e = 0; e < n; ++e)
+        if (!(fabsf(v[e]) <= 3.4028235e38f)) {  // (sum_again)
+          const float *p = (const float*)a.a + (int64_t)row * a.lda, *q = (const float*)a.b + (int64_t)(col + e) * a.ldb;
+          float s = 0.f;
+          for (int k = 0; k < a.K; ++k) s = fmaf(p[k], q[k], s);
+          v[e] = s;
+        }
+    }
+    finish<S, ACT>(a, row, col, v, n);
+  }
+}
+
 template <class T> __global__ void __launch_bounds__(256) clear_kernel(T* p, int64_t rows, int cols, int64_t ld) {
   const int64_t n = rows * cols;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i / cols * ld + i % cols] = from_f32<T>(0.f);
@@ -319,8 +460,6 @@ template <class O, class T, bool AR, bool BR, int ACT> void run_product(hipStrea
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-// whether groups of eight neighbouring columns of a matrix begin at 16-byte boundaries (fp32: 16 bytes of each half)
-bool wide(const void* p, int64_t ld, int esize) { return aligned16(p) && ld * esize % 16 == 0; }
 // whether a 16-bit matrix can be an operand as it lies
 bool direct(const void* p, int64_t ld, int cols) { return aligned16(p) && ld % 8 == 0 && cols % 8 == 0; }
 
@@ -340,8 +479,7 @@ ProductShape shape_of(int64_t M, int64_t N, int64_t K) {
 
 template <class S, class T, int PL>
 void pack(hipStream_t st, const void* src, int64_t ld, int64_t rows, int cols, void* dst) {
-  OSEQ_LAUNCH((pack_kernel<S, T, PL>), dim3(grid_of(rows * ((cols + 7) / 8))), dim3(256), 0, st, (const S*)src, ld, rows, cols,
-              wide(src, ld, sizeof(S)), (T*)dst);
+  OSEQ_LAUNCH((pack_kernel<S, T, PL>), dim3(grid_of(rows * ((cols + 7) / 8))), dim3(256), 0, st, (const S*)src, ld, rows, cols, (T*)dst);
 }
 
 template <class S, class T, int PL, int ACT> void run_dz(hipStream_t st, const optorch_linear_t& a, const LinearPlan& p) {
@@ -350,13 +488,34 @@ template <class S, class T, int PL, int ACT> void run_dz(hipStream_t st, const o
   d.dy = a.dy; d.lddy = a.lddy; d.z = a.z; d.ldz = a.ldz;
   d.rows = a.rows; d.cols = a.out_features;
   d.rows_per_block = ceil_div(a.rows, p.sum_blocks);
-  d.wide_dy = wide(a.dy, a.lddy, sizeof(S)); d.wide_z = ACT != OPTORCH_ACT_NONE && wide(a.z, a.ldz, sizeof(S));
   d.write = p.make_dz;
   d.dz = ws + p.off_dz;
   d.sums = a.dbias ? (float*)(ws + p.off_sums) : nullptr;
   OSEQ_LAUNCH((dz_kernel<S, T, PL, ACT>), dim3(ceil_div(d.cols, 256), p.sum_blocks), dim3(256), 0, st, d);
   if (a.dbias)
     OSEQ_LAUNCH(dbias_kernel, dim3(ceil_div(d.cols, 16)), dim3(256), 0, st, (const float*)d.sums, p.sum_blocks, d.cols, a.dbias);
+}
+
+constexpr int SKINNY_ROWS = 64;
+
+template <class S, class T, int MB, bool WIDE, int ACT> void run_skinny_of(hipStream_t st, ProductArgs& p) {
+  SkinnyArgs g;
+  g.p = p;
+  // wavefronts of at least 128 values of k each; more of them where there are few blocks
+  const int blocks = ceil_div(p.N, 16), most = blocks >= 1024 ? 4 : blocks >= 256 ? 8 : 16;
+  int waves = 4;
+  while (waves < most && waves * 256 <= p.K) waves *= 2;
+  g.k_wave = (ceil_div(p.K, waves) + 31) & ~31;
+  OSEQ_LAUNCH((skinny_kernel<S, T, MB, WIDE, ACT>), dim3(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, g);
+}
+template <class S, class T, int ACT> void run_skinny(hipStream_t st, ProductArgs& p, bool wide_operands) {
+  if (p.M <= 16) {
+    if (wide_operands) run_skinny_of<S, T, 1, true, ACT>(st, p); else run_skinny_of<S, T, 1, false, ACT>(st, p);
+  } else if (p.M <= 32) {
+    if (wide_operands) run_skinny_of<S, T, 2, true, ACT>(st, p); else run_skinny_of<S, T, 2, false, ACT>(st, p);
+  } else {
+    if (wide_operands) run_skinny_of<S, T, 4, true, ACT>(st, p); else run_skinny_of<S, T, 4, false, ACT>(st, p);
+  }
 }
 
 struct Where { const void* p; int ld; };
@@ -367,6 +526,7 @@ template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, c
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
   const int row = row_of<PL>(a.in_features);
+  const bool few = a.rows <= SKINNY_ROWS;
   Where x{a.x, (int)a.ldx}, w{a.w, (int)a.ldw};
   if (p.pack_x) { pack<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x); x = {ws + p.off_x, row}; }
   if (p.pack_w) { pack<S, T, PL>(st, a.w, a.ldw, a.out_features, a.in_features, ws + p.off_w); w = {ws + p.off_w, row}; }
@@ -376,9 +536,20 @@ template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, c
   g.M = a.rows; g.N = a.out_features; g.K = (int)up8(a.in_features);  // (up to the zeros behind a row)
   g.partial = (float*)(ws + p.off_parts);
   g.bias = a.bias;
-  g.residual = a.residual; g.ldr = a.ldr; g.wide_r = a.residual && wide(a.residual, a.ldr, sizeof(S));
-  g.out = a.y; g.ldo = a.ldy; g.wide_out = wide(a.y, a.ldy, sizeof(S));
-  g.z = a.z; g.ldz = a.ldz; g.wide_z = a.z && wide(a.z, a.ldz, sizeof(S));
+  g.residual = a.residual; g.ldr = a.ldr;
+  g.out = a.y; g.ldo = a.ldy;
+  g.z = a.z; g.ldz = a.ldz;
+  if (few) {
+    g.K = a.in_features;
+    const bool wide_operands = a.in_features % 8 == 0;
+    switch (a.activation) {
+      case OPTORCH_ACT_NONE: run_skinny<S, T, OPTORCH_ACT_NONE>(st, g, wide_operands); break;
+      case OPTORCH_ACT_RELU: run_skinny<S, T, OPTORCH_ACT_RELU>(st, g, wide_operands); break;
+      case OPTORCH_ACT_GELU: run_skinny<S, T, OPTORCH_ACT_GELU>(st, g, wide_operands); break;
+      default: run_skinny<S, T, OPTORCH_ACT_SILU>(st, g, wide_operands);
+    }
+    return;
+  }
   switch (a.activation) {
     case OPTORCH_ACT_NONE: run_product<S, T, false, false, OPTORCH_ACT_NONE>(st, g, p.y); break;
     case OPTORCH_ACT_RELU: run_product<S, T, false, false, OPTORCH_ACT_RELU>(st, g, p.y); break;
@@ -407,13 +578,13 @@ template <class S, class T, int PL> void backward_of(const optorch_linear_t& a, 
   if (a.dx) {
     g.b = w.p; g.ldb = w.ld;
     g.M = a.rows; g.N = a.in_features; g.K = a.out_features;
-    g.out = a.dx; g.ldo = a.lddx; g.wide_out = wide(a.dx, a.lddx, sizeof(S));
+    g.out = a.dx; g.ldo = a.lddx;
     run_product<S, T, false, true, -1>(st, g, p.dx);
   }
   if (a.dw) {
     g.b = x.p; g.ldb = x.ld;
     g.M = a.out_features; g.N = a.in_features; g.K = (int)a.rows;
-    g.out = a.dw; g.ldo = a.lddw; g.wide_out = wide(a.dw, a.lddw, sizeof(S));
+    g.out = a.dw; g.ldo = a.lddw;
     run_product<S, T, true, true, -1>(st, g, p.dw);
   }
 }
@@ -431,7 +602,8 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
   const bool f32 = a.precision == OPTORCH_FP32;
   const uint64_t in_row = 2 * (uint64_t)(f32 ? row_of<3>(a.in_features) : row_of<1>(a.in_features));
   const uint64_t out_row = 2 * (uint64_t)(f32 ? row_of<3>(a.out_features) : row_of<1>(a.out_features));
-  const bool need_x = !backward || a.dw, need_w = !backward || a.dx;
+  const bool few = !backward && a.rows <= SKINNY_ROWS;
+  const bool need_x = backward ? a.dw != nullptr : !few, need_w = backward ? a.dx != nullptr : !few;
   p.pack_x = need_x && (f32 || !direct(a.x, a.ldx, a.in_features));
   p.pack_w = need_w && (f32 || !direct(a.w, a.ldw, a.in_features));
   p.make_dz = backward && (a.dx || a.dw) && (f32 || a.activation != OPTORCH_ACT_NONE || !direct(a.dy, a.lddy, a.out_features));
@@ -445,12 +617,14 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
     s = shape_of(M, N, K * (f32 ? 6 : 1));
     if (s.parts > 1) parts = std::max(parts, (uint64_t)s.parts * M * up8(N) * 4);
   };
-  if (!backward) {
+  if (few) {
+    // (straight from memory)
+  } else if (!backward) {
     product(p.y, a.rows, a.out_features, a.in_features);
   } else {
-    // row blocks of the dz pass: enough of them for every CU, sums of at least 32 rows each
+    // row blocks of the dz pass: four blocks for every CU, sums of at least 32 rows each
     const int64_t across = (a.out_features + 255) / 256;
-    p.sum_blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 2048 / across)));
+    p.sum_blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 1024 / across)));
     if (a.dbias) p.off_sums = take((uint64_t)p.sum_blocks * a.out_features * 4);
     if (a.dx) product(p.dx, a.rows, a.in_features, a.out_features);
     if (a.dw) product(p.dw, a.out_features, a.in_features, a.rows);

@@ -40,17 +40,21 @@ __device__ __forceinline__ void load_planes(const f16_t* row, int c, float (&v)[
   for (int e = 0; e < 8; ++e) v[e] += l[e];
 }
 
+// eight neighbouring values, n of them inside, at any address
+template <class T> struct Loose8 { T v[8]; } __attribute__((packed, aligned(alignof(T))));
 template <class T> __device__ __forceinline__ void get8(const T* p, int n, float (&v)[8]) {
-  if (n == 8 && ((uintptr_t)p & 15) == 0) {
-    load_f32<T, 8>(p, v);
+  if (n == 8) {
+    const Loose8<T> t = *reinterpret_cast<const Loose8<T>*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = to_f32(t.v[e]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(p[e]) : 0.f;
   }
 }
 template <class T> __device__ __forceinline__ void put8(T* p, int n, const float (&v)[8]) {
-  if (n == 8 && ((uintptr_t)p & 15) == 0) {
-    store_f32<T, 8>(p, v);
+  if (n == 8) {
+    *reinterpret_cast<Loose8<T>*>(p) = __builtin_bit_cast(Loose8<T>, round_vec<T, 8>(v));
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)

@@ -188,7 +188,7 @@ constexpr int group_of(int set, int i, int mi) {
   return 0;
 }
 
-constexpr int ring_slots(int w) { return w == 128 ? 5 : w == 64 ? 8 : 16; }
+constexpr int ring_slots(int w) { return w == 128 ? 5 : w == 64 ? 5 : 6; }
 
 template <class T, int PL, int W, bool AR, bool BR>
 struct Tile {

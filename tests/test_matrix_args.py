@@ -19,7 +19,7 @@ def _built():
 def _linear(**kw):
     """Arguments of both directions that pass every check; the addresses are never read."""
     a = B.optorch_linear_t()
-    a.precision, a.activation, a.rows, a.in_features, a.out_features = 1, 2, 16, 64, 32
+    a.precision, a.activation, a.rows, a.in_features, a.out_features = 1, 2, 160, 64, 32
     for n, cols in (("x", 64), ("w", 64), ("residual", 32), ("y", 32), ("z", 32), ("dy", 32), ("dx", 64), ("dw", 64)):
         setattr(a, n, 1 << 20)
         setattr(a, "ldr" if n == "residual" else "ld" + n, cols)
@@ -35,12 +35,14 @@ def test_workspace_of_aligned_16_bit_operands_holds_no_copies():
                                                         ldz=512, ldr=512)), 0) == 0
     # rows that are no multiple of 16 bytes apart, and addresses off a 16-byte boundary, are laid out anew
     odd = lib.optorch_linear_workspace(C.byref(_linear(ldx=65)), 0)
-    assert odd >= 16 * 64 * 2
+    assert odd >= 160 * 64 * 2
     assert lib.optorch_linear_workspace(C.byref(_linear(x=(1 << 20) + 2)), 0) == odd
     # fp32: three planes of each operand
-    assert lib.optorch_linear_workspace(C.byref(_linear(precision=0)), 0) >= (16 + 32) * 64 * 6
+    assert lib.optorch_linear_workspace(C.byref(_linear(precision=0)), 0) >= (160 + 32) * 64 * 6
     # backward with an activation keeps dz
-    assert lib.optorch_linear_workspace(C.byref(_linear()), 1) >= 16 * 32 * 2
+    assert lib.optorch_linear_workspace(C.byref(_linear()), 1) >= 160 * 32 * 2
+    # a forward pass of few samples reads its operands as they lie
+    assert lib.optorch_linear_workspace(C.byref(_linear(rows=16, ldx=65, precision=0)), 0) == 0
     assert lib.optorch_linear_workspace(C.byref(_linear(rows=0)), 0) == 0
 
 
