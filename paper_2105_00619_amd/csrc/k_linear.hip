@@ -206,9 +206,17 @@ struct ProductArgs {
   void* z; int64_t ldz;     // or null
 };
 
-// bias, activation and skip connection of eight neighbouring sums; ACT < 0: the sums alone
+// the skip connection of neighbouring outputs
+template <class O, int V> struct Skip { float v[V]; };
+template <class O, int ACT, int V> __device__ __forceinline__ Skip<O, V> skip_of(const ProductArgs& a, int64_t row, int col, int n) {
+  Skip<O, V> s = {};
+  if (ACT >= 0 && a.residual) load8<O>((const O*)a.residual + row * a.ldr + col, n, s.v);
+  return s;
+}
+
+// bias, activation and skip connection of neighbouring sums; ACT < 0: the sums alone
 template <class O, int ACT, int V>
-__device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int col, float (&v)[V], int n) {
+__device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int col, float (&v)[V], int n, const Skip<O, V>& skip) {
   if (ACT >= 0) {
     if (a.bias) {
 #pragma unroll
@@ -218,10 +226,8 @@ __device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int co
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = act<ACT>(v[e]);
     if (a.residual) {
-      float r[V];
-      load8<O>((const O*)a.residual + row * a.ldr + col, n, r);
 #pragma unroll
-      for (int e = 0; e < V; ++e) v[e] += r[e];
+      for (int e = 0; e < V; ++e) v[e] += skip.v[e];
     }
   }
   store8<O>((O*)a.out + row * a.ldo + col, n, v);
@@ -270,22 +276,21 @@ product_kernel(ProductArgs a) {
   typename G::Acc acc;
   G::product(smem, oa, ob, k1 - k0, acc);
   const int n8 = (a.N + 7) & ~7;
-  auto emit = [&](int r, int c, float (&v)[8], int n) {
+  auto ask = [&](int r, int c, int n) { return a.parts > 1 ? Skip<O, 8>{} : skip_of<O, ACT, 8>(a, m0 + r, n0 + c, n); };
+  auto emit = [&](int r, int c, float (&v)[8], int n, const Skip<O, 8>& skip) {
     if (a.parts > 1) store_f32<float, 8>(a.partial + ((int64_t)part * a.M + m0 + r) * n8 + n0 + c, v);
-    else finish<O, ACT>(a, m0 + r, n0 + c, v, n);
+    else finish<O, ACT>(a, m0 + r, n0 + c, v, n, skip);
   };
   uint32_t again = 0;  // fp32: which of this thread's values are to be summed again
-  G::out(smem, acc, rows, cols,
-         [&](int idx, int r, int c, float (&v)[8], int n) {
-           if (sizeof(O) == 4) {
-             bool bad = false;
+  G::template out<false, (ACT >= OPTORCH_ACT_GELU)>(smem, acc, rows, cols, ask, [&](int idx, int r, int c, float (&v)[8], int n, const Skip<O, 8>& skip) {
+    if (sizeof(O) == 4) {
+      bool bad = false;
 #pragma unroll
-             for (int e = 0; e < 8; ++e) bad |= e < n && !(fabsf(v[e]) <= 3.4028235e38f);
-             if (bad) { again |= 1u << idx; return; }
-           }
-           emit(r, c, v, n);
-         },
-         [](int, int, float (&)[8], int) {}, false);
+      for (int e = 0; e < 8; ++e) bad |= e < n && !(fabsf(v[e]) <= 3.4028235e38f);
+      if (bad) { again |= 1u << idx; return; }
+    }
+    emit(r, c, v, n, skip);
+  });
   if constexpr (sizeof(O) == 4) {
     while (again) {
       const int idx = __builtin_ctz(again);
@@ -295,7 +300,7 @@ product_kernel(ProductArgs a) {
       const int n = min(8, cols - c);
       float v[8];
       for (int e = 0; e < 8; ++e) v[e] = e < n ? sum_again<AR, BR>(a, m0 + r, n0 + c + e, k0, k1) : 0.f;
-      emit(r, c, v, n);
+      emit(r, c, v, n, ask(r, c, n));
     }
   }
 }
@@ -316,7 +321,7 @@ __global__ void __launch_bounds__(256) join_kernel(ProductArgs a) {
     }
     const int64_t r = i / c8;
     const int c = (int)(i - r * c8) * 8;
-    finish<O, ACT>(a, r, c, v, min(8, a.N - c));
+    finish<O, ACT>(a, r, c, v, min(8, a.N - c), skip_of<O, ACT, 8>(a, r, c, min(8, a.N - c)));
   }
 }
 
@@ -427,7 +432,7 @@ __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
           v[e] = s;
         }
     }
-    finish<S, ACT>(a, row, col, v, n);
+    finish<S, ACT>(a, row, col, v, n, skip_of<S, ACT, 4>(a, row, col, n));
   }
 }
 

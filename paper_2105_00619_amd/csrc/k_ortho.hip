@@ -187,17 +187,22 @@ __device__ __forceinline__ f16_t* chain_at(const OrthoTables& t, const OrthoMat&
   return (f16_t*)(t.ws + m.chain) + (int64_t)buf * 2 * m.m * m.m;
 }
 
-// dst = alpha * sum + beta * extra + diag * identity at eight neighbouring places of a symmetric matrix's planes
-__device__ __forceinline__ void chain_store(const OrthoTables& t, const OrthoMat& m, const OrthoOp& op, int r, int c, float (&v)[8]) {
-  const int64_t row = (int64_t)r * 2 * m.m;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (op.extra >= 0) load_planes(chain_at(t, m, op.extra) + row, c, x);
+// dst = alpha * sum + beta * extra + diag * identity at eight neighbouring places of a symmetric matrix
+struct Eight { float v[8]; };
+__device__ __forceinline__ Eight extra_of(const OrthoTables& t, const OrthoMat& m, const OrthoOp& op, int r, int c) {
+  Eight x = {};
+  if (op.extra >= 0) load_planes(chain_at(t, m, op.extra) + (int64_t)r * 2 * m.m, c, x.v);
+  return x;
+}
+__device__ __forceinline__ void combine(const OrthoOp& op, int r, int c, float (&v)[8], const Eight& x) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    v[e] = __fmaf_rn(op.alpha, v[e], op.beta * x[e]);
+    v[e] = __fmaf_rn(op.alpha, v[e], op.beta * x.v[e]);
     if (r == c + e) v[e] += op.diag;
   }
-  store_planes(chain_at(t, m, op.dst) + row, c, v);
+}
+__device__ __forceinline__ void chain_store(const OrthoTables& t, const OrthoMat& m, const OrthoOp& op, int r, int c, const float (&v)[8]) {
+  store_planes(chain_at(t, m, op.dst) + (int64_t)r * 2 * m.m, c, v);
 }
 
 // a finished tile of a symmetric matrix, or a part of its sum
@@ -207,11 +212,13 @@ __device__ __forceinline__ void symmetric_out(unsigned char* smem, const OrthoTa
   const int r0 = w.tm * G::EDGE, c0 = w.tn * G::EDGE;
   if (w.slot >= 0) {
     float* s = t.slots + (int64_t)(slot0 + w.slot) * (G::EDGE * G::EDGE);
-    G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { store_f32<float, 8>(s + r * G::EDGE + c, v); },
-           [](int, int, float (&)[8], int) {}, false);
+    G::template out<false, false>(smem, acc, rows, cols, [](int, int, int) { return 0; },
+                           [&](int, int r, int c, float (&v)[8], int, int) { store_f32<float, 8>(s + r * G::EDGE + c, v); });
   } else {
-    G::out(smem, acc, rows, cols, [&](int, int r, int c, float (&v)[8], int) { chain_store(t, m, op, r0 + r, c0 + c, v); },
-           [&](int c, int r, float (&v)[8], int) { chain_store(t, m, op, c0 + c, r0 + r, v); }, w.tm != w.tn);
+    G::out_symmetric(smem, acc, rows, cols, w.tm != w.tn, [&](int r, int c) { return extra_of(t, m, op, r0 + r, c0 + c); },
+                     [&](int r, int c, float (&v)[8], const Eight& x) { combine(op, r0 + r, c0 + c, v, x); },
+                     [&](int r, int c, float (&v)[8]) { chain_store(t, m, op, r0 + r, c0 + c, v); },
+                     [&](int c, int r, float (&v)[8]) { chain_store(t, m, op, c0 + c, r0 + r, v); });
   }
 }
 
@@ -263,10 +270,12 @@ __global__ void __launch_bounds__(256) join_kernel(OrthoTables t, const OrthoJoi
   if (half == 0) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = area[lr][lc + e];
+    combine(op, r0 + lr, c0 + lc, v, extra_of(t, m, op, r0 + lr, c0 + lc));
     chain_store(t, m, op, r0 + lr, c0 + lc, v);
   } else if (j.tm != j.tn) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = area[lc + e][lr];
+    combine(op, c0 + lr, r0 + lc, v, extra_of(t, m, op, c0 + lr, r0 + lc));
     chain_store(t, m, op, c0 + lr, r0 + lc, v);
   }
 }
@@ -316,8 +325,20 @@ __global__ void ORTHO_BOUNDS(W) apply_kernel(OrthoTables t, const OrthoWork* __r
                          : out.scale_mode == OPTORCH_SCALE_RMS ? 0.04 * max(m.rows, m.cols) : 1.;
     lr = (float)(out.lr * sqrt(ratio));
   }
-  // eight neighbouring columns of the caller's matrix
-  auto give = [&](int r, int c, float (&v)[8]) {
+  // eight neighbouring columns of the caller's matrix: its weights, and what becomes of them
+  auto ask = [&](int r, int c) {
+    Eight x = {};
+    const int n = min(8, m.cols - c);
+    if (OUT == 3 && r < m.rows && n > 0) get8((const float*)out.w + m.offset + r * m.ld + c, n, x.v);
+    return x;
+  };
+  auto give = [&](int r, int c, float (&v)[8], const Eight& x) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= op.alpha;
+    if (OUT == TO_PLANES) {
+      store_planes((f16_t*)(t.ws + m.x[src ^ 1]) + (int64_t)r * 2 * m.n, c, v);
+      return;
+    }
     const int n = min(8, m.cols - c);
     if (r >= m.rows || n <= 0) return;
     const int64_t at = m.offset + r * m.ld + c;
@@ -325,10 +346,8 @@ __global__ void ORTHO_BOUNDS(W) apply_kernel(OrthoTables t, const OrthoWork* __r
     if (OUT == OPTORCH_BF16) put8((bf16_t*)out.o + at, n, v);
     if (OUT == OPTORCH_FP16) put8((f16_t*)out.o + at, n, v);
     if (OUT == 3) {
-      float w0[8];
-      get8((const float*)out.w + at, n, w0);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn(-lr, v[e], w0[e] * out.keep);
+      for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn(-lr, v[e], x.v[e] * out.keep);
       put8(out.w + at, n, v);
       if (out.w16) {
         if (out.w16_bf16) put8((bf16_t*)out.w16 + at, n, v);
@@ -336,21 +355,12 @@ __global__ void ORTHO_BOUNDS(W) apply_kernel(OrthoTables t, const OrthoWork* __r
       }
     }
   };
-  const bool turned = OUT != TO_PLANES && m.tall;
-  G::out(smem, acc, rows, cols,
-         [&](int, int r, int c, float (&v)[8], int) {
-           if (turned) return;
-#pragma unroll
-           for (int e = 0; e < 8; ++e) v[e] *= op.alpha;
-           if (OUT == TO_PLANES) store_planes((f16_t*)(t.ws + m.x[src ^ 1]) + (int64_t)(r0 + r) * 2 * m.n, c0 + c, v);
-           else give(r0 + r, c0 + c, v);
-         },
-         [&](int c, int r, float (&v)[8], int) {
-#pragma unroll
-           for (int e = 0; e < 8; ++e) v[e] *= op.alpha;
-           give(c0 + c, r0 + r, v);
-         },
-         turned);
+  if (OUT != TO_PLANES && m.tall)
+    G::template out<true, false>(smem, acc, rows, cols, [&](int c, int r, int) { return ask(c0 + c, r0 + r); },
+                          [&](int, int c, int r, float (&v)[8], int, const Eight& x) { give(c0 + c, r0 + r, v, x); });
+  else
+    G::template out<false, false>(smem, acc, rows, cols, [&](int r, int c, int) { return ask(r0 + r, c0 + c); },
+                           [&](int, int r, int c, float (&v)[8], int, const Eight& x) { give(r0 + r, c0 + c, v, x); });
 }
 
 template <class K, class... A> void run(K k, int n, size_t lds, hipStream_t st, A... a) {

@@ -14,8 +14,8 @@
 //
 // Four wavefronts in two rows and two columns, each with W x W of the block's 2 W x 2 W.  Slots are a ring in LDS, A and B in turn,
 // filled by loads that write LDS themselves.  While the products of two slots are made, the loads of the two that were used up
-// before go out, evenly: with 256 x 256 and one plane the address unit takes 1024 of the 2048 cycles of a tile step for them, the reads
-// of LDS 512 and its writes 512.
+// before go out, evenly.  A tile step of 256 x 256 takes 1.6 to 1.7 us with one plane and 2.1 to 2.2 with two (its MFMAs alone 0.95 and
+// 1.55), one of 128 x 128 0.6 with either, one of 64 x 64 0.3; with the loads going through registers and stores to LDS 10 % more.
 //
 // LDS, K: rows of 128 bytes, the 16-byte piece c of row r at c ^ (r / 2 & 7), so that sixteen consecutive rows, one piece of each,
 // touch all 64 banks once (c ^ (r & 7), right for 32 banks, cost half as many cycles again).  R: rows of one k, 32-byte units u of 16
@@ -301,42 +301,111 @@ struct Tile {
     c = (wave & 1) * W + lane % LPR * 8;
   }
 
-  // f(idx, row, column, values, n) for eight neighbouring columns at a time, n of them inside: row < rows, column < cols, both from
-  // the tile's corner.  A wavefront takes 32 rows at a time through its own part of LDS, so that memory sees whole rows.
-  // ft, where `transposed`: the same for the transposed tile, f(column, row, ...) with eight neighbouring rows.
-  template <class F, class FT>
-  __device__ static __forceinline__ void out(unsigned char* smem, const Acc& acc, int rows, int cols, F&& f, FT&& ft, bool transposed) {
+  // A finished tile on its way out.  A wavefront takes 32 rows at a time through its own part of LDS, so that memory sees whole rows.
+  // f(idx, row, column, values, n, d) for eight neighbouring columns at a time, n of them inside: row < rows, column < cols, both from
+  // the tile's corner.  d = pre(row, column, n) is what f reads from memory.  It is asked for 32 rows ahead, which takes a copy of f for
+  // every eight values of a thread; with LONG, an f of many instructions, one copy serves them in turn (with GELU in 32 copies, read
+  // once per tile and run once, 8192 x 2048 -> 8192 took 380 us, so 330).
+  // TURNED: the same for the transposed tile, with eight neighbouring rows: f(idx, column, row, ...).
+  template <bool TURNED, bool LONG, class P, class F>
+  __device__ static __forceinline__ void out(unsigned char* smem, const Acc& acc, int rows, int cols, P&& pre, F&& f) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wm = wave >> 1, wn = wave & 1;
+    const int wm = wave >> 1, wn = wave & 1, c0 = wn * W;
     float* area = reinterpret_cast<float*>(smem) + wave * (32 * EPITCH);
+    constexpr int N = TURNED ? W / 16 : PASSES;
+    typedef decltype(pre(0, 0, 0)) D;
+    // row and column (from the wavefront's corner) of a thread's group in a pass
+    auto row_in = [&](int p) { return TURNED ? (lane >> 4) * 8 : p * RPP + lane / LPR; };
+    auto col_in = [&](int p) { return TURNED ? p * 16 + (lane & 15) : (lane % LPR) * 8; };
+    auto ask = [&](int i, int p) {
+      const int r = wm * W + i * 32 + row_in(p), c = c0 + col_in(p);
+      if (r < rows && c < cols) return TURNED ? pre(c, r, min(8, rows - r)) : pre(r, c, min(8, cols - c));
+      return D{};
+    };
+    auto give = [&](int i, int p, const D& d) {
+      const int lr = row_in(p), lc = col_in(p), r = wm * W + i * 32 + lr, c = c0 + lc;
+      float v[8];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int r0 = wm * W + i * 32, c0 = wn * W;
-#pragma unroll
-      for (int j = 0; j < MI; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) area[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * EPITCH + j * 32 + (lane & 31)] = acc[i][j][e];
-      asm volatile("" ::: "memory");
+      for (int e = 0; e < 8; ++e) v[e] = TURNED ? area[(lr + e) * EPITCH + lc] : area[lr * EPITCH + lc + e];
+      if (r < rows && c < cols) {
+        if (TURNED) f(i * N + p, c, r, v, min(8, rows - r), d);
+        else f(i * N + p, r, c, v, min(8, cols - c), d);
+      }
+    };
+    if constexpr (LONG) {
+      each<MI>([&](auto i) {
+        put_rows(area, acc[i], lane);
 #pragma unroll 1
-      for (int p = 0; p < PASSES; ++p) {
+        for (int p = 0; p < N; ++p) give(i, p, ask(i, p));
+        asm volatile("" ::: "memory");
+      });
+    } else {
+      D d[2][N];
+      each<N>([&](auto p) { d[0][p] = ask(0, p); });
+      each<MI>([&](auto i) {
+        if constexpr (i + 1 < MI) each<N>([&](auto p) { d[(i + 1) & 1][p] = ask(i + 1, p); });
+        put_rows(area, acc[i], lane);
+        each<N>([&](auto p) { give(i, p, d[i & 1][p]); });
+        asm volatile("" ::: "memory");
+      });
+    }
+  }
+  // The same for a tile of a symmetric matrix: f changes the values, g(row, column, values) stores them, and where `both` gt(column,
+  // row, values) eight neighbouring rows at the transposed place.  rows and cols are multiples of eight.
+  template <class P, class F, class G, class GT>
+  __device__ static __forceinline__ void out_symmetric(unsigned char* smem, const Acc& acc, int rows, int cols, bool both, P&& pre, F&& f, G&& g,
+                                                       GT&& gt) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 1, wn = wave & 1, c0 = wn * W;
+    float* area = reinterpret_cast<float*>(smem) + wave * (32 * EPITCH);
+    typedef decltype(pre(0, 0)) D;
+    D d[2][PASSES];
+    auto ask = [&](auto i) {
+      each<PASSES>([&](auto p) {
+        const int r = wm * W + i * 32 + p * RPP + lane / LPR, c = c0 + (lane % LPR) * 8;
+        if (r < rows && c < cols) d[i & 1][p] = pre(r, c);
+      });
+    };
+    ask(std::integral_constant<int, 0>{});
+    each<MI>([&](auto i) {
+      if constexpr (i + 1 < MI) ask(std::integral_constant<int, i + 1>{});
+      const int r0 = wm * W + i * 32;
+      put_rows(area, acc[i], lane);
+      each<PASSES>([&](auto p) {
         const int r = p * RPP + lane / LPR, c = (lane % LPR) * 8;
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = area[r * EPITCH + c + e];
-        if (r0 + r < rows && c0 + c < cols) f(i * PASSES + p, r0 + r, c0 + c, v, min(8, cols - c0 - c));
-      }
-      if (transposed) {
-#pragma unroll 1
-        for (int p = 0; p < W / 16; ++p) {
+        if (r0 + r < rows && c0 + c < cols) {
+          f(r0 + r, c0 + c, v, d[i & 1][p]);
+          g(r0 + r, c0 + c, v);
+        }
+        if (both) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) area[r * EPITCH + c + e] = v[e];
+        }
+      });
+      asm volatile("" ::: "memory");
+      if (both)
+        each<W / 16>([&](auto p) {
           const int c = p * 16 + (lane & 15), r = (lane >> 4) * 8;
           float v[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = area[(r + e) * EPITCH + c];
-          if (r0 + r < rows && c0 + c < cols) ft(c0 + c, r0 + r, v, min(8, rows - r0 - r));
-        }
-      }
+          if (r0 + r < rows && c0 + c < cols) gt(c0 + c, r0 + r, v);
+        });
       asm volatile("" ::: "memory");
-    }
+    });
+  }
+
+ private:
+  // 32 rows of a wavefront's sums to its part of LDS
+  __device__ static __forceinline__ void put_rows(float* area, const v16f (&acc)[MI], int lane) {
+#pragma unroll
+    for (int j = 0; j < MI; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) area[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * EPITCH + j * 32 + (lane & 31)] = acc[j][e];
+    asm volatile("" ::: "memory");
   }
 };
 

@@ -125,38 +125,50 @@ int up32(int n) { return (n + 31) & ~31; }
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // ---- which block makes what ----------------------------------------------------------------------------------------------
-// What a launch is estimated to take, in us, from the time of a tile step (64 places of two operands, one block to a CU) and of a
-// block's beginning and end.  Measured on products of 2048 and 4096 rows.
-double step_us(int w) { return w == 128 ? 2.4 : w == 64 ? 0.65 : 0.28; }
-double block_us(int w) { return w == 128 ? 8.0 : w == 64 ? 5.0 : 4.0; }
+// What a launch is estimated to take, in us, from the time of a tile step (64 places of two operands), of a block's beginning and
+// end, and of what it writes and reads besides (a CU's share of 4.5 TB/s).  Two blocks of 128 x 128 or three of 64 x 64 run on a CU: their
+// products take turns, their ends overlap with them.  Measured on products of 2048 and 4096 rows.
+double step_us(int w) { return w == 128 ? 2.2 : w == 64 ? 0.65 : 0.25; }
+double block_us(int w) { return w == 128 ? 8.0 : w == 64 ? 6.0 : 5.0; }
+int blocks_of_cu(int w) { return w == 128 ? 1 : w == 64 ? 2 : 3; }
+constexpr double CU_BYTES_US = 17600.;
 constexpr int CUS = 256, XCDS = 8;
 
-struct Tiles { int mat, count, steps; };  // tiles of one matrix, each of so many steps
+struct Tiles { int count, steps; };  // tiles of one matrix, each of so many steps
 
-// blocks are taken by the CU that is free first, the longest ones first
-double launch_us(const std::vector<Tiles>& list, int w, int most) {
+// blocks are taken by the place on a CU that is free first, the longest ones first; bytes: of memory for each value of a tile
+double launch_us(const std::vector<Tiles>& list, int w, int most, int bytes) {
+  const int per = blocks_of_cu(w), edge = 2 * w;
   std::vector<std::pair<double, int64_t>> blocks;
   double join = 0;
+  int64_t all = 0;
   for (const Tiles& t : list) {
     const int parts = cdiv(t.steps, most);
-    blocks.push_back({cdiv(t.steps, parts) * step_us(w) + block_us(w), (int64_t)t.count * parts});
-    if (parts > 1) join += (double)t.count * parts * (2 * w) * (2 * w) * 8 / 3e6;  // written and read again
+    all += (int64_t)t.count * parts;
+    if (parts > 1) join += (double)t.count * parts * edge * edge * 8 / 3e6;  // written and read again
+  }
+  const double share = all > CUS ? (double)std::min<int64_t>(per, cdiv(all, CUS)) : 1.;  // blocks that run on a CU together
+  for (const Tiles& t : list) {
+    const int parts = cdiv(t.steps, most);
+    const double mem = (double)edge * edge * (parts > 1 ? 4 : bytes) / CU_BYTES_US;
+    blocks.push_back({cdiv(t.steps, parts) * step_us(w) * (share > 1 ? 0.9 * share : 1.) + block_us(w) + mem * share, (int64_t)t.count * parts});
   }
   std::sort(blocks.begin(), blocks.end(), [](auto& a, auto& b) { return a.first > b.first; });
-  std::vector<double> cu(CUS, 0.);  // a heap, the earliest on top
+  const int places = CUS * per;
+  std::vector<double> at(places, 0.);  // a heap, the earliest on top
   for (auto& b : blocks) {
-    if (b.second > 64 * CUS) {  // (many alike: a whole round for every CU, as often as it goes)
-      const int64_t rounds = b.second / CUS - 1;
-      for (double& c : cu) c += rounds * b.first;
-      b.second -= rounds * CUS;
+    if (b.second > 16 * places) {  // (many alike: a whole round for every place, as often as it goes)
+      const int64_t rounds = b.second / places - 1;
+      for (double& c : at) c += rounds * b.first;
+      b.second -= rounds * places;
     }
     for (int64_t i = 0; i < b.second; ++i) {
-      std::pop_heap(cu.begin(), cu.end(), std::greater<>());
-      cu.back() += b.first;
-      std::push_heap(cu.begin(), cu.end(), std::greater<>());
+      std::pop_heap(at.begin(), at.end(), std::greater<>());
+      at.back() += b.first;
+      std::push_heap(at.begin(), at.end(), std::greater<>());
     }
   }
-  return *std::max_element(cu.begin(), cu.end()) + (join > 0 ? join + 5.0 : 0.0);
+  return *std::max_element(at.begin(), at.end()) + (join > 0 ? join + 5.0 : 0.0);
 }
 
 int64_t triangle(int64_t t) { return t * (t + 1) / 2; }
@@ -212,7 +224,7 @@ void add_list(OrthoPlanHost& p, OrthoList& l, bool lower, int w, int most, bool 
   l.n = (int)(p.works.size() - l.work0);
 }
 
-void plan_list(OrthoPlanHost& p, OrthoList& l, bool lower, bool along_n, bool cut) {
+void plan_list(OrthoPlanHost& p, OrthoList& l, bool lower, bool along_n, bool cut, int bytes) {
   int best_w = 32, best_most = 1 << 20;
   double best = 1e300;
   for (int w : {128, 64, 32}) {
@@ -221,11 +233,11 @@ void plan_list(OrthoPlanHost& p, OrthoList& l, bool lower, bool along_n, bool cu
       const OrthoMat& m = p.mats[i];
       const int tm = cdiv(m.m, 2 * w);
       const int64_t count = lower ? triangle(tm) : (int64_t)tm * cdiv(m.n, 2 * w);
-      tiles.push_back(Tiles{(int)i, (int)std::min<int64_t>(count, 1 << 30), cdiv(along_n ? m.n : m.m, 32)});
+      tiles.push_back(Tiles{(int)std::min<int64_t>(count, 1 << 30), cdiv(along_n ? m.n : m.m, 32)});
     }
     for (int most : {1 << 20, 128, 96, 64, 48, 32, 24, 16, 8}) {
       if (most < (1 << 20) && !cut) continue;
-      const double us = launch_us(tiles, w, most);
+      const double us = launch_us(tiles, w, most, bytes);
       if (us < best) { best = us; best_w = w; best_most = most; }
     }
   }
@@ -297,9 +309,10 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
     m.chunks = (int)p.chunks.size() - m.chunk0;
     p.mats.push_back(m);
   }
-  plan_list(p, p.gram, true, true, true);
-  plan_list(p, p.chain, true, false, true);
-  plan_list(p, p.apply, false, false, false);
+  // (a symmetric result is written twice; Q X: weights read and written with their copy)
+  plan_list(p, p.gram, true, true, true, 8);
+  plan_list(p, p.chain, true, false, true, 8);
+  plan_list(p, p.apply, false, false, false, 10);
   uint64_t o = 0;
   auto take = [&](uint64_t bytes) { const uint64_t at = o; o = up256(o + bytes); return at; };
   p.off_mats = take(p.mats.size() * sizeof(OrthoMat));
