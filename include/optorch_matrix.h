@@ -41,7 +41,7 @@ typedef enum {
 typedef struct {
   int32_t precision, activation;
   int64_t rows;                       /* samples; 0 is allowed */
-  int32_t in_features, out_features;  /* 1 .. 2^22 - 8, leading dimensions too */
+  int32_t in_features, out_features;  /* 1 .. 2^22 - 8, leading dimensions too; fp32: 1 .. 2^20 - 16 */
   const void* x; int64_t ldx;         /* rows x in */
   const void* w; int64_t ldw;         /* out x in */
   const float* bias;                  /* out, or NULL */

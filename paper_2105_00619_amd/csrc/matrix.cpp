@@ -34,7 +34,8 @@ static int bytes_of(int32_t p) { return p == OPTORCH_FP32 ? 4 : 2; }
 
 // ---- linear layers -----------------------------------------------------------------------------------------------------
 
-static constexpr int64_t kMaxFeatures = (1 << 22) - 8;  // offsets inside a tile are 32-bit
+// Offsets inside a tile are 32-bit: 256 rows take less than 2^31 bytes.  A row of fp32 values laid out as planes takes 8 bytes a value.
+static constexpr int64_t kMaxFeatures = (1 << 22) - 8, kMaxFeatures32 = (1 << 20) - 16;
 
 static int linear_check(const optorch_linear_t* a, bool backward) {
   if (!a) return oseq_mat_err(OPTORCH_E_INVALID, "null arguments");
@@ -43,6 +44,8 @@ static int linear_check(const optorch_linear_t* a, bool backward) {
   if (a->rows < 0 || a->rows > 0x7fffff00) return oseq_mat_err(OPTORCH_E_INVALID, "rows must be 0 .. 2^31 - 256");
   if (a->in_features < 1 || a->out_features < 1 || a->in_features > kMaxFeatures || a->out_features > kMaxFeatures)
     return oseq_mat_err(OPTORCH_E_INVALID, "in_features and out_features must be 1 .. 2^22 - 8");
+  if (a->precision == OPTORCH_FP32 && (a->in_features > kMaxFeatures32 || a->out_features > kMaxFeatures32))
+    return oseq_mat_err(OPTORCH_E_INVALID, "in fp32 in_features and out_features must be 1 .. 2^20 - 16");
   const int esize = bytes_of(a->precision);
   // a matrix that is used: present, its rows apart, its elements aligned
   auto matrix = [&](const void* p, int64_t ld, int32_t cols, const char* name) {

@@ -71,6 +71,21 @@ def test_linear_refusals(kw, backward, word):
     assert word in lib.optorch_matrix_last_error().decode()
 
 
+def test_fp32_rows_of_planes_stay_inside_32_bit_offsets():
+    """256 rows of a tile are addressed by 32-bit offsets, and a row of fp32 values as planes takes 8 bytes a value."""
+    lib = B.load_library()
+    most = (1 << 20) - 16
+    assert 256 * 8 * most < 1 << 31 < 256 * 8 * (most + 16) + 1
+    wide = dict(ldx=most + 1, ldw=most + 1, lddx=most + 1, lddw=most + 1)
+    long = dict(ldy=most + 1, ldz=most + 1, ldr=most + 1, lddy=most + 1)
+    for backward in (0, 1):
+        for name, lds in (("in_features", wide), ("out_features", long)):
+            assert lib.optorch_linear_workspace(C.byref(_linear(precision=0, **{name: most}, **lds)), backward) > 0
+            assert lib.optorch_linear_workspace(C.byref(_linear(precision=0, **{name: most + 1}, **lds)), backward) == E_INVALID
+            assert "fp32" in lib.optorch_matrix_last_error().decode()
+            assert lib.optorch_linear_workspace(C.byref(_linear(**{name: most + 1}, **lds)), backward) >= 0
+
+
 def test_linear_refuses_a_missing_small_or_misaligned_workspace():
     lib = B.load_library()
     a = _linear(precision=0)
