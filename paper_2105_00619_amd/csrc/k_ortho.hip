@@ -1,7 +1,7 @@
 // Orthogonalised updates: the kernels of the plan made in ortho.cpp.  Every launch does its part for all matrices of the list; a
 // block finds its matrix and tile in a table.
 //   norms    sum of squares of each piece of a matrix, in 64 bits
-//   scales   1 / max(norm, eps) per matrix, and whether all its elements are finite
+//   scales   1 / max(norm, eps) per matrix, and whether all its elements are finite (with few pieces: part of the next)
 //   planes   the first iterate: elements times the scale as two fp16 planes, padded with zeros; momentum is updated on the way
 //   products X X^T, then m x m products (half of the tiles: they are symmetric), then Q X (ortho.cpp)
 #include <math.h>
@@ -121,39 +121,50 @@ __global__ void __launch_bounds__(256) norms_kernel(OrthoTables t, Source s) {
   if (threadIdx.x == 0) t.partial[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__global__ void __launch_bounds__(256) scales_kernel(OrthoTables t, float eps, double times) {
-  __shared__ double part[4];
-  const OrthoMat& m = t.mats[blockIdx.x];
+// sum of squares of a matrix from its pieces', by a block, and the scale of its first iterate
+__device__ __forceinline__ double norm2_of(const OrthoTables& t, const OrthoMat& m, double (&part)[4]) {
   double sum = 0.;
   for (int i = threadIdx.x; i < m.chunks; i += 256) sum += t.partial[m.chunk0 + i];
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
   __syncthreads();
+  return (part[0] + part[1]) + (part[2] + part[3]);
+}
+__device__ __forceinline__ double scale_of(double norm2, float eps, double times) {
+  const double norm = sqrt(norm2);
+  return times / (norm < (double)eps ? (double)eps : norm);  // (NaN stays NaN)
+}
+
+__global__ void __launch_bounds__(256) scales_kernel(OrthoTables t, float eps, double times) {
+  __shared__ double part[4];
+  const double sum = norm2_of(t, t.mats[blockIdx.x], part);
   if (threadIdx.x == 0) {
-    sum = (part[0] + part[1]) + (part[2] + part[3]);
-    const double norm = sqrt(sum);
-    t.scale[blockIdx.x] = times / (norm < (double)eps ? (double)eps : norm);  // (NaN stays NaN)
+    t.scale[blockIdx.x] = scale_of(sum, eps, times);
     t.bad[blockIdx.x] = sum <= 1.7976931348623157e308 ? 0 : 1;
   }
 }
 
-template <class G, bool MUON>
-__global__ void __launch_bounds__(256) planes_kernel(OrthoTables t, Source s, int32_t* skipped) {
+// FEW pieces (FEW_CHUNKS) in all: every block makes its scale from the pieces' sums itself, which saves a launch
+constexpr int FEW_CHUNKS = 256;
+template <class G, bool MUON, bool FEW>
+__global__ void __launch_bounds__(256) planes_kernel(OrthoTables t, Source s, int32_t* skipped, float eps, double times) {
   __shared__ float turn[128][65];  // a tall matrix' piece on its way to its transposed place
+  __shared__ double part[4];
   const OrthoChunk c = t.chunks[blockIdx.x];
   const OrthoMat& m = t.mats[c.mat];
   bool skip = false;
   if (MUON) {
     bool any = false;
-    for (int i = threadIdx.x; i < t.nmat; i += 256) any |= t.bad[i] != 0;
+    if (FEW) any = (int)threadIdx.x < t.nchunks && !(t.partial[threadIdx.x] <= 1.7976931348623157e308);
+    else for (int i = threadIdx.x; i < t.nmat; i += 256) any |= t.bad[i] != 0;
     skip = __syncthreads_or(any);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
       t.skip[0] = skip;
       if (skipped) *skipped = skip;
     }
   }
-  const double scale = t.scale[c.mat];
+  const double scale = FEW ? scale_of(norm2_of(t, m, part), eps, times) : t.scale[c.mat];
   f16_t* x = (f16_t*)(t.ws + m.x[0]);
   groups_of(c, m, [&](int64_t at, int n, int r, int col) {
     float u[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, vn[8];
@@ -298,6 +309,172 @@ __global__ void ORTHO_BOUNDS(W) chain_kernel(OrthoTables t, const OrthoWork* __r
   symmetric_out<G>(smem, t, m, w, op, second ? slots : 0, rows, cols, acc);
 }
 
+// ---- small matrices ----------------------------------------------------------------------------------------------------
+// All the m x m products between two iterates of a matrix with m <= 128, by one block, a wavefront for each 32 x 32 tile of the lower
+// triangle.  A (then C = P A, then the new A) and P stay in LDS, Q in memory.  A launch for each product takes 3.5 (m = 32) to 5 us
+// (m = 128), most of it waiting for memory and the next launch; here a product takes 1.1 to 3.6, half of that the instructions that
+// round and store a tile: update of matrices of 8 x 27, 8 x 72 and 10 x 8 71 -> 42 us, 100 x 512 orthogonalised 105 -> 96.
+//
+// LDS: rows as in memory, 512 bytes apart, the 16-byte piece i of row r at i ^ (r & 15), so that sixteen neighbouring rows touch all banks
+// and an address is a lane's own part with a constant in exclusive or and a constant offset.
+constexpr int SMALL_PITCH = 4 * ORTHO_SMALL;
+constexpr int small_lds(int m) { return 2 * m * SMALL_PITCH; }
+typedef Op<f16_t>::V V8;
+typedef Vec<f16_t, 4> V4;
+
+__global__ void __launch_bounds__(640) small_chain_kernel(OrthoTables t, OrthoOps ops) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const OrthoMat& mat = t.mats[blockIdx.x];
+  constexpr int pitch = SMALL_PITCH;
+  const int m = mat.m, nt = m / 32;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int ti = 0;
+  while ((ti + 1) * (ti + 2) / 2 <= wave) ++ti;
+  const int tj = wave - ti * (ti + 1) / 2, r0 = ti * 32, c0 = tj * 32, l = lane & 31, h = lane >> 5;
+  const bool mine = ti < nt;
+  const uint32_t area[2] = {0u, (uint32_t)(m * pitch)};
+  auto fold = [](int r) { return (uint32_t)(r & 15); };
+  // whole matrices between memory and LDS
+  const int per = m / 4, inverse = (1 << 18) / per + 1;  // (exact up to i = 4096)
+  auto piece_at = [&](int i) {
+    const int r = (i * inverse) >> 18;
+    return (uint32_t)(r * pitch) + (((uint32_t)(i - r * per) ^ fold(r)) << 4);
+  };
+  auto copy_out = [&](uint32_t from, int buf) {
+    f16_t* d = chain_at(t, mat, buf);
+    for (int i = threadIdx.x; i < m * per; i += blockDim.x)
+      *reinterpret_cast<Vec<f16_t, 8>*>(d + i * 8) = *reinterpret_cast<const Vec<f16_t, 8>*>(smem + from + piece_at(i));
+  };
+  {
+    const f16_t* a = chain_at(t, mat, OB_A);
+    for (int i = threadIdx.x; i < m * per; i += blockDim.x)
+      *reinterpret_cast<Vec<f16_t, 8>*>(smem + piece_at(i)) = *reinterpret_cast<const Vec<f16_t, 8>*>(a + i * 8);
+  }
+  __syncthreads();
+  // a lane's part of the addresses: operands of the tile's rows and columns; four neighbouring rows of its column, transposed; its column
+  const uint32_t row_at = (uint32_t)((r0 + l) * pitch) + (((uint32_t)h ^ fold(l)) << 4), col_at = (uint32_t)((c0 + l) * pitch) + (((uint32_t)h ^ fold(l)) << 4);
+  const uint32_t four_at = (uint32_t)((c0 + l) * pitch) + (((uint32_t)(ti * 8) ^ fold(l)) << 4) + h * 8;
+  const uint32_t one_at = (((uint32_t)(tj * 8 + (l >> 3)) ^ (uint32_t)(4 * h)) << 4) + (l & 7) * 2;
+  // Addresses of a store are made again each time: kept over the loop they spill
+  auto fresh = [](uint32_t v) { asm volatile("" : "+v"(v)); return v; };
+  auto operand = [&](uint32_t at, int k, int g, int plane) {
+    return *reinterpret_cast<const V8*>(smem + (at ^ (uint32_t)((k * 8 + plane * 4 + g * 2) << 4)));
+  };
+  auto products = [&](v16f& acc, const V8& ah, const V8& al, const V8& bh, const V8& bl) {
+    acc = Op<f16_t>::mma(ah, bl, acc);
+    acc = Op<f16_t>::mma(al, bh, acc);
+    acc = Op<f16_t>::mma(ah, bh, acc);
+  };
+  V4 hi[4], lo[4];  // a finished tile: four neighbouring rows at a time
+  auto finish = [&](const OrthoOp& op, const v16f& acc, bool poly) {
+    const uint32_t from = fresh(four_at);
+    each<4>([&](auto q) {
+      float v[4], w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = op.alpha * acc[q * 4 + e];
+      if (poly) {  // (A is symmetric)
+        load_f32<f16_t, 4>(reinterpret_cast<const f16_t*>(smem + (from ^ (q * 16u))), w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __fmaf_rn(op.beta, w[e], v[e]);
+        load_f32<f16_t, 4>(reinterpret_cast<const f16_t*>(smem + (from ^ (q * 16u + 64u))), w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __fmaf_rn(op.beta, w[e], v[e]);
+        if (ti == tj) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] += 8 * q + 4 * h + e == l ? op.diag : 0.f;
+        }
+      }
+      hi[q] = round_vec<f16_t, 4>(v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = v[e] - (float)hi[q].v[e];
+      lo[q] = round_vec<f16_t, 4>(w);
+    });
+  };
+  auto to_lds = [&](uint32_t to) {
+    const uint32_t four = fresh(to + four_at);
+    each<4>([&](auto q) {
+      *reinterpret_cast<V4*>(smem + (four ^ (q * 16u))) = hi[q];
+      *reinterpret_cast<V4*>(smem + (four ^ (q * 16u + 64u))) = lo[q];
+    });
+    if (ti == tj) return;
+    const uint32_t row = fresh(to + (uint32_t)((r0 + 4 * h) * pitch) + one_at);
+    each<16>([&](auto i) {  // (row r0 + 8 q + 4 h + e is folded by 8 (q & 1) + 4 h + e)
+      constexpr int q = i / 4, e = i % 4;
+      *reinterpret_cast<f16_t*>(smem + (row ^ ((8u * (q & 1) + e) << 4)) + (8 * q + e) * pitch) = hi[q].v[e];
+      *reinterpret_cast<f16_t*>(smem + (row ^ ((8u * (q & 1) + e + 4u) << 4)) + (8 * q + e) * pitch) = lo[q].v[e];
+    });
+  };
+  auto to_memory = [&](int buf) {
+    f16_t* d = chain_at(t, mat, buf);
+    const int ld = 2 * m;
+    f16_t* four = d + fresh((c0 + l) * ld + ti * 64 + 4 * h);
+    each<4>([&](auto q) {
+      *reinterpret_cast<V4*>(four + 8 * q) = hi[q];
+      *reinterpret_cast<V4*>(four + 8 * q + 32) = lo[q];
+    });
+    if (ti == tj) return;
+    f16_t* one = d + fresh((r0 + 4 * h) * ld + tj * 64 + l);
+    each<16>([&](auto i) {
+      constexpr int q = i / 4, e = i % 4;
+      one[0] = hi[q].v[e];
+      one[32] = lo[q].v[e];
+      one += e == 3 ? 5 * ld : ld;
+    });
+  };
+  for (int o = 0; o < ops.n; ++o) {
+    const OrthoOp op = ops.op[o];
+    v16f acc;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    const bool to_q = op.dst == OB_Q0 || op.dst == OB_Q1, poly = op.extra >= 0;
+    if (poly) {  // P from A; the first one is Q too
+      if (mine) {
+        for (int k = 0; k < nt; ++k)
+          each<2>([&](auto g) {
+            products(acc, operand(row_at, k, g, 0), operand(row_at, k, g, 1), operand(col_at, k, g, 0), operand(col_at, k, g, 1));
+          });
+        finish(op, acc, true);
+        to_lds(area[1]);
+      }
+      __syncthreads();
+      if (to_q) copy_out(area[1], op.dst);
+    } else if (to_q) {  // Q <- P Q
+      if (mine) {
+        const f16_t* q = chain_at(t, mat, op.b) + (c0 + l) * (2 * m) + h * 8;
+        V8 b[ORTHO_SMALL / 32][4];  // (all of them on their way at once)
+        each<ORTHO_SMALL / 32>([&](auto k) {
+          each<4>([&](auto i) { b[k][i] = *reinterpret_cast<const V8*>(q + min((int)k, nt - 1) * 64 + i * 16); });
+        });
+        each<ORTHO_SMALL / 32>([&](auto k) {
+          if (k < nt)
+            each<2>([&](auto g) {
+              products(acc, operand(area[1] + row_at, k, g, 0), operand(area[1] + row_at, k, g, 1), b[k][g], b[k][g + 2]);
+            });
+        });
+        finish(op, acc, false);
+      }
+      if (o + 1 < ops.n) {
+        if (mine) to_memory(op.dst);
+        __syncthreads();
+      } else {  // (A's place is free)
+        if (mine) to_lds(area[0]);
+        __syncthreads();
+        copy_out(area[0], op.dst);
+      }
+    } else {  // C from P and A, the new A from C and P: they take A's place, which every wavefront has read
+      const uint32_t a_at = row_at + area[op.a == OB_C ? 0 : 1], b_at = col_at + area[op.a == OB_C ? 1 : 0];
+      if (mine) {
+        for (int k = 0; k < nt; ++k)
+          each<2>([&](auto g) { products(acc, operand(a_at, k, g, 0), operand(a_at, k, g, 1), operand(b_at, k, g, 0), operand(b_at, k, g, 1)); });
+        finish(op, acc, false);
+      }
+      __syncthreads();
+      if (mine) to_lds(area[0]);
+      __syncthreads();
+    }
+  }
+}
+
 struct Target {
   void* o;                               // orthogonalize
   float* w; void* w16; int w16_bf16;     // muon
@@ -375,10 +552,21 @@ template <int OUT> void run_apply(hipStream_t st, const OrthoTables& t, const Or
   else run(apply_kernel<32, OUT>, l.n, lds_of<32>(), st, t, w, c.src, c.op[0], o);
 }
 
+void run_small(hipStream_t st, const OrthoTables& t, int m, const OrthoOps& ops) {
+  const int tiles = m / 32 * (m / 32 + 1) / 2, lds = small_lds(m);
+  if (lds > 65536) (void)hipFuncSetAttribute((const void*)small_chain_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  OSEQ_LAUNCH(small_chain_kernel, dim3(t.nmat), dim3(tiles * 64), lds, st, t, ops);
+}
+
 template <class G, bool MUON> void run_elements(hipStream_t st, const OrthoTables& t, const OrthoPlanHost& p, const Source& s, int32_t* skipped) {
   OSEQ_LAUNCH((norms_kernel<G, MUON>), dim3(t.nchunks), dim3(256), 0, st, t, s);
-  OSEQ_LAUNCH(scales_kernel, dim3(t.nmat), dim3(256), 0, st, t, p.eps, (double)p.first_scale);
-  OSEQ_LAUNCH((planes_kernel<G, MUON>), dim3(t.nchunks), dim3(256), 0, st, t, s, skipped);
+  const double times = p.first_scale;
+  if (t.nchunks <= FEW_CHUNKS) {
+    OSEQ_LAUNCH((planes_kernel<G, MUON, true>), dim3(t.nchunks), dim3(256), 0, st, t, s, skipped, p.eps, times);
+  } else {
+    OSEQ_LAUNCH(scales_kernel, dim3(t.nmat), dim3(256), 0, st, t, p.eps, times);
+    OSEQ_LAUNCH((planes_kernel<G, MUON, false>), dim3(t.nchunks), dim3(256), 0, st, t, s, skipped, p.eps, times);
+  }
 }
 
 }  // namespace
@@ -418,13 +606,21 @@ void launch_ortho(hipStream_t st, const OrthoPlanHost& p, char* ws, const OrthoR
     run(join_kernel, l.joins * c.ops * per * per, 0, st, t, joins + l.join0, l.joins, l.slots, edge, c.op[0], c.op[1]);
   };
   // what is stored in fp32 as it is takes the more exact steps
-  for (const OrthoLaunch& c : p.launches[!r.muon && r.o_precision == OPTORCH_FP32]) {
+  const std::vector<OrthoLaunch>& launches = p.launches[!r.muon && r.o_precision == OPTORCH_FP32];
+  for (size_t i = 0; i < launches.size(); ++i) {
+    const OrthoLaunch& c = launches[i];
     if (c.kind == OL_GRAM) {
       const OrthoWork* w = works + p.gram.work0;
       if (p.gram.w == 128) run(gram_kernel<128>, p.gram.n, lds_of<128>(), st, t, w, c.src, c.op[0]);
       else if (p.gram.w == 64) run(gram_kernel<64>, p.gram.n, lds_of<64>(), st, t, w, c.src, c.op[0]);
       else run(gram_kernel<32>, p.gram.n, lds_of<32>(), st, t, w, c.src, c.op[0]);
       join(p.gram, c);
+    } else if (c.kind == OL_CHAIN && p.most_m <= ORTHO_SMALL) {
+      OrthoOps ops = {};
+      for (; launches[i].kind == OL_CHAIN; ++i)  // (an apply follows)
+        for (int k = 0; k < launches[i].ops; ++k) ops.op[ops.n++] = launches[i].op[k];
+      --i;
+      run_small(st, t, p.most_m, ops);
     } else if (c.kind == OL_CHAIN) {
       const OrthoList& l = p.chain;
       const OrthoWork* w = works + l.work0;
@@ -433,12 +629,13 @@ void launch_ortho(hipStream_t st, const OrthoPlanHost& p, char* ws, const OrthoR
       else run(chain_kernel<32>, l.n * c.ops, lds_of<32>(), st, t, w, l.n, l.slots, c.op[0], c.op[1]);
       join(l, c);
     } else {
-      const OrthoWork* w = works + p.apply.work0;
-      if (!c.last) run_apply<TO_PLANES>(st, t, p.apply, w, c, o);
-      else if (r.muon) run_apply<3>(st, t, p.apply, w, c, o);
-      else if (r.o_precision == OPTORCH_FP32) run_apply<OPTORCH_FP32>(st, t, p.apply, w, c, o);
-      else if (r.o_precision == OPTORCH_BF16) run_apply<OPTORCH_BF16>(st, t, p.apply, w, c, o);
-      else run_apply<OPTORCH_FP16>(st, t, p.apply, w, c, o);
+      const OrthoList& l = c.last ? p.last[r.muon] : p.apply;
+      const OrthoWork* w = works + l.work0;
+      if (!c.last) run_apply<TO_PLANES>(st, t, l, w, c, o);
+      else if (r.muon) run_apply<3>(st, t, l, w, c, o);
+      else if (r.o_precision == OPTORCH_FP32) run_apply<OPTORCH_FP32>(st, t, l, w, c, o);
+      else if (r.o_precision == OPTORCH_BF16) run_apply<OPTORCH_BF16>(st, t, l, w, c, o);
+      else run_apply<OPTORCH_FP16>(st, t, l, w, c, o);
     }
   }
 }

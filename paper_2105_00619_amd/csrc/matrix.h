@@ -52,6 +52,12 @@ struct OrthoJoin { int32_t mat, tm, tn, slot, parts; };
 // dst = alpha * (a b) + beta * extra + diag * identity, all of it in planes (extra < 0: none)
 struct OrthoOp { int32_t a, b, dst, extra; float alpha, beta, diag; };
 
+// Lists of small matrices: all steps on A between two iterates in one launch
+constexpr int ORTHO_SMALL = 128;                   // padded shorter side at most
+constexpr int ORTHO_RESTART = 3;                   // steps between two iterates at most
+constexpr int ORTHO_SEGMENT_OPS = 4 * ORTHO_RESTART - 3;
+struct OrthoOps { int n; OrthoOp op[ORTHO_SEGMENT_OPS]; };
+
 // the blocks of one kind of product, in launch order, with wavefront tiles of w
 struct OrthoList {
   int w = 32, n = 0, joins = 0, slots = 0;
@@ -77,8 +83,9 @@ struct OrthoPlanHost {
   std::vector<OrthoChunk> chunks;
   std::vector<OrthoWork> works;   // all lists, one behind the other
   std::vector<OrthoJoin> joins;
-  OrthoList gram, chain, apply;
+  OrthoList gram, chain, apply, last[2];  // last: Q X to the caller's vectors; [1]: to weights
   std::vector<OrthoLaunch> launches[2];  // [1]: for results of fp32
+  int most_m = 0;                        // the largest padded shorter side
   float eps = 1e-7f, first_scale = 1.f;  // first_scale: power of two of the first iterate's planes
   int64_t span = 0;
   uint64_t off_mats = 0, off_chunks = 0, off_works = 0, off_joins = 0, off_partial = 0, off_scale = 0, off_bad = 0, off_slots = 0,

@@ -38,7 +38,7 @@ namespace {
 // beyond 2^12 (the low plane of a value of 2^-12 then still has all its bits)
 float plane_scale(double bound) { return (float)std::exp2(std::min(12.0, std::floor(std::log2(16384.0 / std::max(bound, 1e-3))))); }
 
-constexpr int RESTART[2] = {3, 2};  // steps on A between two iterates; [1]: for results of fp32
+constexpr int RESTART[2] = {ORTHO_RESTART, 2};  // steps on A between two iterates; [1]: for results of fp32
 
 // The launches and their scales.  Returns false where the steps let a singular value grow too far.
 bool plan_steps(OrthoPlanHost& p, std::vector<OrthoLaunch>& launches, int restart, int steps, const float* co) {
@@ -126,32 +126,68 @@ int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // ---- which block makes what ----------------------------------------------------------------------------------------------
 // What a launch is estimated to take, in us, from the time of a tile step (64 places of two operands), of a block's beginning and
-// end, and of what it writes and reads besides (a CU's share of 4.5 TB/s).  Two blocks of 128 x 128 or three of 64 x 64 run on a CU: their
-// products take turns, their ends overlap with them.  Measured on products of 2048 and 4096 rows.
-double step_us(int w) { return w == 128 ? 2.2 : w == 64 ? 0.65 : 0.25; }
+// end, and of what it writes and reads besides (a CU's share of 4.5 TB/s; alone on its CU a block does not reach it).  Two blocks of
+// 128 x 128 or three of 64 x 64 run on a CU: their products take turns, their ends overlap with them.  Measured on products of 2048 and
+// 4096 rows and on ResNet-152's, whose last products take 380 us as 256 x 256 tiles and 310 as 128 x 128.
+double step_us(int w) { return w == 128 ? 2.0 : w == 64 ? 0.65 : 0.25; }
 double block_us(int w) { return w == 128 ? 8.0 : w == 64 ? 6.0 : 5.0; }
 int blocks_of_cu(int w) { return w == 128 ? 1 : w == 64 ? 2 : 3; }
-constexpr double CU_BYTES_US = 17600.;
+constexpr double CU_BYTES_US = 17600., CU_BYTES_US_ALONE = 11000.;
 constexpr int CUS = 256, XCDS = 8;
 
-struct Tiles { int count, steps; };  // tiles of one matrix, each of so many steps
+// How the tiles of one matrix are cut: the first `whole` in one block each, the others' sums in `parts` of `per` steps
+struct Cut { int64_t count, whole; int steps, parts, per; };
+
+int64_t triangle(int64_t t) { return t * (t + 1) / 2; }
+
+// Sums of more than `most` steps are cut; with `tail` only those of the tiles that do not fill a round of all places (the shortest
+// sums), which come last.
+std::vector<Cut> cuts_of(const OrthoPlanHost& p, bool lower, bool along_n, int w, int most, bool tail) {
+  std::vector<Cut> cuts;
+  std::vector<int> order;
+  int64_t all = 0;
+  for (size_t i = 0; i < p.mats.size(); ++i) {
+    const OrthoMat& m = p.mats[i];
+    const int tm = cdiv(m.m, 2 * w), K = along_n ? m.n : m.m;
+    Cut c = {};
+    c.count = lower ? triangle(tm) : (int64_t)tm * cdiv(m.n, 2 * w);
+    c.steps = cdiv(K, 32);
+    c.per = cdiv(c.steps, cdiv(c.steps, most));
+    c.parts = cdiv(c.steps, c.per);
+    cuts.push_back(c);
+    order.push_back((int)i);
+    all += c.count;
+  }
+  const int places = CUS * blocks_of_cu(w);
+  int64_t whole = tail ? all / places * places : 0;
+  std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return cuts[a].steps > cuts[b].steps; });
+  for (int i : order) {
+    Cut& c = cuts[i];
+    c.whole = c.parts == 1 ? c.count : std::min(whole, c.count);
+    whole -= std::min(whole, c.count);
+  }
+  return cuts;
+}
 
 // blocks are taken by the place on a CU that is free first, the longest ones first; bytes: of memory for each value of a tile
-double launch_us(const std::vector<Tiles>& list, int w, int most, int bytes) {
+double launch_us(const std::vector<Cut>& list, int w, int bytes) {
   const int per = blocks_of_cu(w), edge = 2 * w;
   std::vector<std::pair<double, int64_t>> blocks;
   double join = 0;
   int64_t all = 0;
-  for (const Tiles& t : list) {
-    const int parts = cdiv(t.steps, most);
-    all += (int64_t)t.count * parts;
-    if (parts > 1) join += (double)t.count * parts * edge * edge * 8 / 3e6;  // written and read again
+  for (const Cut& c : list) {
+    const int64_t n = (c.count - c.whole) * c.parts;
+    all += c.whole + n;
+    if (c.parts > 1) join += (double)n * edge * edge * 8 / 3e6;  // written and read again
   }
   const double share = all > CUS ? (double)std::min<int64_t>(per, cdiv(all, CUS)) : 1.;  // blocks that run on a CU together
-  for (const Tiles& t : list) {
-    const int parts = cdiv(t.steps, most);
-    const double mem = (double)edge * edge * (parts > 1 ? 4 : bytes) / CU_BYTES_US;
-    blocks.push_back({cdiv(t.steps, parts) * step_us(w) * (share > 1 ? 0.9 * share : 1.) + block_us(w) + mem * share, (int64_t)t.count * parts});
+  auto add = [&](int steps, int value_bytes, int64_t n) {
+    const double mem = (double)edge * edge * value_bytes / (w == 128 ? CU_BYTES_US_ALONE : CU_BYTES_US);
+    if (n) blocks.push_back({steps * step_us(w) * (share > 1 ? 0.9 * share : 1.) + block_us(w) + mem * share, n});
+  };
+  for (const Cut& c : list) {
+    add(c.steps, bytes, c.whole);
+    add(c.per, c.parts > 1 ? 4 : bytes, (c.count - c.whole) * c.parts);
   }
   std::sort(blocks.begin(), blocks.end(), [](auto& a, auto& b) { return a.first > b.first; });
   const int places = CUS * per;
@@ -171,11 +207,9 @@ double launch_us(const std::vector<Tiles>& list, int w, int most, int bytes) {
   return *std::max_element(at.begin(), at.end()) + (join > 0 ? join + 5.0 : 0.0);
 }
 
-int64_t triangle(int64_t t) { return t * (t + 1) / 2; }
-
-// The blocks of a product: its tiles (all of rows x cols, or the lower triangle), sums longer than `most` steps cut.
+// The blocks of a product: its tiles (all of rows x cols, or the lower triangle), cut as `cuts` says.
 // Tiles are taken in squares of four by four, so that neighbours share operands, and neighbours go to one XCD: each has its own L2.
-void add_list(OrthoPlanHost& p, OrthoList& l, bool lower, int w, int most, bool along_n) {
+void add_list(OrthoPlanHost& p, OrthoList& l, bool lower, int w, const std::vector<Cut>& cuts, bool along_n) {
   l.w = w;
   l.work0 = p.works.size();
   l.join0 = p.joins.size();
@@ -183,24 +217,25 @@ void add_list(OrthoPlanHost& p, OrthoList& l, bool lower, int w, int most, bool 
   std::vector<Unit> units;
   for (size_t i = 0; i < p.mats.size(); ++i) {
     const OrthoMat& m = p.mats[i];
-    const int e = 2 * w, tm = cdiv(m.m, e), tn = lower ? tm : cdiv(m.n, e), K = along_n ? m.n : m.m, steps = cdiv(K, 32);
-    int parts = cdiv(steps, most);
-    const int per = cdiv(steps, parts) * 32;
-    parts = cdiv(K, per);
-    const int64_t all = (lower ? triangle(tm) : (int64_t)tm * tn) * parts;
-    const int unit = (int)std::max<int64_t>(1, std::min<int64_t>(32, cdiv(all, XCDS)));
+    const Cut& cut = cuts[i];
+    const int e = 2 * w, tm = cdiv(m.m, e), tn = lower ? tm : cdiv(m.n, e), K = along_n ? m.n : m.m;
+    // an eighth of the uncut tiles, of the others' parts
+    const size_t unit_whole = std::max(1, cdiv(cut.whole, XCDS)), unit_parts = std::max(1, cdiv((cut.count - cut.whole) * cut.parts, XCDS));
+    int64_t tile = 0;
     Unit u;
     auto flush = [&]() { if (!u.works.empty()) units.push_back(std::move(u)); u = Unit(); };
     for (int a4 = 0; a4 < tm; a4 += 4)
       for (int b4 = 0; b4 < (lower ? a4 + 1 : tn); b4 += 4)
         for (int a = a4; a < std::min(tm, a4 + 4); ++a)
-          for (int b = b4; b < std::min(lower ? a + 1 : tn, b4 + 4); ++b) {
+          for (int b = b4; b < std::min(lower ? a + 1 : tn, b4 + 4); ++b, ++tile) {
+            if (tile == cut.whole) flush();
+            const int parts = tile < cut.whole ? 1 : cut.parts, per = parts > 1 ? cut.per : cut.steps;
             if (parts > 1) p.joins.push_back(OrthoJoin{(int)i, a, b, l.slots, parts});
             for (int s = 0; s < parts; ++s) {
-              u.works.push_back(OrthoWork{(int)i, a, b, s * per, std::min(K, (s + 1) * per), parts > 1 ? l.slots + s : -1});
-              u.steps = per / 32;
-              u.cost += u.steps * step_us(w) + block_us(w);
-              if ((int)u.works.size() >= unit) flush();
+              u.works.push_back(OrthoWork{(int)i, a, b, s * per * 32, std::min(K, (s + 1) * per * 32), parts > 1 ? l.slots + s : -1});
+              u.steps = per;
+              u.cost += per * step_us(w) + block_us(w);
+              if (u.works.size() >= (tile < cut.whole ? unit_whole : unit_parts)) flush();
             }
             if (parts > 1) l.slots += parts;
           }
@@ -225,23 +260,19 @@ void add_list(OrthoPlanHost& p, OrthoList& l, bool lower, int w, int most, bool 
 }
 
 void plan_list(OrthoPlanHost& p, OrthoList& l, bool lower, bool along_n, bool cut, int bytes) {
-  int best_w = 32, best_most = 1 << 20;
+  int best_w = 32;
   double best = 1e300;
-  for (int w : {128, 64, 32}) {
-    std::vector<Tiles> tiles;
-    for (size_t i = 0; i < p.mats.size(); ++i) {
-      const OrthoMat& m = p.mats[i];
-      const int tm = cdiv(m.m, 2 * w);
-      const int64_t count = lower ? triangle(tm) : (int64_t)tm * cdiv(m.n, 2 * w);
-      tiles.push_back(Tiles{(int)std::min<int64_t>(count, 1 << 30), cdiv(along_n ? m.n : m.m, 32)});
-    }
-    for (int most : {1 << 20, 128, 96, 64, 48, 32, 24, 16, 8}) {
+  std::vector<Cut> cuts;
+  for (int w : {128, 64, 32})
+    for (int most : {1 << 20, 256, 128, 96, 64, 48, 32, 24, 16, 8}) {
       if (most < (1 << 20) && !cut) continue;
-      const double us = launch_us(tiles, w, most, bytes);
-      if (us < best) { best = us; best_w = w; best_most = most; }
+      for (bool tail : {false, true}) {
+        std::vector<Cut> c = cuts_of(p, lower, along_n, w, most, tail);
+        const double us = launch_us(c, w, bytes);
+        if (us < best) { best = us; best_w = w; cuts = std::move(c); }
+      }
     }
-  }
-  add_list(p, l, lower, best_w, best_most, along_n);
+  add_list(p, l, lower, best_w, cuts, along_n);
 }
 
 }  // namespace
@@ -307,12 +338,16 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
       for (int64_t g = 0; g < groups; g += ORTHO_GROUPS) p.chunks.push_back(OrthoChunk{i, (int32_t)g, 0});
     }
     m.chunks = (int)p.chunks.size() - m.chunk0;
+    p.most_m = std::max(p.most_m, m.m);
     p.mats.push_back(m);
   }
-  // (a symmetric result is written twice; Q X: weights read and written with their copy)
+  // bytes of memory for each value of a tile: a symmetric result is written twice; Q X: planes, the caller's values, weights read and
+  // written with their copy
   plan_list(p, p.gram, true, true, true, 8);
   plan_list(p, p.chain, true, false, true, 8);
-  plan_list(p, p.apply, false, false, false, 10);
+  plan_list(p, p.apply, false, false, false, 8);
+  plan_list(p, p.last[0], false, false, false, 6);
+  plan_list(p, p.last[1], false, false, false, 14);
   uint64_t o = 0;
   auto take = [&](uint64_t bytes) { const uint64_t at = o; o = up256(o + bytes); return at; };
   p.off_mats = take(p.mats.size() * sizeof(OrthoMat));
