@@ -102,7 +102,8 @@ int optorch_ortho_bind(optorch_ortho_t* h, void* workspace_dev, uint64_t workspa
 /* For every matrix G of the list: X = G / max(|G|, eps) (2-norm of its elements), then `steps` times
  * X <- a X + (b X X^T + c (X X^T)^2) X, towards the orthogonal factor of G.  g and o are flat vectors of the given
  * precisions, elements of o outside the matrices are left alone; o may be g.  The arithmetic is as exact as fp32's
- * whatever the precision of g and o: a step multiplies what is lost in small singular directions by up to `a`.
+ * whatever the precision of g, since a step multiplies what is lost in small singular directions by up to `a`; where o is bf16
+ * up to a third of its rounding is added for matrices with a few large singular values and many small ones.
  * A zero matrix gives zeros, one with an infinity or NaN gives NaN throughout; the others are not touched by it. */
 int optorch_orthogonalize(optorch_ortho_t* h, int32_t g_precision, const void* g, int32_t o_precision, void* o, void* hip_stream);
 

@@ -626,9 +626,10 @@ def linear_forward(x, w, bias=None, *, residual=None, activation="none", save_pr
     return (out, z) if save_pre else out
 
 
-def linear_backward(dy, x, w, z=None, *, activation="none", need=("dx", "dw", "dbias")):
+def linear_backward(dy, x, w, z=None, *, activation="none", need=("dx", "dw", "dbias"), dx=None, dw=None, dbias=None):
     """The gradients (dx, dw, dbias) of `linear_forward` from dy [rows, out] and what forward was given and saved; those not
-    in `need` are not computed and come back as None.  dbias is float32, the others have x's type."""
+    in `need` are not computed and come back as None.  dbias is float32, the others have x's type.  dx, dw, dbias: tensors to write
+    them to (dw may be a view of a flat vector of gradients)."""
     import torch
     rows, cin = x.shape
     cout = w.shape[0]
@@ -644,15 +645,23 @@ def linear_backward(dy, x, w, z=None, *, activation="none", need=("dx", "dw", "d
             raise ValueError("z (linear_forward's save_pre) is needed for the slope of %s" % activation)
         _check_matrix("z", z, rows, cout, x)
         a.z, a.ldz = z.data_ptr(), _ld(z)
-    dx = dw = dbias = None
+    for name, t in (("dx", dx), ("dw", dw), ("dbias", dbias)):
+        if t is not None and name not in need:
+            raise ValueError("%s: given, but not in need" % name)
     if "dx" in need:
-        dx = torch.empty((rows, cin), dtype=x.dtype, device=x.device)
-        a.dx, a.lddx = dx.data_ptr(), cin
+        if dx is None:
+            dx = torch.empty((rows, cin), dtype=x.dtype, device=x.device)
+        _check_matrix("dx", dx, rows, cin, x)
+        a.dx, a.lddx = dx.data_ptr(), _ld(dx)
     if "dw" in need:
-        dw = torch.empty((cout, cin), dtype=x.dtype, device=x.device)
-        a.dw, a.lddw = dw.data_ptr(), cin
+        if dw is None:
+            dw = torch.empty((cout, cin), dtype=x.dtype, device=x.device)
+        _check_matrix("dw", dw, cout, cin, x)
+        a.dw, a.lddw = dw.data_ptr(), _ld(dw)
     if "dbias" in need:
-        dbias = torch.empty(cout, dtype=torch.float32, device=x.device)
+        if dbias is None:
+            dbias = torch.empty(cout, dtype=torch.float32, device=x.device)
+        _check_vector("dbias", dbias, cout, x)
         a.dbias = dbias.data_ptr()
     lib = load_library()
     _linear_call(torch, lib, lib.optorch_linear_backward, a, 1, x.device)

@@ -54,7 +54,7 @@ struct OrthoOp { int32_t a, b, dst, extra; float alpha, beta, diag; };
 
 // Lists of small matrices: all steps on A between two iterates in one launch
 constexpr int ORTHO_SMALL = 128;                   // padded shorter side at most
-constexpr int ORTHO_RESTART = 3;                   // steps between two iterates at most
+constexpr int ORTHO_RESTART = 5;                   // steps between two iterates at most
 constexpr int ORTHO_SEGMENT_OPS = 4 * ORTHO_RESTART - 3;
 struct OrthoOps { int n; OrthoOp op[ORTHO_SEGMENT_OPS]; };
 
@@ -71,6 +71,9 @@ struct OrthoLaunch {
   bool last;           // OL_APPLY: to the caller's output
 };
 
+// What the result is stored as says how exact the steps have to be (ortho.cpp): fp16 or an update of fp32 weights, fp32, bf16
+enum { OUT_OTHER = 0, OUT_FP32, OUT_BF16, OUT_COUNT };
+
 struct OrthoTables {   // device pointers and sizes, by value to every kernel
   char* ws;
   const OrthoMat* mats; int nmat;
@@ -84,7 +87,7 @@ struct OrthoPlanHost {
   std::vector<OrthoWork> works;   // all lists, one behind the other
   std::vector<OrthoJoin> joins;
   OrthoList gram, chain, apply, last[2];  // last: Q X to the caller's vectors; [1]: to weights
-  std::vector<OrthoLaunch> launches[2];  // [1]: for results of fp32
+  std::vector<OrthoLaunch> launches[OUT_COUNT];
   int most_m = 0;                        // the largest padded shorter side
   float eps = 1e-7f, first_scale = 1.f;  // first_scale: power of two of the first iterate's planes
   int64_t span = 0;

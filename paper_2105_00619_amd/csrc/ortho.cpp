@@ -3,10 +3,12 @@
 // A Newton-Schulz step X <- (a + b A + c A^2) X with A = X X^T changes the singular values of X alone, so that the steps can be
 // made on A: with P = a + b A + c A^2,  A <- P A P  and  Q <- P Q,  and in the end X <- Q X.  Only A = X X^T at the start and
 // Q X at the end touch the long side of X; all other products are m x m and symmetric, so that half of their tiles are made.  For
-// m = n that costs what the steps on X cost (20 m^3 for five steps), for n = 4 m 38 m^3 instead of 65.  But an error of A grows by
+// m = n that costs what the steps on X cost (20 m^3 for five steps), for n = 4 m 29 m^3 instead of 65 (38 with X made once on the way).  But an error of A grows by
 // a^2 a step in the directions of small singular values, and rounding errors of A are not small against those: after five
-// steps on A the result is off by up to 3e-4.  So after three steps X is made and A from it again: 1e-6 to 2e-5, up to twice what the
-// steps on X give in fp32; after two where the result of more steps is stored in fp32: no more than theirs (47 m^3 for n = 4 m).
+// steps on A the result is off by 2e-6 for a matrix of samples, by up to 6e-4 for one with a few large singular values and many small
+// ones.  A result stored in bf16 is rounded by 1.7e-3, which that leaves at 1.8e-3: it takes five steps on A (29 m^3).  Else X is made
+// after three steps and A from it again: 1e-6 to 8e-5, up to twice what the steps on X give in fp32; after two where the result of more
+// steps is stored in fp32: no more than theirs (47 m^3 for n = 4 m).
 //
 // The operands are pairs of fp16 planes (hi + lo, 22 bits and a sign), times a power of two for each kind of matrix, since
 // the bounds of all of them are known (host: from the polynomials): three products of 16-bit matrix cores for one, with an error
@@ -38,10 +40,13 @@ namespace {
 // beyond 2^12 (the low plane of a value of 2^-12 then still has all its bits)
 float plane_scale(double bound) { return (float)std::exp2(std::min(12.0, std::floor(std::log2(16384.0 / std::max(bound, 1e-3))))); }
 
-constexpr int RESTART[2] = {ORTHO_RESTART, 2};  // steps on A between two iterates; [1]: for results of fp32
+// Steps on A between two iterates at most, and how far they may let an error of A grow (the product of their a^2): with larger
+// coefficients a restart comes sooner
+struct Restart { int steps; double growth; };
+constexpr Restart RESTART[OUT_COUNT] = {{3, 2e3}, {2, 150.}, {ORTHO_RESTART, 2.5e5}};
 
 // The launches and their scales.  Returns false where the steps let a singular value grow too far.
-bool plan_steps(OrthoPlanHost& p, std::vector<OrthoLaunch>& launches, int restart, int steps, const float* co) {
+bool plan_steps(OrthoPlanHost& p, std::vector<OrthoLaunch>& launches, Restart restart, int steps, const float* co) {
   constexpr int GRID = 4096;
   std::vector<double> l(GRID + 1), q(GRID + 1);
   for (int i = 0; i <= GRID; ++i) l[i] = (double)i / GRID;  // squares of singular values; sampled, the bounds have a margin
@@ -51,7 +56,11 @@ bool plan_steps(OrthoPlanHost& p, std::vector<OrthoLaunch>& launches, int restar
   p.first_scale = plane_scale(1.0);
   float sx = p.first_scale;
   for (int s = 0; s < steps;) {
-    const int e = std::min(steps, s + restart);
+    int e = s;
+    for (double growth = 1; e < steps && e < s + restart.steps; ++e) {
+      growth *= (double)co[3 * e] * co[3 * e];
+      if (e > s && growth > restart.growth) break;
+    }
     const double amax = top([&](int i) { return l[i]; });
     float sa = plane_scale(amax), sq = 1.f;
     OrthoLaunch g = {};
@@ -320,8 +329,15 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
   OrthoPlanHost& p = h->p;
   p.eps = cfg->eps > 0 ? cfg->eps : 1e-7f;
   p.span = span;
-  if (!plan_steps(p, p.launches[0], RESTART[0], steps, co.data()) || !plan_steps(p, p.launches[1], RESTART[steps > RESTART[0]], steps, co.data()))
-    return oseq_mat_err(OPTORCH_E_INVALID, "the coefficients let a singular value grow beyond 64");
+  size_t iterates = 0;  // that are made on the way
+  for (int k = 0; k < OUT_COUNT; ++k) {
+    const int kind = k == OUT_FP32 && steps <= RESTART[OUT_OTHER].steps ? OUT_OTHER : k;
+    if (!plan_steps(p, p.launches[k], RESTART[kind], steps, co.data()))
+      return oseq_mat_err(OPTORCH_E_INVALID, "the coefficients let a singular value grow beyond 64");
+    size_t n = 0;
+    for (const OrthoLaunch& l : p.launches[k]) n += l.kind == OL_APPLY && !l.last;
+    iterates = std::max(iterates, n);
+  }
   for (int i = 0; i < n; ++i) {
     const optorch_matrix_t& s = matrices[i];
     OrthoMat m = {};
@@ -358,10 +374,9 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
   p.off_scale = take(p.mats.size() * 8);
   p.off_bad = take(p.mats.size() * 4 + 4);
   p.off_slots = take(std::max((uint64_t)p.gram.slots * p.gram.w * p.gram.w, 2 * (uint64_t)p.chain.slots * p.chain.w * p.chain.w) * 16);
-  const bool two = steps > RESTART[0];
   for (OrthoMat& m : p.mats) {
     m.x[0] = take((uint64_t)m.m * m.n * 4);
-    m.x[1] = two ? take((uint64_t)m.m * m.n * 4) : m.x[0];
+    m.x[1] = iterates ? take((uint64_t)m.m * m.n * 4) : m.x[0];
     m.chain = take((uint64_t)OB_COUNT * m.m * m.m * 4);
   }
   p.bytes = o;
