@@ -108,16 +108,20 @@ template <int PL, class T> __device__ __forceinline__ void store_planes8(T* row,
 }
 
 // S: type in memory; T: type of the planes.  Columns are filled up to whole blocks (block_of) with zeros.
+struct Pack { const void* src; int64_t ld, rows; int cols; void* dst; int blocks; };
+// x and w in one launch, w's blocks behind x's
 template <class S, class T, int PL>
-__global__ void __launch_bounds__(256) pack_kernel(const S* __restrict__ src, int64_t ld, int64_t rows, int cols, T* __restrict__ dst) {
-  const int c8 = (cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
-  const int64_t n = rows * c8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+__global__ void __launch_bounds__(256) pack_kernel(Pack x, Pack w) {
+  const bool second = (int)blockIdx.x >= x.blocks;
+  const Pack p = second ? w : x;
+  const int c8 = (p.cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
+  const int64_t n = p.rows * c8;
+  for (int64_t i = (int64_t)(blockIdx.x - (second ? x.blocks : 0)) * 256 + threadIdx.x; i < n; i += (int64_t)p.blocks * 256) {
     const int64_t r = i / c8;
     const int c = (int)(i - r * c8) * 8;
     float v[8];
-    load8<S>(src + r * ld + c, min(8, cols - c), v);
-    store_planes8<PL, T>(dst + r * c8 * (8 * span_of(PL)), c, v);
+    load8<S>((const S*)p.src + r * p.ld + c, min(8, p.cols - c), v);
+    store_planes8<PL, T>((T*)p.dst + r * c8 * (8 * span_of(PL)), c, v);
   }
 }
 
@@ -495,11 +499,6 @@ ProductShape shape_of(int64_t M, int64_t N, int64_t K) {
   return {w, (int)parts};
 }
 
-template <class S, class T, int PL>
-void pack(hipStream_t st, const void* src, int64_t ld, int64_t rows, int cols, void* dst) {
-  OSEQ_LAUNCH((pack_kernel<S, T, PL>), dim3(grid_of(rows * ((cols + 7) / 8))), dim3(256), 0, st, (const S*)src, ld, rows, cols, (T*)dst);
-}
-
 template <class S, class T, int PL, int ACT> void run_dz(hipStream_t st, const optorch_linear_t& a, const LinearPlan& p) {
   char* ws = (char*)a.workspace;
   DzArgs d;
@@ -540,14 +539,28 @@ struct Where { const void* p; int ld; };
 // places of a row of n columns laid out anew
 template <int PL> int row_of(int n) { return (n + block_of(PL) - 1) / block_of(PL) * block_of(PL) * span_of(PL); }
 
+// x and w as operands: as they lie, or laid out anew
+template <class S, class T, int PL> void operands(const optorch_linear_t& a, const LinearPlan& p, Where& x, Where& w) {
+  char* ws = (char*)a.workspace;
+  const int row = row_of<PL>(a.in_features);
+  x = {a.x, (int)a.ldx};
+  w = {a.w, (int)a.ldw};
+  Pack px = {}, pw = {};
+  auto anew = [&](Where& o, Pack& q, const void* src, int64_t ld, int64_t rows, uint64_t off) {
+    o = {ws + off, row};
+    q = {src, ld, rows, a.in_features, ws + off, grid_of(rows * ((a.in_features + 7) / 8))};
+  };
+  if (p.pack_x) anew(x, px, a.x, a.ldx, a.rows, p.off_x);
+  if (p.pack_w) anew(w, pw, a.w, a.ldw, a.out_features, p.off_w);
+  if (px.blocks + pw.blocks) OSEQ_LAUNCH((pack_kernel<S, T, PL>), dim3(px.blocks + pw.blocks), dim3(256), 0, (hipStream_t)a.hip_stream, px, pw);
+}
+
 template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, const LinearPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
-  const int row = row_of<PL>(a.in_features);
   const bool few = a.rows <= SKINNY_ROWS;
-  Where x{a.x, (int)a.ldx}, w{a.w, (int)a.ldw};
-  if (p.pack_x) { pack<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x); x = {ws + p.off_x, row}; }
-  if (p.pack_w) { pack<S, T, PL>(st, a.w, a.ldw, a.out_features, a.in_features, ws + p.off_w); w = {ws + p.off_w, row}; }
+  Where x, w;
+  operands<S, T, PL>(a, p, x, w);
   ProductArgs g = {};
   g.a = x.p; g.lda = x.ld;
   g.b = w.p; g.ldb = w.ld;
@@ -579,17 +592,15 @@ template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, c
 template <class S, class T, int PL> void backward_of(const optorch_linear_t& a, const LinearPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
-  const int row = row_of<PL>(a.in_features);
   if (p.make_dz || a.dbias) switch (a.activation) {
     case OPTORCH_ACT_NONE: run_dz<S, T, PL, OPTORCH_ACT_NONE>(st, a, p); break;
     case OPTORCH_ACT_RELU: run_dz<S, T, PL, OPTORCH_ACT_RELU>(st, a, p); break;
     case OPTORCH_ACT_GELU: run_dz<S, T, PL, OPTORCH_ACT_GELU>(st, a, p); break;
     default: run_dz<S, T, PL, OPTORCH_ACT_SILU>(st, a, p);
   }
-  Where dz{a.dy, (int)a.lddy}, x{a.x, (int)a.ldx}, w{a.w, (int)a.ldw};
+  Where dz{a.dy, (int)a.lddy}, x, w;
   if (p.make_dz) dz = {ws + p.off_dz, row_of<PL>(a.out_features)};
-  if (p.pack_x) { pack<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x); x = {ws + p.off_x, row}; }
-  if (p.pack_w) { pack<S, T, PL>(st, a.w, a.ldw, a.out_features, a.in_features, ws + p.off_w); w = {ws + p.off_w, row}; }
+  operands<S, T, PL>(a, p, x, w);
   ProductArgs g = {};
   g.a = dz.p; g.lda = dz.ld;
   g.partial = (float*)(ws + p.off_parts);
