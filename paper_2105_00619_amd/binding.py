@@ -590,7 +590,7 @@ def _linear_call(torch, lib, fn, a, backward, device):
     if n:
         ws = torch.empty(n, dtype=torch.uint8, device=device)  # (torch aligns allocations to 512 bytes)
         a.workspace, a.workspace_bytes = ws.data_ptr(), n
-    a.hip_stream = torch.cuda.current_stream().cuda_stream
+    a.hip_stream = torch._C._cuda_getCurrentRawStream(device.index)  # (current_stream() makes an object: 2.6 us of a call's 12)
     rc = fn(C.byref(a))
     if rc != OK:
         _mat_fail(rc)

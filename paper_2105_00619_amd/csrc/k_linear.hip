@@ -518,10 +518,10 @@ constexpr int SKINNY_ROWS = 64;
 template <class S, class T, int MB, bool WIDE, int ACT> void run_skinny_of(hipStream_t st, ProductArgs& p) {
   SkinnyArgs g;
   g.p = p;
-  // wavefronts of at least 128 values of k each; more of them where there are few blocks
+  // wavefronts of at least 256 values of k each, what they ask for at once; more of them where there are few blocks
   const int blocks = ceil_div(p.N, 16), most = blocks >= 1024 ? 4 : blocks >= 256 ? 8 : 16;
   int waves = 4;
-  while (waves < most && waves * 256 <= p.K) waves *= 2;
+  while (waves < most && waves * 512 <= p.K) waves *= 2;
   g.k_wave = (ceil_div(p.K, waves) + 31) & ~31;
   OSEQ_LAUNCH((skinny_kernel<S, T, MB, WIDE, ACT>), dim3(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, g);
 }

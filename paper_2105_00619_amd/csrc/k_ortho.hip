@@ -360,6 +360,8 @@ __global__ void __launch_bounds__(640) small_chain_kernel(OrthoTables t, OrthoOp
   auto operand = [&](uint32_t at, int k, int g, int plane) {
     return *reinterpret_cast<const V8*>(smem + (at ^ (uint32_t)((k * 8 + plane * 4 + g * 2) << 4)));
   };
+  // (A tile is stored transposed and, off the diagonal, as it is.  On the diagonal the operands change places, so that there too a
+  // product is stored as it is: transposed, what rounding leaves of asymmetry made results of m = 32 four times less exact.)
   auto products = [&](v16f& acc, const V8& ah, const V8& al, const V8& bh, const V8& bl) {
     acc = Op<f16_t>::mma(ah, bl, acc);
     acc = Op<f16_t>::mma(al, bh, acc);
@@ -448,7 +450,9 @@ __global__ void __launch_bounds__(640) small_chain_kernel(OrthoTables t, OrthoOp
         each<ORTHO_SMALL / 32>([&](auto k) {
           if (k < nt)
             each<2>([&](auto g) {
-              products(acc, operand(area[1] + row_at, k, g, 0), operand(area[1] + row_at, k, g, 1), b[k][g], b[k][g + 2]);
+              const V8 ph = operand(area[1] + row_at, k, g, 0), pl = operand(area[1] + row_at, k, g, 1);
+              if (ti == tj) products(acc, b[k][g], b[k][g + 2], ph, pl);
+              else products(acc, ph, pl, b[k][g], b[k][g + 2]);
             });
         });
         finish(op, acc, false);
@@ -462,7 +466,8 @@ __global__ void __launch_bounds__(640) small_chain_kernel(OrthoTables t, OrthoOp
         copy_out(area[0], op.dst);
       }
     } else {  // C from P and A, the new A from C and P: they take A's place, which every wavefront has read
-      const uint32_t a_at = row_at + area[op.a == OB_C ? 0 : 1], b_at = col_at + area[op.a == OB_C ? 1 : 0];
+      const bool swap = (op.a == OB_C) == (ti != tj);
+      const uint32_t a_at = row_at + area[swap ? 0 : 1], b_at = col_at + area[swap ? 1 : 0];
       if (mine) {
         for (int k = 0; k < nt; ++k)
           each<2>([&](auto g) { products(acc, operand(a_at, k, g, 0), operand(a_at, k, g, 1), operand(b_at, k, g, 0), operand(b_at, k, g, 1)); });
