@@ -353,15 +353,32 @@ typedef __attribute__((ext_vector_type(4))) float v4f;
 __device__ __forceinline__ v4f mma16(Op<bf16_t>::V a, Op<bf16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ v4f mma16(Op<f16_t>::V a, Op<f16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// eight values of a row from k on (up to the row's end, zeros behind it) as loaded; WIDE: all or none of them exist
+// Eight values of a row as loaded, those that the eight places from k on have before `end`.  Not SINGLE (at least eight values before
+// `end`): at the end they are the row's last eight, those that an earlier group has taken as zeros: the same ones in either operand.
+// ODD: 16-bit values off the boundaries of 32 bits, from the 32-bit words that hold them (16-byte loads at such addresses: 9705 x 2687
+// -> 37 in bf16 92 us, so ODD_US).
+enum Loads { WIDE, ODD, SINGLE };
 template <class S> struct Raw8 { Chunk c[sizeof(S) / 2]; };
-template <class S, bool WIDE> __device__ __forceinline__ Raw8<S> raw8(const S* row, int k, int end) {
+template <class S, Loads L> __device__ __forceinline__ Raw8<S> raw8(const S* row, int k, int end) {
   Raw8<S> r;
-  if (WIDE) {
-    r = __builtin_bit_cast(Raw8<S>, *reinterpret_cast<const Loose<S, 8>*>(row + min(k, end - 8)));
+  if (L != SINGLE) {
+    const S* p = row + min(k, end - 8);
+    if constexpr (L == ODD) {
+      const uint32_t half = (uint32_t)(uintptr_t)p & 2u;
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p) - half);
+      struct Words { uint32_t v[4]; } const w = *reinterpret_cast<const Words*>(q);
+      const uint32_t last = q[half ? 4 : 3];
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(S) / 2; ++i)
-      if (k >= end) r.c[i] = zero_chunk();
+      for (int i = 0; i < 4; ++i) r.c[0][i] = __builtin_amdgcn_alignbit(i < 3 ? w.v[i + 1] : last, w.v[i], half * 8);
+    } else {
+      r = __builtin_bit_cast(Raw8<S>, *reinterpret_cast<const Loose<S, 8>*>(p));
+    }
+    if (k + 8 > end) {
+      Vec<S, 8> v = __builtin_bit_cast(Vec<S, 8>, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.v[e] = end - 8 + e < k ? from_f32<S>(0.f) : v.v[e];
+      r = __builtin_bit_cast(Raw8<S>, v);
+    }
   } else {
     Vec<S, 8> v;
 #pragma unroll
@@ -370,58 +387,68 @@ template <class S, bool WIDE> __device__ __forceinline__ Raw8<S> raw8(const S* r
   }
   return r;
 }
-// ... as MFMA operands
+// ... as MFMA operands.  (Planes without planes_of's cases: what is not finite, or rounds to infinity, makes the sum not finite, which
+// is then made again from the values.)
 template <class S, class T> __device__ __forceinline__ void planes8(const Raw8<S>& r, typename Op<T>::V (&p)[sizeof(S) == 4 ? 3 : 1]) {
   if constexpr (sizeof(S) == 2) {
     p[0] = __builtin_bit_cast(typename Op<T>::V, r.c[0]);
   } else {
     const Vec<float, 8> v = __builtin_bit_cast(Vec<float, 8>, r);
+    float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      bf16_t t[3];
-      planes_of(v.v[e], t);
+    for (int e = 0; e < 8; ++e) x[e] = v.v[e];
 #pragma unroll
-      for (int k = 0; k < 3; ++k) p[k][e] = t[k];
+    for (int k = 0; k < 3; ++k) {
+      const Vec<bf16_t, 8> q = round_vec<bf16_t, 8>(x);
+      p[k] = __builtin_bit_cast(typename Op<T>::V, q);
+      if (k < 2) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] -= (float)q.v[e];
+      }
     }
   }
 }
 
-// S: type in memory; T: of the planes; MB: blocks of 16 samples
-template <class S, class T, int MB, bool WIDE, int ACT>
+// S: type in memory; T: of the planes; MB: blocks of 16 samples, of a block's 16 outputs.  NARROW: MB blocks of 16 outputs, of a block's
+// 16 samples.
+template <class S, class T, int MB, Loads L, bool NARROW, int ACT>
 __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
-  constexpr int PL = sizeof(S) == 4 ? 3 : 1, U = PL == 3 ? (MB == 4 ? 1 : 2) : !WIDE ? 1 : MB == 4 ? 4 : 8;
+  constexpr int PL = sizeof(S) == 4 ? 3 : 1, U = PL == 3 ? (MB == 4 ? 1 : 2) : L == SINGLE ? 1 : MB == 4 || L == ODD ? 4 : 8;
   typedef typename Op<T>::V V;
   extern __shared__ float red[];  // [wavefront][MB][256]
   const ProductArgs& a = g.p;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int n0 = blockIdx.x * 16, r16 = lane & 15, kc = (lane >> 4) * 8;
+  const int64_t first = (int64_t)blockIdx.x * 16;
+  const int r16 = lane & 15, kc = (lane >> 4) * 8;
   const int k0 = wave * g.k_wave, k1 = min(a.K, k0 + g.k_wave);
-  const S* w = (const S*)a.b + (int64_t)min(n0 + r16, a.N - 1) * a.ldb;
-  const S* x[MB];
+  // one: the operand of which a block has 16 rows (w, NARROW: x), many: the other one
+  const S* one = NARROW ? (const S*)a.a + min(first + r16, a.M - 1) * a.lda : (const S*)a.b + min(first + r16, (int64_t)a.N - 1) * a.ldb;
+  const S* many[MB];
 #pragma unroll
-  for (int m = 0; m < MB; ++m) x[m] = (const S*)a.a + min<int64_t>(m * 16 + r16, a.M - 1) * a.lda;
+  for (int m = 0; m < MB; ++m)
+    many[m] = NARROW ? (const S*)a.b + (int64_t)min(m * 16 + r16, a.N - 1) * a.ldb : (const S*)a.a + min<int64_t>(m * 16 + r16, a.M - 1) * a.lda;
   v4f acc[MB];
 #pragma unroll
   for (int m = 0; m < MB; ++m) acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
   for (int k = k0; k < k1; k += 32 * U) {
-    Raw8<S> rw[U], rx[U][MB];
+    Raw8<S> ro[U], rm[U][MB];
 #pragma unroll
-    for (int u = 0; u < U; ++u) rw[u] = raw8<S, WIDE>(w, k + u * 32 + kc, k1);
+    for (int u = 0; u < U; ++u) ro[u] = raw8<S, L>(one, k + u * 32 + kc, k1);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int m = 0; m < MB; ++m) rx[u][m] = raw8<S, WIDE>(x[m], k + u * 32 + kc, k1);
+      for (int m = 0; m < MB; ++m) rm[u][m] = raw8<S, L>(many[m], k + u * 32 + kc, k1);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      V pw[PL], px[PL];
-      planes8<S, T>(rw[u], pw);
+      V po[PL], pm[PL];
+      planes8<S, T>(ro[u], po);
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
-        planes8<S, T>(rx[u][m], px);
+        planes8<S, T>(rm[u][m], pm);
 #pragma unroll
         for (int i = PL - 1; i >= 0; --i)
 #pragma unroll
-          for (int j = PL - 1 - i; j >= 0; --j) acc[m] = mma16(pw[i], px[j], acc[m]);
+          for (int j = PL - 1 - i; j >= 0; --j) acc[m] = NARROW ? mma16(pm[i], po[j], acc[m]) : mma16(po[i], pm[j], acc[m]);
       }
     }
   }
@@ -430,7 +457,8 @@ __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
   __syncthreads();
   // a thread has four neighbouring outputs of a sample
   for (int i = threadIdx.x; i < MB * 64; i += blockDim.x) {
-    const int row = (i >> 6) * 16 + (i & 15), col = n0 + ((i & 63) >> 4) * 4, n = min(4, a.N - col);
+    const int64_t row = (NARROW ? first : (i >> 6) * 16) + (i & 15);
+    const int col = (NARROW ? (i >> 6) * 16 : (int)first) + ((i & 63) >> 4) * 4, n = min(4, a.N - col);
     if (row >= a.M || n <= 0) continue;
     float v[4] = {0.f, 0.f, 0.f, 0.f};
     for (int q = 0; q < waves; ++q) {
@@ -441,7 +469,7 @@ __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
     if constexpr (PL == 3) {
       for (int e = 0; e < n; ++e)
         if (!(fabsf(v[e]) <= 3.4028235e38f)) {  // (sum_again)
-          const float *p = (const float*)a.a + (int64_t)row * a.lda, *q = (const float*)a.b + (int64_t)(col + e) * a.ldb;
+          const float *p = (const float*)a.a + row * a.lda, *q = (const float*)a.b + (int64_t)(col + e) * a.ldb;
           float s = 0.f;
           for (int k = 0; k < a.K; ++k) s = fmaf(p[k], q[k], s);
           v[e] = s;
@@ -526,26 +554,31 @@ template <class S, class T, int PL, int ACT> void run_dz(hipStream_t st, const o
     OSEQ_LAUNCH(dbias_kernel, dim3(ceil_div(d.cols, 16)), dim3(256), 0, st, (const float*)d.sums, p.sum_blocks, d.cols, a.dbias);
 }
 
-constexpr int SKINNY_ROWS = 64;
+constexpr int SKINNY_ROWS = 64, NARROW_ROWS = 512;
 
-template <class S, class T, int MB, bool WIDE, int ACT> void run_skinny_of(hipStream_t st, ProductArgs& p) {
+template <class S, class T, int MB, Loads L, bool NARROW, int ACT> void run_skinny_of(hipStream_t st, ProductArgs& p) {
   SkinnyArgs g;
   g.p = p;
   // wavefronts of at least 256 values of k each, what they ask for at once; more of them where there are few blocks
-  const int blocks = ceil_div(p.N, 16), most = blocks >= 1024 ? 4 : blocks >= 256 ? 8 : 16;
+  const int blocks = ceil_div(NARROW ? p.M : (int64_t)p.N, 16), most = blocks >= 1024 ? 4 : blocks >= 256 ? 8 : 16;
   int waves = 4;
   while (waves < most && waves * 512 <= p.K) waves *= 2;
   g.k_wave = (ceil_div(p.K, waves) + 31) & ~31;
-  OSEQ_LAUNCH((skinny_kernel<S, T, MB, WIDE, ACT>), dim3(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, g);
+  OSEQ_LAUNCH((skinny_kernel<S, T, MB, L, NARROW, ACT>), dim3(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, g);
 }
-template <class S, class T, int ACT> void run_skinny(hipStream_t st, ProductArgs& p, bool wide_operands) {
-  if (p.M <= 16) {
-    if (wide_operands) run_skinny_of<S, T, 1, true, ACT>(st, p); else run_skinny_of<S, T, 1, false, ACT>(st, p);
-  } else if (p.M <= 32) {
-    if (wide_operands) run_skinny_of<S, T, 2, true, ACT>(st, p); else run_skinny_of<S, T, 2, false, ACT>(st, p);
-  } else {
-    if (wide_operands) run_skinny_of<S, T, 4, true, ACT>(st, p); else run_skinny_of<S, T, 4, false, ACT>(st, p);
+template <class S, class T, Loads L, bool NARROW, int ACT> void run_skinny_by(hipStream_t st, ProductArgs& p) {
+  const int64_t rows = NARROW ? p.N : p.M;  // of the operand that every block reads
+  if (rows <= 16) run_skinny_of<S, T, 1, L, NARROW, ACT>(st, p);
+  else if (rows <= 32) run_skinny_of<S, T, 2, L, NARROW, ACT>(st, p);
+  else run_skinny_of<S, T, 4, L, NARROW, ACT>(st, p);
+}
+template <class S, class T, bool NARROW, int ACT> void run_skinny(hipStream_t st, ProductArgs& p) {
+  const bool odd = sizeof(S) == 2 && (p.K % 2 || p.lda % 2 || p.ldb % 2 || (uintptr_t)p.a % 4 || (uintptr_t)p.b % 4);
+  if (p.K < 8) return run_skinny_by<S, T, SINGLE, NARROW, ACT>(st, p);
+  if constexpr (sizeof(S) == 2) {
+    if (odd) return run_skinny_by<S, T, ODD, NARROW, ACT>(st, p);
   }
+  run_skinny_by<S, T, WIDE, NARROW, ACT>(st, p);
 }
 
 struct Where { const void* p; int ld; };
@@ -571,7 +604,6 @@ template <class S, class T, int PL> void operands(const optorch_linear_t& a, con
 template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, const LinearPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
-  const bool few = a.rows <= SKINNY_ROWS;
   Where x, w;
   operands<S, T, PL>(a, p, x, w);
   ProductArgs g = {};
@@ -583,14 +615,16 @@ template <class S, class T, int PL> void forward_of(const optorch_linear_t& a, c
   g.residual = a.residual; g.ldr = a.ldr;
   g.out = a.y; g.ldo = a.ldy;
   g.z = a.z; g.ldz = a.ldz;
-  if (few) {
+  if (p.straight) {
     g.K = a.in_features;
-    const bool wide_operands = a.in_features % 8 == 0;
+    auto run = [&](auto act) {
+      if (a.rows > SKINNY_ROWS) run_skinny<S, T, true, act>(st, g); else run_skinny<S, T, false, act>(st, g);
+    };
     switch (a.activation) {
-      case OPTORCH_ACT_NONE: run_skinny<S, T, OPTORCH_ACT_NONE>(st, g, wide_operands); break;
-      case OPTORCH_ACT_RELU: run_skinny<S, T, OPTORCH_ACT_RELU>(st, g, wide_operands); break;
-      case OPTORCH_ACT_GELU: run_skinny<S, T, OPTORCH_ACT_GELU>(st, g, wide_operands); break;
-      default: run_skinny<S, T, OPTORCH_ACT_SILU>(st, g, wide_operands);
+      case OPTORCH_ACT_NONE: run(std::integral_constant<int, OPTORCH_ACT_NONE>{}); break;
+      case OPTORCH_ACT_RELU: run(std::integral_constant<int, OPTORCH_ACT_RELU>{}); break;
+      case OPTORCH_ACT_GELU: run(std::integral_constant<int, OPTORCH_ACT_GELU>{}); break;
+      default: run(std::integral_constant<int, OPTORCH_ACT_SILU>{});
     }
     return;
   }
@@ -644,10 +678,13 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
   const bool f32 = a.precision == OPTORCH_FP32;
   const uint64_t in_row = 2 * (uint64_t)(f32 ? row_of<3>(a.in_features) : row_of<1>(a.in_features));
   const uint64_t out_row = 2 * (uint64_t)(f32 ? row_of<3>(a.out_features) : row_of<1>(a.out_features));
-  const bool few = !backward && a.rows <= SKINNY_ROWS;
-  const bool need_x = backward ? a.dw != nullptr : !few, need_w = backward ? a.dx != nullptr : !few;
-  p.pack_x = need_x && (f32 || !direct(a.x, a.ldx, a.in_features));
-  p.pack_w = need_w && (f32 || !direct(a.w, a.ldw, a.in_features));
+  const bool anew_x = f32 || !direct(a.x, a.ldx, a.in_features), anew_w = f32 || !direct(a.w, a.ldw, a.in_features);
+  // Few samples, or few outputs and samples that would be laid out anew (9705 x 2688 -> 37 in fp32: 120 us as tiles, SKINNY_NARROW us
+  // straight from memory)
+  p.straight = !backward && (a.rows <= SKINNY_ROWS || (a.rows >= NARROW_ROWS && a.out_features <= SKINNY_ROWS && anew_x));
+  const bool need_x = backward ? a.dw != nullptr : !p.straight, need_w = backward ? a.dx != nullptr : !p.straight;
+  p.pack_x = need_x && anew_x;
+  p.pack_w = need_w && anew_w;
   p.make_dz = backward && (a.dx || a.dw) && (f32 || a.activation != OPTORCH_ACT_NONE || !direct(a.dy, a.lddy, a.out_features));
   uint64_t o = 0;
   auto take = [&](uint64_t n) { const uint64_t at = o; o = up256(o + n); return at; };
@@ -659,8 +696,8 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
     s = shape_of(M, N, K, f32);
     if (s.parts > 1) parts = std::max(parts, (uint64_t)s.parts * M * up8(N) * 4);
   };
-  if (few) {
-    // (straight from memory)
+  if (p.straight) {
+    // (no workspace)
   } else if (!backward) {
     product(p.y, a.rows, a.out_features, a.in_features);
   } else {

@@ -18,7 +18,8 @@ struct ProductShape { int wave, parts; };
 
 // What a linear layer's call does with its workspace: where each piece begins, and how the products run
 struct LinearPlan {
-  bool pack_x, pack_w, pack_dy, make_dz;  // operands that are laid out anew (fp32, or not aligned for 16-byte loads)
+  bool straight;                    // forward: both operands straight from memory, no workspace
+  bool pack_x, pack_w, make_dz;     // operands that are laid out anew (fp32, or not aligned for 16-byte loads)
   uint64_t off_x, off_w, off_dz, off_sums, off_parts, bytes;
   int sum_blocks;                   // blocks of rows whose dbias sums are kept apart
   ProductShape y, dx, dw;

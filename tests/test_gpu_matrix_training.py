@@ -109,3 +109,33 @@ def test_bf16_results_where_one_direction_outweighs_the_others(small):
     out = torch.empty(192 * 700, dtype=torch.bfloat16, device="cuda")
     B.Orthogonalizer([(192, 700)]).orthogonalize(g.reshape(-1).cuda(), out)
     assert float((out.double().cpu().view(192, 700) - x).norm()) <= (2.0 ** -8 + 2.0 ** -10) * float(x.norm())
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,cin,cout", [(512, 8, 1), (513, 9, 3), (700, 263, 16), (1111, 517, 17), (530, 4099, 33), (600, 7, 64), (520, 1031, 64),
+                                           (3, 8, 5), (5, 11, 7), (40, 4505, 70), (17, 519, 33), (64, 1001, 15)])
+def test_forward_straight_from_memory(rows, cin, cout, name):
+    """Few samples or few outputs, rows at any address.  Products are exact (16 bits) or off by 2^-24 (fp32 as planes); at most a fourth
+    of them (six plane pairs in fp32) is added one after the other, cut off at 2^-23 of the absolute sum; one rounding at the end."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[name]
+    gen = torch.Generator(device="cuda").manual_seed(rows + cin)
+    make = lambda r, c: torch.randn(r, c + 3, generator=gen, device="cuda").to(dt)[:, 1:1 + c]  # noqa: E731
+    x, w, res = make(rows, cin), make(cout, cin), make(rows, cout)
+    bias = torch.randn(cout, generator=gen, device="cuda")
+    y, z = B.linear_forward(x, w, bias, residual=res, activation="relu", save_pre=True)
+    zr = torch.mm(x.double(), w.double().T.contiguous()) + bias.double()
+    sums = torch.mm(x.double().abs(), w.double().abs().T.contiguous()) + bias.double().abs()
+    off = (cin / 4 * (6 if name == "fp32" else 1) + 48) * 2.0 ** -23 * sums
+    e = 1.01 * torch.finfo(dt).eps / 2
+    assert bool(((z.double() - zr).abs() <= e * zr.abs() + off).all())
+    yr = zr.clamp_min(0) + res.double()
+    assert bool(((y.double() - yr).abs() <= e * yr.abs() + off + 2.0 ** -23 * (zr.abs() + yr.abs())).all())
+    # an infinity and a NaN reach their sample or output only, at the row's end too
+    for at in (0, cin - 1):
+        x2, w2 = x.clone(), w.clone()
+        x2[rows - 1, at], w2[cout - 1, at] = float("inf"), float("nan")
+        y2 = B.linear_forward(x2, w2, bias)
+        ref = torch.mm(x2.double(), w2.double().T.contiguous()) + bias.double()
+        assert torch.equal(torch.isnan(y2), torch.isnan(ref)) and torch.equal(torch.isinf(y2), torch.isinf(ref))
