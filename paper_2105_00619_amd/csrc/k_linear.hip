@@ -341,9 +341,9 @@ __global__ void __launch_bounds__(256) join_kernel(ProductArgs a) {
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------------
-// Up to 64 samples: the weights are what is read, once, straight into the operands of 16 x 16 MFMAs.  A block has 16 outputs of all
-// samples, its wavefronts (4 to 16) share the reduction and add up through LDS.  1 x 4096 -> 16384 in bf16, 134 MB: 30 us (4.4 TB/s);
-// as tiles of 64 x 64 with the reduction in four parts 38.
+// Up to 64 samples: the weights are what is read, once, straight into the operands of 16 x 16 MFMAs.  A block has 16 outputs of all samples,
+// its wavefronts (4 to 16) share the reduction and add up through LDS.  Few outputs: the same with the two operands in each other's
+// place.  1 x 4096 -> 16384 in bf16, 134 MB: 27 us (4.9 TB/s, a copy's rate); as tiles of 64 x 64 with the reduction in four parts 38.
 struct SkinnyArgs {
   ProductArgs p;       // a: x, b: w as they lie in memory; tiles and parts unused
   int k_wave;          // what a wavefront takes of the reduction, a multiple of 32
@@ -356,7 +356,7 @@ __device__ __forceinline__ v4f mma16(Op<f16_t>::V a, Op<f16_t>::V b, v4f c) { re
 // Eight values of a row as loaded, those that the eight places from k on have before `end`.  Not SINGLE (at least eight values before
 // `end`): at the end they are the row's last eight, those that an earlier group has taken as zeros: the same ones in either operand.
 // ODD: 16-bit values off the boundaries of 32 bits, from the 32-bit words that hold them (16-byte loads at such addresses: 9705 x 2687
-// -> 37 in bf16 92 us, so ODD_US).
+// -> 37 in bf16 92 us, so 49).
 enum Loads { WIDE, ODD, SINGLE };
 template <class S> struct Raw8 { Chunk c[sizeof(S) / 2]; };
 template <class S, Loads L> __device__ __forceinline__ Raw8<S> raw8(const S* row, int k, int end) {
@@ -514,9 +514,9 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 bool direct(const void* p, int64_t ld, int cols) { return aligned16(p) && ld % 8 == 0 && cols % 8 == 0; }
 
 // Tiles and parts of a product, by what it would take in us: tile steps (64 places of two operands), a block's beginning and end, the
-// join of parts (a launch, reading them, and the epilogue's memory by itself).  Two blocks of 128 x 128 or three of 64 x 64 share a CU, which makes their steps a
-// fifth shorter.  Fitted to 12 products of 67 MFLOP to 69 GFLOP, bf16 and fp32, with all tiles and 1 to 32 parts: the choice is within 10 % of
-// the best of them.  (By filling the CUs alone, 1024 x 1024 x 1024 in bf16 took 14.3 us in two parts, 8.3 in one, and
+// join of parts (a launch, reading them, and the epilogue's memory by itself).  Two blocks of 128 x 128 or three of 64 x 64 share a CU,
+// which makes their steps a fifth shorter.  Fitted to 12 products of 67 MFLOP to 69 GFLOP, bf16 and fp32, with all tiles and 1 to 32 parts: the choice is within 10 % of the
+// best of them.  (By filling the CUs alone, 1024 x 1024 x 1024 in bf16 took 14.3 us in two parts, 8.3 in one, and
 // 432 x 13952 x 2968 79 us as 64 x 64 tiles, 56 as 128 x 128 in four parts; in fp32 636 and 383.)
 ProductShape shape_of(int64_t M, int64_t N, int64_t K, bool f32) {
   constexpr int CUS = 256;
@@ -679,9 +679,11 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
   const uint64_t in_row = 2 * (uint64_t)(f32 ? row_of<3>(a.in_features) : row_of<1>(a.in_features));
   const uint64_t out_row = 2 * (uint64_t)(f32 ? row_of<3>(a.out_features) : row_of<1>(a.out_features));
   const bool anew_x = f32 || !direct(a.x, a.ldx, a.in_features), anew_w = f32 || !direct(a.w, a.ldw, a.in_features);
-  // Few samples, or few outputs and samples that would be laid out anew (9705 x 2688 -> 37 in fp32: 120 us as tiles, SKINNY_NARROW us
-  // straight from memory)
-  p.straight = !backward && (a.rows <= SKINNY_ROWS || (a.rows >= NARROW_ROWS && a.out_features <= SKINNY_ROWS && anew_x));
+  // Few samples, or few outputs and samples that would be laid out anew.  As tiles / straight from memory, in us: fp32 9705 x 2688 -> 37
+  // 120 / 60; bf16 off its alignment 20000 x 333 -> 10 18 / 8, 4000 x 1001 -> 64 16 / 10, but 40000 x 77 -> 40 12 / 22 and
+  // 9705 x 2687 -> 37 33 / 50: in 16 bits by the operations of the second way.
+  const double straight = (double)a.rows * std::max(a.in_features, 128) * ((a.out_features + 15) & ~15);
+  p.straight = !backward && (a.rows <= SKINNY_ROWS || (a.rows >= NARROW_ROWS && a.out_features <= SKINNY_ROWS && anew_x && (f32 || straight < 3e8)));
   const bool need_x = backward ? a.dw != nullptr : !p.straight, need_w = backward ? a.dx != nullptr : !p.straight;
   p.pack_x = need_x && anew_x;
   p.pack_w = need_w && anew_w;

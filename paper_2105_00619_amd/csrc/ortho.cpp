@@ -3,9 +3,9 @@
 // A Newton-Schulz step X <- (a + b A + c A^2) X with A = X X^T changes the singular values of X alone, so that the steps can be
 // made on A: with P = a + b A + c A^2,  A <- P A P  and  Q <- P Q,  and in the end X <- Q X.  Only A = X X^T at the start and
 // Q X at the end touch the long side of X; all other products are m x m and symmetric, so that half of their tiles are made.  For
-// m = n that costs what the steps on X cost (20 m^3 for five steps), for n = 4 m 29 m^3 instead of 65 (38 with X made once on the way).  But an error of A grows by
-// a^2 a step in the directions of small singular values, and rounding errors of A are not small against those: after five
-// steps on A the result is off by 2e-6 for a matrix of samples, by up to 6e-4 for one with a few large singular values and many small
+// m = n that costs what the steps on X cost (20 m^3 for five steps), for n = 4 m 29 m^3 instead of 65 (38 with X made once on the
+// way).  But an error of A grows by a^2 a step in the directions of small singular values, and rounding errors of A are not small
+// against those: after five steps on A the result is off by 2e-6 for a matrix of samples, by up to 6e-4 for one with a few large singular values and many small
 // ones.  A result stored in bf16 is rounded by 1.7e-3, which that leaves at 1.8e-3: it takes five steps on A (29 m^3).  Else X is made
 // after three steps and A from it again: 1e-6 to 8e-5, up to twice what the steps on X give in fp32; after two where the result of more
 // steps is stored in fp32: no more than theirs (47 m^3 for n = 4 m).
