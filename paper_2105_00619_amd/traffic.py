@@ -60,12 +60,13 @@ DATAFLOW_KERNELS = {
 
 
 DATAFLOW_ONLY = ("k_dataflow.hip", "dataflow.cpp")          # sources of the data-flow kernels alone
+MATRIX_ONLY = ("mat_core.h", "matrix.h", "matrix.cpp", "k_linear.hip", "ortho.cpp", "k_ortho.hip")  # ... of the matrix operators
 SHARED = ("dev_common.h", "launch.h")                         # device helpers both kinds of kernels are built from
 
 
 def source_hash(workload: str = "") -> str:
     """Hash of the sources a workload's kernels are built from: the data-flow files and the shared device helpers for
-    the data-flow benchmark; everything but the data-flow files for a training workload."""
+    the data-flow benchmark; everything but these and the matrix operators for a training workload."""
     dataflow = workload.startswith("dataflow")
     h = hashlib.sha1()
     for f in sorted(glob.glob(os.path.join(HERE, "csrc", "*"))):
@@ -74,7 +75,7 @@ def source_hash(workload: str = "") -> str:
             continue
         if dataflow and name not in DATAFLOW_ONLY + SHARED:
             continue
-        if not dataflow and name in DATAFLOW_ONLY:
+        if not dataflow and name in DATAFLOW_ONLY + MATRIX_ONLY:
             continue
         h.update(name.encode())
         h.update(open(f, "rb").read())

@@ -17,3 +17,12 @@ def test_every_convolution_and_batchnorm_kernel_is_in_one_group():
     for k in sorted(counted):
         groups = [g for g, fragments in T.GROUP_KERNELS.items() if any(f in "void oseq::(anonymous namespace)::%s<" % k for f in fragments)]
         assert len(groups) == 1, (k, groups)
+
+
+def test_matrix_operators_are_built_apart_from_the_workloads_kernels():
+    """Counted bytes stand while the sources of a workload's kernels do; those of the matrix operators are none of them."""
+    sources = {os.path.basename(f): open(f).read() for f in glob.glob(os.path.join(CSRC, "*"))}
+    assert set(T.MATRIX_ONLY) <= set(sources)
+    for name, text in sources.items():
+        if name not in T.MATRIX_ONLY:
+            assert not re.search(r'#include "(mat_core|matrix)\.h"', text), name
