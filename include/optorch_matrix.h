@@ -101,9 +101,9 @@ int optorch_ortho_bind(optorch_ortho_t* h, void* workspace_dev, uint64_t workspa
 
 /* For every matrix G of the list: X = G / max(|G|, eps) (2-norm of its elements), then `steps` times
  * X <- a X + (b X X^T + c (X X^T)^2) X, towards the orthogonal factor of G.  g and o are flat vectors of the given
- * precisions, elements of o outside the matrices are left alone; o may be g.  The arithmetic is as exact as fp32's
- * whatever the precision of g, since a step multiplies what is lost in small singular directions by up to `a`; where o is bf16
- * up to a third of its rounding is added for matrices with a few large singular values and many small ones.
+ * precisions, elements of o outside the matrices are left alone; o may be g.  Whatever the precision of g, the result is off by
+ * what fp32 arithmetic makes of the steps (in the 2-norm about 1e-6, up to 1e-4 where all but a few singular values are below 1e-3
+ * of the largest) and 7e-6 more, 1e-4 more where o is bf16, before it is rounded.
  * A zero matrix gives zeros, one with an infinity or NaN gives NaN throughout; the others are not touched by it. */
 int optorch_orthogonalize(optorch_ortho_t* h, int32_t g_precision, const void* g, int32_t o_precision, void* o, void* hip_stream);
 

@@ -610,7 +610,7 @@ void launch_ortho(hipStream_t st, const OrthoPlanHost& p, char* ws, const OrthoR
     const int edge = 2 * l.w, per = edge / 32;
     run(join_kernel, l.joins * c.ops * per * per, 0, st, t, joins + l.join0, l.joins, l.slots, edge, c.op[0], c.op[1]);
   };
-  const int kind = r.muon ? OUT_OTHER : r.o_precision == OPTORCH_FP32 ? OUT_FP32 : r.o_precision == OPTORCH_BF16 ? OUT_BF16 : OUT_OTHER;
+  const int kind = !r.muon && r.o_precision == OPTORCH_BF16 ? OUT_BF16 : OUT_OTHER;
   const std::vector<OrthoLaunch>& launches = p.launches[kind];
   for (size_t i = 0; i < launches.size(); ++i) {
     const OrthoLaunch& c = launches[i];

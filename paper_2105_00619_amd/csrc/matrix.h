@@ -55,7 +55,7 @@ struct OrthoOp { int32_t a, b, dst, extra; float alpha, beta, diag; };
 
 // Lists of small matrices: all steps on A between two iterates in one launch
 constexpr int ORTHO_SMALL = 128;                   // padded shorter side at most
-constexpr int ORTHO_RESTART = 5;                   // steps between two iterates at most
+constexpr int ORTHO_RESTART = 3;                   // steps between two iterates at most
 constexpr int ORTHO_SEGMENT_OPS = 4 * ORTHO_RESTART - 3;
 struct OrthoOps { int n; OrthoOp op[ORTHO_SEGMENT_OPS]; };
 
@@ -72,8 +72,8 @@ struct OrthoLaunch {
   bool last;           // OL_APPLY: to the caller's output
 };
 
-// What the result is stored as says how exact the steps have to be (ortho.cpp): fp16 or an update of fp32 weights, fp32, bf16
-enum { OUT_OTHER = 0, OUT_FP32, OUT_BF16, OUT_COUNT };
+// What the result is stored as says how exact the steps have to be (ortho.cpp): fp32, fp16 or an update of fp32 weights; bf16
+enum { OUT_OTHER = 0, OUT_BF16, OUT_COUNT };
 
 struct OrthoTables {   // device pointers and sizes, by value to every kernel
   char* ws;

@@ -2,13 +2,14 @@
 //
 // A Newton-Schulz step X <- (a + b A + c A^2) X with A = X X^T changes the singular values of X alone, so that the steps can be
 // made on A: with P = a + b A + c A^2,  A <- P A P  and  Q <- P Q,  and in the end X <- Q X.  Only A = X X^T at the start and
-// Q X at the end touch the long side of X; all other products are m x m and symmetric, so that half of their tiles are made.  For
-// m = n that costs what the steps on X cost (20 m^3 for five steps), for n = 4 m 29 m^3 instead of 65 (38 with X made once on the
-// way).  But an error of A grows by a^2 a step in the directions of small singular values, and rounding errors of A are not small
-// against those: after five steps on A the result is off by 2e-6 for a matrix of samples, by up to 6e-4 for one with a few large singular values and many small
-// ones.  A result stored in bf16 is rounded by 1.7e-3, which that leaves at 1.8e-3: it takes five steps on A (29 m^3).  Else X is made
-// after three steps and A from it again: 1e-6 to 8e-5, up to twice what the steps on X give in fp32; after two where the result of more
-// steps is stored in fp32: no more than theirs (47 m^3 for n = 4 m).
+// Q X at the end touch the long side of X; all other products are m x m and symmetric, so that half of their tiles are made.
+//
+// But a rounding of A (about 2^-23 of its largest value) grows by a^2 a step in the directions of small singular values, where P
+// passes it on to the result.  Largest errors over m = 2 .. 512 with one or m / 16 singular values of 1 and the others 0.5 .. 1e-4, five
+// steps (emulated; the steps on X in fp32: 0.6e-6 to 8e-5, the more the smaller the others):
+//   X made anew after every step: as the steps on X;  after two: up to 7e-6 more;  three: 8e-5;  four: 2.3e-4;  five: 1.8e-3.
+// A result stored in bf16 is rounded by 1.7e-3 and takes three steps on A, any other two.  (For n = 4 m that is 38 and 47 m^3 of
+// products, 65 with steps on X.)
 //
 // The operands are pairs of fp16 planes (hi + lo, 22 bits and a sign), times a power of two for each kind of matrix, since
 // the bounds of all of them are known (host: from the polynomials): three products of 16-bit matrix cores for one, with an error
@@ -43,7 +44,7 @@ float plane_scale(double bound) { return (float)std::exp2(std::min(12.0, std::fl
 // Steps on A between two iterates at most, and how far they may let an error of A grow (the product of their a^2): with larger
 // coefficients a restart comes sooner
 struct Restart { int steps; double growth; };
-constexpr Restart RESTART[OUT_COUNT] = {{3, 2e3}, {2, 150.}, {ORTHO_RESTART, 2.5e5}};
+constexpr Restart RESTART[OUT_COUNT] = {{2, 150.}, {ORTHO_RESTART, 2e3}};
 
 // The launches and their scales.  Returns false where the steps let a singular value grow too far.
 bool plan_steps(OrthoPlanHost& p, std::vector<OrthoLaunch>& launches, Restart restart, int steps, const float* co) {
@@ -331,8 +332,7 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
   p.span = span;
   size_t iterates = 0;  // that are made on the way
   for (int k = 0; k < OUT_COUNT; ++k) {
-    const int kind = k == OUT_FP32 && steps <= RESTART[OUT_OTHER].steps ? OUT_OTHER : k;
-    if (!plan_steps(p, p.launches[k], RESTART[kind], steps, co.data()))
+    if (!plan_steps(p, p.launches[k], RESTART[k], steps, co.data()))
       return oseq_mat_err(OPTORCH_E_INVALID, "the coefficients let a singular value grow beyond 64");
     size_t n = 0;
     for (const OrthoLaunch& l : p.launches[k]) n += l.kind == OL_APPLY && !l.last;
@@ -374,9 +374,11 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
   p.off_scale = take(p.mats.size() * 8);
   p.off_bad = take(p.mats.size() * 4 + 4);
   p.off_slots = take(std::max((uint64_t)p.gram.slots * p.gram.w * p.gram.w, 2 * (uint64_t)p.chain.slots * p.chain.w * p.chain.w) * 16);
+  // A single iterate on the way is made where the first one lies if a block has all rows of its columns: it has read them before it writes.
+  const bool in_place = iterates == 0 || (iterates == 1 && p.most_m <= 2 * p.apply.w);
   for (OrthoMat& m : p.mats) {
     m.x[0] = take((uint64_t)m.m * m.n * 4);
-    m.x[1] = iterates ? take((uint64_t)m.m * m.n * 4) : m.x[0];
+    m.x[1] = in_place ? m.x[0] : take((uint64_t)m.m * m.n * 4);
     m.chain = take((uint64_t)OB_COUNT * m.m * m.m * 4);
   }
   p.bytes = o;

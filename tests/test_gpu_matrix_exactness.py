@@ -1,0 +1,78 @@
+"""How exact the matrix operators are in the 2-norm, where the limits of single elements (test_gpu_matrix.py) see little."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+CO = (3.4445, -4.7750, 2.0315)
+
+
+def _steps(g, dtype, steps=5):
+    """Newton-Schulz steps in elementary operations of one type, on the CPU."""
+    import torch
+    a, b, c = CO
+    x = (g.double() / g.double().norm()).to(dtype)
+    for _ in range(steps):
+        s = torch.mm(x, x.T.contiguous())
+        x = a * x + torch.mm(b * s + c * torch.mm(s, s), x)
+    return x
+
+
+def _spectrum(m, n, small, large, seed):
+    """An m x n matrix of `large` singular values of 1, the others `small`."""
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    u = torch.linalg.qr(torch.randn(m, m, generator=gen, dtype=torch.float64))[0]
+    v = torch.linalg.qr(torch.randn(n, m, generator=gen, dtype=torch.float64))[0]
+    s = torch.full((m,), small, dtype=torch.float64)
+    s[:large] = 1.0
+    return torch.mm(u * s, v.T.contiguous()).float()
+
+
+def _far(x, ref):
+    return float((x.double().cpu() - ref).norm() / ref.norm())
+
+
+@pytest.mark.parametrize("steps", [2, 3, 4, 5])
+@pytest.mark.parametrize("m,n", [(2, 5), (8, 72), (10, 64), (32, 64), (64, 300), (100, 512), (192, 700)])
+def test_orthogonalize_where_few_directions_outweigh_the_others(m, n, steps):
+    """An error d of A grows by at most a^2 = 11.9 until the next step on A, whose P is then off by 4.775 / 3.4445 of that, relative to what it
+    does to small directions.  With three roundings of 2^-23 a product: two steps on A between iterates, 11.9 * 1.39 * 3 * 2^-23 = 6e-6 < 2^-17 beside the
+    error of the same steps in fp32 (its roundings and these are not the same ones: twice); three steps, 11.9 times as much, < 2^-13."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    for small in (0.5, 0.2, 0.1, 0.05, 0.02, 0.01, 3e-3, 1e-3):
+        for large in {1, max(1, m // 16)}:
+            g = _spectrum(m, n, small, large, seed=m + n)
+            ref = _steps(g, torch.float64, steps)
+            plain = _far(_steps(g, torch.float32, steps), ref)
+            plan = B.Orthogonalizer([(m, n)], steps=steps)
+            for dt, more in ((torch.float32, 2.0 ** -17), (torch.float16, 2.0 ** -17), (torch.bfloat16, 2.0 ** -13)):
+                out = torch.empty(m * n, dtype=dt, device="cuda")
+                plan.orthogonalize(g.reshape(-1).cuda(), out)
+                rounding = _far(ref.to(dt), ref) if dt != torch.float32 else 0.0
+                assert _far(out.view(m, n), ref) <= 2 * plain + more + 1.05 * rounding, (small, large, dt, plain)
+            # an update of nothing but this step
+            w, v = torch.zeros(m * n, device="cuda"), torch.zeros(m * n, device="cuda")
+            plan.muon_update(w, v, g.reshape(-1).cuda(), lr=1.0, momentum=0.0, scale="none")
+            assert _far(-w.view(m, n), ref) <= 2 * plain + 2.0 ** -17 + 2.0 ** -23, (small, large, "update", plain)
+            plan.close()
+
+
+def test_an_iterate_made_in_place_is_the_one_made_apart():
+    """Three steps take one iterate on the way, which low matrices make where the first one lies; beside a taller matrix they do not."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    gen = torch.Generator().manual_seed(3)
+    low, tall = [(40, 3000), (3000, 40)], [(600, 640)]
+    n = sum(r * c for r, c in low)
+    g = torch.randn(n + 600 * 640, generator=gen).cuda()
+    one, two = B.Orthogonalizer(low, steps=3), B.Orthogonalizer(low + tall, steps=3)
+    assert one.workspace_bytes < 2 * 4 * 2 * 64 * 3008
+    a, b = one.orthogonalize(g[:n].clone()), two.orthogonalize(g)
+    for at in (0, 40 * 3000):
+        ref = _steps(g[at:at + 120000].cpu().view((40, 3000) if at == 0 else (3000, 40)), torch.float64, 3) if at == 0 else \
+            _steps(g[at:at + 120000].cpu().view(3000, 40).T.contiguous(), torch.float64, 3).T
+        for o in (a, b):
+            assert _far(o[at:at + 120000].view(ref.shape), ref) <= 1e-5
