@@ -75,16 +75,21 @@ template <class T, int V> __device__ __forceinline__ void store8(T* p, int n, co
   }
 }
 
+__device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.4028235e38f; }
+
 // ---- operands laid out anew --------------------------------------------------------------------------------------------
 // A value as three bf16 planes: the value rounded, what that leaves, what the two leave.  Where rounding would leave the range of
-// bf16 the first plane is cut off instead; a value that is not finite has it in the first plane alone.
+// bf16 the first two are cut off instead, so that they do not add up to more than the value; a value that is not finite has it in the
+// first plane alone.
+__device__ __forceinline__ float cut_off(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u); }
 __device__ __forceinline__ void planes_of(float x, bf16_t (&p)[3]) {
   p[0] = (bf16_t)x;
   p[1] = p[2] = (bf16_t)0.f;
-  if (!(fabsf(x) <= 3.4028235e38f)) return;
-  if (!(fabsf((float)p[0]) <= 3.4028235e38f)) p[0] = (bf16_t)copysignf(3.3895314e38f, x);
+  if (!finite(x)) return;
+  const bool large = !finite((float)p[0]);
+  if (large) p[0] = (bf16_t)cut_off(x);
   x -= (float)p[0];
-  p[1] = (bf16_t)x;
+  p[1] = (bf16_t)(large ? cut_off(x) : x);
   p[2] = (bf16_t)(x - (float)p[1]);
 }
 
@@ -240,22 +245,28 @@ __device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int co
   store8<O>((O*)a.out + row * a.ldo + col, n, v);
 }
 
-// The value at (r, k) of an operand of three planes
-template <bool R> __device__ __forceinline__ float value_of(const bf16_t* p, int64_t ld, int64_t r, int64_t k) {
-  p += R ? k * ld + place_of<3>(r) : r * ld + place_of<3>(k);
-  const float hi = (float)p[0];
-  return fabsf(hi) <= 3.4028235e38f ? (hi + (float)p[16]) + (float)p[32] : hi;
-}
-
-// An infinity among the operands makes sums of planes NaN (infinity times a plane of zero): such a sum is made again, one product
-// after the other, so that infinities and NaNs come out as from fp32 arithmetic
-template <bool AR, bool BR>
-__device__ __forceinline__ float sum_again(const ProductArgs& a, int64_t m, int n, int k0, int k1) {
-  float s = 0.f;
-  for (int k = k0; k < k1; ++k)
-    s = fmaf(value_of<AR>((const bf16_t*)a.a, a.lda, m, k), value_of<BR>((const bf16_t*)a.b, a.ldb, n, k), s);
-  return s;
-}
+// What sums that are not finite have to become, two bits a value (1: NaN, 2: infinity, 3: -infinity, 0: as summed), eight values a group
+template <int GROUPS> struct Classes {
+  uint32_t bits[(GROUPS + 1) / 2];
+  // (the group is a constant but where the epilogue is a loop: then a select for each word)
+  __device__ __forceinline__ void set(int group, const float (&v)[8]) {
+    uint32_t c = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c |= (finite(v[e]) ? 0u : v[e] != v[e] ? 1u : v[e] > 0.f ? 2u : 3u) << (2 * e);
+#pragma unroll
+    for (int i = 0; i < (GROUPS + 1) / 2; ++i)
+      if (i == group / 2) bits[i] |= c << (group % 2 * 16);
+  }
+  __device__ __forceinline__ void apply(int group, float (&v)[8]) const {
+    uint32_t c = 0;
+#pragma unroll
+    for (int i = 0; i < (GROUPS + 1) / 2; ++i)
+      if (i == group / 2) c = bits[i] >> (group % 2 * 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e, c >>= 2)
+      if (c & 3) v[e] = (c & 3) == 1 ? __builtin_nanf("") : (c & 3) == 2 ? __builtin_inff() : -__builtin_inff();
+  }
+};
 
 // O: type of the result; T: of the planes
 template <class O, class T, int W, bool AR, bool BR, int ACT>
@@ -286,35 +297,42 @@ product_kernel(ProductArgs a) {
   int br, bc;
   G::place(0, br, bc);
   if (a.parts == 1) bias_of<ACT>(a, n0 + bc, cols - bc, bias);
-  typename G::Acc acc;
-  G::product(smem, oa, ob, k1 - k0, acc);
   const int n8 = (a.N + 7) & ~7;
   auto ask = [&](int r, int c, int n) { return a.parts > 1 ? Skip<O, 8>{} : skip_of<O, ACT, 8>(a, m0 + r, n0 + c, n); };
   auto emit = [&](int r, int c, float (&v)[8], int n, const Skip<O, 8>& skip) {
     if (a.parts > 1) store_f32<float, 8>(a.partial + ((int64_t)part * a.M + m0 + r) * n8 + n0 + c, v);
     else finish<O, ACT>(a, m0 + r, n0 + c, v, n, bias, skip);
   };
-  uint32_t again = 0;  // fp32: which of this thread's values are to be summed again
-  G::template out<false, (ACT >= OPTORCH_ACT_GELU)>(smem, acc, rows, cols, ask, [&](int idx, int r, int c, float (&v)[8], int n, const Skip<O, 8>& skip) {
-    if (sizeof(O) == 4) {
+  constexpr bool LONG = ACT >= OPTORCH_ACT_GELU;
+  typename G::Acc acc;
+  uint32_t wait = 0;  // planes: which groups have a sum that is not finite
+  G::product(smem, oa, ob, k1 - k0, acc);
+  G::template out<false, LONG>(smem, acc, rows, cols, ask, [&](int idx, int r, int c, float (&v)[8], int n, const Skip<O, 8>& skip) {
+    if (PL > 1) {
       bool bad = false;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) bad |= e < n && !(fabsf(v[e]) <= 3.4028235e38f);
-      if (bad) { again |= 1u << idx; return; }
+      for (int e = 0; e < 8; ++e) bad |= e < n && !finite(v[e]);
+      if (bad) { wait |= 1u << idx; return; }
     }
     emit(r, c, v, n, skip);
   });
-  if constexpr (sizeof(O) == 4) {
-    while (again) {
-      const int idx = __builtin_ctz(again);
-      again &= again - 1;
-      int r, c;
-      G::place(idx, r, c);
-      const int n = min(8, cols - c);
-      float v[8];
-      for (int e = 0; e < 8; ++e) v[e] = e < n ? sum_again<AR, BR>(a, m0 + r, n0 + c + e, k0, k1) : 0.f;
+  if constexpr (PL > 1) {
+    // An infinity among the operands makes sums of planes NaN (infinity times a plane of zero).  The groups that wait: the tile is made of the
+    // first planes alone, which says what these sums are, and once more for the others of a group.  So a tile that holds any costs three.
+    if (!G::any_of(smem, wait != 0)) return;
+    __syncthreads();
+    Classes<G::GROUPS> classes = {};
+    G::template product<true>(smem, oa, ob, k1 - k0, acc);
+    G::template out<false, false>(smem, acc, rows, cols, [](int, int, int) { return 0; }, [&](int idx, int, int, float (&v)[8], int, int) {
+      if (wait >> idx & 1) classes.set(idx, v);
+    });
+    __syncthreads();  // (the rows on their way out lie where the next slots go)
+    G::product(smem, oa, ob, k1 - k0, acc);
+    G::template out<false, true>(smem, acc, rows, cols, [](int, int, int) { return 0; }, [&](int idx, int r, int c, float (&v)[8], int n, int) {
+      if (!(wait >> idx & 1)) return;
+      classes.apply(idx, v);
       emit(r, c, v, n, ask(r, c, n));
-    }
+    });
   }
 }
 
@@ -387,16 +405,32 @@ template <class S, Loads L> __device__ __forceinline__ Raw8<S> raw8(const S* row
   }
   return r;
 }
-// ... as MFMA operands.  (Planes without planes_of's cases: what is not finite, or rounds to infinity, makes the sum not finite, which
-// is then made again from the values.)
+// ... as MFMA operands, values as planes_of has them: with its cases only where there is a value beyond the largest bf16 (a NaN makes all of its
+// planes NaN here; what counts is the first)
 template <class S, class T> __device__ __forceinline__ void planes8(const Raw8<S>& r, typename Op<T>::V (&p)[sizeof(S) == 4 ? 3 : 1]) {
   if constexpr (sizeof(S) == 2) {
     p[0] = __builtin_bit_cast(typename Op<T>::V, r.c[0]);
   } else {
     const Vec<float, 8> v = __builtin_bit_cast(Vec<float, 8>, r);
-    float x[8];
+    float x[8], most = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = v.v[e];
+    for (int e = 0; e < 8; ++e) {
+      x[e] = v.v[e];
+      most = fmaxf(most, fabsf(x[e]));
+    }
+    if (__builtin_expect(most > 3.3895314e38f, 0)) {
+      Vec<bf16_t, 8> q[3];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        bf16_t t[3];
+        planes_of(x[e], t);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) q[k].v[e] = t[k];
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k) p[k] = __builtin_bit_cast(typename Op<T>::V, q[k]);
+      return;
+    }
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
       const Vec<bf16_t, 8> q = round_vec<bf16_t, 8>(x);
@@ -427,9 +461,13 @@ __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
 #pragma unroll
   for (int m = 0; m < MB; ++m)
     many[m] = NARROW ? (const S*)a.b + (int64_t)min(m * 16 + r16, a.N - 1) * a.ldb : (const S*)a.a + min<int64_t>(m * 16 + r16, a.M - 1) * a.lda;
-  v4f acc[MB];
+  // fp32: the products of the first planes apart from the others: where they are not finite, they are the sum (Tile::product)
+  v4f acc[MB], rest[PL == 3 ? MB : 1];
 #pragma unroll
-  for (int m = 0; m < MB; ++m) acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int m = 0; m < MB; ++m) {
+    acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
+    if constexpr (PL == 3) rest[m] = acc[m];
+  }
   for (int k = k0; k < k1; k += 32 * U) {
     Raw8<S> ro[U], rm[U][MB];
 #pragma unroll
@@ -448,12 +486,21 @@ __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
 #pragma unroll
         for (int i = PL - 1; i >= 0; --i)
 #pragma unroll
-          for (int j = PL - 1 - i; j >= 0; --j) acc[m] = NARROW ? mma16(pm[i], po[j], acc[m]) : mma16(po[i], pm[j], acc[m]);
+          for (int j = PL - 1 - i; j >= 0; --j) {
+            v4f& sum = i + j ? rest[PL == 3 ? m : 0] : acc[m];
+            sum = NARROW ? mma16(pm[i], po[j], sum) : mma16(po[i], pm[j], sum);
+          }
       }
     }
   }
 #pragma unroll
-  for (int m = 0; m < MB; ++m) *reinterpret_cast<v4f*>(red + ((wave * MB + m) * 64 + lane) * 4) = acc[m];
+  for (int m = 0; m < MB; ++m) {
+    if constexpr (PL == 3) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[m][e] += finite(acc[m][e]) ? rest[m][e] : 0.f;
+    }
+    *reinterpret_cast<v4f*>(red + ((wave * MB + m) * 64 + lane) * 4) = acc[m];
+  }
   __syncthreads();
   // a thread has four neighbouring outputs of a sample
   for (int i = threadIdx.x; i < MB * 64; i += blockDim.x) {
@@ -465,15 +512,6 @@ __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
       const v4f t = *reinterpret_cast<const v4f*>(red + (q * MB * 64 + i) * 4);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += t[e];
-    }
-    if constexpr (PL == 3) {
-      for (int e = 0; e < n; ++e)
-        if (!(fabsf(v[e]) <= 3.4028235e38f)) {  // (sum_again)
-          const float *p = (const float*)a.a + row * a.lda, *q = (const float*)a.b + (int64_t)(col + e) * a.ldb;
-          float s = 0.f;
-          for (int k = 0; k < a.K; ++k) s = fmaf(p[k], q[k], s);
-          v[e] = s;
-        }
     }
     float bias[4];
     bias_of<ACT>(a, col, n, bias);

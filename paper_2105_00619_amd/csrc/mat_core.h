@@ -198,11 +198,13 @@ struct Tile {
   typedef Steps<PL> S;
   static constexpr int SLOT = FA::BYTES, LDS = RING * SLOT;
   static constexpr int EPITCH = W + 4;  // floats of a row on its way out
-  static_assert(4 * 32 * EPITCH * 4 <= LDS, "the epilogue's rows do not fit");
+  static_assert(4 * 32 * EPITCH * 4 + 16 <= LDS, "the epilogue's rows and a word for each wavefront do not fit");
   typedef typename Op<T>::V V;
   typedef v16f Acc[MI][MI];
 
-  // the sum over k in [0, K)
+  // The sum over k in [0, K).  LEADING: of the first planes' products alone, which are what an infinity or a NaN makes of a sum (infinity
+  // times a later plane, which may be zero or of the other sign, is not).
+  template <bool LEADING = false>
   __device__ static __forceinline__ void product(unsigned char* smem, const Operand<T>& a, const Operand<T>& b, int K, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave >> 1, wn = wave & 1;
@@ -273,7 +275,8 @@ struct Tile {
         __builtin_amdgcn_sched_barrier(0);
         constexpr int set = S::reads(s), count = __builtin_popcount(set) * MI, per = (count + MFMAS - 1) / MFMAS;
         each<MFMAS>([&](auto n) {
-          acc[n / MI][n % MI] = Op<T>::mma(fa[S::a(s)][n / MI], fb[S::b(s)][n % MI], acc[n / MI][n % MI]);
+          if constexpr (!LEADING || (S::a(s) == 0 && S::b(s) == 0))
+            acc[n / MI][n % MI] = Op<T>::mma(fa[S::a(s)][n / MI], fb[S::b(s)][n % MI], acc[n / MI][n % MI]);
           __builtin_amdgcn_sched_barrier(0);
           each<per>([&](auto j) {  // (of the last tile step: what is read is not used)
             constexpr int i = n * per + j;
@@ -293,8 +296,19 @@ struct Tile {
     asm volatile("" ::: "memory");
   }
 
+  // After `out`: whether any thread's flag is set.  (Not __syncthreads_or, which waits until memory has taken the tile.)
+  __device__ static __forceinline__ bool any_of(unsigned char* smem, bool flag) {
+    volatile uint32_t* words = reinterpret_cast<volatile uint32_t*>(smem + LDS - 16);
+    const uint32_t any = __any(flag);
+    if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = any;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    return (words[0] | words[1] | words[2] | words[3]) != 0;
+  }
+
   // the place in the tile of a thread's eight values number `idx` on their way out
-  static constexpr int LPR = W / 8, RPP = 64 / LPR, PASSES = 32 / RPP;  // lanes per row, rows per pass
+  static constexpr int LPR = W / 8, RPP = 64 / LPR, PASSES = 32 / RPP, GROUPS = MI * PASSES;  // lanes per row, rows per pass; groups of a thread
   __device__ static __forceinline__ void place(int idx, int& r, int& c) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     r = (wave >> 1) * W + idx / PASSES * 32 + idx % PASSES * RPP + lane / LPR;
