@@ -64,9 +64,9 @@ int64_t optorch_linear_workspace(const optorch_linear_t* a, int32_t backward);
 /* y = activation(x w^T + bias) + residual */
 int optorch_linear_forward(const optorch_linear_t* a);
 
-/* dz = dy * activation'(z);  dx = dz w,  dw = dz^T x,  dbias = column sums of dz.  In 16-bit precision dz is rounded to
- * the storage type once before the two products; dbias sums it unrounded.  The slope of ReLU at 0 is 0.  The
- * gradient of the skip connection is dy itself.  With rows = 0, dw and dbias are zero. */
+/* dz = dy * activation'(z);  dx = dz w,  dw = dz^T x,  dbias = column sums of dz.  In 16-bit precision dz is held as two
+ * values of the storage type for the two products, which keeps 16 (bf16) or 22 (fp16) of its bits; dbias sums it unrounded.
+ * The slope of ReLU at 0 is 0.  The gradient of the skip connection is dy itself.  With rows = 0, dw and dbias are zero. */
 int optorch_linear_backward(const optorch_linear_t* a);
 
 /* ---- orthogonalised updates ------------------------------------------------------------------------ */

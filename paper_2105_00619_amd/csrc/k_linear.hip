@@ -130,14 +130,31 @@ __global__ void __launch_bounds__(256) pack_kernel(Pack x, Pack w) {
   }
 }
 
+// A value in two 16-bit planes: rounded, and what that leaves.  Where rounding would leave the range of the type (a slope of GELU goes up to
+// 1.13) the first is the type's largest; a value that is not finite has it in the first plane alone.
+template <class T> __device__ __forceinline__ void two_planes8(const float (&v)[8], Vec<T, 8>& hi, Vec<T, 8>& lo) {
+  constexpr float MOST = __is_same(T, bf16_t) ? 3.3895314e38f : 65504.f;
+  hi = round_vec<T, 8>(v);
+  float l[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (finite(v[e]) && !finite((float)hi.v[e])) hi.v[e] = from_f32<T>(copysignf(MOST, v[e]));
+    l[e] = finite(v[e]) ? v[e] - (float)hi.v[e] : 0.f;
+  }
+  lo = round_vec<T, 8>(l);
+}
+
 // dz and the sums of its columns over this block's rows.  Thirty-two threads take a row's 256 columns, eight rows at a time.
 struct DzArgs {
   const void* dy; int64_t lddy; const void* z; int64_t ldz;
   int64_t rows; int cols, rows_per_block;
   bool write;
   void* dz;       // laid out as the products want it
+  int64_t second; // where the second plane is, in values (slopes_of_two)
   float* sums;    // [row blocks][cols], or null
 };
+// 16 bits: whether dz has more of them than dy
+constexpr bool slopes_of_two(int precision, int act) { return precision != OPTORCH_FP32 && (act == OPTORCH_ACT_GELU || act == OPTORCH_ACT_SILU); }
 template <class S, class T, int PL, int ACT>
 __global__ void __launch_bounds__(256) dz_kernel(DzArgs a) {
   __shared__ float part[8][256 + 8];
@@ -160,7 +177,17 @@ __global__ void __launch_bounds__(256) dz_kernel(DzArgs a) {
         if (e >= n) v[e] = 0.f;
         sum[e] += v[e];
       }
-      if (a.write) store_planes8<PL, T>((T*)a.dz + r * padded * span_of(PL), c, v);
+      if (a.write) {
+        T* row = (T*)a.dz + r * padded * span_of(PL);
+        if constexpr (PL == 1 && slopes_of_two(OPTORCH_BF16, ACT)) {
+          Vec<T, 8> hi, lo;
+          two_planes8<T>(v, hi, lo);
+          *reinterpret_cast<Vec<T, 8>*>(row + c) = hi;
+          *reinterpret_cast<Vec<T, 8>*>(row + a.second + c) = lo;
+        } else {
+          store_planes8<PL, T>(row, c, v);
+        }
+      }
     }
   if (!a.sums) return;
 #pragma unroll
@@ -203,6 +230,7 @@ __global__ void __launch_bounds__(256) dbias_kernel(const float* __restrict__ su
 // ---- the products ------------------------------------------------------------------------------------------------------
 struct ProductArgs {
   const void* a; int lda;  // the operands, mat_core.h
+  int64_t second;          // TWICE: from a to its second plane
   const void* b; int ldb;
   int64_t M;
   int N, K;
@@ -269,11 +297,12 @@ template <int GROUPS> struct Classes {
 };
 
 // O: type of the result; T: of the planes
-template <class O, class T, int W, bool AR, bool BR, int ACT>
+template <class O, class T, int W, bool AR, bool BR, int ACT, bool TWICE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
 product_kernel(ProductArgs a) {
   constexpr int PL = sizeof(O) == 4 ? 3 : 1;
-  typedef Tile<T, PL, W, AR, BR> G;
+  constexpr bool PLANES = PL > 1 || TWICE;
+  typedef Tile<T, PL, W, AR, BR, TWICE> G;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   // neighbouring tiles on one XCD: each of the eight takes a run of them, eight rows of tiles at a time
   const int total = a.tiles_m * a.tiles_n * a.parts;
@@ -288,7 +317,7 @@ product_kernel(ProductArgs a) {
   const int k0 = part * a.k_part, k1 = min(a.K, k0 + a.k_part);
   Operand<T> oa, ob;
   oa.base = (const T*)a.a + (AR ? (int64_t)k0 * a.lda + place_of<PL>(m0) : m0 * a.lda + place_of<PL>(k0));
-  oa.ld = a.lda; oa.rows = rows;
+  oa.ld = a.lda; oa.rows = rows; oa.second = a.second;
   ob.base = (const T*)a.b + (BR ? (int64_t)k0 * a.ldb + place_of<PL>(n0) : (int64_t)n0 * a.ldb + place_of<PL>(k0));
   ob.ld = a.ldb; ob.rows = cols;
   // A thread's outputs are of the same eight columns throughout.  (With the bias read for every eight outputs, each read waited for,
@@ -308,7 +337,7 @@ product_kernel(ProductArgs a) {
   uint32_t wait = 0;  // planes: which groups have a sum that is not finite
   G::product(smem, oa, ob, k1 - k0, acc);
   G::template out<false, LONG>(smem, acc, rows, cols, ask, [&](int idx, int r, int c, float (&v)[8], int n, const Skip<O, 8>& skip) {
-    if (PL > 1) {
+    if (PLANES) {
       bool bad = false;
 #pragma unroll
       for (int e = 0; e < 8; ++e) bad |= e < n && !finite(v[e]);
@@ -316,7 +345,7 @@ product_kernel(ProductArgs a) {
     }
     emit(r, c, v, n, skip);
   });
-  if constexpr (PL > 1) {
+  if constexpr (PLANES) {
     // An infinity among the operands makes sums of planes NaN (infinity times a plane of zero).  The groups that wait: the tile is made of the
     // first planes alone, which says what these sums are, and once more for the others of a group.  So a tile that holds any costs three.
     if (!G::any_of(smem, wait != 0)) return;
@@ -526,25 +555,25 @@ template <class T> __global__ void __launch_bounds__(256) clear_kernel(T* p, int
 
 int grid_of(int64_t n) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, 4096)); }
 
-template <class O, class T, int W, bool AR, bool BR, int ACT> void run_product_w(hipStream_t st, ProductArgs& a) {
+template <class O, class T, int W, bool AR, bool BR, int ACT, bool TWICE> void run_product_w(hipStream_t st, ProductArgs& a) {
   constexpr int PL = sizeof(O) == 4 ? 3 : 1;
-  typedef Tile<T, PL, W, AR, BR> G;
+  typedef Tile<T, PL, W, AR, BR, TWICE> G;
   const int per = (a.tiles_m * a.tiles_n * a.parts + 7) / 8;
-  auto k = product_kernel<O, T, W, AR, BR, ACT>;
+  auto k = product_kernel<O, T, W, AR, BR, ACT, TWICE>;
   // (more LDS than a launch gets unasked; set again on every launch: which devices know it is not ours to remember)
   if (G::LDS > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
   OSEQ_LAUNCH(k, dim3(per * 8), dim3(256), G::LDS, st, a);
   if (a.parts > 1) OSEQ_LAUNCH((join_kernel<O, ACT>), dim3(grid_of(a.M * ((a.N + 7) / 8))), dim3(256), 0, st, a);
 }
 
-template <class O, class T, bool AR, bool BR, int ACT> void run_product(hipStream_t st, ProductArgs& a, const ProductShape& s) {
+template <class O, class T, bool AR, bool BR, int ACT, bool TWICE = false> void run_product(hipStream_t st, ProductArgs& a, const ProductShape& s) {
   const int b = 2 * s.wave;
   a.tiles_m = ceil_div(a.M, b); a.tiles_n = ceil_div(a.N, b);
   a.k_part = (int)(((int64_t)ceil_div(a.K, 64) + s.parts - 1) / s.parts) * 64;
   a.parts = ceil_div(a.K, a.k_part);
-  if (s.wave == 128) run_product_w<O, T, 128, AR, BR, ACT>(st, a);
-  else if (s.wave == 64) run_product_w<O, T, 64, AR, BR, ACT>(st, a);
-  else run_product_w<O, T, 32, AR, BR, ACT>(st, a);
+  if (s.wave == 128) run_product_w<O, T, 128, AR, BR, ACT, TWICE>(st, a);
+  else if (s.wave == 64) run_product_w<O, T, 64, AR, BR, ACT, TWICE>(st, a);
+  else run_product_w<O, T, 32, AR, BR, ACT, TWICE>(st, a);
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -586,6 +615,7 @@ template <class S, class T, int PL, int ACT> void run_dz(hipStream_t st, const o
   d.rows_per_block = ceil_div(a.rows, p.sum_blocks);
   d.write = p.make_dz;
   d.dz = ws + p.off_dz;
+  d.second = p.dz_second;
   d.sums = a.dbias ? (float*)(ws + p.off_sums) : nullptr;
   OSEQ_LAUNCH((dz_kernel<S, T, PL, ACT>), dim3(ceil_div(d.cols, 256), p.sum_blocks), dim3(256), 0, st, d);
   if (a.dbias)
@@ -687,19 +717,22 @@ template <class S, class T, int PL> void backward_of(const optorch_linear_t& a, 
   if (p.make_dz) dz = {ws + p.off_dz, row_of<PL>(a.out_features)};
   operands<S, T, PL>(a, p, x, w);
   ProductArgs g = {};
-  g.a = dz.p; g.lda = dz.ld;
+  g.a = dz.p; g.lda = dz.ld; g.second = p.dz_second;
   g.partial = (float*)(ws + p.off_parts);
+  constexpr bool CAN = PL == 1;  // (two planes of dz: 16 bits only)
   if (a.dx) {
     g.b = w.p; g.ldb = w.ld;
     g.M = a.rows; g.N = a.in_features; g.K = a.out_features;
     g.out = a.dx; g.ldo = a.lddx;
-    run_product<S, T, false, true, -1>(st, g, p.dx);
+    if (CAN && p.dz_second) run_product<S, T, false, true, -1, CAN>(st, g, p.dx);
+    else run_product<S, T, false, true, -1>(st, g, p.dx);
   }
   if (a.dw) {
     g.b = x.p; g.ldb = x.ld;
     g.M = a.out_features; g.N = a.in_features; g.K = (int)a.rows;
     g.out = a.dw; g.ldo = a.lddw;
-    run_product<S, T, true, true, -1>(st, g, p.dw);
+    if (CAN && p.dz_second) run_product<S, T, true, true, -1, CAN>(st, g, p.dw);
+    else run_product<S, T, true, true, -1>(st, g, p.dw);
   }
 }
 
@@ -730,7 +763,12 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
   auto take = [&](uint64_t n) { const uint64_t at = o; o = up256(o + n); return at; };
   if (p.pack_x) p.off_x = take((uint64_t)a.rows * in_row);
   if (p.pack_w) p.off_w = take((uint64_t)a.out_features * in_row);
-  if (p.make_dz) p.off_dz = take((uint64_t)a.rows * out_row);
+  // dz of 16-bit layers: rounded once it adds as much as the results' own rounding (dx and dw in bf16 2.3e-3 off, so 1.7e-3), and in fp16 a
+  // large dy times a slope above 1 is infinite.  So it has two planes, and the products twice as much to do (8192 x 2048 -> 8192 in bf16:
+  // 508 us with one, so 975).  ReLU and no activation leave the bits of dy.
+  const bool two = p.make_dz && slopes_of_two(a.precision, a.activation);
+  if (p.make_dz) p.off_dz = take((uint64_t)a.rows * out_row * (two ? 2 : 1));
+  if (two) p.dz_second = (int64_t)a.rows * (int64_t)(out_row / 2);
   uint64_t parts = 0;
   auto product = [&](ProductShape& s, int64_t M, int64_t N, int64_t K) {
     s = shape_of(M, N, K, f32);
@@ -745,8 +783,8 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
     const int64_t across = (a.out_features + 255) / 256;
     p.sum_blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, std::max<int64_t>(1, 1024 / across)));
     if (a.dbias) p.off_sums = take((uint64_t)p.sum_blocks * a.out_features * 4);
-    if (a.dx) product(p.dx, a.rows, a.in_features, a.out_features);
-    if (a.dw) product(p.dw, a.out_features, a.in_features, a.rows);
+    if (a.dx) product(p.dx, a.rows, a.in_features, (int64_t)a.out_features * (two ? 2 : 1));
+    if (a.dw) product(p.dw, a.out_features, a.in_features, a.rows * (two ? 2 : 1));
   }
   if (parts) p.off_parts = take(parts);
   p.bytes = o;

@@ -10,7 +10,7 @@
 //   three planes   16 columns of plane 0, of plane 1, of plane 2, 16 unused; ...
 // "Places" below are positions in a row so laid out.  64 places of an operand along k are a slot: four groups of 16, each group one
 // plane of 16 values of k.  (Planes apart in memory, one product of planes after the other, take half as many loads again with two
-// planes and twice as many with three.)
+// planes and twice as many with three; that is what a product of an operand of two planes with one of 16 bits does, TWICE below.)
 //
 // Four wavefronts in two rows and two columns, each with W x W of the block's 2 W x 2 W.  Slots are a ring in LDS, A and B in turn,
 // filled by loads that write LDS themselves.  While the products of two slots are made, the loads of the two that were used up
@@ -51,10 +51,11 @@ template <int PL> __host__ __device__ constexpr int64_t place_of(int64_t c, int 
 
 // One operand of a tile: `base` is its first place (first row of the tile, k = 0), ld the places from one row of memory to the next
 // (a multiple of 8; base 16-byte aligned), `rows` how many of the tile's rows exist (at least 1).  Memory holds whole blocks of columns
-// (block_of; one plane: of eight).
+// (block_of; one plane: of eight).  TWICE: places from here to the second plane, a matrix like this one (or 0: the same once more).
 template <class T> struct Operand {
   const T* base;
   int ld, rows;
+  int64_t second = 0;
 };
 
 constexpr int SLOT_K = 64;                 // places of a slot along k (R: values of k and their planes)
@@ -75,8 +76,8 @@ __device__ __forceinline__ void load_to_lds(const v4i& buf, uint32_t off, uint32
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(buf));
 }
 
-// The loads and reads of one operand: B rows of a tile
-template <class T, int PL, int B, bool R>
+// The loads and reads of one operand: B rows of a tile.  TWICE: the reduction once, and once more with the second plane.
+template <class T, int PL, int B, bool R, bool TWICE = false>
 struct Feed {
   static constexpr int BYTES = B * SLOT_K * 2, NLD = BYTES / 4096;  // of a slot; loads per thread
   static constexpr int SPAN = span_of(PL);
@@ -92,6 +93,8 @@ struct Feed {
   int64_t step;
   v4i buf;
   int left;  // of the reduction from the next slot on; what lies beyond is filled with zeros
+  const T* again;  // TWICE: where the second plane begins, and how long it is
+  int whole;
 
   __device__ __forceinline__ void init(const Operand<T>& o, int K, int wave, int lane) {
 #pragma unroll
@@ -113,6 +116,7 @@ struct Feed {
     buf = buffer_of(next);
     step = R ? (int64_t)KS * o.ld : KS;
     left = K;
+    if (TWICE) { again = o.base + o.second; whole = K; }
   }
   __device__ __forceinline__ void load(int i, uint32_t lds, int wave) const {
     uint32_t o = off[i];
@@ -130,6 +134,7 @@ struct Feed {
   __device__ __forceinline__ void advance() {
     left -= KS;
     next += step;
+    if (TWICE && left <= 0) { next = again; left = whole; }
     buf = buffer_of(next);
   }
   // the MFMA operand of group g, rows [row, row + 32) of the tile
@@ -190,11 +195,12 @@ constexpr int group_of(int set, int i, int mi) {
 
 constexpr int ring_slots(int w) { return w == 128 ? 5 : w == 64 ? 5 : 6; }
 
-template <class T, int PL, int W, bool AR, bool BR>
+template <class T, int PL, int W, bool AR, bool BR, bool TWICE = false>
 struct Tile {
+  static_assert(!TWICE || PL == 1, "planes apart in memory are 16-bit operands");
   static constexpr int RING = ring_slots(W), EDGE = 2 * W, MI = W / 32;
-  typedef Feed<T, PL, EDGE, AR> FA;
-  typedef Feed<T, PL, EDGE, BR> FB;
+  typedef Feed<T, PL, EDGE, AR, TWICE> FA;
+  typedef Feed<T, PL, EDGE, BR, TWICE> FB;
   typedef Steps<PL> S;
   static constexpr int SLOT = FA::BYTES, LDS = RING * SLOT;
   static constexpr int EPITCH = W + 4;  // floats of a row on its way out
@@ -215,7 +221,7 @@ struct Tile {
     fda.init(a, AR ? K : kv, wave, lane);
     fdb.init(b, BR ? K : kv, wave, lane);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    const int total = (kv + SLOT_K - 1) / SLOT_K;
+    const int once = (kv + SLOT_K - 1) / SLOT_K, total = TWICE && !LEADING ? 2 * once : once;
     constexpr int NLD = FA::NLD, MFMAS = MI * MI, PLACES = S::N * MFMAS;
     // Load n of the sequence A, B, A, B, ... goes to slot n mod RING; from the hand-over of tile step t - 1 to that of t, loads
     // 2 t + RING - 2 and the next go out

@@ -21,6 +21,7 @@ struct LinearPlan {
   bool straight;                    // forward: both operands straight from memory, no workspace
   bool pack_x, pack_w, make_dz;     // operands that are laid out anew (fp32, or not aligned for 16-byte loads)
   uint64_t off_x, off_w, off_dz, off_sums, off_parts, bytes;
+  int64_t dz_second;                // dz in two planes: values from the first to the second, else 0
   int sum_blocks;                   // blocks of rows whose dbias sums are kept apart
   ProductShape y, dx, dw;
 };

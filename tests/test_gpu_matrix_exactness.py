@@ -76,3 +76,58 @@ def test_an_iterate_made_in_place_is_the_one_made_apart():
             _steps(g[at:at + 120000].cpu().view(3000, 40).T.contiguous(), torch.float64, 3).T
         for o in (a, b):
             assert _far(o[at:at + 120000].view(ref.shape), ref) <= 1e-5
+
+
+def _slope64(act, z):
+    import torch
+    if act == "gelu":
+        return 0.5 * torch.special.erfc(-z / math.sqrt(2)) + z * torch.exp(-z * z / 2) / math.sqrt(2 * math.pi)
+    if act == "silu":
+        s = torch.sigmoid(z)
+        return s * (1 + z * (1 - s))
+    return (z > 0).double() if act == "relu" else torch.ones_like(z)
+
+
+@pytest.mark.parametrize("name", ["bf16", "fp16"])
+@pytest.mark.parametrize("act", ["gelu", "silu", "relu", "none"])
+@pytest.mark.parametrize("rows,cin,cout", [(3, 40, 24), (257, 333, 514), (1000, 64, 8), (2100, 520, 2056), (24, 1000, 4100)])
+def test_gradients_in_16_bits_are_rounded_once(rows, cin, cout, act, name):
+    """What the rounding of the result makes, and nothing of its size beside it: dz is held to twice the bits of the type (2^-16 and
+    less), its products are exact and added in fp32 (2^-20 and less of a result whose terms have either sign)."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    dt = {"bf16": torch.bfloat16, "fp16": torch.float16}[name]
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    make = lambda r, c, s=1.0: (torch.randn(r, c, generator=gen, device="cuda") * s).to(dt)  # noqa: E731
+    dy, x, w, z = make(rows, cout), make(rows, cin), make(cout, cin, cin ** -0.5), make(rows, cout, 1.5)
+    dx, dw, _ = B.linear_backward(dy, x, w, z, activation=act)
+    dz = dy.double() * _slope64(act, z.double())
+    for got, ref in ((dx, torch.mm(dz, w.double())), (dw, torch.mm(dz.T.contiguous(), x.double()))):
+        once = float((ref.to(dt).double() - ref).norm() / ref.norm())
+        assert float((got.double() - ref).norm() / ref.norm()) <= once * (1 + 2.0 ** -6) + 2.0 ** -16
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("rows,cin,cout", [(5, 24, 16), (300, 264, 520), (1100, 72, 40)])
+def test_gradients_in_fp16_have_the_range_of_their_results(rows, cin, cout, act):
+    """dy near the largest fp16 times a slope above 1 is no infinity where dx and dw are none; an infinite weight or sample makes the
+    infinities and NaNs that one product of fp32 values makes, whatever the planes of dz."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    dy = torch.randint(-3, 4, (rows, cout), generator=gen, device="cuda").half()
+    z = torch.randn(rows, cout, generator=gen, device="cuda").half()
+    x, w = (torch.randn(rows, cin, generator=gen, device="cuda") * 1e-3).half(), (torch.randn(cout, cin, generator=gen, device="cuda") * 1e-2).half()
+    dy[2, 3], dy[4, 7], z[2, 3], z[4, 7] = 65000.0, -65000.0, 1.5, 2.25
+    slope = _slope64(act, z.double())
+    assert float((dy.double() * slope).abs().max()) > 65504 * 1.05
+    dx, dw, db = B.linear_backward(dy, x, w, z, activation=act)
+    dz = dy.double() * slope
+    for got, ref in ((dx, torch.mm(dz, w.double())), (dw, torch.mm(dz.T.contiguous(), x.double()))):
+        once = float((ref.half().double() - ref).norm() / ref.norm())
+        assert float((got.double() - ref).norm() / ref.norm()) <= once * (1 + 2.0 ** -6) + 2.0 ** -16
+    w[5, 2], x[3, 1], x[1, 0] = float("inf"), float("-inf"), float("nan")
+    dx, dw, db = B.linear_backward(dy, x, w, z, activation=act)
+    for got, ref in ((dx, torch.mm(dz, w.double())), (dw, torch.mm(dz.T.contiguous(), x.double()))):
+        assert torch.equal(torch.isnan(got), torch.isnan(ref))
+        assert torch.equal(torch.isposinf(got), torch.isposinf(ref)) and torch.equal(torch.isneginf(got), torch.isneginf(ref))
