@@ -718,7 +718,8 @@ class OrthoPlan:
 
 class Orthogonalizer(OrthoPlan):
     """A bound plan: workspace allocated through torch, calls on torch's current stream.  Calls of one object share the
-    workspace: on different streams they have to be ordered by the caller."""
+    workspace: on different streams they have to be ordered by the caller.  An object may be dropped while its calls are still under way on any
+    stream, but a graph that has captured one needs it alive for as long as it is replayed."""
 
     def __init__(self, matrices, *, device="cuda:0", **kw):
         import torch
@@ -729,6 +730,7 @@ class Orthogonalizer(OrthoPlan):
             raise RuntimeError("no GPU visible: the matrix operators only run on the HIP path")
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
+            self.home = torch.cuda.current_stream(self.device).cuda_stream  # whose work the allocator waits for before it gives the memory away
             # (the memory may have been another stream's until now)
             torch.cuda.current_stream(self.device).synchronize()
             self._check(self.lib.optorch_ortho_bind(self.handle, self.workspace.data_ptr(), self.workspace_bytes))
@@ -744,7 +746,10 @@ class Orthogonalizer(OrthoPlan):
         return p
 
     def _stream(self):
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+        s = self.torch.cuda.current_stream(self.device)
+        if s.cuda_stream != self.home and not self.torch.cuda.is_current_stream_capturing():
+            self.workspace.record_stream(s)  # or it goes back to its first stream alone, tables and all, while this one's kernels read it
+        return s.cuda_stream
 
     def orthogonalize(self, g, out=None):
         """Newton-Schulz steps on every matrix of the flat tensor g, into out (g's type by default)."""

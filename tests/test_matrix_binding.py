@@ -1,0 +1,50 @@
+"""The Python side of the matrix operators without a GPU: what it asks of torch and of the library."""
+import contextlib
+import os
+import types
+
+import pytest
+
+from paper_2105_00619_amd import binding as B
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2105_00619_amd import build
+        build.build(verbose=False)
+
+
+class _Bound(B.Orthogonalizer):
+    """An Orthogonalizer whose device is made up: stream numbers, a workspace that notes the streams it is told of, a library that does nothing."""
+
+    def __init__(self, home):
+        self.stream, self.capturing, self.told, self.home = home, False, [], home
+        cuda = types.SimpleNamespace(
+            current_stream=lambda device: types.SimpleNamespace(cuda_stream=self.stream),
+            is_current_stream_capturing=lambda: self.capturing, device=lambda d: contextlib.nullcontext())
+        self.torch = types.SimpleNamespace(cuda=cuda)
+        self.device, self.handle = "cuda:0", None
+        self.workspace = types.SimpleNamespace(record_stream=lambda s: self.told.append(s.cuda_stream))
+        self.calls = []
+        self.lib = types.SimpleNamespace(optorch_orthogonalize=lambda *a: self.calls.append(a[-1]) or B.OK,
+                                         optorch_muon_update=lambda *a: self.calls.append(a[-1]) or B.OK)
+
+    def _flat(self, name, t, dtypes=None):
+        return 0
+
+
+def test_the_allocator_is_told_of_every_stream_that_uses_a_workspace():
+    v = types.SimpleNamespace(data_ptr=lambda: 1 << 20)
+    o = _Bound(home=7)
+    o.orthogonalize(v, v)
+    assert o.told == [] and o.calls == [7]
+    o.stream = 9
+    o.orthogonalize(v, v)
+    assert o.told == [9] and o.calls == [7, 9]
+    o.stream = 11
+    o.muon_update(v, v, v, lr=0.1)
+    assert o.told == [9, 11] and o.calls == [7, 9, 11]
+    o.capturing = True  # (nothing runs; the graph's user keeps the object)
+    o.orthogonalize(v, v)
+    assert o.told == [9, 11]
