@@ -7,6 +7,7 @@
 
 #include "mat_core.h"
 #include "matrix.h"
+#include "parts.h"
 
 namespace oseq {
 
@@ -234,7 +235,8 @@ struct ProductArgs {
   const void* b; int ldb;
   int64_t M;
   int N, K;
-  int tiles_m, tiles_n, parts, k_part;
+  int tiles_m, tiles_n, parts;
+  Parts cut;          // of K, in `parts`
   float* partial;     // parts > 1: [parts][M][up8(N)] sums
   // what becomes of a sum
   const float* bias;
@@ -314,7 +316,7 @@ product_kernel(ProductArgs a) {
   const int64_t m0 = (int64_t)tm * G::EDGE;
   const int n0 = tn * G::EDGE;
   const int rows = (int)min<int64_t>(G::EDGE, a.M - m0), cols = min(G::EDGE, a.N - n0);
-  const int k0 = part * a.k_part, k1 = min(a.K, k0 + a.k_part);
+  const int k0 = a.cut.first(part), k1 = a.cut.end(part);
   Operand<T> oa, ob;
   oa.base = (const T*)a.a + (AR ? (int64_t)k0 * a.lda + place_of<PL>(m0) : m0 * a.lda + place_of<PL>(k0));
   oa.ld = a.lda; oa.rows = rows; oa.second = a.second;
@@ -569,8 +571,8 @@ template <class O, class T, int W, bool AR, bool BR, int ACT, bool TWICE> void r
 template <class O, class T, bool AR, bool BR, int ACT, bool TWICE = false> void run_product(hipStream_t st, ProductArgs& a, const ProductShape& s) {
   const int b = 2 * s.wave;
   a.tiles_m = ceil_div(a.M, b); a.tiles_n = ceil_div(a.N, b);
-  a.k_part = (int)(((int64_t)ceil_div(a.K, 64) + s.parts - 1) / s.parts) * 64;
-  a.parts = ceil_div(a.K, a.k_part);
+  a.cut = parts_of(a.K, s.parts);
+  a.parts = a.cut.count;
   if (s.wave == 128) run_product_w<O, T, 128, AR, BR, ACT, TWICE>(st, a);
   else if (s.wave == 64) run_product_w<O, T, 64, AR, BR, ACT, TWICE>(st, a);
   else run_product_w<O, T, 32, AR, BR, ACT, TWICE>(st, a);

@@ -217,11 +217,12 @@ struct Tile {
     FA fda;
     FB fdb;
     // what a slot takes: values of k where the operand lies across it, places where along
-    const int kv = PL == 1 ? K : (K + block_of(PL) - 1) / block_of(PL) * SLOT_K;
+    const int once = PL == 1 ? (K + SLOT_K - 1) / SLOT_K : (K + block_of(PL) - 1) / block_of(PL);  // slots
+    const int kv = PL == 1 ? K : AR && BR ? 0 : once * SLOT_K;  // (along: at most the places of a row)
     fda.init(a, AR ? K : kv, wave, lane);
     fdb.init(b, BR ? K : kv, wave, lane);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)smem;
-    const int once = (kv + SLOT_K - 1) / SLOT_K, total = TWICE && !LEADING ? 2 * once : once;
+    const int total = TWICE && !LEADING ? 2 * once : once;
     constexpr int NLD = FA::NLD, MFMAS = MI * MI, PLACES = S::N * MFMAS;
     // Load n of the sequence A, B, A, B, ... goes to slot n mod RING; from the hand-over of tile step t - 1 to that of t, loads
     // 2 t + RING - 2 and the next go out

@@ -60,7 +60,7 @@ DATAFLOW_KERNELS = {
 
 
 DATAFLOW_ONLY = ("k_dataflow.hip", "dataflow.cpp")          # sources of the data-flow kernels alone
-MATRIX_ONLY = ("mat_core.h", "matrix.h", "matrix.cpp", "k_linear.hip", "ortho.cpp", "k_ortho.hip")  # ... of the matrix operators
+MATRIX_ONLY = ("mat_core.h", "matrix.h", "parts.h", "matrix.cpp", "k_linear.hip", "ortho.cpp", "k_ortho.hip")  # ... of the matrix operators
 SHARED = ("dev_common.h", "launch.h")                         # device helpers both kinds of kernels are built from
 
 
