@@ -672,7 +672,7 @@ class OrthoPlan:
     """optorch_ortho_create + optorch_ortho_query: the host-side plan for a list of matrices, no device needed.
 
     matrices: (rows, cols) each, one behind the other in a flat vector, or (offset, rows, cols, ld) for other places.
-    coefficients: (a, b, c) for every step, or one such triple per step."""
+    steps: 5 where none or fewer are asked for.  coefficients: (a, b, c) for every step, or one such triple per step."""
 
     def __init__(self, matrices, *, steps: int = 5, coefficients=None, eps: float = 1e-7):
         self.lib = load_library()
@@ -684,6 +684,7 @@ class OrthoPlan:
                 m = (at, m[0], m[1], m[1])
             arr[i] = optorch_matrix_t(*[int(v) for v in m])
             at = m[0] + (m[1] - 1) * m[3] + m[2]
+        steps = steps if steps > 0 else 5  # (what the library takes it for, and reads coefficients of)
         cfg = optorch_ortho_config_t()
         cfg.steps, cfg.eps = steps, eps
         if coefficients is not None:

@@ -48,3 +48,20 @@ def test_the_allocator_is_told_of_every_stream_that_uses_a_workspace():
     o.capturing = True  # (nothing runs; the graph's user keeps the object)
     o.orthogonalize(v, v)
     assert o.told == [9, 11]
+
+
+def test_no_steps_are_five_and_so_are_their_coefficients(monkeypatch):
+    """The library takes steps <= 0 for five and reads three coefficients of each."""
+    seen = []
+
+    def create(arr, n, cfg, out):
+        cfg = cfg._obj
+        seen.append((cfg.steps, [cfg.coefficients[i] for i in range(3 * cfg.steps)]))
+        return B.OK
+
+    monkeypatch.setattr(B, "load_library", lambda: types.SimpleNamespace(
+        optorch_ortho_create=create, optorch_ortho_query=lambda *a: B.OK, optorch_ortho_destroy=lambda h: None))
+    for steps in (0, -3, 5):
+        B.OrthoPlan([(4, 4)], steps=steps, coefficients=(2.0, -1.5, 0.5))
+        B.OrthoPlan([(4, 4)], steps=steps, coefficients=[(2.0, -1.5, 0.5)] * 5)
+    assert seen == [(5, [2.0, -1.5, 0.5] * 5)] * 6
