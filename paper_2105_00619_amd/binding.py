@@ -546,6 +546,14 @@ def _mat_fail(rc: int):
     raise OptorchError(rc, (load_library().optorch_matrix_last_error() or b"").decode())
 
 
+def _int32(name, v):
+    """v as an int that its C field holds (ctypes cuts off what does not fit)."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError("%s: %d is too large" % (name, v))
+    return v
+
+
 def _check_matrix(name, t, rows, cols, like):
     """A rows x cols matrix of like's type and device whose rows lie one behind the other (any distance)."""
     if tuple(t.shape) != (rows, cols):
@@ -576,7 +584,7 @@ def _linear_args(x, activation, rows, cin, cout):
         raise ValueError("the operands must be on the GPU")
     a = optorch_linear_t()
     a.precision, a.activation = _precision(x.dtype), ACTIVATIONS[activation]
-    a.rows, a.in_features, a.out_features = rows, cin, cout
+    a.rows, a.in_features, a.out_features = rows, _int32("in_features", cin), _int32("out_features", cout)
     return a
 
 
@@ -682,7 +690,7 @@ class OrthoPlan:
         for i, m in enumerate(matrices):
             if len(m) == 2:
                 m = (at, m[0], m[1], m[1])
-            arr[i] = optorch_matrix_t(*[int(v) for v in m])
+            arr[i] = optorch_matrix_t(int(m[0]), _int32("rows", m[1]), _int32("cols", m[2]), int(m[3]))
             at = m[0] + (m[1] - 1) * m[3] + m[2]
         steps = steps if steps > 0 else 5  # (what the library takes it for, and reads coefficients of)
         cfg = optorch_ortho_config_t()

@@ -65,3 +65,16 @@ def test_no_steps_are_five_and_so_are_their_coefficients(monkeypatch):
         B.OrthoPlan([(4, 4)], steps=steps, coefficients=(2.0, -1.5, 0.5))
         B.OrthoPlan([(4, 4)], steps=steps, coefficients=[(2.0, -1.5, 0.5)] * 5)
     assert seen == [(5, [2.0, -1.5, 0.5] * 5)] * 6
+
+
+def test_sizes_beyond_their_c_fields_are_refused():
+    """2^32 + 4 is not 4."""
+    import torch
+    for m in ((2 ** 32 + 4, 4), (4, 2 ** 32 + 4), (0, 4, 2 ** 31, 2 ** 31), (0, -2 ** 32 + 4, 4, 4)):
+        with pytest.raises(ValueError, match="too large"):
+            B.OrthoPlan([m])
+    x = types.SimpleNamespace(is_cuda=True, dtype=torch.bfloat16)
+    for cin, cout, name in ((2 ** 32 + 8, 8, "in_features"), (8, 2 ** 32 + 8, "out_features")):
+        with pytest.raises(ValueError, match=name):
+            B._linear_args(x, "none", 0, cin, cout)
+    assert B._linear_args(x, "none", 0, 8, 16).out_features == 16
