@@ -308,8 +308,9 @@ product_kernel(ProductArgs a) {
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   // neighbouring tiles on one XCD: each of the eight takes a run of them, eight rows of tiles at a time
   const int total = a.tiles_m * a.tiles_n * a.parts;
-  const int per = (total + 7) / 8, id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per || id >= total) return;
+  const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
+  const int per = (total + 7) / 8, id = (block & 7) * per + (block >> 3);
+  if ((int)(block >> 3) >= per || id >= total) return;
   const int tiles = a.tiles_m * a.tiles_n, part = id / tiles, t = id - part * tiles;
   const int band = t / (8 * a.tiles_n), rows_in = min(8, a.tiles_m - band * 8), u = t - band * 8 * a.tiles_n;
   const int tn = u / rows_in, tm = band * 8 + u - tn * rows_in;
@@ -483,7 +484,8 @@ __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
   extern __shared__ float red[];  // [wavefront][MB][256]
   const ProductArgs& a = g.p;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int64_t first = (int64_t)blockIdx.x * 16;
+  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16;
+  if (first >= (NARROW ? a.M : (int64_t)a.N)) return;
   const int r16 = lane & 15, kc = (lane >> 4) * 8;
   const int k0 = wave * g.k_wave, k1 = min(a.K, k0 + g.k_wave);
   // one: the operand of which a block has 16 rows (w, NARROW: x), many: the other one
@@ -555,6 +557,13 @@ template <class T> __global__ void __launch_bounds__(256) clear_kernel(T* p, int
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i / cols * ld + i % cols] = from_f32<T>(0.f);
 }
 
+// A launch has fewer than 2^32 threads along x: blocks of at most 1024 threads (a multiple of eight where they go to XCDs in turn), further
+// rows of them along y
+dim3 grid_of_blocks(int64_t blocks) {
+  constexpr int64_t MOST = 1 << 21;
+  return dim3((unsigned)std::min(blocks, MOST), (unsigned)((blocks + MOST - 1) / MOST));
+}
+
 int grid_of(int64_t n) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, 4096)); }
 
 template <class O, class T, int W, bool AR, bool BR, int ACT, bool TWICE> void run_product_w(hipStream_t st, ProductArgs& a) {
@@ -564,7 +573,7 @@ template <class O, class T, int W, bool AR, bool BR, int ACT, bool TWICE> void r
   auto k = product_kernel<O, T, W, AR, BR, ACT, TWICE>;
   // (more LDS than a launch gets unasked; set again on every launch: which devices know it is not ours to remember)
   if (G::LDS > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
-  OSEQ_LAUNCH(k, dim3(per * 8), dim3(256), G::LDS, st, a);
+  OSEQ_LAUNCH(k, grid_of_blocks((int64_t)per * 8), dim3(256), G::LDS, st, a);
   if (a.parts > 1) OSEQ_LAUNCH((join_kernel<O, ACT>), dim3(grid_of(a.M * ((a.N + 7) / 8))), dim3(256), 0, st, a);
 }
 
@@ -634,7 +643,7 @@ template <class S, class T, int MB, Loads L, bool NARROW, int ACT> void run_skin
   int waves = 4;
   while (waves < most && waves * 512 <= p.K) waves *= 2;
   g.k_wave = (ceil_div(p.K, waves) + 31) & ~31;
-  OSEQ_LAUNCH((skinny_kernel<S, T, MB, L, NARROW, ACT>), dim3(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, g);
+  OSEQ_LAUNCH((skinny_kernel<S, T, MB, L, NARROW, ACT>), grid_of_blocks(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, g);
 }
 template <class S, class T, Loads L, bool NARROW, int ACT> void run_skinny_by(hipStream_t st, ProductArgs& p) {
   const int64_t rows = NARROW ? p.N : p.M;  // of the operand that every block reads

@@ -83,3 +83,17 @@ def test_fp32_infinities_beside_ordinary_values(rows, cin, cout):
         ref[ref.abs() >= most] = torch.sign(ref[ref.abs() >= most]) * float("inf")
         assert torch.equal(torch.isnan(got), torch.isnan(ref))
         assert torch.equal(torch.isposinf(got), torch.isposinf(ref)) and torch.equal(torch.isneginf(got), torch.isneginf(ref))
+
+
+@pytest.mark.parametrize("name,rows,cin", [("fp32", 2 ** 28 + 40, 2), ("bf16", 2 ** 30 + 72, 1)])
+def test_batches_of_more_blocks_than_one_row_of_a_grid(name, rows, cin):
+    """2^28 samples of few outputs straight from memory and 2^30 as tiles of 64 are 2^32 threads, more than a launch has along x."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16}[name]
+    x = torch.empty(rows, cin, dtype=dt, device="cuda")
+    x.copy_((torch.arange(rows, device="cuda") % 251 - 125)[:, None])  # (whole numbers that bf16 holds)
+    w = torch.tensor([[0.5, -0.25][:cin]], dtype=dt, device="cuda")
+    y = B.linear_forward(x, w)
+    want = x[:, 0] * (0.25 if cin == 2 else 0.5)
+    assert torch.equal(y[:, 0], want)
