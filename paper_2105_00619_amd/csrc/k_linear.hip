@@ -39,18 +39,19 @@ template <int ACT> __device__ __forceinline__ float act(float z) {
   return z;
 }
 
-template <int ACT> __device__ __forceinline__ float act_slope(float z) {
-  if (ACT == OPTORCH_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+// act'(z) dy.  What ReLU masks is 0, infinities and NaNs too.
+template <int ACT> __device__ __forceinline__ float act_gradient(float z, float dy) {
+  if (ACT == OPTORCH_ACT_RELU) return z > 0.f ? dy : 0.f;
   if (ACT == OPTORCH_ACT_GELU) {
     float e;
     const float c = normal_cdf(z, e);
-    return __fmaf_rn(z * 0.39894228040143268f, e, c);
+    return dy * __fmaf_rn(z * 0.39894228040143268f, e, c);
   }
   if (ACT == OPTORCH_ACT_SILU) {
     const float s = logistic(z);
-    return s * (1.f + z * (1.f - s));
+    return dy * (s * (1.f + z * (1.f - s)));
   }
-  return 1.f;
+  return dy;
 }
 
 // Eight (or four) neighbouring values, n of them inside, at any address (the memory system takes accesses off their alignment; value by
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(256) dz_kernel(DzArgs a) {
       if (ACT != OPTORCH_ACT_NONE) {
         load8<S>((const S*)a.z + r * a.ldz + c, n, z);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= act_slope<ACT>(z[e]);
+        for (int e = 0; e < 8; ++e) v[e] = act_gradient<ACT>(z[e], v[e]);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {

@@ -97,3 +97,19 @@ def test_batches_of_more_blocks_than_one_row_of_a_grid(name, rows, cin):
     y = B.linear_forward(x, w)
     want = x[:, 0] * (0.25 if cin == 2 else 0.5)
     assert torch.equal(y[:, 0], want)
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16", "fp16"])
+def test_what_relu_masks_is_zero(name):
+    """An infinite or NaN gradient of an output that ReLU has cut off reaches nothing."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[name]
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    dy, x, w, z = (torch.randn(s, generator=gen, device="cuda").to(dt) for s in ((70, 33), (70, 20), (33, 20), (70, 33)))
+    z[3], z[5, 7] = 0.0, -1.0
+    masked = z <= 0
+    clean = B.linear_backward(dy, x, w, z, activation="relu")
+    dy[masked] = float("inf")
+    dy[5, 7], dy[3, 1] = float("nan"), float("-inf")
+    assert all(torch.equal(a, b) for a, b in zip(B.linear_backward(dy, x, w, z, activation="relu"), clean))
