@@ -131,3 +131,27 @@ def test_gradients_in_fp16_have_the_range_of_their_results(rows, cin, cout, act)
     for got, ref in ((dx, torch.mm(dz, w.double())), (dw, torch.mm(dz.T.contiguous(), x.double()))):
         assert torch.equal(torch.isnan(got), torch.isnan(ref))
         assert torch.equal(torch.isposinf(got), torch.isposinf(ref)) and torch.equal(torch.isneginf(got), torch.isneginf(ref))
+
+
+@pytest.mark.parametrize("name", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("rows,width", [(40, 40), (1000, 40), (2000, 200)])
+def test_gelu_and_its_slope_have_their_bits_in_the_tail(rows, width, name):
+    """x = z, w = 1: every output is GELU of one value, relative to which (not to 1) it is off by the polynomial (fp32 2e-8, 16 bits 4e-6) and
+    a handful of roundings: 2^-20 and 2^-16, beside the rounding to 16 bits (of values below the smallest normal one: of that)."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    dt = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[name]
+    far = -12.5 if name != "fp16" else -5.0
+    z = torch.linspace(far, 9.0, rows * width, device="cuda", dtype=torch.float64)[torch.randperm(rows * width, device="cuda")].view(rows, width).to(dt)
+    one = torch.eye(width, device="cuda", dtype=dt)
+    y = B.linear_forward(z, one, activation="gelu")
+    phi = 0.5 * torch.special.erfc(-z.double() / math.sqrt(2))
+    density = torch.exp(-z.double() ** 2 / 2) / math.sqrt(2 * math.pi)
+    info = torch.finfo(dt)
+    more, half = (2.0 ** -20, 0.0) if name == "fp32" else (2.0 ** -16, info.eps / 2)
+    least = info.smallest_normal * half
+    want = z.double() * phi
+    assert bool(((y.double() - want).abs() <= (more + half) * want.abs() + least).all())
+    dx, _, _ = B.linear_backward(torch.ones_like(z), z, one, z, activation="gelu")
+    want = phi + z.double() * density
+    assert bool(((dx.double() - want).abs() <= more * (phi + z.double().abs() * density) + half * want.abs() + least).all())
