@@ -77,7 +77,7 @@ class FeedForward:
         d = (p.exp() - torch.nn.functional.one_hot(y, p.shape[1])) / len(y)
         self.backward(d.to(x.dtype), kept)
         self.ortho.muon_update(self.w, self.v, self.g, lr=lr, weight_decay=0.01, weights16=self.w16, skipped=self.skipped)
-        self.b.sub_(torch.where(self.skipped == 0, lr, 0.0) * self.db)
+        self.b.sub_(torch.where(self.skipped == 0, lr * self.db, 0.0))  # (not 0 times what may be infinite)
         return loss
 
 
@@ -102,14 +102,14 @@ def train_cnn(steps=30, batch=64, size=16, classes=10, lr=0.02, report=None):
     units = W.resnet_basic([1, 1], classes, base=16)
     t = B.SeqTrainer(units, k_segments=2, precision=W.BF16, batch=batch, height=size, width=size, channels=3, num_classes=classes)
     w = torch.from_numpy(W.make_params(units, size, size)).cuda()
-    matrices, other, at = [], torch.ones_like(w), 0
+    matrices, other, at = [], torch.ones_like(w, dtype=torch.bool), 0
     for _, shape, role, _ in W.param_layout(units, size, size):
         rows, cols = shape[0], 1
         for n in shape[1:]:
             cols *= n
         if role in ("conv_w", "lin_w"):
             matrices.append((at, rows, cols, cols))
-            other[at:at + rows * cols] = 0
+            other[at:at + rows * cols] = False
         at += rows * cols
     ortho = B.Orthogonalizer(matrices)
     v, g = torch.zeros_like(w), torch.zeros_like(w)
@@ -118,9 +118,11 @@ def train_cnn(steps=30, batch=64, size=16, classes=10, lr=0.02, report=None):
     losses = []
     for i in range(steps):
         t.set_params(w)
-        losses.append(t.step(x, y, lr=0.0, grads=g)["loss"])
-        ortho.muon_update(w, v, g, lr=lr)
-        w.sub_(lr * g * other)
+        step = t.step(x, y, lr=0.0, grads=g)
+        losses.append(step["loss"])
+        if not step["skipped"]:  # (else g holds no gradient)
+            ortho.muon_update(w, v, g, lr=lr)
+            w.sub_(torch.where(other, lr * g, 0.0))
         if report and i % 10 == 0:
             report("cnn", i, losses[-1])
     return losses
