@@ -116,13 +116,14 @@ def train_cnn(steps=30, batch=64, size=16, classes=10, lr=0.02, report=None):
     x = torch.from_numpy(W.make_images(batch, size, size, 3)).cuda()
     y = torch.from_numpy(W.make_labels(batch, classes)).cuda()
     losses = []
+    t.set_params(w)
     for i in range(steps):
-        t.set_params(w)
         step = t.step(x, y, lr=0.0, grads=g)
         losses.append(step["loss"])
         if not step["skipped"]:  # (else g holds no gradient)
             ortho.muon_update(w, v, g, lr=lr)
             w.sub_(torch.where(other, lr * g, 0.0))
+            t.update_params(w)
         if report and i % 10 == 0:
             report("cnn", i, losses[-1])
     return losses

@@ -133,6 +133,10 @@ int optorch_seq_bind(optorch_seq_t* h, void* param_arena_dev, uint64_t param_are
  * device memory, zeroes the momentum, resets BN running statistics and the loss scale, and
  * refreshes the 16-bit copies. */
 int optorch_seq_set_params(optorch_seq_t* h, const float* src, uint64_t n, int32_t is_device);
+
+/* The same for a network in training whose weights an update of the caller's has changed (optorch_matrix.h): momentum, running
+ * statistics and loss scale stay as they are.  After optorch_seq_set_params. */
+int optorch_seq_update_params(optorch_seq_t* h, const float* src, uint64_t n, int32_t is_device);
 int optorch_seq_get_params(const optorch_seq_t* h, float* dst, uint64_t n, int32_t is_device);
 
 /* One training step on one batch.

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "liboptorch_seq.so")
 OK, E_INVALID, E_BUDGET, E_HIP, E_ORDER = 0, -1, -2, -3, -4
 
 SYMBOLS = (
-    "optorch_seq_create", "optorch_seq_query", "optorch_seq_bind", "optorch_seq_set_params",
+    "optorch_seq_create", "optorch_seq_query", "optorch_seq_bind", "optorch_seq_set_params", "optorch_seq_update_params",
     "optorch_seq_get_params", "optorch_seq_step", "optorch_seq_schedule_info", "optorch_seq_last_error",
     "optorch_seq_destroy", "optorch_seq_predict", "optorch_seq_running_stats", "optorch_seq_profile_enable", "optorch_seq_profile_select", "optorch_seq_profile_read", "optorch_seq_profile_read_entries",
     "optorch_seq_step_encoded", "optorch_seq_predict_encoded", "optorch_seq_plan_info", "optorch_seq_step_static", "optorch_seq_debug_unit_output",
@@ -96,6 +96,8 @@ def load_library() -> C.CDLL:
     lib.optorch_seq_bind.restype = C.c_int
     lib.optorch_seq_set_params.argtypes = [H, C.c_void_p, C.c_uint64, C.c_int32]
     lib.optorch_seq_set_params.restype = C.c_int
+    lib.optorch_seq_update_params.argtypes = [H, C.c_void_p, C.c_uint64, C.c_int32]
+    lib.optorch_seq_update_params.restype = C.c_int
     lib.optorch_seq_get_params.argtypes = [H, C.c_void_p, C.c_uint64, C.c_int32]
     lib.optorch_seq_get_params.restype = C.c_int
     lib.optorch_seq_step.argtypes = [H, C.c_void_p, C.c_void_p, C.c_float, C.POINTER(C.c_float), C.c_void_p,
@@ -301,13 +303,20 @@ class SeqTrainer(SeqPlan):
         return cls(w.units, device=device, **kw)
 
     def set_params(self, params):
+        self._put_params(self.lib.optorch_seq_set_params, params)
+
+    def update_params(self, params):
+        """Weights that an update outside of `step` has made: momentum, running statistics and loss scale go on."""
+        self._put_params(self.lib.optorch_seq_update_params, params)
+
+    def _put_params(self, call, params):
         torch = self.torch
         if isinstance(params, np.ndarray):
             p = np.ascontiguousarray(params, dtype=np.float32)
-            self._check(self.lib.optorch_seq_set_params(self.handle, p.ctypes.data, p.size, 0))
+            self._check(call(self.handle, p.ctypes.data, p.size, 0))
         else:
             p = params.to(device=self.device, dtype=torch.float32).contiguous()
-            self._check(self.lib.optorch_seq_set_params(self.handle, p.data_ptr(), p.numel(), 1))
+            self._check(call(self.handle, p.data_ptr(), p.numel(), 1))
 
     def get_params(self) -> np.ndarray:
         out = np.empty(self.param_count, dtype=np.float32)

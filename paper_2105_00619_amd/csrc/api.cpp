@@ -310,6 +310,22 @@ extern "C" int optorch_seq_set_params(optorch_seq_t* h, const float* src, uint64
   return OPTORCH_OK;
 }
 
+extern "C" int optorch_seq_update_params(optorch_seq_t* h, const float* src, uint64_t n, int32_t is_device) {
+  if (!h) return OPTORCH_E_INVALID;
+  if (!h->bound || !h->params_set) return set_err(h, OPTORCH_E_ORDER, "update_params before bind/set_params");
+  if (!src || n != h->plan.n_params) return set_err(h, OPTORCH_E_INVALID, "update_params: wrong parameter count");
+  hipStream_t st = h->stream;
+  hipError_t e = hipMemcpyAsync(h->pbase + h->off_w, src, n * 4, is_device ? hipMemcpyDeviceToDevice : hipMemcpyHostToDevice, st);
+  if (e != hipSuccess) return hip_fail(h, e, "hipMemcpyAsync(params)");
+  launch_cast_params(st, h->dt, (const float*)(h->pbase + h->off_w), h->pbase + h->off_h, (int64_t)n);
+  refresh_transposed_weights(h);
+  e = hipStreamSynchronize(st);
+  if (e != hipSuccess) return hip_fail(h, e, "hipStreamSynchronize");
+  e = hipGetLastError();
+  if (e != hipSuccess) return hip_fail(h, e, "update_params kernels");
+  return OPTORCH_OK;
+}
+
 extern "C" int optorch_seq_get_params(const optorch_seq_t* h, float* dst, uint64_t n, int32_t is_device) {
   if (!h) return OPTORCH_E_INVALID;
   if (!h->bound || !h->params_set) return set_err(h, OPTORCH_E_ORDER, "get_params before bind/set_params");

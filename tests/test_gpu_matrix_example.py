@@ -49,3 +49,38 @@ def test_a_skipped_step_of_a_cnn_changes_no_weight(example, monkeypatch):
     losses = example.train_cnn(steps=30, batch=32)
     assert all(v == v and v < 100 for v in losses) and losses[2] == losses[1]
     assert losses[-1] < 0.5 * losses[0]
+
+
+@pytest.mark.parametrize("precision", ["BF16", "FP16", "FP32"])
+def test_updated_weights_leave_the_training_state_alone(example, precision):
+    """Weights put back as they were between the steps change nothing: neither momentum, nor running statistics, nor loss scale."""
+    import numpy as np
+    import torch
+    W, B = example.W, example.B
+    units = W.resnet_basic([1, 1], 10, base=16)
+    x, y = torch.from_numpy(W.make_images(8, 16, 16, 3)).cuda(), torch.from_numpy(W.make_labels(8, 10)).cuda()
+    seen = []
+    for again in (False, True):
+        t = B.SeqTrainer(units, k_segments=2, precision=getattr(W, precision), batch=8, height=16, width=16, channels=3, num_classes=10, momentum=0.9)
+        t.set_params(W.make_params(units, 16, 16))
+        out = []
+        for i in range(4):
+            out.append(t.step(x, y, lr=0.05))
+            if again and i < 3:
+                p = t.get_params()
+                t.update_params(p if i % 2 else torch.from_numpy(p).cuda())
+        seen.append((out, t.get_params(), t.running_stats(), t.predict(x).cpu()))
+    (a, pa, ra, qa), (b, pb, rb, qb) = seen
+    assert a == b and np.array_equal(pa, pb) and np.array_equal(np.asarray(ra), np.asarray(rb)) and torch.equal(qa, qb)
+
+
+def test_the_cnn_keeps_its_statistics_from_step_to_step(example, monkeypatch):
+    """Inference with the running statistics of the whole training knows the batch that it has learnt."""
+    import torch
+    trainers = []
+    make = example.B.SeqTrainer.__init__
+    monkeypatch.setattr(example.B.SeqTrainer, "__init__", lambda self, *a, **kw: (trainers.append(self), make(self, *a, **kw))[1])
+    example.train_cnn(steps=40, batch=32)
+    t = trainers[0]
+    x, y = torch.from_numpy(example.W.make_images(32, 16, 16, 3)).cuda(), torch.from_numpy(example.W.make_labels(32, 10)).cuda().long()
+    assert float(torch.nn.functional.cross_entropy(t.predict(x), y)) < 1.0  # (guessing: 2.3)

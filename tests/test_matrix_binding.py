@@ -78,3 +78,12 @@ def test_sizes_beyond_their_c_fields_are_refused():
         with pytest.raises(ValueError, match=name):
             B._linear_args(x, "none", 0, cin, cout)
     assert B._linear_args(x, "none", 0, 8, 16).out_features == 16
+
+
+def test_weights_are_updated_after_they_were_set():
+    from paper_2105_00619_amd import workloads as W
+    p = B.SeqPlan.from_workload(W.config(3))
+    lib = B.load_library()
+    src = (B.C.c_float * p.param_count)()
+    assert lib.optorch_seq_update_params(p.handle, src, p.param_count, 0) == B.E_ORDER
+    assert lib.optorch_seq_update_params(None, src, p.param_count, 0) == B.E_INVALID
