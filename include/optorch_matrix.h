@@ -4,8 +4,8 @@
  * update of weight matrices.  C ABI; part of liboptorch_seq.so.
  *
  * Matrices are row-major: element (r, c) at r * ld + c, ld >= columns, any alignment of the element
- * type.  Pointers are DEVICE pointers unless named *_host.  Buffers that are written must not overlap any
- * other buffer of the call unless stated otherwise.
+ * type.  Pointers are DEVICE pointers unless named *_host.  Matrices and vectors that are written must not share an
+ * element with any other of the call unless stated otherwise (refused; rows that lie between each other's are apart).
  *
  * Execution: every call only enqueues kernels on the stream it is given (NULL = the default stream) and
  * returns; it neither allocates nor synchronises and may be captured into a HIP graph.  The caller owns

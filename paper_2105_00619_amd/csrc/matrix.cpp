@@ -80,6 +80,40 @@ static int linear_check(const optorch_linear_t* a, bool backward) {
   return rc;
 }
 
+// What the call writes against everything that it reads or writes besides
+static int linear_overlaps(const optorch_linear_t* a, bool backward, uint64_t workspace_bytes) {
+  struct Named { const char* name; Place p; bool written; } list[10];
+  int n = 0;
+  const int e = bytes_of(a->precision);
+  auto add = [&](const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes, bool written) {
+    if (p && rows > 0 && cols > 0) list[n++] = Named{name, place_in(p, rows, cols, ld, bytes), written};
+  };
+  const int64_t rows = a->rows, in = a->in_features, out = a->out_features;
+  const bool slope = a->activation != OPTORCH_ACT_NONE;
+  if (!backward || a->dw) add("x", a->x, rows, in, a->ldx, e, false);
+  if (!backward || a->dx) add("w", a->w, out, in, a->ldw, e, false);
+  if (!backward || slope) add("z", a->z, rows, out, a->ldz, e, !backward);
+  if (!backward) {
+    add("bias", a->bias, 1, out, out, 4, false);
+    add("residual", a->residual, rows, out, a->ldr, e, false);
+    add("y", a->y, rows, out, a->ldy, e, true);
+  } else {
+    add("dy", a->dy, rows, out, a->lddy, e, false);
+    add("dx", a->dx, rows, in, a->lddx, e, true);
+    add("dw", a->dw, out, in, a->lddw, e, true);
+    add("dbias", a->dbias, 1, out, out, 4, true);
+  }
+  add("workspace", workspace_bytes ? a->workspace : nullptr, 1, (int64_t)workspace_bytes, (int64_t)workspace_bytes, 1, true);
+  for (int i = 0; i < n; ++i)
+    for (int j = i + 1; j < n; ++j) {
+      const Named &p = list[i], &q = list[j];
+      if (!(p.written || q.written) || !overlap(p.p, q.p)) continue;
+      if (!backward && p.p.at == (uintptr_t)a->residual && q.p.at == (uintptr_t)a->y && same_place(p.p, q.p)) continue;
+      return oseq_mat_err(OPTORCH_E_INVALID, std::string(p.name) + " and " + q.name + " overlap");
+    }
+  return OPTORCH_OK;
+}
+
 extern "C" int64_t optorch_linear_workspace(const optorch_linear_t* a, int32_t backward) {
   return guarded([&]() -> int64_t {
     const int rc = linear_check(a, backward != 0);
@@ -98,6 +132,8 @@ static int linear_run(const optorch_linear_t* a, bool backward) {
     if (p.bytes > a->workspace_bytes) return oseq_mat_err(OPTORCH_E_BUDGET, "workspace too small: " + std::to_string(p.bytes) + " bytes are needed");
     if (p.bytes && (uintptr_t)a->workspace % 256) return oseq_mat_err(OPTORCH_E_INVALID, "workspace must be 256-byte aligned");
   }
+  const int apart = linear_overlaps(a, backward, p.bytes);
+  if (apart != OPTORCH_OK) return apart;
   if (!backward && a->rows) launch_linear_forward(*a, p);
   if (backward) launch_linear_backward(*a, p);
   return mat_launched(backward ? "linear_backward" : "linear_forward");

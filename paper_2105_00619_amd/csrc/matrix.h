@@ -13,6 +13,26 @@ namespace oseq {
 inline int64_t up8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 inline uint64_t up256(uint64_t n) { return (n + 255) & ~(uint64_t)255; }
 
+// Where a matrix lies: rows of `width` bytes, `pitch` bytes apart
+struct Place {
+  uintptr_t at; int64_t rows, width, pitch;
+  uintptr_t end() const { return at + (uintptr_t)((rows - 1) * pitch + width); }
+};
+inline Place place_in(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) { return Place{(uintptr_t)p, rows, cols * bytes, ld * bytes}; }
+// Whether two matrices share a byte.  Rows that lie between each other's do not.
+inline bool overlap(const Place& a, const Place& b) {
+  if (a.rows <= 0 || b.rows <= 0 || a.end() <= b.at || b.end() <= a.at) return false;
+  if (a.rows < b.rows) return overlap(b, a);
+  for (int64_t r = 0; r < b.rows; ++r) {
+    // the first of a's rows that ends behind the beginning of this one of b's
+    const int64_t s = (int64_t)(b.at + (uintptr_t)(r * b.pitch)) - (int64_t)a.at;
+    const int64_t i = s < a.width ? 0 : (s - a.width) / a.pitch + 1;
+    if (i < a.rows && i * a.pitch < s + b.width) return true;
+  }
+  return false;
+}
+inline bool same_place(const Place& a, const Place& b) { return a.at == b.at && (a.pitch == b.pitch || a.rows <= 1) && a.width == b.width; }
+
 // How a product M x N over K is cut: block tiles of 2 * wave x 2 * wave, the reduction in `parts`
 struct ProductShape { int wave, parts; };
 

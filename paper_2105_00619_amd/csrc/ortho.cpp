@@ -425,6 +425,31 @@ extern "C" int optorch_ortho_bind(optorch_ortho_t* h, void* workspace_dev, uint6
 static bool known(int32_t precision) { return precision == OPTORCH_FP32 || precision == OPTORCH_BF16 || precision == OPTORCH_FP16; }
 static bool misaligned(const void* p, int32_t precision) { return (uintptr_t)p % (precision == OPTORCH_FP32 ? 4 : 2) != 0; }
 
+// Flat vectors of one list: whether an element of one matrix shares a byte with an element of another vector's
+struct Flat { const char* name; const void* p; int32_t precision; };
+static bool overlap(const OrthoPlanHost& p, const Flat& a, const Flat& b) {
+  auto bytes = [](const Flat& f) { return f.precision == OPTORCH_FP32 ? 4 : 2; };
+  auto place = [&](const Flat& f, const OrthoMat& m) {
+    return place_in((const char*)f.p + m.offset * bytes(f), m.rows, m.cols, m.ld, bytes(f));
+  };
+  const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+  if (pa + (uintptr_t)(p.span * bytes(a)) <= pb || pb + (uintptr_t)(p.span * bytes(b)) <= pa) return false;
+  for (const OrthoMat& m : p.mats)
+    for (const OrthoMat& o : p.mats)
+      if (oseq::overlap(place(a, m), place(b, o))) return true;
+  return false;
+}
+// the same for a check without a device, where no plan is bound (not part of the API)
+namespace oseq {
+bool ortho_vectors_overlap(const optorch_ortho_t* h, const void* a, int32_t a_precision, const void* b, int32_t b_precision);
+bool ortho_vectors_overlap(const optorch_ortho_t* h, const void* a, int32_t a_precision, const void* b, int32_t b_precision) {
+  return ::overlap(h->p, Flat{"a", a, a_precision}, Flat{"b", b, b_precision});
+}
+}  // namespace oseq
+static int overlap_error(const Flat& a, const Flat& b) {
+  return oseq_mat_err(OPTORCH_E_INVALID, std::string(a.name) + " and " + b.name + " overlap");
+}
+
 static int ortho_launched(const char* what) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return oseq_mat_err(OPTORCH_E_HIP, std::string(what) + ": " + hipGetErrorString(e));
@@ -437,6 +462,8 @@ extern "C" int optorch_orthogonalize(optorch_ortho_t* h, int32_t g_precision, co
     if (!h->ws) return oseq_mat_err(OPTORCH_E_ORDER, "orthogonalize before bind");
     if (!known(g_precision) || !known(o_precision)) return oseq_mat_err(OPTORCH_E_INVALID, "unknown precision");
     if (!g || !o || misaligned(g, g_precision) || misaligned(o, o_precision)) return oseq_mat_err(OPTORCH_E_INVALID, "null or misaligned vector");
+    const Flat fg{"g", g, g_precision}, fo{"o", o, o_precision};
+    if (!(g == o && g_precision == o_precision) && overlap(h->p, fg, fo)) return overlap_error(fg, fo);
     OrthoRun r = {};
     r.g_precision = g_precision; r.g = g; r.o_precision = o_precision; r.o = o;
     launch_ortho((hipStream_t)hip_stream, h->p, h->ws, r);
@@ -456,6 +483,10 @@ extern "C" int optorch_muon_update(optorch_ortho_t* h, const optorch_muon_t* a, 
     if (a->scale_mode < OPTORCH_SCALE_NONE || a->scale_mode > OPTORCH_SCALE_RMS) return oseq_mat_err(OPTORCH_E_INVALID, "unknown scale mode");
     if (!std::isfinite(a->lr) || !std::isfinite(a->momentum) || !std::isfinite(a->weight_decay) || !std::isfinite(a->grad_scale))
       return oseq_mat_err(OPTORCH_E_INVALID, "lr, momentum, weight_decay and grad_scale must be finite");
+    const Flat f[4] = {{"g", a->g, a->g_precision}, {"w", a->w, OPTORCH_FP32}, {"v", a->v, OPTORCH_FP32}, {"w16", a->w16, a->w16_precision}};
+    for (int i = 0; i < 4; ++i)
+      for (int j = i + 1; j < (a->w16 ? 4 : 3); ++j)
+        if (overlap(h->p, f[i], f[j])) return overlap_error(f[i], f[j]);
     OrthoRun r = {};
     r.g_precision = a->g_precision; r.g = a->g; r.muon = true; r.m = *a;
     launch_ortho((hipStream_t)hip_stream, h->p, h->ws, r);

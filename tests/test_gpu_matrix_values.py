@@ -113,3 +113,28 @@ def test_what_relu_masks_is_zero(name):
     dy[masked] = float("inf")
     dy[5, 7], dy[3, 1] = float("nan"), float("-inf")
     assert all(torch.equal(a, b) for a, b in zip(B.linear_backward(dy, x, w, z, activation="relu"), clean))
+
+
+def test_buffers_side_by_side_are_apart():
+    """Operands and results whose rows lie between each other's share no element; those that do are refused."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    buf = torch.randn(90, 200, generator=gen, device="cuda")
+    x, y, dy = buf[:, :60], buf[:, 60:100], buf[:, 100:140]
+    w = torch.randn(40, 60, generator=gen, device="cuda")
+    want = B.linear_forward(x, w)
+    assert torch.equal(B.linear_forward(x, w, out=y), want) and torch.equal(y, want)
+    dx = B.linear_backward(dy, x, w, need=("dx",))[0]
+    assert torch.equal(B.linear_backward(dy, x, w, need=("dx",), dx=buf[:, 140:])[0], dx)
+    square = torch.randn(60, 60, generator=gen, device="cuda")
+    with pytest.raises(B.OptorchError, match="x and y overlap"):
+        B.linear_forward(x, square, out=x)
+    with pytest.raises(B.OptorchError, match="dy and dx overlap"):
+        B.linear_backward(x, x, square, need=("dx",), dx=buf[:, 1:61])
+    p = B.Orthogonalizer([(8, 9)])
+    v = torch.randn(300, generator=gen, device="cuda")
+    with pytest.raises(B.OptorchError, match="g and o overlap"):
+        p.orthogonalize(v[:72], v[71:143])
+    with pytest.raises(B.OptorchError, match="w and v overlap"):
+        p.muon_update(v[:72], v[:72], v[100:172], lr=0.1)
