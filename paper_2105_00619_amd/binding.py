@@ -743,9 +743,11 @@ class Orthogonalizer(OrthoPlan):
         import torch
         super().__init__(matrices, **kw)
         self.torch = torch
-        self.device = torch.device(device)
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the matrix operators only run on the HIP path")
+        index = torch.device(device).index
+        self.index = torch.cuda.current_device() if index is None else index
+        self.device = torch.device("cuda", self.index)
         with torch.cuda.device(self.device):
             self.workspace = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=self.device)
             self.home = torch.cuda.current_stream(self.device).cuda_stream  # whose work the allocator waits for before it gives the memory away
@@ -753,8 +755,11 @@ class Orthogonalizer(OrthoPlan):
             torch.cuda.current_stream(self.device).synchronize()
             self._check(self.lib.optorch_ortho_bind(self.handle, self.workspace.data_ptr(), self.workspace_bytes))
 
+    def _here(self, t):
+        return t.is_cuda and t.device.index == self.index
+
     def _flat(self, name, t, dtypes=None):
-        if not t.is_cuda or t.device.index != (self.device.index or 0):
+        if not self._here(t):
             raise TypeError("%s: expected a tensor on %s" % (name, self.device))
         if not t.is_contiguous() or t.numel() < self.span:
             raise ValueError("%s: expected at least %d contiguous elements" % (name, self.span))
@@ -795,8 +800,8 @@ class Orthogonalizer(OrthoPlan):
         a.lr, a.momentum, a.weight_decay, a.grad_scale = lr, momentum, weight_decay, grad_scale
         a.nesterov, a.scale_mode = int(nesterov), SCALE_MODES[scale]
         if skipped is not None:
-            if skipped.dtype != self.torch.int32 or skipped.numel() != 1 or not skipped.is_cuda:
-                raise TypeError("skipped: expected one int32 on the GPU")
+            if skipped.dtype != self.torch.int32 or skipped.numel() != 1 or not self._here(skipped):
+                raise TypeError("skipped: expected one int32 on %s" % self.device)
             a.skipped = skipped.data_ptr()
         with self.torch.cuda.device(self.device):
             self._check(self.lib.optorch_muon_update(self.handle, C.byref(a), self._stream()))

@@ -87,3 +87,18 @@ def test_weights_are_updated_after_they_were_set():
     src = (B.C.c_float * p.param_count)()
     assert lib.optorch_seq_update_params(p.handle, src, p.param_count, 0) == B.E_ORDER
     assert lib.optorch_seq_update_params(None, src, p.param_count, 0) == B.E_INVALID
+
+
+def test_the_flag_of_skipped_updates_is_on_the_plans_device():
+    import torch
+    v = types.SimpleNamespace(data_ptr=lambda: 1 << 20)
+    o = _Bound(home=7)
+    o.index, o.torch.int32 = 1, torch.int32
+    flag = lambda device, cuda=True: types.SimpleNamespace(  # noqa: E731
+        dtype=torch.int32, numel=lambda: 1, is_cuda=cuda, device=types.SimpleNamespace(index=device), data_ptr=lambda: 1 << 20)
+    o.muon_update(v, v, v, lr=0.1, skipped=flag(1))
+    assert o.calls == [7]
+    for bad in (flag(0), flag(2), flag(1, cuda=False)):
+        with pytest.raises(TypeError, match="skipped"):
+            o.muon_update(v, v, v, lr=0.1, skipped=bad)
+    assert o.calls == [7]
