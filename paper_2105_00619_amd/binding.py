@@ -695,12 +695,13 @@ class OrthoPlan:
         self.lib = load_library()
         self.handle = C.c_void_p()
         arr = (optorch_matrix_t * max(1, len(matrices)))()
-        at = 0
+        at = self.elements = 0
         for i, m in enumerate(matrices):
             if len(m) == 2:
                 m = (at, m[0], m[1], m[1])
             arr[i] = optorch_matrix_t(int(m[0]), _int32("rows", m[1]), _int32("cols", m[2]), int(m[3]))
             at = m[0] + (m[1] - 1) * m[3] + m[2]
+            self.elements += m[1] * m[2]
         steps = steps if steps > 0 else 5  # (what the library takes it for, and reads coefficients of)
         cfg = optorch_ortho_config_t()
         cfg.steps, cfg.eps = steps, eps
@@ -775,9 +776,10 @@ class Orthogonalizer(OrthoPlan):
         return s.cuda_stream
 
     def orthogonalize(self, g, out=None):
-        """Newton-Schulz steps on every matrix of the flat tensor g, into out (g's type by default)."""
+        """Newton-Schulz steps on every matrix of the flat tensor g, into out, whose other elements are left alone (by default a new tensor of
+        g's type, zero between the matrices)."""
         if out is None:
-            out = self.torch.empty_like(g)
+            out = self.torch.empty_like(g) if g.numel() == self.elements else self.torch.zeros_like(g)
         gp, op = self._flat("g", g), self._flat("out", out)
         with self.torch.cuda.device(self.device):
             self._check(self.lib.optorch_orthogonalize(self.handle, gp, g.data_ptr(), op, out.data_ptr(), self._stream()))

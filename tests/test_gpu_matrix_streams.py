@@ -26,3 +26,22 @@ def test_a_plan_may_be_dropped_while_another_stream_uses_it():
         o.fill_(255)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_a_new_result_is_zero_between_the_matrices():
+    """Not what the allocation before it left there."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    for mats, n in (([(3, 10, 20, 50), (777, 33, 65, 71)], 777 + 33 * 71), ([(8, 9)], 200)):
+        p = B.Orthogonalizer(mats)
+        g = torch.randn(n, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+        inside = torch.zeros(n, dtype=torch.bool, device="cuda")
+        for m in mats:
+            off, r, c, ld = m if len(m) == 4 else (0, *m, m[1])
+            torch.as_strided(inside, (r, c), (ld, 1), off).fill_(True)
+        for _ in range(3):
+            junk = torch.full((n,), float("nan"), device="cuda")
+            del junk
+            o = p.orthogonalize(g)
+            assert bool((o[~inside] == 0).all()) and bool((o[inside] != 0).all())
+            del o
