@@ -122,6 +122,17 @@ extern "C" int64_t optorch_linear_workspace(const optorch_linear_t* a, int32_t b
   });
 }
 
+// How a product of the call is cut, for the tests that name a kernel by its tile (not part of the API): 1000 * values of a tile's edge +
+// parts; product 0: y, 1: dx, 2: dw.  0: straight from memory.
+namespace oseq {
+int linear_shape(const optorch_linear_t* a, bool backward, int product);
+int linear_shape(const optorch_linear_t* a, bool backward, int product) {
+  const LinearPlan p = plan_linear(*a, backward);
+  const ProductShape s = product == 0 ? p.y : product == 1 ? p.dx : p.dw;
+  return p.straight ? 0 : 2000 * s.wave + s.parts;
+}
+}  // namespace oseq
+
 static int linear_run(const optorch_linear_t* a, bool backward) {
   const int rc = linear_check(a, backward);
   if (rc != OPTORCH_OK) return rc;

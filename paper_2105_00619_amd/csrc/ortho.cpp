@@ -445,6 +445,13 @@ bool ortho_vectors_overlap(const optorch_ortho_t* h, const void* a, int32_t a_pr
 bool ortho_vectors_overlap(const optorch_ortho_t* h, const void* a, int32_t a_precision, const void* b, int32_t b_precision) {
   return ::overlap(h->p, Flat{"a", a, a_precision}, Flat{"b", b, b_precision});
 }
+// how the products of a plan are cut: 1000 * values of a tile's edge + 1 if some sums are cut; list 0: X X^T, 1: m x m, 2: Q X on the way,
+// 3: to the caller's vectors, 4: to weights
+int ortho_shape(const optorch_ortho_t* h, int list);
+int ortho_shape(const optorch_ortho_t* h, int list) {
+  const OrthoList& l = list == 0 ? h->p.gram : list == 1 ? h->p.chain : list == 2 ? h->p.apply : h->p.last[list - 3];
+  return 2000 * l.w + (l.joins ? 1 : 0);
+}
 }  // namespace oseq
 static int overlap_error(const Flat& a, const Flat& b) {
   return oseq_mat_err(OPTORCH_E_INVALID, std::string(a.name) + " and " + b.name + " overlap");
