@@ -66,7 +66,8 @@ int optorch_linear_forward(const optorch_linear_t* a);
 
 /* dz = dy * activation'(z);  dx = dz w,  dw = dz^T x,  dbias = column sums of dz.  In 16-bit precision dz is held as two
  * values of the storage type for the two products, which keeps 16 (bf16) or 22 (fp16) of its bits; dbias sums it unrounded.
- * ReLU's dz is 0 where z is not above 0, whatever dy is there.  The gradient of the skip connection is dy itself.  With rows = 0, dw and dbias are zero. */
+ * ReLU's dz is 0 where z is not above 0, whatever dy is there.  The gradient of the skip connection is dy itself.  With
+ * rows = 0, dw and dbias are zero. */
 int optorch_linear_backward(const optorch_linear_t* a);
 
 /* ---- orthogonalised updates ------------------------------------------------------------------------ */

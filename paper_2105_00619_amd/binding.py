@@ -615,7 +615,9 @@ def _linear_call(torch, lib, fn, a, backward, device):
 
 def linear_forward(x, w, bias=None, *, residual=None, activation="none", save_pre=False, out=None):
     """y = activation(x w^T + bias) + residual: x [rows, in] and w [out, in] in fp32, bf16 or fp16, bias float32 [out],
-    residual [rows, out].  save_pre: also returns z = x w^T + bias, which `linear_backward` reads."""
+    residual [rows, out].  save_pre: also returns z = x w^T + bias, which `linear_backward` reads.  out: where y goes; it may
+    be the residual, and share no element with anything else.  Nothing is recorded for autograd: the gradients are
+    `linear_backward`'s, whether or not the tensors require them."""
     import torch
     rows, cin = x.shape
     cout = w.shape[0]
@@ -646,7 +648,7 @@ def linear_forward(x, w, bias=None, *, residual=None, activation="none", save_pr
 def linear_backward(dy, x, w, z=None, *, activation="none", need=("dx", "dw", "dbias"), dx=None, dw=None, dbias=None):
     """The gradients (dx, dw, dbias) of `linear_forward` from dy [rows, out] and what forward was given and saved; those not
     in `need` are not computed and come back as None.  dbias is float32, the others have x's type.  dx, dw, dbias: tensors to write
-    them to (dw may be a view of a flat vector of gradients)."""
+    them to (dw may be a view of a flat vector of gradients); they share no element with each other or with what is read."""
     import torch
     rows, cin = x.shape
     cout = w.shape[0]

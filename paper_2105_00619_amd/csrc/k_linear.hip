@@ -17,10 +17,11 @@ using namespace mat;
 
 // Phi(z), the normal distribution function, and e = exp(-z^2 / 2), which the density has too:
 //   Phi(-x) = e t q(t),  t = 1 / (1 + p x),  x >= 0,
-// with q fitted to erfcx(x / sqrt 2) / (2 t) for the least relative error on x = 0 .. 14 (reweighted least squares), so that the tail of GELU,
-// where Phi is small, has the same bits as the rest.  FULL (fp32 and all gradients): off by 2e-8, by rounding 4e-7 at most and 1e-7 in the mean, x^2 log2(e) / 2
-// held in two floats as its error is that of e; 16 bits: 4e-6.  (0.5 (1 + erf) in fp32 is 3e-5 off at z = -3.5.)  Layers of 8192 x 64 ->
-// 8192, whose time is that of their outputs: 65 us without an activation, 92 with this in bf16; 125 and 177 in fp32.
+// with q fitted to erfcx(x / sqrt 2) / (2 t) for the least relative error on x = 0 .. 14 (reweighted least squares), so
+// that the tail of GELU, where Phi is small, has the same bits as the rest.  FULL (fp32 and all gradients): off by 2e-8, by
+// rounding 4e-7 at most and 1e-7 in the mean, x^2 log2(e) / 2 held in two floats as its error is that of e; 16 bits: 4e-6.
+// (0.5 (1 + erf) in fp32 is 3e-5 off at z = -3.5.)  Layers of 8192 x 64 -> 8192, whose time is that of their outputs: 65 us
+// without an activation, 92 with this in bf16; 125 and 177 in fp32.
 template <bool FULL> __device__ __forceinline__ float normal_cdf(float z, float& e) {
   float x = fabsf(z);
   x = x > 32.f ? 32.f : x;  // (where e is 0; a NaN stays one)
@@ -78,8 +79,8 @@ template <int ACT> __device__ __forceinline__ float act_gradient(float z, float 
   return dy;
 }
 
-// Eight (or four) neighbouring values, n of them inside, at any address (the memory system takes accesses off their alignment; value by
-// value 20011 rows of 514 took 34 us, so 20)
+// Eight (or four) neighbouring values, n of them inside, at any address (the memory system takes accesses off their
+// alignment; value by value 20011 rows of 514 took 34 us, so 20)
 template <class T, int V> struct Loose { T v[V]; } __attribute__((packed, aligned(alignof(T))));
 template <class T, int V> __device__ __forceinline__ void load8(const T* p, int n, float (&v)[V]) {
   if (n == V) {
@@ -104,9 +105,9 @@ template <class T, int V> __device__ __forceinline__ void store8(T* p, int n, co
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.4028235e38f; }
 
 // ---- operands laid out anew --------------------------------------------------------------------------------------------
-// A value as three bf16 planes: the value rounded, what that leaves, what the two leave.  Where rounding would leave the range of
-// bf16 the first two are cut off instead, so that they do not add up to more than the value; a value that is not finite has it in the
-// first plane alone.
+// A value as three bf16 planes: the value rounded, what that leaves, what the two leave.  Where rounding would leave the
+// range of bf16 the first two are cut off instead, so that they do not add up to more than the value; a value that is not
+// finite has it in the first plane alone.
 __device__ __forceinline__ float cut_off(float x) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, x) & 0xffff0000u); }
 __device__ __forceinline__ void planes_of(float x, bf16_t (&p)[3]) {
   p[0] = (bf16_t)x;
@@ -156,8 +157,8 @@ __global__ void __launch_bounds__(256) pack_kernel(Pack x, Pack w) {
   }
 }
 
-// A value in two 16-bit planes: rounded, and what that leaves.  Where rounding would leave the range of the type (a slope of GELU goes up to
-// 1.13) the first is the type's largest; a value that is not finite has it in the first plane alone.
+// A value in two 16-bit planes: rounded, and what that leaves.  Where rounding would leave the range of the type (a slope
+// of GELU goes up to 1.13) the first is the type's largest; a value that is not finite has it in the first plane alone.
 template <class T> __device__ __forceinline__ void two_planes8(const float (&v)[8], Vec<T, 8>& hi, Vec<T, 8>& lo) {
   constexpr float MOST = __is_same(T, bf16_t) ? 3.3895314e38f : 65504.f;
   hi = round_vec<T, 8>(v);
@@ -180,7 +181,9 @@ struct DzArgs {
   float* sums;    // [row blocks][cols], or null
 };
 // 16 bits: whether dz has more of them than dy
-constexpr bool slopes_of_two(int precision, int act) { return precision != OPTORCH_FP32 && (act == OPTORCH_ACT_GELU || act == OPTORCH_ACT_SILU); }
+constexpr bool slopes_of_two(int precision, int act) {
+  return precision != OPTORCH_FP32 && (act == OPTORCH_ACT_GELU || act == OPTORCH_ACT_SILU);
+}
 template <class S, class T, int PL, int ACT>
 __global__ void __launch_bounds__(256) dz_kernel(DzArgs a) {
   __shared__ float part[8][256 + 8];
@@ -300,7 +303,8 @@ __device__ __forceinline__ void finish(const ProductArgs& a, int64_t row, int co
   store8<O>((O*)a.out + row * a.ldo + col, n, v);
 }
 
-// What sums that are not finite have to become, two bits a value (1: NaN, 2: infinity, 3: -infinity, 0: as summed), eight values a group
+// What sums that are not finite have to become, two bits a value (1: NaN, 2: infinity, 3: -infinity, 0: as summed), eight
+// values a group
 template <int GROUPS> struct Classes {
   uint32_t bits[(GROUPS + 1) / 2];
   // (the group is a constant but where the epilogue is a loop: then a select for each word)
@@ -348,8 +352,8 @@ product_kernel(ProductArgs a) {
   oa.ld = a.lda; oa.rows = rows; oa.second = a.second;
   ob.base = (const T*)a.b + (BR ? (int64_t)k0 * a.ldb + place_of<PL>(n0) : (int64_t)n0 * a.ldb + place_of<PL>(k0));
   ob.ld = a.ldb; ob.rows = cols;
-  // A thread's outputs are of the same eight columns throughout.  (With the bias read for every eight outputs, each read waited for,
-  // 4096 x 4096 x 4096 took 140 us, without a bias 112.)
+  // A thread's outputs are of the same eight columns throughout.  (With the bias read for every eight outputs, each read
+  // waited for, 4096 x 4096 x 4096 took 140 us, without a bias 112.)
   float bias[8];
   int br, bc;
   G::place(0, br, bc);
@@ -374,8 +378,9 @@ product_kernel(ProductArgs a) {
     emit(r, c, v, n, skip);
   });
   if constexpr (PLANES) {
-    // An infinity among the operands makes sums of planes NaN (infinity times a plane of zero).  The groups that wait: the tile is made of the
-    // first planes alone, which says what these sums are, and once more for the others of a group.  So a tile that holds any costs three.
+    // An infinity among the operands makes sums of planes NaN (infinity times a plane of zero).  The groups that wait: the
+    // tile is made of the first planes alone, which says what these sums are, and once more for the others of a group.  So
+    // a tile that holds any costs three.
     if (!G::any_of(smem, wait != 0)) return;
     __syncthreads();
     Classes<G::GROUPS> classes = {};
@@ -416,9 +421,10 @@ __global__ void __launch_bounds__(256) join_kernel(ProductArgs a) {
 }
 
 // ---- few rows ----------------------------------------------------------------------------------------------------------
-// Up to 64 samples: the weights are what is read, once, straight into the operands of 16 x 16 MFMAs.  A block has 16 outputs of all samples,
-// its wavefronts (4 to 16) share the reduction and add up through LDS.  Few outputs: the same with the two operands in each other's
-// place.  1 x 4096 -> 16384 in bf16, 134 MB: 27 us (4.9 TB/s, a copy's rate); as tiles of 64 x 64 with the reduction in four parts 38.
+// Up to 64 samples: the weights are what is read, once, straight into the operands of 16 x 16 MFMAs.  A block has 16
+// outputs of all samples, its wavefronts (4 to 16) share the reduction and add up through LDS.  Few outputs: the same with
+// the two operands in each other's place.  1 x 4096 -> 16384 in bf16, 134 MB: 27 us (4.9 TB/s, a copy's rate); as tiles of
+// 64 x 64 with the reduction in four parts 38.
 struct SkinnyArgs {
   ProductArgs p;       // a: x, b: w as they lie in memory; tiles and parts unused
   int k_wave;          // what a wavefront takes of the reduction, a multiple of 32
@@ -428,10 +434,10 @@ typedef __attribute__((ext_vector_type(4))) float v4f;
 __device__ __forceinline__ v4f mma16(Op<bf16_t>::V a, Op<bf16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ v4f mma16(Op<f16_t>::V a, Op<f16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// Eight values of a row as loaded, those that the eight places from k on have before `end`.  Not SINGLE (at least eight values before
-// `end`): at the end they are the row's last eight, those that an earlier group has taken as zeros: the same ones in either operand.
-// ODD: 16-bit values off the boundaries of 32 bits, from the 32-bit words that hold them (16-byte loads at such addresses: 9705 x 2687
-// -> 37 in bf16 92 us, so 49).
+// Eight values of a row as loaded, those that the eight places from k on have before `end`.  Not SINGLE (at least eight
+// values before `end`): at the end they are the row's last eight, those that an earlier group has taken as zeros: the same
+// ones in either operand. ODD: 16-bit values off the boundaries of 32 bits, from the 32-bit words that hold them (16-byte
+// loads at such addresses: 9705 x 2687 -> 37 in bf16 92 us, so 49).
 enum Loads { WIDE, ODD, SINGLE };
 template <class S> struct Raw8 { Chunk c[sizeof(S) / 2]; };
 template <class S, Loads L> __device__ __forceinline__ Raw8<S> raw8(const S* row, int k, int end) {
@@ -462,8 +468,8 @@ template <class S, Loads L> __device__ __forceinline__ Raw8<S> raw8(const S* row
   }
   return r;
 }
-// ... as MFMA operands, values as planes_of has them: with its cases only where there is a value beyond the largest bf16 (a NaN makes all of its
-// planes NaN here; what counts is the first)
+// ... as MFMA operands, values as planes_of has them: with its cases only where there is a value beyond the largest bf16 (a
+// NaN makes all of its planes NaN here; what counts is the first)
 template <class S, class T> __device__ __forceinline__ void planes8(const Raw8<S>& r, typename Op<T>::V (&p)[sizeof(S) == 4 ? 3 : 1]) {
   if constexpr (sizeof(S) == 2) {
     p[0] = __builtin_bit_cast(typename Op<T>::V, r.c[0]);
@@ -500,8 +506,8 @@ template <class S, class T> __device__ __forceinline__ void planes8(const Raw8<S
   }
 }
 
-// S: type in memory; T: of the planes; MB: blocks of 16 samples, of a block's 16 outputs.  NARROW: MB blocks of 16 outputs, of a block's
-// 16 samples.
+// S: type in memory; T: of the planes; MB: blocks of 16 samples, of a block's 16 outputs.  NARROW: MB blocks of 16 outputs,
+// of a block's 16 samples.
 template <class S, class T, int MB, Loads L, bool NARROW, int ACT>
 __global__ void __launch_bounds__(1024) skinny_kernel(SkinnyArgs g) {
   constexpr int PL = sizeof(S) == 4 ? 3 : 1, U = PL == 3 ? (MB == 4 ? 1 : 2) : L == SINGLE ? 1 : MB == 4 || L == ODD ? 4 : 8;
@@ -582,8 +588,8 @@ template <class T> __global__ void __launch_bounds__(256) clear_kernel(T* p, int
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i / cols * ld + i % cols] = from_f32<T>(0.f);
 }
 
-// A launch has fewer than 2^32 threads along x: blocks of at most 1024 threads (a multiple of eight where they go to XCDs in turn), further
-// rows of them along y
+// A launch has fewer than 2^32 threads along x: blocks of at most 1024 threads (a multiple of eight where they go to XCDs
+// in turn), further rows of them along y
 dim3 grid_of_blocks(int64_t blocks) {
   constexpr int64_t MOST = 1 << 21;
   return dim3((unsigned)std::min(blocks, MOST), (unsigned)((blocks + MOST - 1) / MOST));
@@ -616,11 +622,12 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // whether a 16-bit matrix can be an operand as it lies
 bool direct(const void* p, int64_t ld, int cols) { return aligned16(p) && ld % 8 == 0 && cols % 8 == 0; }
 
-// Tiles and parts of a product, by what it would take in us: tile steps (64 places of two operands), a block's beginning and end, the
-// join of parts (a launch, reading them, and the epilogue's memory by itself).  Two blocks of 128 x 128 or three of 64 x 64 share a CU,
-// which makes their steps a fifth shorter.  Fitted to 12 products of 67 MFLOP to 69 GFLOP, bf16 and fp32, with all tiles and 1 to 32 parts: the choice is within 10 % of the
-// best of them.  (By filling the CUs alone, 1024 x 1024 x 1024 in bf16 took 14.3 us in two parts, 8.3 in one, and
-// 432 x 13952 x 2968 79 us as 64 x 64 tiles, 56 as 128 x 128 in four parts; in fp32 636 and 383.)
+// Tiles and parts of a product, by what it would take in us: tile steps (64 places of two operands), a block's beginning
+// and end, the join of parts (a launch, reading them, and the epilogue's memory by itself).  Two blocks of 128 x 128 or
+// three of 64 x 64 share a CU, which makes their steps a fifth shorter.  Fitted to 12 products of 67 MFLOP to 69 GFLOP,
+// bf16 and fp32, with all tiles and 1 to 32 parts: the choice is within 10 % of the best of them.  (By filling the CUs
+// alone, 1024 x 1024 x 1024 in bf16 took 14.3 us in two parts, 8.3 in one, and 432 x 13952 x 2968 79 us as 64 x 64 tiles,
+// 56 as 128 x 128 in four parts; in fp32 636 and 383.)
 ProductShape shape_of(int64_t M, int64_t N, int64_t K, bool f32) {
   constexpr int CUS = 256;
   ProductShape best = {32, 1};
@@ -786,9 +793,9 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
   const uint64_t in_row = 2 * (uint64_t)(f32 ? row_of<3>(a.in_features) : row_of<1>(a.in_features));
   const uint64_t out_row = 2 * (uint64_t)(f32 ? row_of<3>(a.out_features) : row_of<1>(a.out_features));
   const bool anew_x = f32 || !direct(a.x, a.ldx, a.in_features), anew_w = f32 || !direct(a.w, a.ldw, a.in_features);
-  // Few samples, or few outputs and samples that would be laid out anew.  As tiles / straight from memory, in us: fp32 9705 x 2688 -> 37
-  // 120 / 60; bf16 off its alignment 20000 x 333 -> 10 18 / 8, 4000 x 1001 -> 64 16 / 10, but 40000 x 77 -> 40 12 / 22 and
-  // 9705 x 2687 -> 37 33 / 50: in 16 bits by the operations of the second way.
+  // Few samples, or few outputs and samples that would be laid out anew.  As tiles / straight from memory, in us: fp32 9705
+  // x 2688 -> 37 120 / 60; bf16 off its alignment 20000 x 333 -> 10 18 / 8, 4000 x 1001 -> 64 16 / 10, but 40000 x 77 -> 40
+  // 12 / 22 and 9705 x 2687 -> 37 33 / 50: in 16 bits by the operations of the second way.
   const double straight = (double)a.rows * std::max(a.in_features, 128) * ((a.out_features + 15) & ~15);
   p.straight = !backward && (a.rows <= SKINNY_ROWS || (a.rows >= NARROW_ROWS && a.out_features <= SKINNY_ROWS && anew_x && (f32 || straight < 3e8)));
   const bool need_x = backward ? a.dw != nullptr : !p.straight, need_w = backward ? a.dx != nullptr : !p.straight;
@@ -799,9 +806,9 @@ LinearPlan plan_linear(const optorch_linear_t& a, bool backward) {
   auto take = [&](uint64_t n) { const uint64_t at = o; o = up256(o + n); return at; };
   if (p.pack_x) p.off_x = take((uint64_t)a.rows * in_row);
   if (p.pack_w) p.off_w = take((uint64_t)a.out_features * in_row);
-  // dz of 16-bit layers: rounded once it adds as much as the results' own rounding (dx and dw in bf16 2.3e-3 off, so 1.7e-3), and in fp16 a
-  // large dy times a slope above 1 is infinite.  So it has two planes, and the products twice as much to do (8192 x 2048 -> 8192 in bf16:
-  // 508 us with one, so 975).  ReLU and no activation leave the bits of dy.
+  // dz of 16-bit layers: rounded once it adds as much as the results' own rounding (dx and dw in bf16 2.3e-3 off, so
+  // 1.7e-3), and in fp16 a large dy times a slope above 1 is infinite.  So it has two planes, and the products twice as
+  // much to do (8192 x 2048 -> 8192 in bf16: 508 us with one, so 975).  ReLU and no activation leave the bits of dy.
   const bool two = p.make_dz && slopes_of_two(a.precision, a.activation);
   if (p.make_dz) p.off_dz = take((uint64_t)a.rows * out_row * (two ? 2 : 1));
   if (two) p.dz_second = (int64_t)a.rows * (int64_t)(out_row / 2);

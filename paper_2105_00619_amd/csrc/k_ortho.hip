@@ -82,8 +82,8 @@ __device__ __forceinline__ void source8(const Source& s, int64_t at, int n, floa
   }
 }
 
-// f(place in the flat vectors, n, row of X, column) for groups of eight neighbouring columns of a piece, n of them inside (0: none);
-// a tall matrix' groups run along its own columns: row and column of the transposed group's first value
+// f(place in the flat vectors, n, row of X, column) for groups of eight neighbouring columns of a piece, n of them inside
+// (0: none); a tall matrix' groups run along its own columns: row and column of the transposed group's first value
 template <class F> __device__ __forceinline__ void groups_of(const OrthoChunk& c, const OrthoMat& m, F&& f) {
   if (m.tall) {
     const int col = c.first + (threadIdx.x & 15) * 8;
@@ -310,13 +310,14 @@ __global__ void ORTHO_BOUNDS(W) chain_kernel(OrthoTables t, const OrthoWork* __r
 }
 
 // ---- small matrices ----------------------------------------------------------------------------------------------------
-// All the m x m products between two iterates of a matrix with m <= 128, by one block, a wavefront for each 32 x 32 tile of the lower
-// triangle.  A (then C = P A, then the new A) and P stay in LDS, Q in memory.  A launch for each product takes 3.5 (m = 32) to 5 us
-// (m = 128), most of it waiting for memory and the next launch; here a product takes 1.1 to 3.6, half of that the instructions that
-// round and store a tile: update of matrices of 8 x 27, 8 x 72 and 10 x 8 71 -> 42 us, 100 x 512 orthogonalised 105 -> 96.
+// All the m x m products between two iterates of a matrix with m <= 128, by one block, a wavefront for each 32 x 32 tile of
+// the lower triangle.  A (then C = P A, then the new A) and P stay in LDS, Q in memory.  A launch for each product takes
+// 3.5 (m = 32) to 5 us (m = 128), most of it waiting for memory and the next launch; here a product takes 1.1 to 3.6, half
+// of that the instructions that round and store a tile: update of matrices of 8 x 27, 8 x 72 and 10 x 8 71 -> 42 us with up
+// to three steps between iterates (49 with two, as they are now), 100 x 512 orthogonalised 105 -> 96.
 //
-// LDS: rows as in memory, 512 bytes apart, the 16-byte piece i of row r at i ^ (r & 15), so that sixteen neighbouring rows touch all banks
-// and an address is a lane's own part with a constant in exclusive or and a constant offset.
+// LDS: rows as in memory, 512 bytes apart, the 16-byte piece i of row r at i ^ (r & 15), so that sixteen neighbouring rows
+// touch all banks and an address is a lane's own part with a constant in exclusive or and a constant offset.
 constexpr int SMALL_PITCH = 4 * ORTHO_SMALL;
 constexpr int small_lds(int m) { return 2 * m * SMALL_PITCH; }
 typedef Op<f16_t>::V V8;
@@ -351,7 +352,8 @@ __global__ void __launch_bounds__(640) small_chain_kernel(OrthoTables t, OrthoOp
       *reinterpret_cast<Vec<f16_t, 8>*>(smem + piece_at(i)) = *reinterpret_cast<const Vec<f16_t, 8>*>(a + i * 8);
   }
   __syncthreads();
-  // a lane's part of the addresses: operands of the tile's rows and columns; four neighbouring rows of its column, transposed; its column
+  // a lane's part of the addresses: operands of the tile's rows and columns; four neighbouring rows of its column,
+  // transposed; its column
   const uint32_t row_at = (uint32_t)((r0 + l) * pitch) + (((uint32_t)h ^ fold(l)) << 4), col_at = (uint32_t)((c0 + l) * pitch) + (((uint32_t)h ^ fold(l)) << 4);
   const uint32_t four_at = (uint32_t)((c0 + l) * pitch) + (((uint32_t)(ti * 8) ^ fold(l)) << 4) + h * 8;
   const uint32_t one_at = (((uint32_t)(tj * 8 + (l >> 3)) ^ (uint32_t)(4 * h)) << 4) + (l & 7) * 2;
@@ -360,8 +362,9 @@ __global__ void __launch_bounds__(640) small_chain_kernel(OrthoTables t, OrthoOp
   auto operand = [&](uint32_t at, int k, int g, int plane) {
     return *reinterpret_cast<const V8*>(smem + (at ^ (uint32_t)((k * 8 + plane * 4 + g * 2) << 4)));
   };
-  // (A tile is stored transposed and, off the diagonal, as it is.  On the diagonal the operands change places, so that there too a
-  // product is stored as it is: transposed, what rounding leaves of asymmetry made results of m = 32 four times less exact.)
+  // (A tile is stored transposed and, off the diagonal, as it is.  On the diagonal the operands change places, so that
+  // there too a product is stored as it is: transposed, what rounding leaves of asymmetry made results of m = 32 four times
+  // less exact.)
   auto products = [&](v16f& acc, const V8& ah, const V8& al, const V8& bh, const V8& bl) {
     acc = Op<f16_t>::mma(ah, bl, acc);
     acc = Op<f16_t>::mma(al, bh, acc);

@@ -8,19 +8,21 @@
 //   one plane      columns as they are
 //   two planes     32 columns of plane 0, the same 32 of plane 1; ...
 //   three planes   16 columns of plane 0, of plane 1, of plane 2, 16 unused; ...
-// "Places" below are positions in a row so laid out.  64 places of an operand along k are a slot: four groups of 16, each group one
-// plane of 16 values of k.  (Planes apart in memory, one product of planes after the other, take half as many loads again with two
-// planes and twice as many with three; that is what a product of an operand of two planes with one of 16 bits does, TWICE below.)
+// "Places" below are positions in a row so laid out.  64 places of an operand along k are a slot: four groups of 16, each
+// group one plane of 16 values of k.  (Planes apart in memory, one product of planes after the other, take half as many
+// loads again with two planes and twice as many with three; that is what a product of an operand of two planes with one of
+// 16 bits does, TWICE below.)
 //
-// Four wavefronts in two rows and two columns, each with W x W of the block's 2 W x 2 W.  Slots are a ring in LDS, A and B in turn,
-// filled by loads that write LDS themselves.  While the products of two slots are made, the loads of the two that were used up
-// before go out, evenly.  A tile step of 256 x 256 takes 1.6 to 1.7 us with one plane and 2.1 to 2.2 with two (its MFMAs alone 0.95 and
-// 1.55), one of 128 x 128 0.6 with either, one of 64 x 64 0.3; with the loads going through registers and stores to LDS 10 % more.
+// Four wavefronts in two rows and two columns, each with W x W of the block's 2 W x 2 W.  Slots are a ring in LDS, A and B
+// in turn, filled by loads that write LDS themselves.  While the products of two slots are made, the loads of the two that
+// were used up before go out, evenly.  A tile step of 256 x 256 takes 1.6 to 1.7 us with one plane and 2.1 to 2.2 with two
+// (its MFMAs alone 0.95 and 1.55), one of 128 x 128 0.6 with either, one of 64 x 64 0.3; with the loads going through
+// registers and stores to LDS 10 % more.
 //
-// LDS, K: rows of 128 bytes, the 16-byte piece c of row r at c ^ (r / 2 & 7), so that sixteen consecutive rows, one piece of each,
-// touch all 64 banks once (c ^ (r & 7), right for 32 banks, cost half as many cycles again).  R: rows of one k, 32-byte units u of 16
-// values at u ^ fold(k): the transposing read takes four consecutive k of two blocks of rows at once.  The loads write LDS in lane
-// order, so each lane fetches the piece that belongs there.
+// LDS, K: rows of 128 bytes, the 16-byte piece c of row r at c ^ (r / 2 & 7), so that sixteen consecutive rows, one piece
+// of each, touch all 64 banks once (c ^ (r & 7), right for 32 banks, cost half as many cycles again).  R: rows of one k,
+// 32-byte units u of 16 values at u ^ fold(k): the transposing read takes four consecutive k of two blocks of rows at once.
+// The loads write LDS in lane order, so each lane fetches the piece that belongs there.
 #pragma once
 #include <utility>
 
@@ -49,9 +51,10 @@ template <int PL> __host__ __device__ constexpr int64_t place_of(int64_t c, int 
   return PL == 1 ? c : PL == 2 ? (c >> 5) * 64 + p * 32 + (c & 31) : (c >> 4) * 64 + p * 16 + (c & 15);
 }
 
-// One operand of a tile: `base` is its first place (first row of the tile, k = 0), ld the places from one row of memory to the next
-// (a multiple of 8; base 16-byte aligned), `rows` how many of the tile's rows exist (at least 1).  Memory holds whole blocks of columns
-// (block_of; one plane: of eight).  TWICE: places from here to the second plane, a matrix like this one (or 0: the same once more).
+// One operand of a tile: `base` is its first place (first row of the tile, k = 0), ld the places from one row of memory to
+// the next (a multiple of 8; base 16-byte aligned), `rows` how many of the tile's rows exist (at least 1).  Memory holds
+// whole blocks of columns (block_of; one plane: of eight).  TWICE: places from here to the second plane, a matrix like this
+// one (or 0: the same once more).
 template <class T> struct Operand {
   const T* base;
   int ld, rows;
@@ -154,10 +157,10 @@ struct Feed {
   }
 };
 
-// The products of two slots: step s multiplies group a(s) of A with group b(s) of B.  Every group is read into registers once;
-// `reads` says which ones step s reads behind its MFMAs (bits 0-3: groups of A, 4-7: of B), from the steps HAND on those of the next
-// two slots: a group is read again one step after its last use or later, and a step or more before its next one.  At HAND
-// every group of the two slots has been read, and they change hands.
+// The products of two slots: step s multiplies group a(s) of A with group b(s) of B.  Every group is read into registers
+// once; `reads` says which ones step s reads behind its MFMAs (bits 0-3: groups of A, 4-7: of B), from the steps HAND on
+// those of the next two slots: a group is read again one step after its last use or later, and a step or more before its
+// next one.  At HAND every group of the two slots has been read, and they change hands.
 template <int PL> struct Steps;
 template <> struct Steps<1> {
   static constexpr int N = 4, HAND = 2, FIRST = 0x77;
@@ -208,8 +211,8 @@ struct Tile {
   typedef typename Op<T>::V V;
   typedef v16f Acc[MI][MI];
 
-  // The sum over k in [0, K).  LEADING: of the first planes' products alone, which are what an infinity or a NaN makes of a sum (infinity
-  // times a later plane, which may be zero or of the other sign, is not).
+  // The sum over k in [0, K).  LEADING: of the first planes' products alone, which are what an infinity or a NaN makes of a
+  // sum (infinity times a later plane, which may be zero or of the other sign, is not).
   template <bool LEADING = false>
   __device__ static __forceinline__ void product(unsigned char* smem, const Operand<T>& a, const Operand<T>& b, int K, Acc& acc) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -253,8 +256,8 @@ struct Tile {
       }
       if (n % 2) fdb.advance(); else fda.advance();
     }
-    // every read of the two slots is done and the next two have arrived (younger loads may be on their way): the barrier hands all
-    // four over
+    // every read of the two slots is done and the next two have arrived (younger loads may be on their way): the barrier
+    // hands all four over
     constexpr int FLYING = (RING - 4) * NLD;
     auto hand_over = [&]() {
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(FLYING) : "memory");
@@ -322,11 +325,11 @@ struct Tile {
     c = (wave & 1) * W + lane % LPR * 8;
   }
 
-  // A finished tile on its way out.  A wavefront takes 32 rows at a time through its own part of LDS, so that memory sees whole rows.
-  // f(idx, row, column, values, n, d) for eight neighbouring columns at a time, n of them inside: row < rows, column < cols, both from
-  // the tile's corner.  d = pre(row, column, n) is what f reads from memory.  It is asked for 32 rows ahead, which takes a copy of f for
-  // every eight values of a thread; with LONG, an f of many instructions, one copy serves them in turn (with GELU in 32 copies, read
-  // once per tile and run once, 8192 x 2048 -> 8192 took 50 us more).
+  // A finished tile on its way out.  A wavefront takes 32 rows at a time through its own part of LDS, so that memory sees
+  // whole rows. f(idx, row, column, values, n, d) for eight neighbouring columns at a time, n of them inside: row < rows,
+  // column < cols, both from the tile's corner.  d = pre(row, column, n) is what f reads from memory.  It is asked for 32
+  // rows ahead, which takes a copy of f for every eight values of a thread; with LONG, an f of many instructions, one copy
+  // serves them in turn (with GELU in 32 copies, read once per tile and run once, 8192 x 2048 -> 8192 took 50 us more).
   // TURNED: the same for the transposed tile, with eight neighbouring rows: f(idx, column, row, ...).
   template <bool TURNED, bool LONG, class P, class F>
   __device__ static __forceinline__ void out(unsigned char* smem, const Acc& acc, int rows, int cols, P&& pre, F&& f) {
@@ -371,8 +374,8 @@ struct Tile {
       });
     }
   }
-  // The same for a tile of a symmetric matrix: f changes the values, g(row, column, values) stores them, and where `both` gt(column,
-  // row, values) eight neighbouring rows at the transposed place.  rows and cols are multiples of eight.
+  // The same for a tile of a symmetric matrix: f changes the values, g(row, column, values) stores them, and where `both`
+  // gt(column, row, values) eight neighbouring rows at the transposed place.  rows and cols are multiples of eight.
   template <class P, class F, class G, class GT>
   __device__ static __forceinline__ void out_symmetric(unsigned char* smem, const Acc& acc, int rows, int cols, bool both, P&& pre, F&& f, G&& g,
                                                        GT&& gt) {

@@ -34,7 +34,8 @@ static int bytes_of(int32_t p) { return p == OPTORCH_FP32 ? 4 : 2; }
 
 // ---- linear layers -----------------------------------------------------------------------------------------------------
 
-// Offsets inside a tile are 32-bit: 256 rows take less than 2^31 bytes.  A row of fp32 values laid out as planes takes 8 bytes a value.
+// Offsets inside a tile are 32-bit: 256 rows take less than 2^31 bytes.  A row of fp32 values laid out as planes takes 8
+// bytes a value.
 static constexpr int64_t kMaxFeatures = (1 << 22) - 8, kMaxFeatures32 = (1 << 20) - 16;
 
 static int linear_check(const optorch_linear_t* a, bool backward) {
@@ -122,8 +123,8 @@ extern "C" int64_t optorch_linear_workspace(const optorch_linear_t* a, int32_t b
   });
 }
 
-// How a product of the call is cut, for the tests that name a kernel by its tile (not part of the API): 1000 * values of a tile's edge +
-// parts; product 0: y, 1: dx, 2: dw.  0: straight from memory.
+// How a product of the call is cut, for the tests that name a kernel by its tile (not part of the API): 1000 * values of a
+// tile's edge + parts; product 0: y, 1: dx, 2: dw.  0: straight from memory.
 namespace oseq {
 int linear_shape(const optorch_linear_t* a, bool backward, int product);
 int linear_shape(const optorch_linear_t* a, bool backward, int product) {

@@ -18,7 +18,9 @@ struct Place {
   uintptr_t at; int64_t rows, width, pitch;
   uintptr_t end() const { return at + (uintptr_t)((rows - 1) * pitch + width); }
 };
-inline Place place_in(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) { return Place{(uintptr_t)p, rows, cols * bytes, ld * bytes}; }
+inline Place place_in(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) {
+  return Place{(uintptr_t)p, rows, cols * bytes, ld * bytes};
+}
 // Whether two matrices share a byte.  Rows that lie between each other's do not.
 inline bool overlap(const Place& a, const Place& b) {
   if (a.rows <= 0 || b.rows <= 0 || a.end() <= b.at || b.end() <= a.at) return false;
@@ -31,7 +33,9 @@ inline bool overlap(const Place& a, const Place& b) {
   }
   return false;
 }
-inline bool same_place(const Place& a, const Place& b) { return a.at == b.at && (a.pitch == b.pitch || a.rows <= 1) && a.width == b.width; }
+inline bool same_place(const Place& a, const Place& b) {
+  return a.at == b.at && (a.pitch == b.pitch || a.rows <= 1) && a.width == b.width;
+}
 
 // How a product M x N over K is cut: block tiles of 2 * wave x 2 * wave, the reduction in `parts`
 struct ProductShape { int wave, parts; };
@@ -61,8 +65,8 @@ struct OrthoMat {
 };
 enum { OB_A = 0, OB_P, OB_C, OB_Q0, OB_Q1, OB_COUNT };
 
-// A piece of a matrix: 8192 places of X, as 1024 groups of eight (first: of the groups, row by row), or of a tall one 128 columns from
-// `first` on of 64 rows from `row` on
+// A piece of a matrix: 8192 places of X, as 1024 groups of eight (first: of the groups, row by row), or of a tall one 128
+// columns from `first` on of 64 rows from `row` on
 struct OrthoChunk { int32_t mat, first, row; };
 constexpr int ORTHO_GROUPS = 1024;
 

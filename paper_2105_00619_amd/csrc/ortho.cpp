@@ -4,17 +4,17 @@
 // made on A: with P = a + b A + c A^2,  A <- P A P  and  Q <- P Q,  and in the end X <- Q X.  Only A = X X^T at the start and
 // Q X at the end touch the long side of X; all other products are m x m and symmetric, so that half of their tiles are made.
 //
-// But a rounding of A (about 2^-23 of its largest value) grows by a^2 a step in the directions of small singular values, where P
-// passes it on to the result.  Largest errors over m = 2 .. 512 with one or m / 16 singular values of 1 and the others 0.5 .. 1e-4, five
-// steps (emulated; the steps on X in fp32: 0.6e-6 to 8e-5, the more the smaller the others):
+// But a rounding of A (about 2^-23 of its largest value) grows by a^2 a step in the directions of small singular values,
+// where P passes it on to the result.  Largest errors over m = 2 .. 512 with one or m / 16 singular values of 1 and the
+// others 0.5 .. 1e-4, five steps (emulated; the steps on X in fp32: 0.6e-6 to 8e-5, the more the smaller the others):
 //   X made anew after every step: as the steps on X;  after two: up to 7e-6 more;  three: 8e-5;  four: 2.3e-4;  five: 1.8e-3.
 // A result stored in bf16 is rounded by 1.7e-3 and takes three steps on A, any other two.  (For n = 4 m that is 38 and 47 m^3 of
 // products, 65 with steps on X.)
 //
 // The operands are pairs of fp16 planes (hi + lo, 22 bits and a sign), times a power of two for each kind of matrix, since
-// the bounds of all of them are known (host: from the polynomials): three products of 16-bit matrix cores for one, with an error
-// of 2^-24 a value.  One plane alone would do for a bf16 result of well-conditioned matrices, but is 1e-2 off where a few singular
-// values are large: in small directions an error of the first iterate is multiplied by 485.
+// the bounds of all of them are known (host: from the polynomials): three products of 16-bit matrix cores for one, with an
+// error of 2^-24 a value.  One plane alone would do for a bf16 result of well-conditioned matrices, but is 1e-2 off where a
+// few singular values are large: in small directions an error of the first iterate is multiplied by 485.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -135,10 +135,11 @@ int up32(int n) { return (n + 31) & ~31; }
 int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // ---- which block makes what ----------------------------------------------------------------------------------------------
-// What a launch is estimated to take, in us, from the time of a tile step (64 places of two operands), of a block's beginning and
-// end, and of what it writes and reads besides (a CU's share of 4.5 TB/s; alone on its CU a block does not reach it).  Two blocks of
-// 128 x 128 or three of 64 x 64 run on a CU: their products take turns, their ends overlap with them.  Measured on products of 2048 and
-// 4096 rows and on ResNet-152's, whose last products take 380 us as 256 x 256 tiles and 310 as 128 x 128.
+// What a launch is estimated to take, in us, from the time of a tile step (64 places of two operands), of a block's
+// beginning and end, and of what it writes and reads besides (a CU's share of 4.5 TB/s; alone on its CU a block does not
+// reach it).  Two blocks of 128 x 128 or three of 64 x 64 run on a CU: their products take turns, their ends overlap with
+// them.  Measured on products of 2048 and 4096 rows and on ResNet-152's, whose last products take 380 us as 256 x 256 tiles
+// and 310 as 128 x 128.
 double step_us(int w) { return w == 128 ? 2.0 : w == 64 ? 0.65 : 0.25; }
 double block_us(int w) { return w == 128 ? 8.0 : w == 64 ? 6.0 : 5.0; }
 int blocks_of_cu(int w) { return w == 128 ? 1 : w == 64 ? 2 : 3; }
@@ -150,8 +151,8 @@ struct Cut { int64_t count, whole; int steps, parts, per; };
 
 int64_t triangle(int64_t t) { return t * (t + 1) / 2; }
 
-// Sums of more than `most` steps are cut; with `tail` only those of the tiles that do not fill a round of all places (the shortest
-// sums), which come last.
+// Sums of more than `most` steps are cut; with `tail` only those of the tiles that do not fill a round of all places (the
+// shortest sums), which come last.
 std::vector<Cut> cuts_of(const OrthoPlanHost& p, bool lower, bool along_n, int w, int most, bool tail) {
   std::vector<Cut> cuts;
   std::vector<int> order;
@@ -217,8 +218,8 @@ double launch_us(const std::vector<Cut>& list, int w, int bytes) {
   return *std::max_element(at.begin(), at.end()) + (join > 0 ? join + 5.0 : 0.0);
 }
 
-// The blocks of a product: its tiles (all of rows x cols, or the lower triangle), cut as `cuts` says.
-// Tiles are taken in squares of four by four, so that neighbours share operands, and neighbours go to one XCD: each has its own L2.
+// The blocks of a product: its tiles (all of rows x cols, or the lower triangle), cut as `cuts` says. Tiles are taken in
+// squares of four by four, so that neighbours share operands, and neighbours go to one XCD: each has its own L2.
 void add_list(OrthoPlanHost& p, OrthoList& l, bool lower, int w, const std::vector<Cut>& cuts, bool along_n) {
   l.w = w;
   l.work0 = p.works.size();
@@ -357,8 +358,8 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
     p.most_m = std::max(p.most_m, m.m);
     p.mats.push_back(m);
   }
-  // bytes of memory for each value of a tile: a symmetric result is written twice; Q X: planes, the caller's values, weights read and
-  // written with their copy
+  // bytes of memory for each value of a tile: a symmetric result is written twice; Q X: planes, the caller's values,
+  // weights read and written with their copy
   plan_list(p, p.gram, true, true, true, 8);
   plan_list(p, p.chain, true, false, true, 8);
   plan_list(p, p.apply, false, false, false, 8);
@@ -374,7 +375,8 @@ static int ortho_create(const optorch_matrix_t* matrices, int32_t n, const optor
   p.off_scale = take(p.mats.size() * 8);
   p.off_bad = take(p.mats.size() * 4 + 4);
   p.off_slots = take(std::max((uint64_t)p.gram.slots * p.gram.w * p.gram.w, 2 * (uint64_t)p.chain.slots * p.chain.w * p.chain.w) * 16);
-  // A single iterate on the way is made where the first one lies if a block has all rows of its columns: it has read them before it writes.
+  // A single iterate on the way is made where the first one lies if a block has all rows of its columns: it has read them
+  // before it writes.
   const bool in_place = iterates == 0 || (iterates == 1 && p.most_m <= 2 * p.apply.w);
   for (OrthoMat& m : p.mats) {
     m.x[0] = take((uint64_t)m.m * m.n * 4);
@@ -445,8 +447,8 @@ bool ortho_vectors_overlap(const optorch_ortho_t* h, const void* a, int32_t a_pr
 bool ortho_vectors_overlap(const optorch_ortho_t* h, const void* a, int32_t a_precision, const void* b, int32_t b_precision) {
   return ::overlap(h->p, Flat{"a", a, a_precision}, Flat{"b", b, b_precision});
 }
-// how the products of a plan are cut: 1000 * values of a tile's edge + 1 if some sums are cut; list 0: X X^T, 1: m x m, 2: Q X on the way,
-// 3: to the caller's vectors, 4: to weights
+// how the products of a plan are cut: 1000 * values of a tile's edge + 1 if some sums are cut; list 0: X X^T, 1: m x m, 2:
+// Q X on the way, 3: to the caller's vectors, 4: to weights
 int ortho_shape(const optorch_ortho_t* h, int list);
 int ortho_shape(const optorch_ortho_t* h, int list) {
   const OrthoList& l = list == 0 ? h->p.gram : list == 1 ? h->p.chain : list == 2 ? h->p.apply : h->p.last[list - 3];
@@ -490,7 +492,8 @@ extern "C" int optorch_muon_update(optorch_ortho_t* h, const optorch_muon_t* a, 
     if (a->scale_mode < OPTORCH_SCALE_NONE || a->scale_mode > OPTORCH_SCALE_RMS) return oseq_mat_err(OPTORCH_E_INVALID, "unknown scale mode");
     if (!std::isfinite(a->lr) || !std::isfinite(a->momentum) || !std::isfinite(a->weight_decay) || !std::isfinite(a->grad_scale))
       return oseq_mat_err(OPTORCH_E_INVALID, "lr, momentum, weight_decay and grad_scale must be finite");
-    const Flat f[4] = {{"g", a->g, a->g_precision}, {"w", a->w, OPTORCH_FP32}, {"v", a->v, OPTORCH_FP32}, {"w16", a->w16, a->w16_precision}};
+    const Flat f[4] = {{"g", a->g, a->g_precision}, {"w", a->w, OPTORCH_FP32}, {"v", a->v, OPTORCH_FP32},
+                       {"w16", a->w16, a->w16_precision}};
     for (int i = 0; i < 4; ++i)
       for (int j = i + 1; j < (a->w16 ? 4 : 3); ++j)
         if (overlap(h->p, f[i], f[j])) return overlap_error(f[i], f[j]);

@@ -10,8 +10,8 @@
 
 namespace oseq {
 
-// K values in at most `wanted` parts of whole slots of 64; a part's values are [first, end).  K up to 2^31 - 256: its parts' ends are no sums
-// of two numbers near it, which wrap.
+// K values in at most `wanted` parts of whole slots of 64; a part's values are [first, end).  K up to 2^31 - 256: its
+// parts' ends are no sums of two numbers near it, which wrap.
 struct Parts {
   int K, size, count;
   OSEQ_PARTS_FN int first(int part) const { return part * size; }
