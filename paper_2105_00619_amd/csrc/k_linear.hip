@@ -157,16 +157,21 @@ __global__ void __launch_bounds__(256) pack_kernel(Pack x, Pack w) {
   }
 }
 
-// A value in two 16-bit planes: rounded, and what that leaves.  Where rounding would leave the range of the type (a slope
-// of GELU goes up to 1.13) the first is the type's largest; a value that is not finite has it in the first plane alone.
+// A value of dz in two 16-bit planes, the value rounded and what that leaves; one that is not finite has it in the first alone.
+//   bf16  v = hi + lo.  Where rounding would leave the range of the type, hi is the largest value.
+//   fp16  v = 2 (hi + lo / 2048): a dy near 65504 times a slope of up to 1.13 stays inside the range, and lo is as far above
+//         fp16's smallest values as hi is.  (Unscaled, a dz of 1e-4 kept no more bits in two planes than in one.)
+template <class T> constexpr float two_planes_scale() { return __is_same(T, f16_t) ? 2.f : 1.f; }
 template <class T> __device__ __forceinline__ void two_planes8(const float (&v)[8], Vec<T, 8>& hi, Vec<T, 8>& lo) {
-  constexpr float MOST = __is_same(T, bf16_t) ? 3.3895314e38f : 65504.f;
-  hi = round_vec<T, 8>(v);
-  float l[8];
+  constexpr float SCALE = two_planes_scale<T>();
+  float h[8], l[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) h[e] = v[e] * (1.f / SCALE);
+  hi = round_vec<T, 8>(h);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    if (finite(v[e]) && !finite((float)hi.v[e])) hi.v[e] = from_f32<T>(copysignf(MOST, v[e]));
-    l[e] = finite(v[e]) ? v[e] - (float)hi.v[e] : 0.f;
+    if (__is_same(T, bf16_t) && finite(v[e]) && !finite((float)hi.v[e])) hi.v[e] = from_f32<T>(copysignf(3.3895314e38f, v[e]));
+    l[e] = finite(v[e]) ? (h[e] - (float)hi.v[e]) * (__is_same(T, f16_t) ? 2048.f : 1.f) : 0.f;
   }
   lo = round_vec<T, 8>(l);
 }
@@ -349,7 +354,9 @@ product_kernel(ProductArgs a) {
   const int k0 = a.cut.first(part), k1 = a.cut.end(part);
   Operand<T> oa, ob;
   oa.base = (const T*)a.a + (AR ? (int64_t)k0 * a.lda + place_of<PL>(m0) : m0 * a.lda + place_of<PL>(k0));
-  oa.ld = a.lda; oa.rows = rows; oa.second = a.second;
+  oa.ld = a.lda; oa.rows = rows;
+  const Operand<T> first = oa;
+  if (TWICE) { oa.base += a.second; oa.second = -a.second; }  // (what rounding left of the first plane, then that)
   ob.base = (const T*)a.b + (BR ? (int64_t)k0 * a.ldb + place_of<PL>(n0) : (int64_t)n0 * a.ldb + place_of<PL>(k0));
   ob.ld = a.ldb; ob.rows = cols;
   // A thread's outputs are of the same eight columns throughout.  (With the bias read for every eight outputs, each read
@@ -367,8 +374,13 @@ product_kernel(ProductArgs a) {
   constexpr bool LONG = ACT >= OPTORCH_ACT_GELU;
   typename G::Acc acc;
   uint32_t wait = 0;  // planes: which groups have a sum that is not finite
+  auto scaled = [](float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= TWICE ? two_planes_scale<T>() : 1.f;
+  };
   G::product(smem, oa, ob, k1 - k0, acc);
   G::template out<false, LONG>(smem, acc, rows, cols, ask, [&](int idx, int r, int c, float (&v)[8], int n, const Skip<O, 8>& skip) {
+    scaled(v);
     if (PLANES) {
       bool bad = false;
 #pragma unroll
@@ -384,7 +396,7 @@ product_kernel(ProductArgs a) {
     if (!G::any_of(smem, wait != 0)) return;
     __syncthreads();
     Classes<G::GROUPS> classes = {};
-    G::template product<true>(smem, oa, ob, k1 - k0, acc);
+    G::template product<true>(smem, first, ob, k1 - k0, acc);
     G::template out<false, false>(smem, acc, rows, cols, [](int, int, int) { return 0; }, [&](int idx, int, int, float (&v)[8], int, int) {
       if (wait >> idx & 1) classes.set(idx, v);
     });
@@ -392,6 +404,7 @@ product_kernel(ProductArgs a) {
     G::product(smem, oa, ob, k1 - k0, acc);
     G::template out<false, true>(smem, acc, rows, cols, [](int, int, int) { return 0; }, [&](int idx, int r, int c, float (&v)[8], int n, int) {
       if (!(wait >> idx & 1)) return;
+      scaled(v);
       classes.apply(idx, v);
       emit(r, c, v, n, ask(r, c, n));
     });

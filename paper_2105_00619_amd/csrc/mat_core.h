@@ -210,6 +210,9 @@ struct Tile {
   static_assert(4 * 32 * EPITCH * 4 + 16 <= LDS, "the epilogue's rows and a word for each wavefront do not fit");
   typedef typename Op<T>::V V;
   typedef v16f Acc[MI][MI];
+  // TWICE: what the first plane's sum is multiplied by before the second plane's is added (fp16: the first plane is held larger by as
+  // much, or it would be lost below the type's smallest values)
+  static constexpr float BETWEEN = __is_same(T, f16_t) ? 1.f / 2048.f : 1.f;
 
   // The sum over k in [0, K).  LEADING: of the first planes' products alone, which are what an infinity or a NaN makes of a
   // sum (infinity times a later plane, which may be zero or of the other sign, is not).
@@ -277,6 +280,9 @@ struct Tile {
     each<(S::N - S::HAND) * MFMAS>([&](auto n) { load_place(n, (RING - 2) * SLOT, (RING - 1) * SLOT); });
     each<__builtin_popcount(S::FIRST) * MI>([&](auto i) { read_of(std::integral_constant<int, S::FIRST>{}, i, smem, smem + SLOT); });
     for (int t = 0; t < total; ++t) {
+      if constexpr (TWICE && !LEADING && BETWEEN != 1.f) {
+        if (t == once) times_between(acc);
+      }
       const unsigned char *sa = smem + at, *sb = smem + after(at, 1), *na = smem + after(at, 2), *nb = smem + after(after(at, 2), 1);
       const int free0 = after(at, RING - 2), free1 = after(at, RING - 1);
       // Nothing is moved across the bars between MFMAs, or the compiler reads each operand right before its use.
@@ -423,6 +429,18 @@ struct Tile {
   }
 
  private:
+  // Sums times BETWEEN, each where it lies.  (As ordinary multiplications the compiler moves all of a 256 x 256 tile's out of the
+  // accumulation registers at once and spills, in the loop too.)  It does not see into the block, so what an MFMA and a use of its result
+  // have to be apart is said here: 19 cycles before, 2 behind.
+  __device__ static __forceinline__ void times_between(Acc& acc) {
+    asm volatile("s_nop 15\n\ts_nop 15");
+    each<MI * MI * 16>([&](auto n) {
+      float x = acc[n / 16 / MI][n / 16 % MI][n % 16], t;
+      asm volatile("v_accvgpr_read_b32 %1, %0\n\tv_mul_f32 %1, %2, %1\n\tv_accvgpr_write_b32 %0, %1" : "+a"(x), "=&v"(t) : "s"(BETWEEN));
+      acc[n / 16 / MI][n / 16 % MI][n % 16] = x;
+    });
+    asm volatile("s_nop 7");
+  }
   // 32 rows of a wavefront's sums to its part of LDS
   __device__ static __forceinline__ void put_rows(float* area, const v16f (&acc)[MI], int lane) {
 #pragma unroll

@@ -155,3 +155,21 @@ def test_gelu_and_its_slope_have_their_bits_in_the_tail(rows, width, name):
     dx, _, _ = B.linear_backward(torch.ones_like(z), z, one, z, activation="gelu")
     want = phi + z.double() * density
     assert bool(((dx.double() - want).abs() <= more * (phi + z.double().abs() * density) + half * want.abs() + least).all())
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("size", [1e-1, 1e-3, 1e-4, 2e-5])
+@pytest.mark.parametrize("rows,cin,cout", [(130, 264, 96), (520, 1032, 2056), (3085, 4104, 72), (72, 3080, 4104)])
+def test_small_gradients_in_fp16_keep_their_bits(rows, cin, cout, size, act):
+    """dy near fp16's smallest values, weights and samples of order one: dz = dy act'(z) has more bits than fp16 has there, and so have the
+    results, which are rounded once."""
+    import torch
+    from paper_2105_00619_amd import binding as B
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    make = lambda r, c, s=1.0: (torch.randn(r, c, generator=gen, device="cuda") * s).half()  # noqa: E731
+    dy, x, w, z = make(rows, cout, size), make(rows, cin), make(cout, cin), make(rows, cout, 1.5)
+    dx, dw, _ = B.linear_backward(dy, x, w, z, activation=act)
+    dz = dy.double() * _slope64(act, z.double())
+    for got, ref in ((dx, torch.mm(dz, w.double())), (dw, torch.mm(dz.T.contiguous(), x.double()))):
+        once = float((ref.half().double() - ref).norm() / ref.norm())
+        assert float((got.double() - ref).norm() / ref.norm()) <= once * (1 + 2.0 ** -6) + 2.0 ** -16
