@@ -1,7 +1,7 @@
 /*
  * optorch_matrix -- matrix operators on the device, for AMD MI355X (gfx950): linear layers with bias,
- * activation and skip connection in the product's epilogue, their gradients, and the orthogonalised
- * update of weight matrices.  C ABI; part of liboptorch_seq.so.
+ * activation and skip connection in the product's epilogue, layer norms, losses over many classes, their
+ * gradients, and the orthogonalised update of weight matrices.  C ABI; part of liboptorch_seq.so.
  *
  * Matrices are row-major: element (r, c) at r * ld + c, ld >= columns, any alignment of the element
  * type.  Pointers are DEVICE pointers unless named *_host.  Matrices and vectors that are written must not share an
@@ -69,6 +69,90 @@ int optorch_linear_forward(const optorch_linear_t* a);
  * ReLU's dz is 0 where z is not above 0, whatever dy is there.  The gradient of the skip connection is dy itself.  With
  * rows = 0, dw and dbias are zero. */
 int optorch_linear_backward(const optorch_linear_t* a);
+
+/* ---- layer norm ------------------------------------------------------------------------------------ */
+
+/* Arguments of both directions.  `precision` is the type of x, y, dy, residual and dx; everything else is fp32, what is
+ * computed too, and a result is rounded once. */
+typedef struct {
+  int32_t precision, cols;            /* cols: 1 .. 2^22 - 8, leading dimensions too */
+  int64_t rows;                       /* 0 is allowed */
+  const void* x; int64_t ldx;         /* rows x cols */
+  const float* weight;                /* cols, or NULL: ones */
+  const float* bias;                  /* forward: cols, or NULL: zeros */
+  float eps;                          /* forward: added to the variance; >= 0, finite */
+  int32_t reserved;
+  void* y; int64_t ldy;               /* forward: rows x cols */
+  float* mean; float* rstd;           /* rows.  Forward: written, or both NULL; backward: read */
+  const void* dy; int64_t lddy;       /* backward: rows x cols */
+  const void* residual; int64_t ldr;  /* backward: rows x cols, added to dx, or NULL; may be dx itself */
+  void* dx; int64_t lddx;             /* backward: rows x cols, or NULL */
+  float* dweight; float* dbias;       /* backward: cols, or NULL */
+  void* workspace; uint64_t workspace_bytes; /* 256-byte aligned */
+  void* hip_stream;
+} optorch_layer_norm_t;
+
+/* Bytes of workspace that the backward call needs with these arguments (the workspace fields are ignored; the forward call
+ * needs none); negative code on invalid arguments. */
+int64_t optorch_layer_norm_workspace(const optorch_layer_norm_t* a);
+
+/* mean and variance of every row (over its cols values), rstd = 1 / sqrt(variance + eps), y = (x - mean) rstd weight + bias.
+ * The squares of a row's deviations have to stay in fp32's range. */
+int optorch_layer_norm_forward(const optorch_layer_norm_t* a);
+
+/* With h = (x - mean) rstd and u = dy weight, means over a row:
+ *   dx = rstd (u - mean(u) - h mean(u h)) + residual;  dweight = sum over rows of dy h;  dbias = sum over rows of dy.
+ * With rows = 0, dweight and dbias are zero. */
+int optorch_layer_norm_backward(const optorch_layer_norm_t* a);
+
+/* ---- losses over many classes ---------------------------------------------------------------------- */
+
+/* Losses of p = softmax(s), s = x w^T + bias (a teacher: divided by the temperature), against a target for every row, with the
+ * product included: the logits s are never held but for a piece of the classes at a time.  The target is either a label or a
+ * teacher's distribution over some classes:
+ *   labels            q = 1 at the label.  label_smoothing e: (1 - e) q + e / classes.  A negative label leaves the row out; the loss
+ *                     and gradients of a row whose label is not below `classes` are NaN.
+ *   indices, teacher  q = softmax(teacher / temperature) over the row's `top` entries; the probabilities of entries of one class add
+ *                     up.  Entries with a negative index or a logit of -infinity are unused; a row without any other is left out.  An
+ *                     index not below `classes` makes the row's loss and gradients NaN, and so does a logit that is NaN or infinite.
+ * Rows left out have a loss of zero and no gradient, whatever their x is.  `precision` is the type of x, w, dx and dw; everything
+ * else is fp32.  Products are summed in fp32 (fp32 operands as three bf16 planes, sums that are not finite come out as NaN). */
+typedef struct {
+  int32_t precision, teacher_precision;
+  int64_t rows;                       /* 0 is allowed */
+  int32_t in_features, classes;       /* 1 .. 2^22 - 8, leading dimensions too; fp32: 1 .. 2^20 - 16 */
+  const void* x; int64_t ldx;         /* rows x in */
+  const void* w; int64_t ldw;         /* classes x in */
+  const float* bias;                  /* classes, or NULL; -infinity leaves a class out */
+  const int32_t* labels;              /* rows, or NULL: a teacher */
+  const int32_t* indices; int64_t ldi;/* rows x top */
+  const void* teacher; int64_t ldt;   /* rows x top */
+  int32_t top;                        /* 1 .. 1024 */
+  float temperature;                  /* above 0; labels: not used */
+  float label_smoothing, z_loss;      /* labels: 0 .. 1, and a weight >= 0; a teacher: 0 */
+  float* loss;                        /* forward: rows */
+  float* lse;                         /* rows: log of the sum of exp(s).  Forward: written; backward: read */
+  const float* dloss;                 /* backward: rows */
+  void* dx; int64_t lddx;             /* backward: rows x in, or NULL */
+  void* dw; int64_t lddw;             /* backward: classes x in, or NULL */
+  float* dbias;                       /* backward: classes, or NULL */
+  void* workspace; uint64_t workspace_bytes; /* 256-byte aligned */
+  void* hip_stream;
+} optorch_softmax_loss_t;
+
+/* Bytes of workspace that the forward (backward = 0) or backward call needs with these arguments (the workspace
+ * fields are ignored); negative code on invalid arguments. */
+int64_t optorch_softmax_loss_workspace(const optorch_softmax_loss_t* a, int32_t backward);
+
+/* labels:     loss = lse - (target . s) + z_loss lse^2
+ * a teacher:  loss = sum of q (log q - log p), the divergence of p from the teacher */
+int optorch_softmax_loss_forward(const optorch_softmax_loss_t* a);
+
+/* ds = dloss (p - q), with labels dloss ((1 + 2 z_loss lse) p - target), with a teacher over the temperature;
+ *   dx = ds w,  dw = ds^T x,  dbias = column sums of ds.
+ * p is made from the logits, made again, and the given lse.  In 16-bit precision ds is rounded to the storage type for the two
+ * products, relative to its row's dloss; dbias sums it unrounded.  With rows = 0, dw and dbias are zero. */
+int optorch_softmax_loss_backward(const optorch_softmax_loss_t* a);
 
 /* ---- orthogonalised updates ------------------------------------------------------------------------ */
 

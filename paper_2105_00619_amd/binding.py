@@ -24,7 +24,9 @@ SYMBOLS = (
     "optorch_seq_step_encoded", "optorch_seq_predict_encoded", "optorch_seq_plan_info", "optorch_seq_step_static", "optorch_seq_debug_unit_output",
     "optorch_encoded_words", "optorch_encode", "optorch_decode", "optorch_decode_normalized", "optorch_encode_lossless",
     "optorch_decode_lossless", "optorch_dataflow_last_error",
-    "optorch_linear_workspace", "optorch_linear_forward", "optorch_linear_backward", "optorch_ortho_create", "optorch_ortho_query",
+    "optorch_linear_workspace", "optorch_linear_forward", "optorch_linear_backward",
+    "optorch_layer_norm_workspace", "optorch_layer_norm_forward", "optorch_layer_norm_backward",
+    "optorch_softmax_loss_workspace", "optorch_softmax_loss_forward", "optorch_softmax_loss_backward", "optorch_ortho_create", "optorch_ortho_query",
     "optorch_ortho_bind", "optorch_orthogonalize", "optorch_muon_update", "optorch_ortho_destroy", "optorch_matrix_last_error",
 )
 
@@ -56,6 +58,27 @@ class optorch_linear_t(C.Structure):
         ("z", C.c_void_p), ("ldz", C.c_int64), ("dy", C.c_void_p), ("lddy", C.c_int64), ("dx", C.c_void_p),
         ("lddx", C.c_int64), ("dw", C.c_void_p), ("lddw", C.c_int64), ("dbias", C.c_void_p), ("workspace", C.c_void_p),
         ("workspace_bytes", C.c_uint64), ("hip_stream", C.c_void_p),
+    ]
+
+
+class optorch_layer_norm_t(C.Structure):
+    _fields_ = [
+        ("precision", C.c_int32), ("cols", C.c_int32), ("rows", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64),
+        ("weight", C.c_void_p), ("bias", C.c_void_p), ("eps", C.c_float), ("reserved", C.c_int32), ("y", C.c_void_p),
+        ("ldy", C.c_int64), ("mean", C.c_void_p), ("rstd", C.c_void_p), ("dy", C.c_void_p), ("lddy", C.c_int64),
+        ("residual", C.c_void_p), ("ldr", C.c_int64), ("dx", C.c_void_p), ("lddx", C.c_int64), ("dweight", C.c_void_p),
+        ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("hip_stream", C.c_void_p),
+    ]
+
+
+class optorch_softmax_loss_t(C.Structure):
+    _fields_ = [
+        ("precision", C.c_int32), ("teacher_precision", C.c_int32), ("rows", C.c_int64), ("in_features", C.c_int32),
+        ("classes", C.c_int32), ("x", C.c_void_p), ("ldx", C.c_int64), ("w", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+        ("labels", C.c_void_p), ("indices", C.c_void_p), ("ldi", C.c_int64), ("teacher", C.c_void_p), ("ldt", C.c_int64),
+        ("top", C.c_int32), ("temperature", C.c_float), ("label_smoothing", C.c_float), ("z_loss", C.c_float), ("loss", C.c_void_p),
+        ("lse", C.c_void_p), ("dloss", C.c_void_p), ("dx", C.c_void_p), ("lddx", C.c_int64), ("dw", C.c_void_p), ("lddw", C.c_int64),
+        ("dbias", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("hip_stream", C.c_void_p),
     ]
 
 
@@ -137,6 +160,20 @@ def load_library() -> C.CDLL:
     lib.optorch_linear_forward.restype = C.c_int
     lib.optorch_linear_backward.argtypes = [L]
     lib.optorch_linear_backward.restype = C.c_int
+    N = C.POINTER(optorch_layer_norm_t)
+    lib.optorch_layer_norm_workspace.argtypes = [N]
+    lib.optorch_layer_norm_workspace.restype = C.c_int64
+    lib.optorch_layer_norm_forward.argtypes = [N]
+    lib.optorch_layer_norm_forward.restype = C.c_int
+    lib.optorch_layer_norm_backward.argtypes = [N]
+    lib.optorch_layer_norm_backward.restype = C.c_int
+    X = C.POINTER(optorch_softmax_loss_t)
+    lib.optorch_softmax_loss_workspace.argtypes = [X, C.c_int32]
+    lib.optorch_softmax_loss_workspace.restype = C.c_int64
+    lib.optorch_softmax_loss_forward.argtypes = [X]
+    lib.optorch_softmax_loss_forward.restype = C.c_int
+    lib.optorch_softmax_loss_backward.argtypes = [X]
+    lib.optorch_softmax_loss_backward.restype = C.c_int
     lib.optorch_ortho_create.argtypes = [C.POINTER(optorch_matrix_t), C.c_int32, C.POINTER(optorch_ortho_config_t), C.POINTER(H)]
     lib.optorch_ortho_create.restype = C.c_int
     lib.optorch_ortho_query.argtypes = [H, C.POINTER(C.c_uint64), C.POINTER(C.c_int64)]
@@ -597,16 +634,18 @@ def _linear_args(x, activation, rows, cin, cout):
     return a
 
 
-def _linear_call(torch, lib, fn, a, backward, device):
+def _matrix_call(torch, fn, a, device, workspace=None):
+    """fn(a) on device's current stream; workspace(a): the bytes it needs."""
     if torch.cuda.current_device() != device.index:
         with torch.cuda.device(device):
-            return _linear_call(torch, lib, fn, a, backward, device)
-    n = lib.optorch_linear_workspace(C.byref(a), backward)
-    if n < 0:
-        _mat_fail(n)
-    if n:
-        ws = torch.empty(n, dtype=torch.uint8, device=device)  # (torch aligns allocations to 512 bytes)
-        a.workspace, a.workspace_bytes = ws.data_ptr(), n
+            return _matrix_call(torch, fn, a, device, workspace)
+    if workspace is not None:
+        n = workspace(a)
+        if n < 0:
+            _mat_fail(n)
+        if n:
+            ws = torch.empty(n, dtype=torch.uint8, device=device)  # (torch aligns allocations to 512 bytes)
+            a.workspace, a.workspace_bytes = ws.data_ptr(), n
     a.hip_stream = torch._C._cuda_getCurrentRawStream(device.index)  # (current_stream() makes an object: 2.6 us of a call's 12)
     rc = fn(C.byref(a))
     if rc != OK:
@@ -641,7 +680,7 @@ def linear_forward(x, w, bias=None, *, residual=None, activation="none", save_pr
         z = torch.empty((rows, cout), dtype=x.dtype, device=x.device)
         a.z, a.ldz = z.data_ptr(), cout
     lib = load_library()
-    _linear_call(torch, lib, lib.optorch_linear_forward, a, 0, x.device)
+    _matrix_call(torch, lib.optorch_linear_forward, a, x.device, lambda a: lib.optorch_linear_workspace(C.byref(a), 0))
     return (out, z) if save_pre else out
 
 
@@ -683,8 +722,207 @@ def linear_backward(dy, x, w, z=None, *, activation="none", need=("dx", "dw", "d
         _check_vector("dbias", dbias, cout, x)
         a.dbias = dbias.data_ptr()
     lib = load_library()
-    _linear_call(torch, lib, lib.optorch_linear_backward, a, 1, x.device)
+    _matrix_call(torch, lib.optorch_linear_backward, a, x.device, lambda a: lib.optorch_linear_workspace(C.byref(a), 1))
     return dx, dw, dbias
+
+
+def _norm_args(x, weight):
+    if not x.is_cuda:
+        raise ValueError("the operands must be on the GPU")
+    rows, cols = x.shape
+    a = optorch_layer_norm_t()
+    a.precision, a.cols, a.rows = _precision(x.dtype), _int32("cols", cols), rows
+    _check_matrix("x", x, rows, cols, x)
+    a.x, a.ldx = x.data_ptr(), _ld(x)
+    if weight is not None:
+        _check_vector("weight", weight, cols, x)
+        a.weight = weight.data_ptr()
+    return a, rows, cols
+
+
+def layer_norm_forward(x, weight=None, bias=None, *, eps=1e-5, save_stats=False, out=None):
+    """y = (x - mean) / sqrt(variance + eps) * weight + bias for every row of x [rows, cols] in fp32, bf16 or fp16; weight and
+    bias float32 [cols], without them ones and zeros.  save_stats: returns (y, mean, rstd), which `layer_norm_backward` reads, float32
+    [rows] each.  out: where y goes; it shares no element with anything else.  Nothing is recorded for autograd."""
+    import torch
+    a, rows, cols = _norm_args(x, weight)
+    if bias is not None:
+        _check_vector("bias", bias, cols, x)
+        a.bias = bias.data_ptr()
+    a.eps = eps
+    if out is None:
+        out = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    else:
+        _check_matrix("out", out, rows, cols, x)
+    a.y, a.ldy = out.data_ptr(), _ld(out)
+    if save_stats:
+        stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+        mean, rstd = stats[0], stats[1]
+        a.mean = stats.data_ptr()
+        a.rstd = a.mean + 4 * rows if rows else a.mean
+    _matrix_call(torch, load_library().optorch_layer_norm_forward, a, x.device)
+    return (out, mean, rstd) if save_stats else out
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, *, residual=None, need=("dx", "dweight", "dbias"), dx=None, dweight=None, dbias=None):
+    """The gradients (dx, dweight, dbias) of `layer_norm_forward` from dy [rows, cols], what it was given and the mean and rstd that
+    it returned; those not in `need` are not computed and come back as None.  residual [rows, cols]: added to dx, the gradient that
+    reaches x past the norm.  dweight and dbias are float32, dx has x's type.  dx, dweight, dbias: tensors to write them to; dx may be
+    the residual, otherwise they share no element with each other or with what is read."""
+    import torch
+    a, rows, cols = _norm_args(x, weight)
+    if not need or not set(need) <= {"dx", "dweight", "dbias"}:
+        raise ValueError("need must name some of dx, dweight, dbias")
+    for name, t in (("dx", dx), ("dweight", dweight), ("dbias", dbias)):
+        if t is not None and name not in need:
+            raise ValueError("%s: given, but not in need" % name)
+    _check_matrix("dy", dy, rows, cols, x)
+    _check_vector("mean", mean, rows, x)
+    _check_vector("rstd", rstd, rows, x)
+    a.dy, a.lddy, a.mean, a.rstd = dy.data_ptr(), _ld(dy), mean.data_ptr(), rstd.data_ptr()
+    if residual is not None:
+        if "dx" not in need:
+            raise ValueError("residual: given, but dx is not in need")
+        _check_matrix("residual", residual, rows, cols, x)
+        a.residual, a.ldr = residual.data_ptr(), _ld(residual)
+    if "dx" in need:
+        if dx is None:
+            dx = torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+        _check_matrix("dx", dx, rows, cols, x)
+        a.dx, a.lddx = dx.data_ptr(), _ld(dx)
+    if "dweight" in need:
+        if dweight is None:
+            dweight = torch.empty(cols, dtype=torch.float32, device=x.device)
+        _check_vector("dweight", dweight, cols, x)
+        a.dweight = dweight.data_ptr()
+    if "dbias" in need:
+        if dbias is None:
+            dbias = torch.empty(cols, dtype=torch.float32, device=x.device)
+        _check_vector("dbias", dbias, cols, x)
+        a.dbias = dbias.data_ptr()
+    lib = load_library()
+    _matrix_call(torch, lib.optorch_layer_norm_backward, a, x.device, lambda a: lib.optorch_layer_norm_workspace(C.byref(a)))
+    return dx, dweight, dbias
+
+
+def _loss_args(x, w, bias):
+    if not x.is_cuda:
+        raise ValueError("the operands must be on the GPU")
+    rows, cin = x.shape
+    classes = w.shape[0]
+    a = optorch_softmax_loss_t()
+    a.precision, a.rows, a.in_features, a.classes = _precision(x.dtype), rows, _int32("in_features", cin), _int32("classes", classes)
+    _check_matrix("x", x, rows, cin, x)
+    _check_matrix("w", w, classes, cin, x)
+    a.x, a.ldx, a.w, a.ldw = x.data_ptr(), _ld(x), w.data_ptr(), _ld(w)
+    if bias is not None:
+        _check_vector("bias", bias, classes, x)
+        a.bias = bias.data_ptr()
+    return a
+
+
+def _labels(a, x, labels, label_smoothing, z_loss):
+    import torch
+    if labels.dtype != torch.int32 or labels.device != x.device:
+        raise TypeError("labels: expected int32 on %s, got %s on %s" % (x.device, labels.dtype, labels.device))
+    if labels.numel() != a.rows or not labels.is_contiguous():
+        raise ValueError("labels: expected %d contiguous values" % a.rows)
+    a.labels, a.label_smoothing, a.z_loss = labels.data_ptr(), label_smoothing, z_loss
+
+
+def _teacher(a, x, indices, teacher, temperature):
+    import torch
+    if indices.dtype != torch.int32 or indices.device != x.device or teacher.device != x.device:
+        raise TypeError("expected int32 indices and the teacher's logits on %s, got %s on %s and %s" % (x.device, indices.dtype, indices.device, teacher.device))
+    if indices.dim() != 2 or indices.shape[0] != a.rows or indices.shape != teacher.shape:
+        raise ValueError("indices and teacher: expected two matrices of %d rows and the same columns, got %s and %s" % (
+            a.rows, tuple(indices.shape), tuple(teacher.shape)))
+    if a.rows and indices.shape[1] > 1 and (indices.stride(1) != 1 or teacher.stride(1) != 1):
+        raise ValueError("indices and teacher: the elements of a row must lie next to each other")
+    a.teacher_precision, a.top, a.temperature = _precision(teacher.dtype), indices.shape[1], temperature
+    a.indices, a.ldi, a.teacher, a.ldt = indices.data_ptr(), _ld(indices), teacher.data_ptr(), _ld(teacher)
+
+
+def _loss_forward(a, x):
+    import torch
+    out = torch.empty((2, a.rows), dtype=torch.float32, device=x.device)
+    loss, lse = out[0], out[1]
+    a.loss = out.data_ptr()
+    a.lse = a.loss + 4 * a.rows if a.rows else None
+    lib = load_library()
+    _matrix_call(torch, lib.optorch_softmax_loss_forward, a, x.device, lambda a: lib.optorch_softmax_loss_workspace(C.byref(a), 0))
+    return loss, lse
+
+
+def _loss_backward(a, dloss, x, lse, bias, need, dx, dw, dbias):
+    import torch
+    rows, cin, classes = a.rows, a.in_features, a.classes
+    if need is None:
+        need = ("dx", "dw") if bias is None else ("dx", "dw", "dbias")
+    if not need or not set(need) <= {"dx", "dw", "dbias"}:
+        raise ValueError("need must name some of dx, dw, dbias")
+    for name, t in (("dx", dx), ("dw", dw), ("dbias", dbias)):
+        if t is not None and name not in need:
+            raise ValueError("%s: given, but not in need" % name)
+    _check_vector("dloss", dloss, rows, x)
+    _check_vector("lse", lse, rows, x)
+    a.dloss, a.lse = dloss.data_ptr(), lse.data_ptr()
+    if "dx" in need:
+        if dx is None:
+            dx = torch.empty((rows, cin), dtype=x.dtype, device=x.device)
+        _check_matrix("dx", dx, rows, cin, x)
+        a.dx, a.lddx = dx.data_ptr(), _ld(dx)
+    if "dw" in need:
+        if dw is None:
+            dw = torch.empty((classes, cin), dtype=x.dtype, device=x.device)
+        _check_matrix("dw", dw, classes, cin, x)
+        a.dw, a.lddw = dw.data_ptr(), _ld(dw)
+    if "dbias" in need:
+        if dbias is None:
+            dbias = torch.empty(classes, dtype=torch.float32, device=x.device)
+        _check_vector("dbias", dbias, classes, x)
+        a.dbias = dbias.data_ptr()
+    lib = load_library()
+    _matrix_call(torch, lib.optorch_softmax_loss_backward, a, x.device, lambda a: lib.optorch_softmax_loss_workspace(C.byref(a), 1))
+    return dx, dw, dbias
+
+
+def cross_entropy_forward(x, w, labels, bias=None, *, label_smoothing=0.0, z_loss=0.0):
+    """(loss, lse), float32 [rows] each: with s = x w^T + bias, lse = log(sum(exp(s))) and loss = lse - (target . s) + z_loss lse^2 for
+    every row, where target is 1 at the row's label, or 1 - label_smoothing there and label_smoothing / classes everywhere.  x [rows, in]
+    and w [classes, in] in fp32, bf16 or fp16, labels int32 [rows], bias float32 [classes] (-infinity leaves a class out).  A
+    negative label leaves the row out: its loss is zero; a label not below `classes` makes it NaN.  The logits are never held.  Nothing
+    is recorded for autograd: the gradients are `cross_entropy_backward`'s."""
+    a = _loss_args(x, w, bias)
+    _labels(a, x, labels, label_smoothing, z_loss)
+    return _loss_forward(a, x)
+
+
+def cross_entropy_backward(dloss, x, w, labels, lse, bias=None, *, label_smoothing=0.0, z_loss=0.0, need=None, dx=None, dw=None, dbias=None):
+    """The gradients (dx, dw, dbias) of sum(dloss * loss) from dloss, float32 [rows], what `cross_entropy_forward` was given and the
+    lse that it returned; those not in `need` (all, dbias with a bias) are not computed and come back as None.  dbias is float32, the
+    others have x's type.  dx, dw, dbias: tensors to write them to; they share no element with each other or with what is read."""
+    a = _loss_args(x, w, bias)
+    _labels(a, x, labels, label_smoothing, z_loss)
+    return _loss_backward(a, dloss, x, lse, bias, need, dx, dw, dbias)
+
+
+def distillation_forward(x, w, indices, teacher, bias=None, *, temperature=1.0):
+    """(loss, lse), float32 [rows] each: the divergence sum(q (log q - log p)) of p = softmax(s), s = (x w^T + bias) / temperature,
+    from a teacher's distribution q = softmax(teacher / temperature) over the classes of a row's indices, and lse = log(sum(exp(s))).
+    indices int32 and teacher (fp32, bf16 or fp16) [rows, top]; entries with a negative index or a logit of -infinity are unused, a row
+    without any other is left out, with a loss of zero; entries of one class add up; an index not below `classes` makes the loss NaN.
+    x, w, bias as in `cross_entropy_forward`.  (The gradients of a temperature's loss are smaller by its square: multiply dloss by it.)"""
+    a = _loss_args(x, w, bias)
+    _teacher(a, x, indices, teacher, temperature)
+    return _loss_forward(a, x)
+
+
+def distillation_backward(dloss, x, w, indices, teacher, lse, bias=None, *, temperature=1.0, need=None, dx=None, dw=None, dbias=None):
+    """The gradients (dx, dw, dbias) of sum(dloss * loss) of `distillation_forward`; arguments and results as in `cross_entropy_backward`."""
+    a = _loss_args(x, w, bias)
+    _teacher(a, x, indices, teacher, temperature)
+    return _loss_backward(a, dloss, x, lse, bias, need, dx, dw, dbias)
 
 
 class OrthoPlan:

@@ -1,0 +1,647 @@
+// Losses of softmax(s), s = (x w^T + bias) / temperature, against a label or a teacher's distribution over some classes:
+//   loss = sum over classes of q (log q - s) + lse(s),   ds = p - q,   p = exp(s - lse).
+// The logits are made tile by tile (mat_core.h) and never leave the block that makes them: forward it keeps of each row the maximum of its
+// columns, the sum of their exponentials above it and the targets' logits, which a second kernel joins; backward it turns them into ds, in
+// the storage type and for a piece of the classes at a time, which the gradients' products read (k_loss_grad.hip).  What a row's target is at some of its
+// columns is put into the tile on its way through LDS, where the row's values lie side by side.
+#include "mat_layout.h"
+#include "parts.h"
+
+namespace oseq {
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct Logits {
+  const void *x, *w; int ldx, ldw;  // operands, mat_core.h
+  int64_t M;
+  int N, K, first;                  // classes of this piece, values of a row, the piece's first class
+  int tiles_m, tiles_n;
+  const float* bias;                // of all classes, or null
+  float per_temperature;
+  const int32_t* labels;
+  // a teacher: its entries in order of their classes, `top` a row; where those of a run of W columns begin
+  int top, columns;
+  const int32_t* index; const float2* target; const uint16_t* start;
+  // forward
+  float2* sums; float* totals; float* picked;
+  // backward
+  const float4* info;
+  float spread, hit, scale;         // label_smoothing / classes; 1 - label_smoothing; what ds is held times
+  void* ds; int64_t ds_row;
+  float* bias_sums;
+};
+
+// What the backward pass knows of a row, four floats: its lse; what p and the target are multiplied by (the second is 0 in a row that is
+// left out); the factor of everything that comes of the row.
+
+template <class S, class T, int W, bool TOP, bool GRAD>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
+logits_kernel(Logits a) {
+  constexpr int PL = sizeof(S) == 4 ? 3 : 1;
+  typedef Tile<T, PL, W, false, false> G;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const int total = a.tiles_m * a.tiles_n;
+  const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
+  // neighbouring tiles on one XCD: each of the eight takes a run of them, eight rows of tiles at a time
+  const int per = (total + 7) / 8, id = (block & 7) * per + (block >> 3);
+  if ((int)(block >> 3) >= per || id >= total) return;
+  const int band = id / (8 * a.tiles_n), rows_in = min(8, a.tiles_m - band * 8), u = id - band * 8 * a.tiles_n;
+  const int tn = u / rows_in, tm = band * 8 + u - tn * rows_in;
+  const int64_t m0 = (int64_t)tm * G::EDGE;
+  const int n0 = tn * G::EDGE, rows = (int)min<int64_t>(G::EDGE, a.M - m0), cols = min(G::EDGE, a.N - n0);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  float4 info = {};
+  if (GRAD && tid < rows) info = a.info[m0 + tid];
+  typename G::Acc acc;
+  G::product(smem, Operand<T>{(const T*)a.x + m0 * a.ldx, a.ldx, rows}, Operand<T>{(const T*)a.w + (int64_t)n0 * a.ldw, a.ldw, cols}, a.K, acc);
+  float* area = reinterpret_cast<float*>(smem) + wave * (32 * G::EPITCH);
+  float* row_lse = reinterpret_cast<float*>(smem) + 4 * 32 * G::EPITCH;
+  float *row_p = row_lse + G::EDGE, *row_target = row_p + G::EDGE, *row_factor = row_target + G::EDGE;
+  static_assert((4 * 32 * G::EPITCH + 4 * G::EDGE) * 4 <= G::LDS, "the rows' values do not fit behind those on their way out");
+  if (GRAD) {
+    if (tid < G::EDGE) { row_lse[tid] = info.x; row_p[tid] = info.y; row_target[tid] = info.z; row_factor[tid] = info.w; }
+    __syncthreads();
+  }
+  const int c0 = wn * W, piece_col = n0 + c0, column = (a.first + piece_col) / W;  // the run of W columns, counted over all classes
+  float bias[G::MI];
+#pragma unroll
+  for (int j = 0; j < G::MI; ++j) {
+    const int c = c0 + j * 32 + (lane & 31);
+    bias[j] = a.bias && c < cols ? a.bias[a.first + n0 + c] : 0.f;
+  }
+  // a lane's row of the 32 on their way (two lanes each) and what it has of the targets among these columns
+  const int lr = lane >> 1, half = lane & 1;
+  auto targets = [&](int r, auto f) {  // f(place in the row's W columns, entry)
+    if (half || r >= rows || c0 >= cols) return;
+    const int64_t row = m0 + r;
+    if (TOP) {
+      const uint16_t* s = a.start + row * (a.columns + 1) + column;
+      const int end = s[1];
+      for (int k = s[0]; k < end; ++k) f(a.index[row * a.top + k] - (a.first + piece_col), k);
+    } else {
+      const int y = a.labels[row];
+      if (y >= a.first + piece_col && y < a.first + n0 + min(cols, c0 + W)) f(y - (a.first + piece_col), 0);
+    }
+  };
+  float sums[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  each<G::MI>([&](auto i) {
+    // (as the accumulators have them: a lane one column of each 32, of rows 4 (lane / 32) + 8 (e / 4) + e % 4)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4) {
+      const int r = wm * W + i * 32 + e4 * 8 + (lane >> 5) * 4;
+      float4 l = {}, p = {}, q = {};
+      if (GRAD) {
+        l = *reinterpret_cast<const float4*>(row_lse + r);
+        p = *reinterpret_cast<const float4*>(row_p + r);
+        q = *reinterpret_cast<const float4*>(row_target + r);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < G::MI; ++j) {
+          float v = acc[i][j][e4 * 4 + e];
+          const bool in = c0 + j * 32 + (lane & 31) < cols;
+          v = (v + bias[j]) * a.per_temperature;
+          if (GRAD) {
+            v = __builtin_amdgcn_exp2f((v - (&l.x)[e]) * LOG2E) * (&p.x)[e] - a.spread * (&q.x)[e];
+            v = in ? v : 0.f;
+          } else {
+            v = in ? v : -__builtin_inff();
+          }
+          acc[i][j][e4 * 4 + e] = v;
+        }
+    }
+    G::put_rows(area, acc[i], lane);
+    const int r = wm * W + i * 32 + lr;  // of the tile
+    if constexpr (!GRAD) {
+      targets(r, [&](int c, int k) { a.picked[TOP ? (m0 + r) * a.top + k : m0 + r] = area[lr * G::EPITCH + c]; });
+      float v[W / 2];
+#pragma unroll
+      for (int c = 0; c < W / 2; c += 4)
+        *reinterpret_cast<float4*>(v + c) = *reinterpret_cast<const float4*>(area + lr * G::EPITCH + half * (W / 2) + c);
+      float most = v[0];
+#pragma unroll
+      for (int c = 1; c < W / 2; ++c) most = fmaxf(most, v[c]);
+      most = fmaxf(most, __shfl_xor(most, 1));
+      // (nothing but -infinity: a sum of zero; an infinity: an infinite sum, above the largest finite maximum)
+      const bool infinite = most == __builtin_inff();
+      const float above = infinite || most == -__builtin_inff() ? 0.f : most;
+      float sum = 0.f, all = 0.f;
+#pragma unroll
+      for (int c = 0; c < W / 2; ++c) {
+        sum += __builtin_amdgcn_exp2f((v[c] - above) * LOG2E);
+        if (a.totals) all += c0 + half * (W / 2) + c < cols ? v[c] : 0.f;
+      }
+      sum += __shfl_xor(sum, 1);
+      if (a.totals) all += __shfl_xor(all, 1);
+      if (!half && r < rows && c0 < cols) {
+        const int64_t at = (int64_t)column * a.M + m0 + r;
+        a.sums[at] = make_float2(infinite ? 3.4028235e38f : most, sum);
+        if (a.totals) a.totals[at] = all;
+      }
+    } else {
+      targets(r, [&](int c, int k) {
+        const float q = TOP ? a.target[(m0 + r) * a.top + k].x : a.hit;
+        area[lr * G::EPITCH + c] -= q * row_target[r];
+      });
+      asm volatile("" ::: "memory");
+      each<G::PASSES>([&](auto pass) {
+        const int or_ = pass * G::RPP + lane / G::LPR, oc = lane % G::LPR * 8, tr = wm * W + i * 32 + or_;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = area[or_ * G::EPITCH + oc + e];
+        const bool used = tr < rows && row_target[tr] != 0.f;
+        const float factor = row_factor[tr];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          v[e] = used ? v[e] : 0.f;
+          sums[e] = __fmaf_rn(v[e], used ? factor : 0.f, sums[e]);
+          v[e] *= a.scale;
+        }
+        const int padded = (a.N + block_of(PL) - 1) / block_of(PL) * block_of(PL), c = n0 + c0 + oc;
+        if (tr < rows && c < padded) store_planes8<PL, T>((T*)a.ds + (m0 + tr) * a.ds_row, c, v);
+      });
+    }
+    asm volatile("" ::: "memory");
+  });
+  if constexpr (GRAD) {
+    if (!a.bias_sums) return;
+#pragma unroll
+    for (int o = G::LPR; o < 64; o *= 2)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sums[e] += __shfl_xor(sums[e], o);
+    const int oc = lane * 8;
+    if (lane < G::LPR) {
+      float* out = a.bias_sums + (int64_t)(tm * 2 + wm) * a.N;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c0 + oc + e < cols) out[n0 + c0 + oc + e] = sums[e];
+    }
+  }
+}
+
+// ---- a teacher's entries -----------------------------------------------------------------------------------------------
+// Those of a row in order of their classes (then of their places), entries of one class added up in the first of them; softmax of their logits;
+// where the entries of each run of `width` classes begin.  Threads N a row, N a power of two of at least `top`.
+struct Teacher {
+  const int32_t* indices; int64_t ldi;
+  const void* logits; int64_t ldt;
+  int64_t rows;
+  int top, classes, width, columns;
+  float per_temperature;
+  int32_t* index; float2* target; uint16_t* start; float* flag;
+};
+
+template <int N, class F> __device__ __forceinline__ float over_row(float v, float* lds, int t, F&& f) {
+  for (int o = N / 2; o > 0; o >>= 1) {
+    lds[t] = v;
+    __syncthreads();
+    v = f(v, lds[t ^ o]);
+    __syncthreads();
+  }
+  return v;
+}
+
+template <class S, int N>
+__global__ void __launch_bounds__(N < 256 ? 256 : N) teacher_kernel(Teacher a) {
+  constexpr int BLOCK = N < 256 ? 256 : N, ROWS = BLOCK / N;
+  __shared__ uint32_t keys[ROWS][N];
+  __shared__ float values[ROWS][N];
+  const int t = threadIdx.x % N, r = threadIdx.x / N;
+  const int64_t wanted = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + r, row = min(wanted, a.rows - 1);
+  int c = -1;
+  float v = -__builtin_inff();
+  if (t < a.top) {
+    c = a.indices[row * a.ldi + t];
+    if (c >= 0) v = to_f32(((const S*)a.logits)[row * a.ldt + t]) * a.per_temperature;
+  }
+  const bool valid = c >= 0 && v != -__builtin_inff(), wrong = valid && (c >= a.classes || !(fabsf(v) <= 3.4028235e38f));
+  if (!valid) v = -__builtin_inff();
+  auto most_of = [](float p, float q) { return fmaxf(p, q); };
+  auto sum_of = [](float p, float q) { return p + q; };
+  const float most = over_row<N>(v, values[r], t, most_of);
+  const float e = valid ? __builtin_amdgcn_exp2f((v - most) * LOG2E) : 0.f;
+  const float sum = over_row<N>(e, values[r], t, sum_of);
+  const float any_wrong = over_row<N>(wrong ? 1.f : 0.f, values[r], t, most_of);
+  const float log_q = v - most - logf(sum);
+  uint32_t key = valid && !wrong ? (uint32_t)c << 10 | t : 0xffffffffu;
+  // bitonic: pairs of keys at a distance of `o` in runs of `run`
+  for (int run = 2; run <= N; run *= 2)
+    for (int o = run / 2; o > 0; o >>= 1) {
+      keys[r][t] = key;
+      __syncthreads();
+      const uint32_t other = keys[r][t ^ o];
+      const bool least = ((t & o) == 0) == ((t & run) == 0);
+      key = least ? min(key, other) : max(key, other);
+      __syncthreads();
+    }
+  keys[r][t] = key;
+  values[r][t] = log_q;
+  __syncthreads();
+  const bool real = wanted < a.rows;
+  if (real && t < a.top && key != 0xffffffffu) {
+    const uint32_t mine = key >> 10;
+    float q = 0.f, lq = 0.f;
+    if (t == 0 || keys[r][t - 1] >> 10 != mine) {  // the first of its class
+      lq = values[r][key & 1023];
+      q = expf(lq);
+      bool alone = true;
+      for (int k = t + 1; k < N && keys[r][k] != 0xffffffffu && keys[r][k] >> 10 == mine; ++k, alone = false) q += expf(values[r][keys[r][k] & 1023]);
+      if (!alone) lq = logf(q);
+    }
+    a.index[row * a.top + t] = (int32_t)mine;
+    a.target[row * a.top + t] = make_float2(q, lq);
+  }
+  if (real && t == 0) a.flag[row] = any_wrong != 0.f ? __builtin_nanf("") : most == -__builtin_inff() ? 0.f : 1.f;
+  for (int s = t; s <= a.columns; s += N) {
+    // entries of lower classes than the run's first
+    const uint64_t bound = (uint64_t)s * a.width << 10;
+    int lo = 0, hi = N;
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (keys[r][mid] != 0xffffffffu && (s == a.columns || keys[r][mid] < bound)) lo = mid + 1; else hi = mid;
+    }
+    if (real) a.start[row * (a.columns + 1) + s] = (uint16_t)lo;
+  }
+}
+
+// ---- forward: a row's sums joined --------------------------------------------------------------------------------------
+struct Join {
+  const float2* sums; const float* totals; const float* picked;
+  int64_t rows;
+  int columns, log_rows;           // a block's rows: 1 << log_rows
+  const int32_t* labels; int classes;
+  float smoothing, z_loss;
+  int top; const float2* target; const float* flag; const uint16_t* start;
+  float *loss, *lse;
+};
+
+constexpr int JOIN_THREADS = 512;
+__global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
+  __shared__ float2 part[JOIN_THREADS];
+  __shared__ float more[JOIN_THREADS];
+  const int rows = 1 << a.log_rows, rl = threadIdx.x & (rows - 1), slot = threadIdx.x >> a.log_rows, slots = JOIN_THREADS >> a.log_rows;
+  const int64_t wanted = (int64_t)blockIdx.x * rows + rl, row = min(wanted, a.rows - 1);
+  float most = -__builtin_inff(), sum = 0.f, extra = 0.f;
+  auto join = [](float& m, float& l, float m2, float l2) {
+    // (a maximum that is NaN has a sum that is; one of -infinity a sum of zero)
+    const float top = fmaxf(m, m2);
+    if (top != -__builtin_inff()) l = l * __builtin_amdgcn_exp2f((m - top) * LOG2E) + l2 * __builtin_amdgcn_exp2f((m2 - top) * LOG2E);
+    else l += l2;
+    m = top;
+  };
+  // four runs of columns at a time
+  float m4[4], l4[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) { m4[q] = -__builtin_inff(); l4[q] = 0.f; }
+  for (int c = slot; c < a.columns; c += 4 * slots) {
+    float2 t[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int at = c + q * slots;
+      t[q] = at < a.columns ? a.sums[(int64_t)at * a.rows + row] : make_float2(-__builtin_inff(), 0.f);
+      if (a.totals && at < a.columns) extra += a.totals[(int64_t)at * a.rows + row];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) join(m4[q], l4[q], t[q].x, t[q].y);
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q) join(most, sum, m4[q], l4[q]);
+  // a teacher: its entries in turn; q (log q - s), and the sum of q for lse
+  float entropy = 0.f, q_all = 0.f;
+  const bool teacher = a.labels == nullptr;
+  if (teacher) {
+    const int n = a.start[row * (a.columns + 1) + a.columns];
+    for (int k = slot; k < n; k += slots) {
+      const float2 q = a.target[row * a.top + k];
+      if (q.x > 0.f) entropy += q.x * (q.y - a.picked[row * a.top + k]);
+      q_all += q.x;
+    }
+  }
+  part[threadIdx.x] = make_float2(most, sum);
+  more[threadIdx.x] = extra;
+  __syncthreads();
+  for (int o = slots / 2; o > 0; o >>= 1) {
+    if (slot < o) {
+      float2 p = part[threadIdx.x];
+      const float2 q = part[threadIdx.x + (o << a.log_rows)];
+      join(p.x, p.y, q.x, q.y);
+      part[threadIdx.x] = p;
+      more[threadIdx.x] += more[threadIdx.x + (o << a.log_rows)];
+    }
+    __syncthreads();
+  }
+  const float2 all = part[rl];
+  const float total = more[rl];
+  __syncthreads();
+  if (teacher) {
+    part[threadIdx.x] = make_float2(entropy, q_all);
+    __syncthreads();
+    for (int o = slots / 2; o > 0; o >>= 1) {
+      if (slot < o) {
+        part[threadIdx.x].x += part[threadIdx.x + (o << a.log_rows)].x;
+        part[threadIdx.x].y += part[threadIdx.x + (o << a.log_rows)].y;
+      }
+      __syncthreads();
+    }
+  }
+  if (slot || wanted >= a.rows) return;
+  const float lse = all.x + logf(all.y);
+  float loss;
+  if (teacher) {
+    const float flag = a.flag[row];
+    loss = flag == 0.f ? 0.f : flag != flag ? flag : part[rl].x + lse * part[rl].y;
+  } else {
+    const int y = a.labels[row];
+    loss = lse;
+    if (y >= a.classes) loss = __builtin_nanf("");
+    else if (y >= 0) loss = lse - (1.f - a.smoothing) * a.picked[row] + a.z_loss * lse * lse;
+    else loss = 0.f;
+    if (a.totals && y >= 0) loss -= a.smoothing * (total / (float)a.classes);
+  }
+  a.loss[row] = loss;
+  a.lse[row] = lse;
+}
+
+// ---- backward: what a row's values are multiplied by ----------------------------------------------------------------------
+// With f = max(1, 1 + 2 z_loss lse) ds is held as (p (1 + 2 z_loss lse) - target) / f, which stays within 2, and dloss f / temperature is the factor of
+// what comes of it: of dx afterwards, of dw in x, relative to the largest factor.  (A factor inside ds would round every value anew; so
+// a dloss that is the same for all rows, a mean's, costs dw nothing.)  One block: 8192 rows take 6 us.
+struct Rows {
+  const float *dloss, *lse, *flag;
+  const int32_t* labels;
+  int64_t rows;
+  int classes;
+  float z_loss, per_temperature;
+  float4* info; float* scale;
+};
+__global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
+  __shared__ float part[1024];
+  float most = 0.f;
+  for (int64_t r = threadIdx.x; r < a.rows; r += 1024) {
+    bool used, wrong;
+    if (a.labels) {
+      const int y = a.labels[r];
+      used = y >= 0;
+      wrong = y >= a.classes;
+    } else {
+      const float f = a.flag[r];
+      used = f != 0.f;
+      wrong = f != f;
+    }
+    const float lse = a.lse[r], p = a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * lse : 1.f, f = fmaxf(1.f, fabsf(p)), g = a.dloss[r] * a.per_temperature * f;
+    const float nan = __builtin_nanf("");
+    float4 o = make_float4(lse, wrong ? nan : p / f, wrong ? nan : 1.f / f, g);
+    if (!used) o = make_float4(0.f, 0.f, 0.f, 0.f);
+    a.info[r] = o;
+    most = fmaxf(most, fabsf(o.w));
+  }
+  part[threadIdx.x] = most;
+  __syncthreads();
+  for (int o = 512; o > 0; o >>= 1) {
+    if ((int)threadIdx.x < o) part[threadIdx.x] = fmaxf(part[threadIdx.x], part[threadIdx.x + o]);
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *a.scale = part[0];
+}
+
+// ---- operands laid out anew --------------------------------------------------------------------------------------------
+// Columns are filled up to whole blocks (block_of) with zeros.  With `info`, rows times their factor over the largest one.
+struct Layout { const void* src; int64_t ld, rows; int cols; void* dst; const float4* info; const float* scale; };
+template <class S, class T, int PL>
+__global__ void __launch_bounds__(256) layout_kernel(Layout a) {
+  const int c8 = (a.cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
+  const int64_t n = a.rows * c8;
+  const float largest = a.info ? *a.scale : 1.f;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / c8;
+    const int c = (int)(i - r * c8) * 8;
+    float v[8];
+    load8<S>((const S*)a.src + r * a.ld + c, max(0, min(8, a.cols - c)), v);
+    if (a.info) {
+      const float4 row = a.info[r];
+      const float f = largest == 0.f ? 0.f : row.w / largest;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = row.z == 0.f ? 0.f : v[e] * f;
+    }
+    store_planes8<PL, T>((T*)a.dst + r * c8 * (8 * span_of(PL)), c, v);
+  }
+}
+
+template <class S, class T, int PL>
+void lay_out(hipStream_t st, const void* src, int64_t ld, int64_t rows, int cols, void* dst, const float4* info = nullptr, const float* scale = nullptr) {
+  Layout l = {src, ld, rows, cols, dst, info, scale};
+  OSEQ_LAUNCH((layout_kernel<S, T, PL>), dim3(grid_of(rows * ((cols + 7) / 8))), dim3(256), 0, st, l);
+}
+
+template <class S, class T, int W, bool TOP, bool GRAD> void run_logits_w(hipStream_t st, Logits& l) {
+  typedef Tile<T, sizeof(S) == 4 ? 3 : 1, W, false, false> G;
+  l.tiles_m = ceil_div(l.M, 2 * W);
+  l.tiles_n = ceil_div(l.N, 2 * W);
+  const int64_t per = ((int64_t)l.tiles_m * l.tiles_n + 7) / 8;
+  auto k = logits_kernel<S, T, W, TOP, GRAD>;
+  // (more LDS than a launch gets unasked; set again on every launch: which devices know it is not ours to remember)
+  if (G::LDS > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+  OSEQ_LAUNCH(k, grid_of_blocks(per * 8), dim3(256), G::LDS, st, l);
+}
+template <class S, class T, bool GRAD> void run_logits(hipStream_t st, Logits& l, int wave) {
+  if (l.labels) {
+    if (wave == 128) run_logits_w<S, T, 128, false, GRAD>(st, l);
+    else if (wave == 64) run_logits_w<S, T, 64, false, GRAD>(st, l);
+    else run_logits_w<S, T, 32, false, GRAD>(st, l);
+  } else {
+    if (wave == 128) run_logits_w<S, T, 128, true, GRAD>(st, l);
+    else if (wave == 64) run_logits_w<S, T, 64, true, GRAD>(st, l);
+    else run_logits_w<S, T, 32, true, GRAD>(st, l);
+  }
+}
+
+template <class S> void run_teacher(hipStream_t st, const Teacher& t) {
+  if (t.top <= 64) OSEQ_LAUNCH((teacher_kernel<S, 64>), grid_of_blocks((t.rows + 3) / 4), dim3(256), 0, st, t);
+  else if (t.top <= 256) OSEQ_LAUNCH((teacher_kernel<S, 256>), grid_of_blocks(t.rows), dim3(256), 0, st, t);
+  else OSEQ_LAUNCH((teacher_kernel<S, 1024>), grid_of_blocks(t.rows), dim3(1024), 0, st, t);
+}
+
+// what both directions begin with
+template <class S, class T, int PL> Logits begin(const optorch_softmax_loss_t& a, const LossPlan& p) {
+  hipStream_t st = (hipStream_t)a.hip_stream;
+  char* ws = (char*)a.workspace;
+  Logits l = {};
+  l.x = a.x; l.ldx = (int)a.ldx;
+  if (p.pack_x) {
+    lay_out<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x);
+    l.x = ws + p.off_x; l.ldx = row_of<PL>(a.in_features);
+  }
+  l.M = a.rows; l.K = (int)up8(a.in_features);  // (up to the zeros behind a row)
+  l.bias = a.bias;
+  l.per_temperature = a.labels ? 1.f : 1.f / a.temperature;
+  l.labels = a.labels;
+  l.columns = p.columns;
+  if (!a.labels) {
+    Teacher t = {a.indices, a.ldi, a.teacher, a.ldt, a.rows, a.top, a.classes, p.wave, p.columns, l.per_temperature,
+                 (int32_t*)(ws + p.off_index), (float2*)(ws + p.off_target), (uint16_t*)(ws + p.off_start), (float*)(ws + p.off_flag)};
+    if (a.teacher_precision == OPTORCH_FP32) run_teacher<float>(st, t);
+    else if (a.teacher_precision == OPTORCH_BF16) run_teacher<bf16_t>(st, t);
+    else run_teacher<f16_t>(st, t);
+    l.top = a.top;
+    l.index = t.index; l.target = t.target; l.start = t.start;
+  }
+  return l;
+}
+
+// f(first class, classes) for each piece, its weights in l
+template <class S, class T, int PL, class F> void each_piece(const optorch_softmax_loss_t& a, const LossPlan& p, Logits& l, F&& f) {
+  char* ws = (char*)a.workspace;
+  for (int v = 0; v < a.classes; v += p.piece) {
+    const int n = std::min(p.piece, a.classes - v);
+    const S* w = (const S*)a.w + v * a.ldw;
+    l.w = w; l.ldw = (int)a.ldw;
+    if (p.pack_w) {
+      lay_out<S, T, PL>((hipStream_t)a.hip_stream, w, a.ldw, n, a.in_features, ws + p.off_w);
+      l.w = ws + p.off_w; l.ldw = row_of<PL>(a.in_features);
+    }
+    l.first = v; l.N = n;
+    f(v, n);
+  }
+}
+
+template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t& a, const LossPlan& p) {
+  hipStream_t st = (hipStream_t)a.hip_stream;
+  char* ws = (char*)a.workspace;
+  Logits l = begin<S, T, PL>(a, p);
+  l.sums = (float2*)(ws + p.off_sums);
+  l.picked = (float*)(ws + p.off_picked);
+  if (a.labels && a.label_smoothing != 0.f) l.totals = (float*)(ws + p.off_totals);
+  each_piece<S, T, PL>(a, p, l, [&](int, int) { run_logits<S, T, false>(st, l, p.wave); });
+  Join j = {};
+  j.sums = l.sums; j.totals = l.totals; j.picked = l.picked;
+  j.rows = a.rows; j.columns = p.columns;
+  while (j.log_rows < 6 && (1 << j.log_rows) < a.rows) ++j.log_rows;
+  j.labels = a.labels; j.classes = a.classes;
+  j.smoothing = a.label_smoothing; j.z_loss = a.z_loss;
+  j.top = a.top; j.target = l.target; j.start = l.start;
+  j.flag = (const float*)(ws + p.off_flag);
+  j.loss = a.loss; j.lse = a.lse;
+  OSEQ_LAUNCH(loss_join_kernel, dim3(ceil_div(a.rows, 1 << j.log_rows)), dim3(JOIN_THREADS), 0, st, j);
+}
+
+template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_t& a, const LossPlan& p) {
+  hipStream_t st = (hipStream_t)a.hip_stream;
+  char* ws = (char*)a.workspace;
+  Logits l = begin<S, T, PL>(a, p);
+  float4* info = (float4*)(ws + p.off_info);
+  float* scale = (float*)(ws + p.off_scale);
+  Rows r = {a.dloss, a.lse, (const float*)(ws + p.off_flag), a.labels, a.rows, a.classes, a.labels ? a.z_loss : 0.f, l.per_temperature, info, scale};
+  OSEQ_LAUNCH(rows_kernel, dim3(1), dim3(1024), 0, st, r);
+  if (a.dw) lay_out<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_xs, info, scale);
+  l.info = info;
+  l.spread = a.labels ? a.label_smoothing / (float)a.classes : 0.f;
+  l.hit = 1.f - a.label_smoothing;
+  l.scale = loss_scale_of(a.precision);
+  l.ds = ws + p.off_ds; l.ds_row = p.ds_row;
+  l.bias_sums = a.dbias ? (float*)(ws + p.off_bias) : nullptr;
+  LossPiece g = {};
+  g.ds = l.ds; g.ds_row = p.ds_row;
+  g.xs = ws + p.off_xs; g.ldxs = row_of<PL>(a.in_features);
+  g.info = info; g.scale = scale;
+  g.acc = (float*)(ws + p.off_acc); g.parts = (float*)(ws + p.off_parts);
+  g.dx = p.dx; g.dw = p.dw;
+  each_piece<S, T, PL>(a, p, l, [&](int v, int n) {
+    run_logits<S, T, true>(st, l, p.wave);
+    if (a.dbias)
+      OSEQ_LAUNCH(dbias_kernel, dim3(ceil_div(n, 16)), dim3(256), 0, st, (const float*)l.bias_sums, 2 * l.tiles_m, n, a.dbias + v);
+    g.w = l.w; g.ldw = l.ldw;
+    g.first = v; g.count = n;
+    g.start = v == 0; g.end = v + n == a.classes;
+    launch_loss_piece(a, g);
+  });
+}
+
+template <class S> __global__ void __launch_bounds__(256) loss_clear_kernel(S* p, int64_t rows, int cols, int64_t ld) {
+  const int64_t n = rows * cols;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) p[i / cols * ld + i % cols] = from_f32<S>(0.f);
+}
+template <class S> void clear_of(const optorch_softmax_loss_t& a) {
+  hipStream_t st = (hipStream_t)a.hip_stream;
+  if (a.dw) OSEQ_LAUNCH(loss_clear_kernel<S>, dim3(grid_of((int64_t)a.classes * a.in_features)), dim3(256), 0, st, (S*)a.dw, (int64_t)a.classes, a.in_features, a.lddw);
+  if (a.dbias) OSEQ_LAUNCH(loss_clear_kernel<float>, dim3(grid_of(a.classes)), dim3(256), 0, st, a.dbias, (int64_t)1, a.classes, (int64_t)a.classes);
+}
+
+// a piece of ds (and of weights that are laid out anew) takes at most about this
+constexpr int64_t LOSS_PIECE_BYTES = 256ll << 20;
+
+}  // namespace
+
+LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
+  LossPlan p = {};
+  const bool f32 = a.precision == OPTORCH_FP32, teacher = a.labels == nullptr;
+  const uint64_t in_row = 2 * (uint64_t)(f32 ? row_of<3>(a.in_features) : row_of<1>(a.in_features));
+  p.pack_x = f32 || !direct(a.x, a.ldx, a.in_features);
+  p.pack_w = f32 || !direct(a.w, a.ldw, a.in_features);
+  // pieces of a multiple of 256 classes, all alike but the last
+  int64_t most = a.classes;
+  const int64_t each = f32 ? 8 : 2;
+  if (backward) most = std::min(most, LOSS_PIECE_BYTES / (each * a.rows));
+  if (p.pack_w) most = std::min(most, LOSS_PIECE_BYTES / (int64_t)in_row);
+  const int64_t pieces = (a.classes + std::max<int64_t>(256, most) - 1) / std::max<int64_t>(256, most);
+  p.piece = pieces == 1 ? a.classes : (int)(((a.classes + pieces - 1) / pieces + 255) / 256 * 256);
+  p.wave = shape_of(a.rows, p.piece, a.in_features, f32, 1).wave;
+  p.columns = (a.classes + p.wave - 1) / p.wave;
+  p.ds_row = f32 ? row_of<3>(p.piece) : row_of<1>(p.piece);
+  uint64_t o = 0;
+  auto take = [&](uint64_t n) { const uint64_t at = o; o = up256(o + n); return at; };
+  const uint64_t rows = a.rows;
+  if (p.pack_x) p.off_x = take(rows * in_row);
+  if (p.pack_w) p.off_w = take((uint64_t)p.piece * in_row);
+  if (teacher) {
+    p.off_index = take(rows * a.top * 4);
+    p.off_target = take(rows * a.top * 8);
+    p.off_start = take(rows * (p.columns + 1) * 2);
+    p.off_flag = take(rows * 4);
+  }
+  if (!backward) {
+    p.off_sums = take(rows * p.columns * 8);
+    if (!teacher && a.label_smoothing != 0.f) p.off_totals = take(rows * p.columns * 4);
+    p.off_picked = take(rows * (teacher ? a.top : 1) * 4);
+  } else {
+    p.off_info = take(rows * 16);
+    p.off_scale = take(4);
+    if (a.dw) p.off_xs = take(rows * in_row);
+    p.off_ds = take(rows * p.ds_row * 2);
+    if (a.dx && p.piece < a.classes) p.off_acc = take(rows * up8(a.in_features) * 4);
+    if (a.dbias) p.off_bias = take((uint64_t)2 * ceil_div(a.rows, 2 * p.wave) * p.piece * 4);
+    uint64_t parts = 0;
+    auto product = [&](ProductShape& s, int64_t M, int64_t N, int64_t K) {
+      s = shape_of(M, N, K, f32);
+      if (s.parts > 1) parts = std::max(parts, (uint64_t)s.parts * M * up8(N) * 4);
+    };
+    if (a.dx) product(p.dx, a.rows, a.in_features, p.piece);
+    if (a.dw) product(p.dw, p.piece, a.in_features, a.rows);
+    if (parts) p.off_parts = take(parts);
+  }
+  p.bytes = o;
+  return p;
+}
+
+void launch_loss_forward(const optorch_softmax_loss_t& a, const LossPlan& p) {
+  if (a.precision == OPTORCH_FP32) forward_of<float, bf16_t, 3>(a, p);
+  else if (a.precision == OPTORCH_BF16) forward_of<bf16_t, bf16_t, 1>(a, p);
+  else forward_of<f16_t, f16_t, 1>(a, p);
+}
+
+void launch_loss_backward(const optorch_softmax_loss_t& a, const LossPlan& p) {
+  if (a.rows == 0) {
+    if (a.precision == OPTORCH_FP32) clear_of<float>(a);
+    else if (a.precision == OPTORCH_BF16) clear_of<bf16_t>(a);
+    else clear_of<f16_t>(a);
+    return;
+  }
+  if (a.precision == OPTORCH_FP32) backward_of<float, bf16_t, 3>(a, p);
+  else if (a.precision == OPTORCH_BF16) backward_of<bf16_t, bf16_t, 1>(a, p);
+  else backward_of<f16_t, f16_t, 1>(a, p);
+}
+
+}  // namespace oseq

@@ -1,0 +1,179 @@
+// The two products of the gradient of a loss over many classes, for a piece of the classes:
+//   dx += ds w (summed in fp32 over the pieces, then times each row's factor),   dw = ds^T x' times one factor,
+// with x' the rows of x times their factors over the largest.  ds is read along the reduction for dx and across it for dw (mat_core.h).
+#include "mat_layout.h"
+#include "parts.h"
+
+namespace oseq {
+
+namespace {
+
+struct Grad {
+  const void* a; int lda;
+  const void* b; int ldb;
+  int64_t M;
+  int N, K;
+  int tiles_m, tiles_n, parts;
+  Parts cut;          // of K, in `parts`
+  float* partial;     // parts > 1: [parts][M][up8(N)] sums
+  float* acc;         // dx: [M][up8(N)], the sums of the pieces before this one, unless `start`; the sums with it, unless `end`
+  bool start, end;
+  const float4* info; // dx: the rows' factors
+  const float* scale; // dw: the factor
+  float unscale;      // and what either is multiplied by besides
+  void* out; int64_t ldo;
+};
+
+struct Before { float v[8]; };
+// the sums of the pieces before this one
+template <bool DW> __device__ __forceinline__ Before before_of(const Grad& g, int64_t row, int col) {
+  Before b = {};
+  if (!DW && !g.start) load_f32<float, 8>(g.acc + row * ((g.N + 7) & ~7) + col, b.v);
+  return b;
+}
+// what becomes of eight neighbouring sums, n of them inside
+template <class O, bool DW> __device__ __forceinline__ void finish(const Grad& g, int64_t row, int col, float (&v)[8], int n, const Before& before) {
+  if (!DW && !g.start) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += before.v[e];
+  }
+  if (!DW && !g.end) {
+    store_f32<float, 8>(g.acc + row * ((g.N + 7) & ~7) + col, v);
+    return;
+  }
+  const float f = (DW ? *g.scale : g.info[row].w) * g.unscale;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] *= f;
+  store8<O>((O*)g.out + row * g.ldo + col, n, v);
+}
+
+// O: type of the result; T: of the planes
+template <class O, class T, int W, bool DW>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
+grad_kernel(Grad a) {
+  constexpr int PL = sizeof(O) == 4 ? 3 : 1;
+  typedef Tile<T, PL, W, DW, true> G;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  // neighbouring tiles on one XCD: each of the eight takes a run of them, eight rows of tiles at a time
+  const int total = a.tiles_m * a.tiles_n * a.parts;
+  const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
+  const int per = (total + 7) / 8, id = (block & 7) * per + (block >> 3);
+  if ((int)(block >> 3) >= per || id >= total) return;
+  const int tiles = a.tiles_m * a.tiles_n, part = id / tiles, t = id - part * tiles;
+  const int band = t / (8 * a.tiles_n), rows_in = min(8, a.tiles_m - band * 8), u = t - band * 8 * a.tiles_n;
+  const int tn = u / rows_in, tm = band * 8 + u - tn * rows_in;
+  const int64_t m0 = (int64_t)tm * G::EDGE;
+  const int n0 = tn * G::EDGE;
+  const int rows = (int)min<int64_t>(G::EDGE, a.M - m0), cols = min(G::EDGE, a.N - n0);
+  const int k0 = a.cut.first(part), k1 = a.cut.end(part);
+  const Operand<T> oa = {(const T*)a.a + (DW ? (int64_t)k0 * a.lda + place_of<PL>(m0) : m0 * a.lda + place_of<PL>(k0)), a.lda, rows};
+  const Operand<T> ob = {(const T*)a.b + (int64_t)k0 * a.ldb + place_of<PL>(n0), a.ldb, cols};
+  const int n8 = (a.N + 7) & ~7;
+  auto ask = [&](int r, int c, int) { return a.parts > 1 ? Before{} : before_of<DW>(a, m0 + r, n0 + c); };
+  auto emit = [&](int r, int c, float (&v)[8], int n, const Before& before) {
+    if (a.parts > 1) store_f32<float, 8>(a.partial + ((int64_t)part * a.M + m0 + r) * n8 + n0 + c, v);
+    else finish<O, DW>(a, m0 + r, n0 + c, v, n, before);
+  };
+  typename G::Acc acc;
+  uint32_t wait = 0;  // planes: which groups have a sum that is not finite
+  G::product(smem, oa, ob, k1 - k0, acc);
+  G::template out<false, false>(smem, acc, rows, cols, ask, [&](int idx, int r, int c, float (&v)[8], int n, const Before& before) {
+    if (PL > 1) {
+      bool bad = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) bad |= e < n && !finite(v[e]);
+      if (bad) { wait |= 1u << idx; return; }
+    }
+    emit(r, c, v, n, before);
+  });
+  if constexpr (PL > 1) {
+    // what the first planes alone say of such sums, and the others of their groups once more (as the layers' products do)
+    if (!G::any_of(smem, wait != 0)) return;
+    __syncthreads();
+    Classes<G::GROUPS> classes = {};
+    G::template product<true>(smem, oa, ob, k1 - k0, acc);
+    G::template out<false, false>(smem, acc, rows, cols, [](int, int, int) { return 0; }, [&](int idx, int, int, float (&v)[8], int, int) {
+      if (wait >> idx & 1) classes.set(idx, v);
+    });
+    __syncthreads();  // (the rows on their way out lie where the next slots go)
+    G::product(smem, oa, ob, k1 - k0, acc);
+    G::template out<false, true>(smem, acc, rows, cols, [](int, int, int) { return 0; }, [&](int idx, int r, int c, float (&v)[8], int n, int) {
+      if (!(wait >> idx & 1)) return;
+      classes.apply(idx, v);
+      emit(r, c, v, n, ask(r, c, n));
+    });
+  }
+}
+
+// the parts' sums, added in order
+template <class O, bool DW>
+__global__ void __launch_bounds__(256) grad_join_kernel(Grad a) {
+  const int c8 = (a.N + 7) / 8;
+  const int64_t n = a.M * c8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / c8;
+    const int c = (int)(i - r * c8) * 8;
+    const Before before = before_of<DW>(a, r, c);
+    float v[8];
+    load_f32<float, 8>(a.partial + i * 8, v);
+    for (int p = 1; p < a.parts; ++p) {
+      float t[8];
+      load_f32<float, 8>(a.partial + ((int64_t)p * n + i) * 8, t);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] += t[e];
+    }
+    finish<O, DW>(a, r, c, v, min(8, a.N - c), before);
+  }
+}
+
+template <class O, class T, int W, bool DW> void run_w(hipStream_t st, Grad& a) {
+  typedef Tile<T, sizeof(O) == 4 ? 3 : 1, W, DW, true> G;
+  a.tiles_m = ceil_div(a.M, 2 * W);
+  a.tiles_n = ceil_div(a.N, 2 * W);
+  const int per = (a.tiles_m * a.tiles_n * a.parts + 7) / 8;
+  auto k = grad_kernel<O, T, W, DW>;
+  // (more LDS than a launch gets unasked; set again on every launch: which devices know it is not ours to remember)
+  if (G::LDS > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+  OSEQ_LAUNCH(k, grid_of_blocks((int64_t)per * 8), dim3(256), G::LDS, st, a);
+  if (a.parts > 1) OSEQ_LAUNCH((grad_join_kernel<O, DW>), dim3(grid_of(a.M * ((a.N + 7) / 8))), dim3(256), 0, st, a);
+}
+template <class O, class T, bool DW> void run(hipStream_t st, Grad& a, const ProductShape& s) {
+  a.cut = parts_of(a.K, s.parts);
+  a.parts = a.cut.count;
+  if (s.wave == 128) run_w<O, T, 128, DW>(st, a);
+  else if (s.wave == 64) run_w<O, T, 64, DW>(st, a);
+  else run_w<O, T, 32, DW>(st, a);
+}
+
+template <class O, class T> void piece_of(const optorch_softmax_loss_t& a, const LossPiece& p) {
+  hipStream_t st = (hipStream_t)a.hip_stream;
+  Grad g = {};
+  g.a = p.ds; g.lda = (int)p.ds_row;
+  g.partial = p.parts;
+  g.info = (const float4*)p.info;
+  g.scale = p.scale;
+  g.unscale = 1.f / loss_scale_of(a.precision);
+  if (a.dx) {
+    g.b = p.w; g.ldb = p.ldw;
+    g.M = a.rows; g.N = a.in_features; g.K = p.count;
+    g.acc = p.acc; g.start = p.start; g.end = p.end;
+    g.out = a.dx; g.ldo = a.lddx;
+    run<O, T, false>(st, g, p.dx);
+  }
+  if (a.dw) {
+    g.b = p.xs; g.ldb = p.ldxs;
+    g.M = p.count; g.N = a.in_features; g.K = (int)a.rows;
+    g.out = (O*)a.dw + p.first * a.lddw; g.ldo = a.lddw;
+    run<O, T, true>(st, g, p.dw);
+  }
+}
+
+}  // namespace
+
+void launch_loss_piece(const optorch_softmax_loss_t& a, const LossPiece& p) {
+  if (a.precision == OPTORCH_FP32) piece_of<float, bf16_t>(a, p);
+  else if (a.precision == OPTORCH_BF16) piece_of<bf16_t, bf16_t>(a, p);
+  else piece_of<f16_t, f16_t>(a, p);
+}
+
+}  // namespace oseq

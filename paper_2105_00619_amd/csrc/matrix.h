@@ -1,4 +1,4 @@
-// Host-callable launchers of the matrix operators (k_linear.hip, k_ortho.hip).  All launches are asynchronous on `st`.
+// Host-callable launchers of the matrix operators (k_linear.hip, k_norm.hip, k_loss.hip, k_ortho.hip).  All launches are asynchronous on `st`.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -52,6 +52,46 @@ struct LinearPlan {
 LinearPlan plan_linear(const optorch_linear_t& a, bool backward);
 void launch_linear_forward(const optorch_linear_t& a, const LinearPlan& p);
 void launch_linear_backward(const optorch_linear_t& a, const LinearPlan& p);
+
+// The gradient of a layer norm: its blocks, whose sums for dweight and dbias lie one behind the other in the workspace
+struct NormPlan { int lanes, rows_at_once, blocks; uint64_t bytes; };
+NormPlan plan_norm_backward(const optorch_layer_norm_t& a);
+void launch_norm_forward(const optorch_layer_norm_t& a);
+void launch_norm_backward(const optorch_layer_norm_t& a, const NormPlan& p);
+
+// What a loss' call does with its workspace.  The classes are taken in pieces (of whole tiles): forward only where their weights
+// are laid out anew, backward as many as keep a piece of ds within LOSS_PIECE_BYTES.
+struct LossPlan {
+  bool pack_x, pack_w;
+  int wave;             // the logits' tiles: 2 * wave x 2 * wave; a row's sums are kept for every `wave` classes
+  int columns;          // how many of those
+  int piece;            // classes of a piece
+  int64_t ds_row;       // places of a row of ds
+  ProductShape dx, dw;
+  uint64_t off_x, off_w, off_sums, off_totals, off_picked;     // operands; [columns][rows] (maximum, sum), sums of logits; targets' logits
+  uint64_t off_index, off_target, off_start, off_flag;         // a teacher's entries in order of their classes
+  uint64_t off_info, off_scale, off_xs, off_ds, off_acc, off_parts, off_bias;
+  uint64_t bytes;
+};
+LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward);
+void launch_loss_forward(const optorch_softmax_loss_t& a, const LossPlan& p);
+void launch_loss_backward(const optorch_softmax_loss_t& a, const LossPlan& p);
+
+// The two products of a loss' gradient for a piece of the classes (k_loss_grad.hip)
+struct LossPiece {
+  const void *ds, *w, *xs;         // operands, with the distances of their rows
+  int64_t ds_row; int ldw, ldxs;
+  int first, count;                // the piece's classes
+  const void* info;                // a row's factor of dx: the fourth of four floats
+  const float* scale;              // the factor of dw
+  float* acc; float* parts;        // dx summed over the pieces; parts of a reduction
+  bool start, end;                 // whether it is the first and the last piece
+  ProductShape dx, dw;
+};
+void launch_loss_piece(const optorch_softmax_loss_t& a, const LossPiece& p);
+// what ds is multiplied by while it is held: its largest values, of up to 2, stay in the type's range, and the smallest ones that
+// count are as far above the smallest it has as they can be
+constexpr float loss_scale_of(int precision) { return precision == OPTORCH_FP16 ? 16384.f : 1.f; }
 
 // ---- orthogonalised updates: what the host plans and the kernels read ----
 

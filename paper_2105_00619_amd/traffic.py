@@ -60,7 +60,7 @@ DATAFLOW_KERNELS = {
 
 
 DATAFLOW_ONLY = ("k_dataflow.hip", "dataflow.cpp")          # sources of the data-flow kernels alone
-MATRIX_ONLY = ("mat_core.h", "matrix.h", "parts.h", "matrix.cpp", "k_linear.hip", "ortho.cpp", "k_ortho.hip")  # ... of the matrix operators
+MATRIX_ONLY = ("mat_core.h", "mat_layout.h", "matrix.h", "parts.h", "args.h", "matrix.cpp", "norm.cpp", "loss.cpp", "k_linear.hip", "k_norm.hip", "k_loss.hip", "k_loss_grad.hip", "ortho.cpp", "k_ortho.hip")  # ... of the matrix operators
 SHARED = ("dev_common.h", "launch.h")                         # device helpers both kinds of kernels are built from
 
 

@@ -1,0 +1,486 @@
+"""Losses over many classes and their gradients against plain float64 computations, through the Python binding.
+
+Tolerances, with u = 2^-24.  A logit is a sum like those of the linear layers: off by at most n 2^-23 times the sum of the absolute products,
+n one addition for each four products and plane pair and a few more, and by u of itself for each of bias, temperature and their rounding.  lse is off by as
+much as the logits, weighted by p, by the additions of its sum (half a tile's columns in a row, the rest joined pairwise or by eight
+threads at least), by 3 u times the mean distance of the logits from their maximum (the exponent's products), and by its own rounding.
+
+ds = dloss (a p - target): p is off, relatively, by its logit's error and 3 u |s - lse| + 8 u.  In 16 bits it is rounded, by eps / 2
+of itself, and in fp16, where it is held 2^14 times larger, by 2^-39 of the row's factor at least; x' is off by eps / 2 of itself
+and in fp16 by 2^-25 of the largest factor.  dx and dw are sums of such products and are rounded once."""
+import ctypes as C
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = ("fp32", "bf16", "fp16")
+U, U23 = 2.0 ** -24, 2.0 ** -23
+
+
+def _t():
+    import torch
+    return torch
+
+
+def _dt(name):
+    torch = _t()
+    return {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}[name]
+
+
+def _randn(*shape, seed, scale=1.0):
+    torch = _t()
+    return torch.randn(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), dtype=torch.float64, device="cuda") * scale
+
+
+def _rand(*shape, seed):
+    torch = _t()
+    return torch.rand(*shape, generator=torch.Generator(device="cuda").manual_seed(seed), dtype=torch.float64, device="cuda")
+
+
+def _strided(v, dt, pad, shift):
+    """v in the type dt on the GPU, its rows `pad` elements further apart and `shift` elements off an aligned address; and the whole buffer."""
+    torch = _t()
+    r, c = v.shape
+    buf = torch.full((shift + r * (c + pad) + 8,), 7.5, dtype=dt, device="cuda")
+    m = buf[shift:shift + r * (c + pad)].view(r, c + pad)[:, :c]
+    m.copy_(v)
+    return m, buf
+
+
+def _within(got, ref, tol, what):
+    bad = ~((got.double() - ref).abs() <= tol)
+    assert not bool(bad.any()), "%s: %d of %d outside, worst %.3g times the tolerance" % (
+        what, int(bad.sum()), bad.numel(), float(((got.double() - ref).abs() / tol.clamp_min(1e-300)).max()))
+
+
+def _adds(k, name):
+    return k / 4 * (6 if name == "fp32" else 1) + 48
+
+
+def _mm(a, b):
+    return _t().mm(a, b.contiguous())
+
+
+class Reference:
+    """The loss' definition in float64, with the errors that its parts may have in the kernels.
+
+    target [rows, classes], zero in rows that are left out; used [rows]; entropy [rows]: sum of target log target (a teacher's)."""
+
+    def __init__(self, name, x, w, bias, target, used, tau=1.0, z_loss=0.0, entropy=None):
+        self.name, self.x, self.w, self.target, self.used = name, x.double(), w.double(), target, used
+        self.tau, self.z_loss = tau, z_loss
+        torch = _t()
+        b = bias.double() if bias is not None else torch.zeros(w.shape[0], dtype=torch.float64, device="cuda")
+        bf = torch.where(b.abs() < math.inf, b, torch.zeros_like(b))
+        s = (_mm(self.x, self.w.T) + b) / tau
+        self.s = s
+        size = _mm(self.x.abs(), self.w.abs().T)
+        self.ds_logit = (_adds(x.shape[1], name) * U23 * size + 3 * U * (size + bf.abs())) / tau
+        self.lse = torch.logsumexp(s, 1)
+        p = torch.exp(s - self.lse[:, None])
+        far = torch.where(p > 0, p * (s.max(1, keepdim=True).values - s), torch.zeros_like(p)).sum(1)
+        self.lse_tol = (p * self.ds_logit).sum(1) + U * (64 + 24 + s.shape[1] / 256 + 3 * far + 4 * self.lse.abs() + 8)
+        fs = torch.where(target > 0, target * s, torch.zeros_like(s))
+        self.loss = torch.where(used, -fs.sum(1) + self.lse * target.sum(1) + z_loss * self.lse ** 2 + (entropy if entropy is not None else 0), torch.zeros_like(self.lse))
+        terms = fs.abs().sum(1)
+        n = 48 + s.shape[1] / 64  # additions of a target's terms
+        self.loss_tol = self.lse_tol * (1 + 2 * z_loss * self.lse.abs()) + (target * self.ds_logit).sum(1) + U * (
+            n * terms + 4 * self.lse.abs() + 6 * z_loss * self.lse ** 2) + (U * 12 * (1 + entropy.abs() + terms) if entropy is not None else 0)
+
+    def gradients(self, lse, dloss):
+        torch = _t()
+        name, dt = self.name, _dt(self.name)
+        e = torch.finfo(dt).eps / 2 if name != "fp32" else U
+        k = lse.double()[:, None]
+        a = 1 + 2 * self.z_loss * k
+        p = torch.exp(self.s - k)
+        g = torch.where(self.used, dloss.double() / self.tau, torch.zeros_like(dloss.double()))[:, None]
+        f = a.abs().clamp_min(1)
+        # (a left out class' logit is -infinity, its p zero)
+        near = torch.where(p > 0, 3 * U * (self.s - k).abs(), torch.zeros_like(p))
+        ds = g * (a * p - self.target)
+        exact = g.abs() * (a.abs() * p * (self.ds_logit + near + 8 * U) + 4 * U * (self.target + a.abs() * p))
+        held = exact + e * ds.abs() + (g.abs() * f * 2.0 ** -39 if name == "fp16" else 0)
+        largest = float((g.abs() * f).max())
+        x, w = self.x, self.w
+        out_floor = 2.0 ** -25 if name == "fp16" else 2.0 ** -134
+        dx, dw = _mm(ds, w), _mm(ds.T, x)
+        dx_fp32 = _mm(held, w.abs()) + (_adds(w.shape[0], name) + 40) * U23 * _mm(ds.abs(), w.abs())
+        xe = e * x.abs() + (2.0 ** -25 * (largest / g.abs().clamp_min(1e-300)).clamp_max(1e30) if name == "fp16" else 0)
+        dw_fp32 = _mm(held.T, x.abs() + xe) + _mm(ds.abs().T, xe) + (_adds(x.shape[0], name) + 40) * U23 * _mm(ds.abs().T, x.abs())
+        eo = torch.finfo(dt).eps / 2
+        db_tol = exact.sum(0) + (80 + x.shape[0] / 16) * U * ds.abs().sum(0)
+        return (dx, dx_fp32 + eo * (dx.abs() + dx_fp32) + out_floor), (dw, dw_fp32 + eo * (dw.abs() + dw_fp32) + out_floor), (ds.sum(0), db_tol)
+
+
+
+# (rows, in, classes): single values, one row, one class, odd sizes, the edges of tiles and of the runs of columns that a row's sums are kept for, many
+# classes with few rows and many rows with few classes
+SIZES = [(1, 1, 1), (1, 8, 2), (3, 5, 7), (2, 64, 1000), (17, 33, 65), (64, 64, 64), (65, 72, 129), (130, 200, 300), (257, 128, 513), (33, 520, 4099),
+         (300, 40, 1031), (5, 1024, 20000), (1000, 24, 10), (520, 256, 2050)]
+
+
+def _operands(rows, cin, classes, name, seed=None):
+    i = SIZES.index((rows, cin, classes)) if seed is None else seed
+    dt, pad, shift = _dt(name), (0, 8, 3)[i % 3], (0, 8, 1)[i % 3]
+    x, _ = _strided(_randn(rows, cin, seed=i), dt, pad, shift)
+    w, _ = _strided(_randn(classes, cin, seed=i + 100, scale=2 * cin ** -0.5), dt, pad, shift)
+    bias = _randn(classes, seed=i + 200).float() if i % 2 else None
+    dloss = (_rand(rows, seed=i + 300) + 0.5).float() if i % 4 else _t().full((rows,), 1.0 / rows, device="cuda")
+    if name == "fp16":
+        dloss = dloss * 64
+    return i, dt, pad, shift, x, w, bias, dloss
+
+
+def _entropy_target(labels, classes, smoothing):
+    torch = _t()
+    used = labels >= 0
+    t = torch.zeros(labels.numel(), classes, dtype=torch.float64, device="cuda")
+    t[used] = smoothing / classes
+    r = used.nonzero()[:, 0]
+    t[r, labels[r].long()] += 1 - smoothing
+    return t, used
+
+
+def _check_gradients(ref, lse, dloss, got, i, pad, shift, dt, call):
+    """dx, dw and dbias, each alone, and into given tensors, nothing beside them written."""
+    torch = _t()
+    (dx, tx), (dw, tw), (db, tb) = ref.gradients(lse, dloss)
+    _within(got[0], dx, tx, "dx")
+    _within(got[1], dw, tw, "dw")
+    _within(got[2], db, tb, "dbias")
+    for k, n in enumerate(("dx", "dw", "dbias")):
+        alone = call(need=(n,))
+        assert torch.equal(alone[k], got[k]) and all(alone[q] is None for q in range(3) if q != k), n
+    outs = [_strided(torch.zeros(*t.shape), dt, pad, shift) for t in got[:2]]
+    before = [b.clone() for _, b in outs]
+    call(need=("dx", "dw"), dx=outs[0][0], dw=outs[1][0])
+    for (m, buf), b, t in zip(outs, before, got):
+        assert torch.equal(m, t)
+        m.zero_()
+        r, c = t.shape
+        b[shift:shift + r * (c + pad)].view(r, c + pad)[:, :c].zero_()
+        assert torch.equal(buf, b), "values outside the result were written"
+
+
+@pytest.mark.parametrize("name", DTYPES)
+@pytest.mark.parametrize("rows,cin,classes", SIZES)
+def test_cross_entropy(rows, cin, classes, name):
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    i, dt, pad, shift, x, w, bias, dloss = _operands(rows, cin, classes, name)
+    kw = {"label_smoothing": (0.0, 0.1, 0.0, 1.0)[i % 4], "z_loss": (0.0, 0.0, 1e-2)[i % 3]}
+    labels = torch.randint(0, classes, (rows,), generator=torch.Generator().manual_seed(i), dtype=torch.int32).cuda()
+    labels[rows // 3:rows // 2] = -1
+    target, used = _entropy_target(labels, classes, kw["label_smoothing"])
+    ref = Reference(name, x, w, bias, target, used, z_loss=kw["z_loss"])
+    loss, lse = B.cross_entropy_forward(x, w, labels, bias, **kw)
+    _within(lse, ref.lse, ref.lse_tol, "lse")
+    _within(loss, ref.loss, ref.loss_tol, "loss")
+    assert not bool(loss[~used].any())
+
+    def call(need=("dx", "dw", "dbias"), **out):
+        return B.cross_entropy_backward(dloss, x, w, labels, lse, bias, need=need, **kw, **out)
+    _check_gradients(ref, lse, dloss, call(), i, pad, shift, dt, call)
+
+
+def _teacher_entries(rows, classes, top, seed, dt):
+    """Indices and logits: unused entries, rows without any, entries of one class."""
+    torch = _t()
+    idx = (_rand(rows, top, seed=seed) * classes).int().clamp_max(classes - 1)
+    t = _randn(rows, top, seed=seed + 1, scale=3.0).to(dt)
+    idx[_rand(rows, top, seed=seed + 2) < 0.1] = -1
+    t[_rand(rows, top, seed=seed + 3) < 0.1] = -math.inf
+    if rows > 2:
+        idx[rows // 2] = -5
+        t[rows - 1] = -math.inf
+    return idx, t
+
+
+def _teacher_target(idx, t, classes, tau):
+    torch = _t()
+    v = (t.double() / tau).masked_fill(idx < 0, -math.inf)
+    used = (v > -math.inf).any(1)
+    q = torch.softmax(v, 1)
+    q = torch.where(used[:, None], q, torch.zeros_like(q))
+    target = torch.zeros(idx.shape[0], classes, dtype=torch.float64, device="cuda")
+    target.scatter_add_(1, idx.clamp_min(0).long(), q.masked_fill(idx < 0, 0.0))
+    entropy = torch.where(target > 0, target * target.clamp_min(1e-300).log(), torch.zeros_like(target)).sum(1)
+    return target, used, entropy
+
+
+TOPS = (1, 2, 5, 10, 64, 65, 100, 256, 300, 1024)
+
+
+@pytest.mark.parametrize("name", DTYPES)
+@pytest.mark.parametrize("rows,cin,classes", SIZES)
+def test_distillation(rows, cin, classes, name):
+    from paper_2105_00619_amd import binding as B
+    i, dt, pad, shift, x, w, bias, dloss = _operands(rows, cin, classes, name)
+    top, tau = TOPS[(i * 3 + DTYPES.index(name)) % len(TOPS)], (1.0, 2.0, 0.7)[i % 3]
+    idx, t = _teacher_entries(rows, classes, top, i + 400, _dt(DTYPES[(i + 1) % 3]))
+    if i % 2:
+        idx, t = _strided(idx, idx.dtype, 3, 1)[0], _strided(t, t.dtype, 1, 3)[0]
+    target, used, entropy = _teacher_target(idx, t, classes, tau)
+    ref = Reference(name, x, w, bias, target, used, tau=tau, entropy=entropy)
+    loss, lse = B.distillation_forward(x, w, idx, t, bias, temperature=tau)
+    _within(lse, ref.lse, ref.lse_tol, "lse")
+    # (a teacher's probabilities are off by their exponent's rounding, 2 u of logits of up to 15 / tau)
+    more = 40 / tau * U * (target * (ref.s - ref.lse[:, None]).abs()).sum(1) if tau else 0
+    _within(loss, ref.loss, ref.loss_tol + more, "loss")
+    assert not bool(loss[~used].any())
+
+    def call(need=("dx", "dw", "dbias"), **out):
+        return B.distillation_backward(dloss, x, w, idx, t, lse, bias, temperature=tau, need=need, **out)
+    ref.target = target
+    got = call()
+    # (the same in the gradients, of the target)
+    slack = ref.ds_logit
+    ref.ds_logit = slack + 40 / tau * U
+    _check_gradients(ref, lse, dloss, got, i, pad, shift, dt, call)
+
+
+def test_distillation_of_one_entry_is_cross_entropy():
+    """A teacher that is sure: the same loss and the same bits of the gradients."""
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    x, w = _randn(70, 136, seed=1).bfloat16(), _randn(333, 136, seed=2, scale=0.2).bfloat16()
+    labels = torch.randint(0, 333, (70,), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+    labels[5] = -1
+    a = B.cross_entropy_forward(x, w, labels)
+    b = B.distillation_forward(x, w, labels[:, None], torch.full((70, 1), -2.0, device="cuda"))
+    assert torch.equal(a[1], b[1])
+    assert float((a[0] - b[0]).abs().max()) <= 4 * U * float(a[1].abs().max())
+    d = torch.rand(70, device="cuda")
+    for p, q in zip(B.cross_entropy_backward(d, x, w, labels, a[1])[:2], B.distillation_backward(d, x, w, labels[:, None], torch.full((70, 1), -2.0, device="cuda"), b[1])):
+        assert torch.equal(p, q)
+
+
+# sizes that take more than one piece of the classes: ds beyond 256 MB; weights that are laid out anew beyond 256 MB
+@pytest.mark.parametrize("name,rows,cin,classes", [("bf16", 20000, 24, 9001), ("fp32", 8200, 17, 5003), ("fp32", 5, 1030, 40009), ("bf16", 7, 1031, 140000), ("fp16", 30011, 8, 4999)])
+def test_pieces_of_the_classes(name, rows, cin, classes):
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    dt = _dt(name)
+    x = _randn(rows, cin, seed=1).to(dt)
+    w = _randn(classes, cin, seed=2, scale=2 * cin ** -0.5).to(dt)
+    bias = _randn(classes, seed=3).float()
+    labels = torch.randint(-1, classes, (rows,), generator=torch.Generator().manual_seed(4), dtype=torch.int32).cuda()
+    target, used = _entropy_target(labels, classes, 0.0)
+    ref = Reference(name, x, w, bias, target, used)
+    loss, lse = B.cross_entropy_forward(x, w, labels, bias)
+    _within(lse, ref.lse, ref.lse_tol, "lse")
+    _within(loss, ref.loss, ref.loss_tol, "loss")
+    dloss = torch.full((rows,), 0.01, device="cuda")
+    got = B.cross_entropy_backward(dloss, x, w, labels, lse, bias)
+    for what, g, (r, tol) in zip(("dx", "dw", "dbias"), got, ref.gradients(lse, dloss)):
+        _within(g, r, tol, what)
+        del r, tol
+    del ref, target
+    # a teacher's entries in every piece
+    idx, t = _teacher_entries(rows, classes, 6, 50, torch.float32)
+    target, used, entropy = _teacher_target(idx, t, classes, 2.0)
+    ref = Reference(name, x, w, bias, target, used, tau=2.0, entropy=entropy)
+    loss, lse = B.distillation_forward(x, w, idx, t, bias, temperature=2.0)
+    _within(lse, ref.lse, ref.lse_tol, "lse")
+    more = 20 * U * (target * (ref.s - ref.lse[:, None]).abs()).sum(1)
+    _within(loss, ref.loss, ref.loss_tol + more, "loss")
+    ref.ds_logit += 20 * U
+    got = B.distillation_backward(dloss, x, w, idx, t, lse, bias, temperature=2.0)
+    for what, g, (r, tol) in zip(("dx", "dw", "dbias"), got, ref.gradients(lse, dloss)):
+        _within(g, r, tol, what)
+
+
+def test_gradients_are_the_forward_calls_differences():
+    """Along a direction, of L = sum(c loss): D(t) = (L(+t) - L(-t)) / 2t is off by a t^2 + ..., so D(t / 2) by about a third of
+    |D(t) - D(t / 2)|, and by the rounding of the losses and the steps over t."""
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    for rows, cin, classes in ((4, 6, 9), (33, 70, 150)):
+        x, w, b = _randn(rows, cin, seed=1).float(), _randn(classes, cin, seed=2, scale=cin ** -0.5).float(), _randn(classes, seed=3).float()
+        c = _randn(rows, seed=4).float()
+        labels = torch.randint(-1, classes, (rows,), generator=torch.Generator().manual_seed(5), dtype=torch.int32).cuda()
+        idx, t = _teacher_entries(rows, classes, 5, 60, torch.float32)
+        for fwd, bwd, args, kw in ((B.cross_entropy_forward, B.cross_entropy_backward, (labels,), {"label_smoothing": 0.2, "z_loss": 0.05}),
+                                   (B.distillation_forward, B.distillation_backward, (idx, t), {"temperature": 1.5})):
+            def value(p):
+                return fwd(p[0], p[1], *args, p[2], **kw)
+            loss, lse = value([x, w, b])
+            grads = bwd(c, x, w, *args, lse, b, **kw)
+            noise = float((c.abs() * (loss.abs() + lse.abs() + 4)).double().sum()) * (_adds(cin, "fp32") + 120) * U23
+            for which in range(3):
+                v = _randn(*grads[which].shape, seed=77).float()
+                v /= v.norm()
+
+                def slope(h):
+                    p, q = [x, w, b], [x, w, b]
+                    p[which], q[which] = p[which] + h * v, q[which] - h * v
+                    step = ((p[which].double() - q[which].double()) * v.double()).sum() / v.double().square().sum()
+                    return float((c.double() * (value(p)[0].double() - value(q)[0].double())).sum() / step)
+                h = 2.0 ** -4
+                wide, near = slope(h), slope(h / 2)
+                want = float((grads[which].double() * v.double()).sum())
+                rounding = 2 * noise / h + 2 * U / h * float((grads[which].abs().double() * [x, w, b][which].abs().double()).sum())
+                assert abs(near - want) <= abs(wide - near) + rounding, (rows, which, near, want, wide)
+
+
+@pytest.mark.parametrize("name", DTYPES)
+def test_left_out_rows_and_classes_and_values_that_are_not_finite(name):
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    dt = _dt(name)
+    x, w = _randn(40, 72, seed=1).to(dt), _randn(200, 72, seed=2, scale=0.2).to(dt)
+    bias = _randn(200, seed=3).float()
+    bias[150:] = -math.inf  # classes that fill the matrix up
+    labels = torch.randint(0, 150, (40,), generator=torch.Generator().manual_seed(4), dtype=torch.int32).cuda()
+    dloss = torch.rand(40, device="cuda") + 0.5
+    loss0, lse0 = B.cross_entropy_forward(x, w, labels, bias)
+    short = B.cross_entropy_forward(x, w[:150].contiguous(), labels, bias[:150].contiguous())
+    assert float((loss0 - short[0]).abs().max()) <= 40 * U * float(lse0.abs().max())
+    dx0, dw0, db0 = B.cross_entropy_backward(dloss, x, w, labels, lse0, bias)
+    assert not bool(dw0[150:].any()) and not bool(db0[150:].any()) and bool(torch.isfinite(dx0).all())
+    # a row that is left out may hold anything
+    labels1 = labels.clone()
+    labels1[[3, 17]] = -7
+    x1, dloss1 = x.clone(), dloss.clone()
+    x1[3], x1[17, 5], dloss1[3] = math.nan, math.inf, math.nan
+    xc, dlossc = x.clone(), dloss.clone()
+    xc[[3, 17]], dlossc[[3, 17]] = 0, 0
+    loss1, lse1 = B.cross_entropy_forward(x1, w, labels1, bias)
+    assert not bool(loss1[[3, 17]].any()) and bool(torch.isfinite(loss1).all())
+    rest = [i for i in range(40) if i not in (3, 17)]
+    assert torch.equal(loss1[rest], loss0[rest])
+    got = B.cross_entropy_backward(dloss1, x1, w, labels1, lse1, bias)
+    want = B.cross_entropy_backward(dlossc, xc, w, labels1, lse0, bias)
+    assert not bool(got[0][[3, 17]].any())
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    # the same, a teacher's rows
+    idx, t = labels1[:, None].repeat(1, 3), torch.zeros(40, 3, device="cuda")
+    idx[:, 1] = (idx[:, 0] + 1).clamp_max(149)
+    idx[[3, 17]] = -1
+    loss2, lse2 = B.distillation_forward(x1, w, idx, t, bias)
+    got = B.distillation_backward(dloss1, x1, w, idx, t, lse2, bias)
+    want = B.distillation_backward(dlossc, xc, w, idx, t, B.distillation_forward(xc, w, idx, t, bias)[1], bias)
+    assert not bool(loss2[[3, 17]].any())
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    # a row in use: NaN in its loss and gradient, and in dw; the other rows' keep their bits
+    loss3, lse3 = B.cross_entropy_forward(x1, w, labels, bias)
+    assert bool(torch.isnan(loss3[3])) and not bool(torch.isfinite(loss3[17])) and torch.equal(loss3[rest], loss0[rest])
+    dx3, dw3, _ = B.cross_entropy_backward(dloss, x1, w, labels, lse3, bias)
+    assert bool(torch.isnan(dx3[3]).all()) and torch.equal(dx3[rest], dx0[rest]) and bool(torch.isnan(dw3[:150]).all())
+    # a label, an index and a teacher's logit that cannot be
+    labels4 = labels.clone()
+    labels4[7] = 200
+    loss4, lse4 = B.cross_entropy_forward(x, w, labels4, bias)
+    assert bool(torch.isnan(loss4[7])) and int(torch.isnan(loss4).sum()) == 1 and torch.equal(lse4, lse0)
+    dx4, dw4, db4 = B.cross_entropy_backward(dloss, x, w, labels4, lse4, bias)
+    assert bool(torch.isnan(dx4[7]).all()) and int(torch.isnan(dx4).any(1).sum()) == 1 and bool(torch.isnan(dw4[:150]).all()) and bool(torch.isnan(db4[:150]).all())
+    for k, (i, v) in enumerate(((200, 0.0), (1 << 22, 0.0), (4, math.nan), (4, math.inf))):
+        idx, t = labels[:, None].repeat(1, 2), torch.zeros(40, 2, device="cuda")
+        idx[:, 1] = -1
+        idx[9, 1], t[9, 1] = i, v
+        loss5, lse5 = B.distillation_forward(x, w, idx, t, bias)
+        assert bool(torch.isnan(loss5[9])) and int(torch.isnan(loss5).sum()) == 1, k
+        dx5 = B.distillation_backward(dloss, x, w, idx, t, lse5, bias)[0]
+        assert bool(torch.isnan(dx5[9]).all()) and int(torch.isnan(dx5).any(1).sum()) == 1, k
+    # no class left: nothing to be sure of
+    none = torch.full((200,), -math.inf, device="cuda")
+    loss6, lse6 = B.cross_entropy_forward(x, w, labels, none)
+    assert bool(torch.isnan(loss6).all()) and bool((lse6 == -math.inf).all())
+
+
+def test_a_sure_student_and_large_logits():
+    """Logits of some hundreds: nothing overflows, the loss of a sure row is the distance of its logits, the gradient of a right one zero."""
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    w = torch.zeros(300, 64, device="cuda")
+    w[:64] = 400 * torch.eye(64, device="cuda")
+    x = torch.eye(64, device="cuda")
+    right = torch.arange(64, dtype=torch.int32, device="cuda")
+    loss, lse = B.cross_entropy_forward(x, w, right)
+    assert bool((lse == 400).all()) and not bool(loss.any())
+    d = torch.ones(64, device="cuda")
+    dx, dw, _ = B.cross_entropy_backward(d, x, w, right, lse)
+    assert not bool(dx.any()) and not bool(dw.any())
+    wrong = (right + 1) % 64
+    loss, lse = B.cross_entropy_forward(x, w, wrong)
+    assert bool((loss == 400).all())
+    dx, dw, _ = B.cross_entropy_backward(d, x, w, wrong, lse)
+    assert torch.equal(dx, 400 * (torch.eye(64, device="cuda") - torch.eye(64, device="cuda").roll(1, 1)))
+
+
+@pytest.mark.parametrize("name", DTYPES)
+def test_factors_of_rows_that_are_far_apart(name):
+    """dloss from 1e-6 to 1: every row's dx as exact as the others', dw as exact as its largest terms."""
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    dt = _dt(name)
+    x, w = _randn(96, 128, seed=1).to(dt), _randn(500, 128, seed=2, scale=4.0).to(dt)
+    labels = torch.randint(0, 500, (96,), generator=torch.Generator().manual_seed(4), dtype=torch.int32).cuda()
+    dloss = (10 ** (-6 * _rand(96, seed=5))).float()
+    target, used = _entropy_target(labels, 500, 0.0)
+    ref = Reference(name, x, w, None, target, used)
+    loss, lse = B.cross_entropy_forward(x, w, labels)
+    got = B.cross_entropy_backward(dloss, x, w, labels, lse)
+    for what, g, (r, tol) in zip(("dx", "dw"), got, ref.gradients(lse, dloss)):
+        _within(g, r, tol, what)
+    zero = B.cross_entropy_backward(torch.zeros(96, device="cuda"), x, w, labels, lse)
+    assert not bool(zero[0].any()) and not bool(zero[1].any())
+
+
+@pytest.mark.parametrize("name", DTYPES)
+def test_empty_batches(name):
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    x, w = torch.empty(0, 72, dtype=_dt(name), device="cuda"), _randn(30, 72, seed=1).to(_dt(name))
+    v, b = torch.empty(0, device="cuda"), torch.zeros(30, device="cuda")
+    labels = torch.empty(0, dtype=torch.int32, device="cuda")
+    loss, lse = B.cross_entropy_forward(x, w, labels, b)
+    assert loss.numel() == 0 and lse.numel() == 0
+    junk = torch.full((30, 72), 3.0, dtype=_dt(name), device="cuda")
+    idx, t = torch.empty(0, 4, dtype=torch.int32, device="cuda"), torch.empty(0, 4, device="cuda")
+    assert B.distillation_forward(x, w, idx, t, b)[0].numel() == 0
+    for call in (lambda: B.cross_entropy_backward(v, x, w, labels, v, b, dw=junk), lambda: B.distillation_backward(v, x, w, idx, t, v, b, dw=junk)):
+        junk.fill_(3.0)
+        got = call()
+        assert got[0].shape == x.shape and got[1] is junk and not bool(junk.any()) and not bool(got[2].any())
+
+
+def test_replayed_in_a_graph_and_on_another_stream():
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    x, w = _randn(300, 256, seed=1).bfloat16(), _randn(2100, 256, seed=2, scale=0.1).bfloat16()
+    labels = torch.randint(-1, 2100, (300,), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+    idx, t = _teacher_entries(300, 2100, 20, 70, torch.bfloat16)
+    d = torch.rand(300, device="cuda")
+    b = _randn(2100, seed=9).float()
+
+    def both():
+        a = B.cross_entropy_forward(x, w, labels, b, label_smoothing=0.1)
+        c = B.distillation_forward(x, w, idx, t, temperature=2.0)
+        return (a + c + B.cross_entropy_backward(d, x, w, labels, a[1], b, label_smoothing=0.1)
+                + B.distillation_backward(d, x, w, idx, t, c[1], temperature=2.0)[:2])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        both()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = both()
+    for k in range(3):
+        x.copy_(_randn(300, 256, seed=10 + k))
+        d.copy_(torch.rand(300, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(kept, both()):
+            assert torch.equal(got, want)
+        with torch.cuda.stream(side):
+            other = both()
+        torch.cuda.synchronize()
+        for got, want in zip(kept, other):
+            assert torch.equal(got, want)

@@ -1,0 +1,73 @@
+"""Host-side checks of the layer norm (no GPU): workspace sizes and refusals.  A refused call launches nothing, so the pointers need
+not be device memory."""
+import ctypes as C
+import os
+
+import pytest
+
+from paper_2105_00619_amd import binding as B
+from paper_2105_00619_amd.binding import E_BUDGET, E_INVALID
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    if not os.path.exists(B.LIB_PATH):
+        from paper_2105_00619_amd import build
+        build.build(verbose=False)
+
+
+def _norm(**kw):
+    """Arguments of both directions that pass every check; the addresses are never read."""
+    a = B.optorch_layer_norm_t()
+    a.precision, a.cols, a.rows, a.eps = 1, 64, 160, 1e-5
+    for i, n in enumerate(("x", "y", "dy", "residual", "dx")):
+        setattr(a, n, (1 + i) << 24)
+        setattr(a, "ldr" if n == "residual" else "ld" + n, 64)
+    for i, n in enumerate(("weight", "bias", "mean", "rstd", "dweight", "dbias")):
+        setattr(a, n, (16 + i) << 24)
+    a.workspace, a.workspace_bytes = 1 << 30, 1 << 24
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("kw,backward,word", [
+    (dict(precision=3), 0, "precision"), (dict(precision=-1), 1, "precision"),
+    (dict(rows=-1), 0, "rows"), (dict(rows=1 << 31), 1, "rows"), (dict(cols=0), 0, "cols"), (dict(cols=1 << 22), 1, "cols"),
+    (dict(eps=-1e-5), 0, "eps"), (dict(eps=float("nan")), 0, "eps"), (dict(eps=float("inf")), 0, "eps"),
+    (dict(x=None), 0, "null x"), (dict(y=None), 0, "null y"), (dict(ldx=63), 0, "leading dimension of x"), (dict(ldy=63), 0, "leading dimension of y"),
+    (dict(x=(1 << 24) + 1), 0, "aligned"), (dict(weight=(1 << 28) + 2), 0, "aligned"), (dict(bias=(1 << 28) + 1), 0, "aligned"),
+    (dict(mean=(1 << 28) + 1), 0, "aligned"), (dict(rstd=None), 0, "mean and rstd"), (dict(mean=None), 0, "mean and rstd"),
+    (dict(dx=None, dweight=None, dbias=None), 1, "no gradient"),
+    (dict(dy=None), 1, "null dy"), (dict(x=None), 1, "null x"), (dict(mean=None), 1, "null mean"), (dict(rstd=None), 1, "null mean or rstd"),
+    (dict(lddy=63), 1, "leading dimension of dy"), (dict(ldr=63), 1, "leading dimension of residual"), (dict(lddx=1 << 22), 1, "leading dimension of dx"),
+    (dict(dweight=(1 << 28) + 2), 1, "aligned"), (dict(precision=0, dx=(1 << 24) + 2), 1, "aligned"),
+    (dict(workspace=None), 1, "null workspace"), (dict(workspace=(1 << 30) + 128), 1, "256-byte"),
+    (dict(y=1 << 24), 0, "overlap"), (dict(y=(1 << 24) + 160 * 128 - 2), 0, "overlap"), (dict(mean=1 << 24), 0, "overlap"), (dict(rstd=(18 << 24) + 4), 0, "overlap"),
+    (dict(dx=3 << 24), 1, "dy and dx"), (dict(dx=1 << 24), 1, "x and dx"), (dict(dx=(4 << 24) + 2, lddx=65), 1, "residual and dx"),
+    (dict(dweight=21 << 24), 1, "dweight and dbias"), (dict(dbias=16 << 24), 1, "weight and dbias"), (dict(workspace=3 << 24), 1, "dy and workspace"),
+])
+def test_refusals(kw, backward, word):
+    lib = B.load_library()
+    fn = lib.optorch_layer_norm_backward if backward else lib.optorch_layer_norm_forward
+    assert fn(C.byref(_norm(**kw))) == E_INVALID
+    assert word in lib.optorch_matrix_last_error().decode()
+
+
+def test_null_arguments_and_a_short_workspace():
+    lib = B.load_library()
+    assert lib.optorch_layer_norm_forward(None) == E_INVALID and lib.optorch_layer_norm_backward(None) == E_INVALID
+    assert lib.optorch_layer_norm_workspace(None) == E_INVALID
+    n = lib.optorch_layer_norm_workspace(C.byref(_norm()))
+    assert n > 0 and n % 256 == 0
+    assert lib.optorch_layer_norm_backward(C.byref(_norm(workspace_bytes=n - 1))) == E_BUDGET
+
+
+def test_workspace_is_that_of_the_sums_asked_for():
+    lib = B.load_library()
+    size = lambda **kw: lib.optorch_layer_norm_workspace(C.byref(_norm(**kw)))  # noqa: E731
+    both = size()
+    assert size(dweight=None) == size(dbias=None) and both >= 2 * size(dbias=None) - 256
+    assert size(dweight=None, dbias=None) == 0 and size(rows=0) == 0 and size(rows=1) == 0
+    assert size(rows=1 << 20, cols=4096, ldx=4096, lddy=4096, lddx=4096, ldr=4096) <= 1 << 26, "it does not grow with the rows"
+    assert size(x=None, mean=None, rstd=None, dx=None, dweight=None) > 0, "dbias needs dy alone"
