@@ -1,6 +1,6 @@
 // The two products of the gradient of a loss over many classes, for a piece of the classes:
 //   dx += ds w (summed in fp32 over the pieces, then times each row's factor),   dw = ds^T x' times one factor,
-// with x' the rows of x times their factors over the largest.  ds is read along the reduction for dx and across it for dw (mat_core.h).
+// with x' the rows of x times their powers of two.  ds is read along the reduction for dx and across it for dw (mat_core.h).
 #include "mat_layout.h"
 #include "parts.h"
 

@@ -6,8 +6,9 @@ much as the logits, weighted by p, by the additions of its sum (half a tile's co
 threads at least), by 3 u times the mean distance of the logits from their maximum (the exponent's products), and by its own rounding.
 
 ds = dloss (a p - target): p is off, relatively, by its logit's error and 3 u |s - lse| + 8 u.  In 16 bits it is rounded, by eps / 2
-of itself, and in fp16, where it is held 2^14 times larger, by 2^-39 of the row's factor at least; x' is off by eps / 2 of itself
-and in fp16 by 2^-25 of the largest factor.  dx and dw are sums of such products and are rounded once."""
+of itself, and in fp16, where it is held over a power of two of up to twice the row's factor and 2^14 times larger, by 2^-38 of the
+factor at least; x times that power over the largest is exact but for 2^-25 in fp16.  dx and dw are sums of such products and are
+rounded once."""
 import ctypes as C
 import math
 
@@ -102,13 +103,13 @@ class Reference:
         near = torch.where(p > 0, 3 * U * (self.s - k).abs(), torch.zeros_like(p))
         ds = g * (a * p - self.target)
         exact = g.abs() * (a.abs() * p * (self.ds_logit + near + 8 * U) + 4 * U * (self.target + a.abs() * p))
-        held = exact + e * ds.abs() + (g.abs() * f * 2.0 ** -39 if name == "fp16" else 0)
+        held = exact + e * ds.abs() + (g.abs() * f * 2.0 ** -38 if name == "fp16" else 0)
         largest = float((g.abs() * f).max())
         x, w = self.x, self.w
         out_floor = 2.0 ** -25 if name == "fp16" else 2.0 ** -134
         dx, dw = _mm(ds, w), _mm(ds.T, x)
         dx_fp32 = _mm(held, w.abs()) + (_adds(w.shape[0], name) + 40) * U23 * _mm(ds.abs(), w.abs())
-        xe = e * x.abs() + (2.0 ** -25 * (largest / g.abs().clamp_min(1e-300)).clamp_max(1e30) if name == "fp16" else 0)
+        xe = (2.0 ** -25 * (largest / g.abs().clamp_min(1e-300)).clamp_max(1e30) if name == "fp16" else torch.zeros_like(g)) + torch.zeros_like(x)
         dw_fp32 = _mm(held.T, x.abs() + xe) + _mm(ds.abs().T, xe) + (_adds(x.shape[0], name) + 40) * U23 * _mm(ds.abs().T, x.abs())
         eo = torch.finfo(dt).eps / 2
         db_tol = exact.sum(0) + (80 + x.shape[0] / 16) * U * ds.abs().sum(0)
