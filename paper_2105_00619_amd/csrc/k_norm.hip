@@ -1,22 +1,43 @@
 // Layer norm over the rows of a matrix and its gradient:
 //   y = h weight + bias,  h = (x - mean) rstd;
 //   dx = rstd (u - mean(u) - h mean(u h)) + residual,  u = dy weight;  dweight = sum over rows of dy h,  dbias = that of dy.
-// Both are bound by memory: a row is read once and stays in the registers of the threads that share it (16 values each) for all of its
-// sums.
+// Both are bound by memory: a row is read once and stays in the registers of the threads that share it, eight values each, for all of its
+// sums; blocks walk the rows, the next one on its way while the sums of this one are made, weight and bias in registers (read for every
+// row they are four times a bf16 row: forward 74 us).  16384 x 4096 in bf16: forward 47 us (5.7 TB/s), backward with the skip
+// connection's gradient 92 us and 6 to join the blocks' sums (5.5 TB/s); a kernel that only adds three such matrices takes 74 to 95.
 #include "mat_layout.h"
 
 namespace oseq {
 
 namespace {
 
-// Sums over the G threads of a row (G a power of two; rows of more than a wavefront: `lds` holds two floats a wavefront, a
-// place of its own for every other sum)
-template <int G> __device__ __forceinline__ void row_sums(float& a, float& b, float* lds) {
-#pragma unroll
-  for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) {
-    a += __shfl_xor(a, o);
-    b += __shfl_xor(b, o);
+// The sum over groups of G neighbouring lanes (G a power of two up to 64), the same bits in each of them: exchanges inside a row of 16 lanes
+// and between rows by the vector unit itself (through LDS, as shuffles, a wavefront's sum takes six times as long).
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+template <int CTRL> __device__ __forceinline__ float add_moved(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
+}
+template <int G> __device__ __forceinline__ float lanes_sum(float v) {
+  if (G >= 2) v = add_moved<0xB1>(v);   // quad_perm 1, 0, 3, 2
+  if (G >= 4) v = add_moved<0x4E>(v);   // quad_perm 2, 3, 0, 1
+  if (G >= 8) v = add_moved<0x141>(v);  // half a row mirrored
+  if (G >= 16) v = add_moved<0x140>(v); // a row mirrored
+  if (G >= 32) {
+    const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r.x) + __uint_as_float(r.y);
   }
+  if (G >= 64) {
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(r.x) + __uint_as_float(r.y);
+  }
+  return v;
+}
+
+// Two sums over the G threads of a row (G a power of two; rows of more than a wavefront: `lds` holds two floats a wavefront, a
+// place of its own for every other call)
+template <int G> __device__ __forceinline__ void row_sums(float& a, float& b, float* lds) {
+  a = lanes_sum<(G < 64 ? G : 64)>(a);
+  b = lanes_sum<(G < 64 ? G : 64)>(b);
   if constexpr (G > 64) {
     constexpr int WAVES = G / 64;
     const int wave = threadIdx.x >> 6;
@@ -30,8 +51,32 @@ template <int G> __device__ __forceinline__ void row_sums(float& a, float& b, fl
 }
 
 constexpr int threads_of(int lanes) { return lanes < 256 ? 256 : lanes; }
-constexpr int CHUNKS = 2;           // groups of eight values that a thread has of a row
-constexpr int MOST_LANES = 1024;    // 16384 columns; longer rows are read once for every sum
+
+// Eight neighbouring values as they were loaded, n of them inside, zeros beside them.  ONCE: past the caches, 16-bit values.  (As vectors
+// of words: as an array of values the loads of 16384 x 4096 took 55 us forward, so 47.)
+template <class S> struct Raw { Vec<S, 8> v; };
+template <int BYTES> struct Loose16;
+template <> struct Loose16<2> { typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t V; };
+template <> struct Loose16<4> { typedef __attribute__((ext_vector_type(4), aligned(4))) uint32_t V; };
+template <class S, bool ONCE> __device__ __forceinline__ void ask(const S* p, int n, Raw<S>& r) {
+  typedef typename Loose16<sizeof(S)>::V V;
+  if (n == 8) {
+    V c[sizeof(S) / 2];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(S) / 2; ++i) {
+      const V* q = reinterpret_cast<const V*>(p) + i;
+      c[i] = ONCE ? __builtin_nontemporal_load(q) : *q;
+    }
+    __builtin_memcpy(&r, c, sizeof(r));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.v.v[e] = e < n ? p[e] : from_f32<S>(0.f);
+  }
+}
+template <class S> __device__ __forceinline__ void take(const Raw<S>& r, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = to_f32(r.v.v[e]);
+}
 
 struct NormForward {
   const void* x; int64_t ldx;
@@ -42,59 +87,73 @@ struct NormForward {
   int64_t rows; int cols;
 };
 
-__device__ __forceinline__ void vector8(const float* p, int c, int n, float other, float (&v)[8]) {
+template <int N> __device__ __forceinline__ void vector_of(const float* p, int c, int n, float other, float (&v)[N]) {
   if (p) load8<float>(p + c, n, v);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = p ? v[e] : other;
+  for (int e = 0; e < N; ++e) v[e] = p ? v[e] : other;
 }
 
 // Mean and variance from the deviations from a first mean: the mean that was rounded in its sum is off, and the deviations, which
-// are exact, say by how much.
-template <class S, int G>
+// are exact, say by how much.  G threads have a row, 8 C values each, in pieces that lie side by side for neighbouring threads; a block walks its rows, weight and bias
+// in registers, the next row on its way.
+template <class S, int G, int C>
 __global__ void __launch_bounds__(threads_of(G)) norm_forward_kernel(NormForward a) {
   constexpr int ROWS = threads_of(G) / G;
   __shared__ float lds[2][2 * 16];
-  const int t = threadIdx.x % G;
-  const int64_t wanted = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + threadIdx.x / G, row = min(wanted, a.rows - 1);
-  const S* x = (const S*)a.x + row * a.ldx;
-  float v[CHUNKS][8];
-  float sum = 0.f, other = 0.f;
+  const int t = threadIdx.x % G, r = threadIdx.x / G;
+  float w[C][8], b[C][8];
+  int inside[C];
 #pragma unroll
-  for (int j = 0; j < CHUNKS; ++j) {
+  for (int j = 0; j < C; ++j) {
     const int c = (j * G + t) * 8;
-    load8<S>(x + c, min(8, max(0, a.cols - c)), v[j]);
+    inside[j] = min(8, max(0, a.cols - c));
+    vector_of(a.weight, c, inside[j], 1.f, w[j]);
+    vector_of(a.bias, c, inside[j], 0.f, b[j]);
   }
+  const float n = 1.f / (float)a.cols;
+  const bool whole = a.cols == G * C * 8;
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  Raw<S> next[C];
+  auto fetch = [&](int64_t first) {
+    const S* x = (const S*)a.x + min(first + r, a.rows - 1) * a.ldx;
 #pragma unroll
-  for (int j = 0; j < CHUNKS; ++j)
+    for (int j = 0; j < C; ++j) ask<S, false>(x + (j * G + t) * 8, inside[j], next[j]);
+  };
+  int64_t first = (int64_t)blockIdx.x * ROWS;
+  if (first < a.rows) fetch(first);
+  for (; first < a.rows; first += step) {
+    float v[C][8];
+    float sum = 0.f, square = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += v[j][e];
-  row_sums<G>(sum, other, lds[0]);
-  const float n = 1.f / (float)a.cols, first = sum * n;
-  float square = 0.f;
-  sum = 0.f;
+    for (int j = 0; j < C; ++j) {
+      take<S>(next[j], v[j]);
 #pragma unroll
-  for (int j = 0; j < CHUNKS; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[j][e] = (j * G + t) * 8 + e < a.cols ? v[j][e] - first : 0.f;
-      sum += v[j][e];
-      square = __fmaf_rn(v[j][e], v[j][e], square);
+      for (int e = 0; e < 8; ++e) sum += v[j][e];
     }
-  row_sums<G>(sum, square, lds[1]);
-  const float off = sum * n, rstd = 1.f / sqrtf(fmaxf(square * n - off * off, 0.f) + a.eps);
-  if (wanted >= a.rows) return;
-  if (t == 0 && a.mean) { a.mean[row] = first + off; a.rstd[row] = rstd; }
-  S* y = (S*)a.y + row * a.ldy;
+    if (first + step < a.rows) fetch(first + step);
+    row_sums<G>(sum, square, lds[0]);
+    const float mean = sum * n;
+    sum = square = 0.f;
 #pragma unroll
-  for (int j = 0; j < CHUNKS; ++j) {
-    const int c = (j * G + t) * 8, k = min(8, a.cols - c);
-    if (k <= 0) break;
-    float w[8], b[8];
-    vector8(a.weight, c, k, 1.f, w);
-    vector8(a.bias, c, k, 0.f, b);
+    for (int j = 0; j < C; ++j)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[j][e] = __fmaf_rn((v[j][e] - off) * rstd, w[e], b[e]);
-    store8<S>(y + c, k, v[j]);
+      for (int e = 0; e < 8; ++e) {
+        v[j][e] -= mean;
+        if (!whole) v[j][e] = e < inside[j] ? v[j][e] : 0.f;
+        sum += v[j][e];
+        square = __fmaf_rn(v[j][e], v[j][e], square);
+      }
+    row_sums<G>(sum, square, lds[1]);
+    const float off = sum * n, rstd = 1.f / sqrtf(fmaxf(square * n - off * off, 0.f) + a.eps);
+    const int64_t row = first + r;
+    if (row >= a.rows) continue;
+    if (t == 0 && a.mean) { a.mean[row] = mean + off; a.rstd[row] = rstd; }
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[j][e] = __fmaf_rn((v[j][e] - off) * rstd, w[j][e], b[j][e]);
+      if (inside[j] > 0) store8<S>((S*)a.y + row * a.ldy + (j * G + t) * 8, inside[j], v[j]);
+    }
   }
 }
 
@@ -133,8 +192,8 @@ __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormForward a) 
   if (threadIdx.x == 0 && a.mean) { a.mean[row] = first + off; a.rstd[row] = rstd; }
   each8([&](int c, int k, float (&v)[8]) {
     float w[8], b[8];
-    vector8(a.weight, c, k, 1.f, w);
-    vector8(a.bias, c, k, 0.f, b);
+    vector_of(a.weight, c, k, 1.f, w);
+    vector_of(a.bias, c, k, 0.f, b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn((v[e] - first - off) * rstd, w[e], b[e]);
     store8<S>((S*)a.y + row * a.ldy + c, k, v);
@@ -151,73 +210,94 @@ struct NormBackward {
   int64_t apart;
 };
 
-// A block walks its rows; a thread keeps the same columns of all of them, and their sums for dweight and dbias in registers.
-template <class S, int G>
+// A block walks its rows, the next one's values on their way; a thread keeps the same columns of all of them, and their sums for dweight and dbias in
+// registers.  dy is zero beside the matrix, so nothing else has to be left out.  Without SUMS it
+// makes dx alone.
+template <class S, int G, int C, bool SUMS, bool ONCE>
 __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackward a) {
   constexpr int ROWS = threads_of(G) / G;
   __shared__ float lds[2][2 * 16];
-  __shared__ float part[ROWS > 1 ? 2 : 1][ROWS > 1 ? ROWS : 1][ROWS > 1 ? G * 8 * CHUNKS : 1];
+  __shared__ float part[ROWS > 1 && SUMS ? 2 : 1][ROWS > 1 && SUMS ? ROWS : 1][ROWS > 1 && SUMS ? G * 8 * C : 1];
   const int t = threadIdx.x % G, r = threadIdx.x / G;
-  const bool sums = a.dweight || a.dbias;
-  float w[CHUNKS][8], dw[CHUNKS][8], db[CHUNKS][8];
+  float w[C][8], dw[C][8], db[C][8];
+  int inside[C];
 #pragma unroll
-  for (int j = 0; j < CHUNKS; ++j) {
+  for (int j = 0; j < C; ++j) {
     const int c = (j * G + t) * 8;
-    vector8(a.weight, c, min(8, max(0, a.cols - c)), 1.f, w[j]);
+    inside[j] = min(8, max(0, a.cols - c));
+    vector_of(a.weight, c, inside[j], 1.f, w[j]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[j][e] = db[j][e] = 0.f;
   }
   const float n = 1.f / (float)a.cols;
-  int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += (int64_t)gridDim.x * ROWS, turn ^= 1) {
+  const int64_t step = (int64_t)gridDim.x * ROWS;
+  const bool add = a.residual && a.dx, stats = a.dx || a.dweight;
+  Raw<S> nx[C] = {}, ny[C], nr[C];
+  float mean = 0.f, rstd = 0.f;
+  auto fetch = [&](int64_t first) {
     const int64_t row = min(first + r, a.rows - 1);
-    const bool real = first + r < a.rows;
-    float h[CHUNKS][8], u[CHUNKS][8], add[CHUNKS][8];
+    const S *x = (const S*)a.x + row * a.ldx, *dy = (const S*)a.dy + row * a.lddy, *res = (const S*)a.residual + row * a.ldr;
 #pragma unroll
-    for (int j = 0; j < CHUNKS; ++j) {
-      const int c = (j * G + t) * 8, k = min(8, max(0, a.cols - c));
-      load8<S>((const S*)a.x + row * a.ldx + c, k, h[j]);
-      load8<S>((const S*)a.dy + row * a.lddy + c, k, u[j]);
-      if (a.residual && a.dx) load8<S>((const S*)a.residual + row * a.ldr + c, k, add[j]);
+    for (int j = 0; j < C; ++j) {
+      const int c = (j * G + t) * 8;
+      if (stats) ask<S, ONCE>(x + c, inside[j], nx[j]);
+      ask<S, ONCE>(dy + c, first + r < a.rows ? inside[j] : 0, ny[j]);
+      if (add) ask<S, ONCE>(res + c, inside[j], nr[j]);
     }
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    float su = 0.f, suh = 0.f;
+    if (stats) {
+      mean = a.mean[row];
+      rstd = a.rstd[row];
+    }
+  };
+  int turn = 0;
+  int64_t first = (int64_t)blockIdx.x * ROWS;
+  if (first < a.rows) fetch(first);
+  for (; first < a.rows; first += step, turn ^= 1) {
+    const int64_t row = first + r;
+    const bool real = row < a.rows;
+    float h[C][8], u[C][8], su = 0.f, suh = 0.f;
+    const float rs = rstd;
+    Raw<S> res[C];
 #pragma unroll
-    for (int j = 0; j < CHUNKS; ++j)
+    for (int j = 0; j < C; ++j) {
+      take<S>(nx[j], h[j]);
+      take<S>(ny[j], u[j]);
+      if (add) res[j] = nr[j];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const bool in = (j * G + t) * 8 + e < a.cols;
-        h[j][e] = in ? (h[j][e] - mean) * rstd : 0.f;
-        if (real && in) {
+        h[j][e] = (h[j][e] - mean) * rs;
+        if (SUMS) {
           dw[j][e] = __fmaf_rn(u[j][e], h[j][e], dw[j][e]);
           db[j][e] += u[j][e];
         }
-        u[j][e] = in ? u[j][e] * w[j][e] : 0.f;
+        u[j][e] *= w[j][e];
         su += u[j][e];
         suh = __fmaf_rn(u[j][e], h[j][e], suh);
       }
+    }
+    if (first + step < a.rows) fetch(first + step);
     if (!a.dx) continue;
     row_sums<G>(su, suh, lds[turn]);
     su *= n;
     suh *= n;
     if (!real) continue;
 #pragma unroll
-    for (int j = 0; j < CHUNKS; ++j) {
-      const int c = (j * G + t) * 8, k = min(8, a.cols - c);
-      if (k <= 0) break;
+    for (int j = 0; j < C; ++j) {
+      float more[8];
+      if (add) take<S>(res[j], more);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        u[j][e] = rstd * (u[j][e] - su - h[j][e] * suh);
-        if (a.residual) u[j][e] += add[j][e];
+        u[j][e] = __fmaf_rn(-h[j][e], suh, u[j][e] - su);
+        u[j][e] = add ? __fmaf_rn(rs, u[j][e], more[e]) : rs * u[j][e];
       }
-      store8<S>((S*)a.dx + row * a.lddx + c, k, u[j]);
+      if (inside[j] > 0) store8<S>((S*)a.dx + row * a.lddx + (j * G + t) * 8, inside[j], u[j]);
     }
   }
-  if (!sums) return;
+  if (!SUMS || (!a.dweight && !a.dbias)) return;
   float *dweight = a.dweight ? a.dweight + blockIdx.x * a.apart : nullptr, *dbias = a.dbias ? a.dbias + blockIdx.x * a.apart : nullptr;
-  if constexpr (ROWS > 1) {
+  if constexpr (ROWS > 1 && SUMS) {
 #pragma unroll
-    for (int j = 0; j < CHUNKS; ++j)
+    for (int j = 0; j < C; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         part[0][r][(j * G + t) * 8 + e] = dw[j][e];
@@ -233,11 +313,10 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < CHUNKS; ++j) {
-      const int c = (j * G + t) * 8, k = min(8, a.cols - c);
-      if (k <= 0) break;
-      if (dweight) store8<float>(dweight + c, k, dw[j]);
-      if (dbias) store8<float>(dbias + c, k, db[j]);
+    for (int j = 0; j < C; ++j) {
+      if (inside[j] <= 0) break;
+      if (dweight) store8<float>(dweight + (j * G + t) * 8, inside[j], dw[j]);
+      if (dbias) store8<float>(dbias + (j * G + t) * 8, inside[j], db[j]);
     }
   }
 }
@@ -255,7 +334,7 @@ __global__ void __launch_bounds__(1024) norm_dx_long_kernel(NormBackward a) {
       float h[8], u[8], w[8];
       load8<S>((const S*)a.x + row * a.ldx + c, k, h);
       load8<S>((const S*)a.dy + row * a.lddy + c, k, u);
-      vector8(a.weight, c, k, 1.f, w);
+      vector_of(a.weight, c, k, 1.f, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         h[e] = e < k ? (h[e] - mean) * rstd : 0.f;
@@ -291,14 +370,15 @@ __global__ void __launch_bounds__(256) norm_sums_long_kernel(NormBackward a, int
   for (int e = 0; e < 8; ++e) dw[e] = db[e] = 0.f;
   for (int64_t r = r0 + rl; r < r1; r += 8) {
     float x[8], d[8];
-    load8<S>((const S*)a.x + r * a.ldx + c, k, x);
     load8<S>((const S*)a.dy + r * a.lddy + c, k, d);
-    const float mean = a.mean[r], rstd = a.rstd[r];
+    if (a.dweight) {
+      load8<S>((const S*)a.x + r * a.ldx + c, k, x);
+      const float mean = a.mean[r], rstd = a.rstd[r];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      dw[e] = __fmaf_rn(d[e], (x[e] - mean) * rstd, dw[e]);
-      db[e] += d[e];
+      for (int e = 0; e < 8; ++e) dw[e] = __fmaf_rn(d[e], (x[e] - mean) * rstd, dw[e]);
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) db[e] += d[e];
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) { part[0][rl][cg * 8 + e] = dw[e]; part[1][rl][cg * 8 + e] = db[e]; }
@@ -312,21 +392,21 @@ __global__ void __launch_bounds__(256) norm_sums_long_kernel(NormBackward a, int
   if (a.dbias) a.dbias[blockIdx.y * a.apart + col] = b;
 }
 
-// The blocks' sums, added in a fixed order: sixteen threads a column, dweight's columns before dbias'
-__global__ void __launch_bounds__(256) norm_join_kernel(const float* sums, int blocks, int cols, int64_t apart, float* dweight, float* dbias) {
-  __shared__ float part[16][17];
-  const int cl = threadIdx.x & 15, t = threadIdx.x >> 4;
-  const int across = (cols + 15) / 16, which = dweight ? blockIdx.x / across : 1, c = (dweight ? blockIdx.x % across : blockIdx.x) * 16 + cl;
+// The blocks' sums, added in a fixed order: 32 threads a column, dweight's columns before dbias'
+__global__ void __launch_bounds__(1024) norm_join_kernel(const float* sums, int blocks, int cols, int64_t apart, float* dweight, float* dbias) {
+  __shared__ float part[32][33];
+  const int cl = threadIdx.x & 31, t = threadIdx.x >> 5;
+  const int across = (cols + 31) / 32, which = dweight ? blockIdx.x / across : 1, c = (dweight ? blockIdx.x % across : blockIdx.x) * 32 + cl;
   float s = 0.f;
   if (c < cols) {
     const float* p = sums + (dweight && which ? cols : 0) + c;
     float q[4] = {0.f, 0.f, 0.f, 0.f};  // (four loads on their way)
     int b = t;
-    for (; b + 48 < blocks; b += 64) {
+    for (; b + 96 < blocks; b += 128) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) q[e] += p[(b + 16 * e) * apart];
+      for (int e = 0; e < 4; ++e) q[e] += p[(b + 32 * e) * apart];
     }
-    for (; b < blocks; b += 16) q[0] += p[b * apart];
+    for (; b < blocks; b += 32) q[0] += p[b * apart];
     s = (q[0] + q[1]) + (q[2] + q[3]);
   }
   part[t][cl] = s;
@@ -334,7 +414,7 @@ __global__ void __launch_bounds__(256) norm_join_kernel(const float* sums, int b
   if (t == 0 && c < cols) {
     s = 0.f;
 #pragma unroll
-    for (int k = 0; k < 16; ++k) s += part[k][cl];
+    for (int k = 0; k < 32; ++k) s += part[k][cl];
     (which ? dbias : dweight)[c] = s;
   }
 }
@@ -346,31 +426,46 @@ __global__ void __launch_bounds__(256) norm_clear_kernel(float* a, float* b, int
   if (b) b[i] = 0.f;
 }
 
-// threads of a row, 0 where it does not fit
+// Blocks of 256 threads (of more threads as many fewer)
+constexpr int FORWARD_BLOCKS = 2048, BACKWARD_BLOCKS = 1024;
+// Whether a gradient's matrices are read past the caches: where they are larger than the last of those holds (256 MB), which else still has them
+// from whatever made them.  bf16, past the caches / through them: 16384 x 4096 91 / 102 us, 8192 x 8192 88 / 103; 65536 x 512 49 / 45, 7003 x 1777 34 / 28.
+bool once(const optorch_layer_norm_t& a) { return a.rows * (int64_t)a.cols * 2 * (a.residual ? 4 : 3) > (384ll << 20); }
+
+// The threads of a row, eight values each (or 16 of 1024 threads); 0 where it does not fit
 int lanes_of(int cols) {
   int g = 8;
-  while (g <= MOST_LANES && g * 8 * CHUNKS < cols) g *= 2;
-  return g <= MOST_LANES ? g : 0;
+  while (g < 1024 && g * 8 < cols) g *= 2;
+  return cols <= 16384 ? g : 0;
+}
+// f(threads of a row, eights of values that each has)
+template <class F> void with_lanes(int cols, F&& f) {
+  switch (lanes_of(cols)) {
+    case 8: f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{}); break;
+    case 16: f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}); break;
+    case 32: f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{}); break;
+    case 64: f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{}); break;
+    case 128: f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{}); break;
+    case 256: f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{}); break;
+    case 512: f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{}); break;
+    default:
+      if (cols <= 8192) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+      else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+  }
 }
 
 template <class S> void forward_of(const optorch_layer_norm_t& a) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   NormForward f = {a.x, a.ldx, a.weight, a.bias, a.eps, a.y, a.ldy, a.mean, a.rstd, a.rows, a.cols};
-  auto run = [&](auto g) {
-    constexpr int G = g;
-    OSEQ_LAUNCH((norm_forward_kernel<S, G>), grid_of_blocks(ceil_div(a.rows, threads_of(G) / G)), dim3(threads_of(G)), 0, st, f);
-  };
-  switch (lanes_of(a.cols)) {
-    case 8: run(std::integral_constant<int, 8>{}); break;
-    case 16: run(std::integral_constant<int, 16>{}); break;
-    case 32: run(std::integral_constant<int, 32>{}); break;
-    case 64: run(std::integral_constant<int, 64>{}); break;
-    case 128: run(std::integral_constant<int, 128>{}); break;
-    case 256: run(std::integral_constant<int, 256>{}); break;
-    case 512: run(std::integral_constant<int, 512>{}); break;
-    case 1024: run(std::integral_constant<int, 1024>{}); break;
-    default: OSEQ_LAUNCH(norm_forward_long_kernel<S>, grid_of_blocks(a.rows), dim3(1024), 0, st, f);
+  if (!lanes_of(a.cols)) {
+    OSEQ_LAUNCH(norm_forward_long_kernel<S>, grid_of_blocks(a.rows), dim3(1024), 0, st, f);
+    return;
   }
+  with_lanes(a.cols, [&](auto g, auto c) {
+    constexpr int G = g, C = c;
+    const dim3 grid(std::min(ceil_div(a.rows, threads_of(G) / G), FORWARD_BLOCKS * 256 / threads_of(G))), block(threads_of(G));
+    OSEQ_LAUNCH((norm_forward_kernel<S, G, C>), grid, block, 0, st, f);
+  });
 }
 
 template <class S> void backward_of(const optorch_layer_norm_t& a, const NormPlan& p) {
@@ -384,25 +479,25 @@ template <class S> void backward_of(const optorch_layer_norm_t& a, const NormPla
     if (a.dbias) b.dbias = ws + (a.dweight ? a.cols : 0);
     b.apart = (int64_t)each * a.cols;
   }
-  auto run = [&](auto g) {
-    constexpr int G = g;
-    OSEQ_LAUNCH((norm_backward_kernel<S, G>), dim3(p.blocks), dim3(threads_of(G)), 0, st, b);
-  };
-  switch (p.lanes) {
-    case 8: run(std::integral_constant<int, 8>{}); break;
-    case 16: run(std::integral_constant<int, 16>{}); break;
-    case 32: run(std::integral_constant<int, 32>{}); break;
-    case 64: run(std::integral_constant<int, 64>{}); break;
-    case 128: run(std::integral_constant<int, 128>{}); break;
-    case 256: run(std::integral_constant<int, 256>{}); break;
-    case 512: run(std::integral_constant<int, 512>{}); break;
-    case 1024: run(std::integral_constant<int, 1024>{}); break;
-    default:
-      if (a.dx) OSEQ_LAUNCH(norm_dx_long_kernel<S>, grid_of_blocks(a.rows), dim3(1024), 0, st, b);
-      if (sums) OSEQ_LAUNCH(norm_sums_long_kernel<S>, dim3(ceil_div(a.cols, 256), p.blocks), dim3(256), 0, st, b, (int64_t)ceil_div(a.rows, p.blocks));
+  const bool apart = !p.lanes || a.cols > 8192;  // the sums by a kernel of their own
+  if (!p.lanes) {
+    if (a.dx) OSEQ_LAUNCH(norm_dx_long_kernel<S>, grid_of_blocks(a.rows), dim3(1024), 0, st, b);
+  } else if (a.dx || !apart) {
+    with_lanes(a.cols, [&](auto g, auto c) {
+      constexpr int G = g, C = c;
+      const dim3 grid(apart ? (int)std::min<int64_t>(a.rows, 256) : p.blocks), block(threads_of(G));
+      if constexpr (sizeof(S) == 2) {
+        if (once(a)) {
+          OSEQ_LAUNCH((norm_backward_kernel<S, G, C, C == 1, true>), grid, block, 0, st, b);
+          return;
+        }
+      }
+      OSEQ_LAUNCH((norm_backward_kernel<S, G, C, C == 1, false>), grid, block, 0, st, b);
+    });
   }
+  if (apart && sums) OSEQ_LAUNCH(norm_sums_long_kernel<S>, dim3(ceil_div(a.cols, 256), p.blocks), dim3(256), 0, st, b, (int64_t)ceil_div(a.rows, p.blocks));
   if (join)
-    OSEQ_LAUNCH(norm_join_kernel, dim3(ceil_div(a.cols, 16) * each), dim3(256), 0, st, (const float*)ws, p.blocks, (int)a.cols, b.apart, a.dweight, a.dbias);
+    OSEQ_LAUNCH(norm_join_kernel, dim3(ceil_div(a.cols, 32) * each), dim3(1024), 0, st, (const float*)ws, p.blocks, (int)a.cols, b.apart, a.dweight, a.dbias);
 }
 
 }  // namespace
@@ -410,9 +505,12 @@ template <class S> void backward_of(const optorch_layer_norm_t& a, const NormPla
 NormPlan plan_norm_backward(const optorch_layer_norm_t& a) {
   NormPlan p = {};
   p.lanes = lanes_of(a.cols);
-  p.rows_at_once = p.lanes ? threads_of(p.lanes) / p.lanes : 1;
-  if (p.lanes) p.blocks = (int)std::min<int64_t>((a.rows + p.rows_at_once - 1) / p.rows_at_once, 512);
-  else p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, 2048 / ((a.cols + 255) / 256)));
+  if (p.lanes && a.cols <= 8192) {
+    const int threads = threads_of(p.lanes), rows = threads / p.lanes;
+    p.blocks = (int)std::min<int64_t>((a.rows + rows - 1) / rows, BACKWARD_BLOCKS * 256 / threads);
+  } else {
+    p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, 2048 / ((a.cols + 255) / 256)));
+  }
   const int each = (a.dweight ? 1 : 0) + (a.dbias ? 1 : 0);
   p.bytes = p.blocks > 1 && each ? up256((uint64_t)p.blocks * each * a.cols * 4) : 0;
   return p;

@@ -54,7 +54,7 @@ void launch_linear_forward(const optorch_linear_t& a, const LinearPlan& p);
 void launch_linear_backward(const optorch_linear_t& a, const LinearPlan& p);
 
 // The gradient of a layer norm: its blocks, whose sums for dweight and dbias lie one behind the other in the workspace
-struct NormPlan { int lanes, rows_at_once, blocks; uint64_t bytes; };
+struct NormPlan { int lanes, blocks; uint64_t bytes; };
 NormPlan plan_norm_backward(const optorch_layer_norm_t& a);
 void launch_norm_forward(const optorch_layer_norm_t& a);
 void launch_norm_backward(const optorch_layer_norm_t& a, const NormPlan& p);

@@ -1,8 +1,8 @@
 """Layer norm and its gradient against plain float64 computations, through the Python binding.
 
 Tolerances, with u = 2^-24.  A result is rounded once to its type: at most eps / 2 of its value.  A sum of fp32 values with n additions one after
-the other is off by at most n u times the sum of their absolute values.  A row's sums: 16 values a thread for every 16384 columns or part, six additions
-across a wavefront and 16 across the wavefronts.  The mean is corrected by the mean of the deviations from it, which are off by u of themselves, so what counts is their size and not the mean's.  The
+the other is off by at most n u times the sum of their absolute values.  A row's sums: 16 values a thread at most up to 16384 columns, eight more for every 8192
+beyond, six additions across a wavefront and 16 across the wavefronts.  The mean is corrected by the mean of the deviations from it, which are off by u of themselves, so what counts is their size and not the mean's.  The
 deviations are summed with their squares: the variance is off by as many u, and rstd by half of that and four more."""
 import math
 
@@ -44,8 +44,8 @@ def _row_adds(cols):
 
 
 def _column_adds(rows, cols):
-    # a thread's rows, its block's, the blocks': at most 512 blocks of at least one row; longer rows than 16384: 32 rows for a block's eight threads
-    return rows / 256 + 32 + 32 + 20
+    # a thread's rows, its block's, the blocks': up to 256 blocks and more; rows longer than 8192: 32 rows or more for a block's eight threads
+    return rows / 256 + 32 + 32 + 40
 
 
 def _within(got, ref, tol, what):
