@@ -11,28 +11,6 @@ namespace oseq {
 
 namespace {
 
-// The sum over groups of G neighbouring lanes (G a power of two up to 64), the same bits in each of them: exchanges inside a row of 16 lanes
-// and between rows by the vector unit itself (through LDS, as shuffles, a wavefront's sum takes six times as long).
-typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-template <int CTRL> __device__ __forceinline__ float add_moved(float v) {
-  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, false));
-}
-template <int G> __device__ __forceinline__ float lanes_sum(float v) {
-  if (G >= 2) v = add_moved<0xB1>(v);   // quad_perm 1, 0, 3, 2
-  if (G >= 4) v = add_moved<0x4E>(v);   // quad_perm 2, 3, 0, 1
-  if (G >= 8) v = add_moved<0x141>(v);  // half a row mirrored
-  if (G >= 16) v = add_moved<0x140>(v); // a row mirrored
-  if (G >= 32) {
-    const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r.x) + __uint_as_float(r.y);
-  }
-  if (G >= 64) {
-    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = __uint_as_float(r.x) + __uint_as_float(r.y);
-  }
-  return v;
-}
-
 // Two sums over the G threads of a row (G a power of two; rows of more than a wavefront: `lds` holds two floats a wavefront, a
 // place of its own for every other call)
 template <int G> __device__ __forceinline__ void row_sums(float& a, float& b, float* lds) {

@@ -5,7 +5,8 @@ n one addition for each four products and plane pair and a few more, and by u of
 much as the logits, weighted by p, by the additions of its sum (half a tile's columns in a row, the rest joined pairwise or by eight
 threads at least), by 3 u times the mean distance of the logits from their maximum (the exponent's products), and by its own rounding.
 
-ds = dloss (a p - target): p is off, relatively, by its logit's error and 3 u |s - lse| + 8 u.  In 16 bits it is rounded, by eps / 2
+ds = dloss (a p - target): p is off, relatively, by its logit's error and 3 u |s - lse| + 8 u; in 16 bits, where the exponent is one multiply-add
+of the logit and lse log2(e), by 2 u of either of them besides.  In 16 bits ds is rounded, by eps / 2
 of itself, and in fp16, where it is held over a power of two of up to twice the row's factor and 2^14 times larger, by 2^-38 of the
 factor at least; x times that power over the largest is exact but for 2^-25 in fp16.  dx and dw are sums of such products and are
 rounded once."""
@@ -100,7 +101,7 @@ class Reference:
         g = torch.where(self.used, dloss.double() / self.tau, torch.zeros_like(dloss.double()))[:, None]
         f = a.abs().clamp_min(1)
         # (a left out class' logit is -infinity, its p zero)
-        near = torch.where(p > 0, 3 * U * (self.s - k).abs(), torch.zeros_like(p))
+        near = torch.where(p > 0, U * (3 * (self.s - k).abs() + (0 if name == "fp32" else 2 * (self.s.abs() + k.abs()))), torch.zeros_like(p))
         ds = g * (a * p - self.target)
         exact = g.abs() * (a.abs() * p * (self.ds_logit + near + 8 * U) + 4 * U * (self.target + a.abs() * p))
         held = exact + e * ds.abs() + (g.abs() * f * 2.0 ** -38 if name == "fp16" else 0)
