@@ -335,82 +335,6 @@ struct SkinnyArgs {
   int k_wave;          // what a wavefront takes of the reduction, a multiple of 32
 };
 
-typedef __attribute__((ext_vector_type(4))) float v4f;
-__device__ __forceinline__ v4f mma16(Op<bf16_t>::V a, Op<bf16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-__device__ __forceinline__ v4f mma16(Op<f16_t>::V a, Op<f16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-
-// Eight values of a row as loaded, those that the eight places from k on have before `end`.  Not SINGLE (at least eight
-// values before `end`): at the end they are the row's last eight, those that an earlier group has taken as zeros: the same
-// ones in either operand. ODD: 16-bit values off the boundaries of 32 bits, from the 32-bit words that hold them (16-byte
-// loads at such addresses: 9705 x 2687 -> 37 in bf16 92 us, so 49).
-enum Loads { WIDE, ODD, SINGLE };
-template <class S> struct Raw8 { Chunk c[sizeof(S) / 2]; };
-template <class S, Loads L> __device__ __forceinline__ Raw8<S> raw8(const S* row, int k, int end) {
-  Raw8<S> r;
-  if (L != SINGLE) {
-    const S* p = row + min(k, end - 8);
-    if constexpr (L == ODD) {
-      const uint32_t half = (uint32_t)(uintptr_t)p & 2u;
-      const uint32_t* q = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p) - half);
-      struct Words { uint32_t v[4]; } const w = *reinterpret_cast<const Words*>(q);
-      const uint32_t last = q[half ? 4 : 3];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) r.c[0][i] = __builtin_amdgcn_alignbit(i < 3 ? w.v[i + 1] : last, w.v[i], half * 8);
-    } else {
-      r = __builtin_bit_cast(Raw8<S>, *reinterpret_cast<const Loose<S, 8>*>(p));
-    }
-    if (k + 8 > end) {
-      Vec<S, 8> v = __builtin_bit_cast(Vec<S, 8>, r);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v.v[e] = end - 8 + e < k ? from_f32<S>(0.f) : v.v[e];
-      r = __builtin_bit_cast(Raw8<S>, v);
-    }
-  } else {
-    Vec<S, 8> v;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v.v[e] = k + e < end ? row[k + e] : from_f32<S>(0.f);
-    r = __builtin_bit_cast(Raw8<S>, v);
-  }
-  return r;
-}
-// ... as MFMA operands, values as planes_of has them: with its cases only where there is a value beyond the largest bf16 (a
-// NaN makes all of its planes NaN here; what counts is the first)
-template <class S, class T> __device__ __forceinline__ void planes8(const Raw8<S>& r, typename Op<T>::V (&p)[sizeof(S) == 4 ? 3 : 1]) {
-  if constexpr (sizeof(S) == 2) {
-    p[0] = __builtin_bit_cast(typename Op<T>::V, r.c[0]);
-  } else {
-    const Vec<float, 8> v = __builtin_bit_cast(Vec<float, 8>, r);
-    float x[8], most = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = v.v[e];
-      most = fmaxf(most, fabsf(x[e]));
-    }
-    if (__builtin_expect(most > 3.3895314e38f, 0)) {
-      Vec<bf16_t, 8> q[3];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        bf16_t t[3];
-        planes_of(x[e], t);
-#pragma unroll
-        for (int k = 0; k < 3; ++k) q[k].v[e] = t[k];
-      }
-#pragma unroll
-      for (int k = 0; k < 3; ++k) p[k] = __builtin_bit_cast(typename Op<T>::V, q[k]);
-      return;
-    }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      const Vec<bf16_t, 8> q = round_vec<bf16_t, 8>(x);
-      p[k] = __builtin_bit_cast(typename Op<T>::V, q);
-      if (k < 2) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] -= (float)q.v[e];
-      }
-    }
-  }
-}
-
 // S: type in memory; T: of the planes; MB: blocks of 16 samples, of a block's 16 outputs.  NARROW: MB blocks of 16 outputs,
 // of a block's 16 samples.
 template <class S, class T, int MB, Loads L, bool NARROW, int ACT>

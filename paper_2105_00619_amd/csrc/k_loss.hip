@@ -274,6 +274,146 @@ logits_kernel(Logits a) {
   }
 }
 
+// ---- few rows ----------------------------------------------------------------------------------------------------------
+// Up to 64 rows whose weights would have to be laid out anew (fp32, or off the alignment of 16 bytes): straight from memory into 16 x 16
+// MFMAs, as the layers do it, 16 classes of all rows a block, its wavefronts (4 to 16) sharing the reduction.  The forward pass alone;
+// a row's sums are of runs of 16 classes.  16 x 2048 -> 65536 in fp32: 890 us by way of planes in memory, so 130.
+constexpr int SKINNY_ROWS = 64;
+template <class S, class T, int MB, Loads L, bool TOP>
+__global__ void __launch_bounds__(1024) few_logits_kernel(Logits a, int k_wave) {
+  constexpr int PL = sizeof(S) == 4 ? 3 : 1, U = PL == 3 ? (MB == 4 ? 1 : 2) : L == SINGLE ? 1 : MB == 4 || L == ODD ? 4 : 8;
+  typedef typename Op<T>::V V;
+  extern __shared__ float red[];  // [wavefront][MB][256]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16;
+  if (first >= a.N) return;
+  const int r16 = lane & 15, kc = (lane >> 4) * 8;
+  const int k0 = wave * k_wave, k1 = min(a.K, k0 + k_wave);
+  const S* one = (const S*)a.w + min(first + r16, (int64_t)a.N - 1) * a.ldw;
+  const S* many[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) many[m] = (const S*)a.x + min<int64_t>(m * 16 + r16, a.M - 1) * a.ldx;
+  v4f acc[MB], rest[PL == 3 ? MB : 1];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
+    if constexpr (PL == 3) rest[m] = acc[m];
+  }
+  for (int k = k0; k < k1; k += 32 * U) {
+    Raw8<S> ro[U], rm[U][MB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) ro[u] = raw8<S, L>(one, k + u * 32 + kc, k1);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int m = 0; m < MB; ++m) rm[u][m] = raw8<S, L>(many[m], k + u * 32 + kc, k1);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      V po[PL], pm[PL];
+      planes8<S, T>(ro[u], po);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) {
+        planes8<S, T>(rm[u][m], pm);
+#pragma unroll
+        for (int i = PL - 1; i >= 0; --i)
+#pragma unroll
+          for (int j = PL - 1 - i; j >= 0; --j) {
+            v4f& sum = i + j ? rest[PL == 3 ? m : 0] : acc[m];
+            sum = mma16(po[i], pm[j], sum);
+          }
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    if constexpr (PL == 3) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[m][e] += finite(acc[m][e]) ? rest[m][e] : 0.f;
+    }
+    *reinterpret_cast<v4f*>(red + ((wave * MB + m) * 64 + lane) * 4) = acc[m];
+  }
+  __syncthreads();
+  // a wavefront has 16 rows, four threads each with four of the classes
+  const int i = threadIdx.x, row = (i >> 6) * 16 + (i & 15), c = (i & 63) >> 4;
+  if (i >= MB * 64) return;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int q = 0; q < waves; ++q) {
+    const v4f t = *reinterpret_cast<const v4f*>(red + (q * MB * 64 + i) * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += t[e];
+  }
+  const bool real = row < a.M;
+  const int cls = a.first + (int)first + c * 4, inside = min(4, (int)(a.N - first) - c * 4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (a.bias && e < inside) v[e] += a.bias[cls + e];
+    v[e] *= a.per_temperature;
+  }
+  const int column = (a.first + (int)first) / 16;
+  if (real) {
+    if (TOP) {
+      const uint16_t* s = a.start + (int64_t)row * (a.columns + 1) + column;
+      for (int t = s[0]; t < s[1]; ++t) {
+        const int at = a.index[row * a.top + t] - cls;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (at == e) a.picked[row * a.top + t] = v[e];
+      }
+    } else {
+      const int at = a.labels[row] - cls;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (at == e && e < inside) a.picked[row] = v[e];
+    }
+  }
+  float all = 0.f, most = -__builtin_inff();
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e < inside) all += v[e];
+    v[e] = e < inside ? v[e] : -__builtin_inff();
+    most = fmaxf(most, v[e]);
+  }
+  most = fmaxf(most, __shfl_xor(most, 16));
+  most = fmaxf(most, __shfl_xor(most, 32));
+  const bool infinite = most == __builtin_inff();  // (as in a tile)
+  const float above = infinite || most == -__builtin_inff() ? 0.f : most;
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) sum += exp_above<true>(v[e], above, LOG2E);
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  all += __shfl_xor(all, 16);
+  all += __shfl_xor(all, 32);
+  if (real && c == 0) {
+    const int64_t at = (int64_t)column * a.M + row;
+    a.sums[at] = make_float2(infinite ? 3.4028235e38f : most, sum);
+    if (a.totals) a.totals[at] = all;
+  }
+}
+
+template <class S, class T, int MB, Loads L> void run_few_of(hipStream_t st, const Logits& l) {
+  // wavefronts of at least 256 values of k each, more of them where there are few blocks
+  const int blocks = ceil_div(l.N, 16), most = blocks >= 1024 ? 4 : blocks >= 256 ? 8 : 16;
+  int waves = 4;
+  while (waves < most && waves * 512 <= l.K) waves *= 2;
+  const int k_wave = (ceil_div(l.K, waves) + 31) & ~31;
+  if (l.labels) OSEQ_LAUNCH((few_logits_kernel<S, T, MB, L, false>), grid_of_blocks(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, l, k_wave);
+  else OSEQ_LAUNCH((few_logits_kernel<S, T, MB, L, true>), grid_of_blocks(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, l, k_wave);
+}
+template <class S, class T, Loads L> void run_few_by(hipStream_t st, const Logits& l) {
+  if (l.M <= 16) run_few_of<S, T, 1, L>(st, l);
+  else if (l.M <= 32) run_few_of<S, T, 2, L>(st, l);
+  else run_few_of<S, T, 4, L>(st, l);
+}
+template <class S, class T> void run_few(hipStream_t st, const Logits& l) {
+  const bool odd = sizeof(S) == 2 && (l.K % 2 || l.ldx % 2 || l.ldw % 2 || (uintptr_t)l.x % 4 || (uintptr_t)l.w % 4);
+  if (l.K < 8) return run_few_by<S, T, SINGLE>(st, l);
+  if constexpr (sizeof(S) == 2) {
+    if (odd) return run_few_by<S, T, ODD>(st, l);
+  }
+  run_few_by<S, T, WIDE>(st, l);
+}
+
 // ---- a teacher's entries -----------------------------------------------------------------------------------------------
 // Those of a row in order of their classes (then of their places), entries of one class added up in the first of them; softmax of their logits;
 // where the entries of each run of `width` classes begin.  Threads N a row, N a power of two of at least `top`.
@@ -465,7 +605,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
 // dw, where a power of two costs no bits.  (All of it in ds would leave fp16's range, all of it in x round every value a second time: dw
 // of 4096 x 2048 -> 65536 with rows that weigh differently was 2.9e-3 off in bf16, so 2.3e-3.)  Where dloss is the same for all rows, a
 // mean's, m is 1, and the value that counts most, -1 at a label that the network does not know, is exact.
-// One block: 8192 rows take 6 us.
+// One block, eight rows a thread on their way at once.
 struct Rows {
   const float *dloss, *lse, *flag;
   const int32_t* labels;
@@ -477,28 +617,34 @@ struct Rows {
 __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
   __shared__ float part[1024];
   const float nan = __builtin_nanf("");
-  // a row's p and target factors, its whole factor
-  auto of = [&](int64_t r, bool& used, bool& wrong, float& lse, float& p, float& f) {
-    if (a.labels) {
-      const int y = a.labels[r];
-      used = y >= 0;
-      wrong = y >= a.classes;
-    } else {
-      const float flag = a.flag[r];
-      used = flag != 0.f;
-      wrong = flag != flag;
+  // f(row, whether it is used, whether its target cannot be, lse, factor of p, f, whole factor)
+  auto each_row = [&](auto f) {
+    for (int64_t base = threadIdx.x; base < a.rows; base += 8192) {
+      float target[8], lse[8], g[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t r = min(base + i * 1024, a.rows - 1);
+        if (a.labels) {
+          const int y = a.labels[r];
+          target[i] = y < 0 ? 0.f : y >= a.classes ? nan : 1.f;
+        } else {
+          target[i] = a.flag[r];
+        }
+        lse[i] = a.lse[r];
+        g[i] = a.dloss[r];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (base + i * 1024 >= a.rows) break;
+        const float p = a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * lse[i] : 1.f, top = fmaxf(1.f, fabsf(p));
+        f(base + i * 1024, target[i] != 0.f, target[i] != target[i], lse[i], p, top, g[i] * a.per_temperature * top);
+      }
     }
-    lse = a.lse[r];
-    p = a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * lse : 1.f;
-    f = fmaxf(1.f, fabsf(p));
-    return a.dloss[r] * a.per_temperature * f;
   };
-  bool used, wrong;
-  float lse, p, f, most = 0.f;
-  for (int64_t r = threadIdx.x; r < a.rows; r += 1024) {
-    const float g = fabsf(of(r, used, wrong, lse, p, f));
-    if (used && finite(g)) most = fmaxf(most, g);
-  }
+  float most = 0.f;
+  each_row([&](int64_t, bool used, bool, float, float, float, float g) {
+    if (used && finite(g)) most = fmaxf(most, fabsf(g));
+  });
   part[threadIdx.x] = most;
   __syncthreads();
   for (int o = 512; o > 0; o >>= 1) {
@@ -507,8 +653,8 @@ __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
   }
   const float c = part[0] == 0.f ? 1.f : part[0];
   if (threadIdx.x == 0) *a.scale = c;
-  for (int64_t r = threadIdx.x; r < a.rows; r += 1024) {
-    float m = of(r, used, wrong, lse, p, f) / c, power = 1.f;
+  each_row([&](int64_t r, bool used, bool wrong, float lse, float p, float f, float g) {
+    float m = g / c, power = 1.f;
     if (finite(m) && m != 0.f) {
       int e;
       frexpf(m, &e);  // |m| in [2^(e - 1), 2^e)
@@ -518,7 +664,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
       m = ldexpf(m, -e);
     }
     a.info[r] = used ? make_float4(lse, wrong ? nan : p / f * m, wrong ? nan : m / f, c * power) : make_float4(0.f, 0.f, 0.f, 0.f);
-  }
+  });
 }
 
 // ---- operands laid out anew --------------------------------------------------------------------------------------------
@@ -628,11 +774,18 @@ template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t
   l.sums = (float2*)(ws + p.off_sums);
   l.picked = (float*)(ws + p.off_picked);
   if (a.labels && a.label_smoothing != 0.f) l.totals = (float*)(ws + p.off_totals);
-  each_piece<S, T, PL>(a, p, l, [&](int, int) { run_logits<S, T, false>(st, l, p.wave); });
+  if (p.few) {
+    l.w = a.w; l.ldw = (int)a.ldw;
+    l.K = a.in_features; l.N = a.classes;
+    run_few<S, T>(st, l);
+  } else {
+    each_piece<S, T, PL>(a, p, l, [&](int, int) { run_logits<S, T, false>(st, l, p.wave); });
+  }
   Join j = {};
   j.sums = l.sums; j.totals = l.totals; j.picked = l.picked;
   j.rows = a.rows; j.columns = p.columns;
-  while ((1 << j.log_rows) < JOIN_ROWS && (1 << j.log_rows) < a.rows) ++j.log_rows;
+  // (few rows: a block each)
+  while (a.rows > SKINNY_ROWS && (1 << j.log_rows) < JOIN_ROWS) ++j.log_rows;
   j.labels = a.labels; j.classes = a.classes;
   j.smoothing = a.label_smoothing; j.z_loss = a.z_loss;
   j.top = a.top; j.target = l.target; j.start = l.start;
@@ -662,10 +815,10 @@ template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_
   g.info = info; g.scale = scale;
   g.acc = (float*)(ws + p.off_acc); g.parts = (float*)(ws + p.off_parts);
   g.dx = p.dx; g.dw = p.dw;
+  g.both = p.both; g.dx_parts = p.dx_parts;
   each_piece<S, T, PL>(a, p, l, [&](int v, int n) {
     run_logits<S, T, true>(st, l, p.wave);
-    if (a.dbias)
-      OSEQ_LAUNCH(dbias_kernel, dim3(ceil_div(n, 16)), dim3(256), 0, st, (const float*)l.bias_sums, 2 * l.tiles_m, n, a.dbias + v);
+    g.bias_sums = l.bias_sums; g.bias_rows = 2 * l.tiles_m;
     g.w = l.w; g.ldw = l.ldw;
     g.first = v; g.count = n;
     g.start = v == 0; g.end = v + n == a.classes;
@@ -683,10 +836,15 @@ template <class S> void clear_of(const optorch_softmax_loss_t& a) {
   if (a.dbias) OSEQ_LAUNCH(loss_clear_kernel<float>, dim3(grid_of(a.classes)), dim3(256), 0, st, a.dbias, (int64_t)1, a.classes, (int64_t)a.classes);
 }
 
-// a piece of ds (and of weights that are laid out anew) takes at most about this
-constexpr int64_t LOSS_PIECE_BYTES = 256ll << 20;
+// A piece of ds (and of weights that are laid out anew) takes at most about this.  In ms with 64 / 256 / 512 / 1024 MB: 8192 x 4096 -> 128000 in
+// bf16 21.4 / 19.9 / 19.8 / 19.8, 4096 x 2048 -> 65536 2.95 / 2.78 / 2.74 / 2.73, 16384 x 512 -> 32000 2.15 / 1.90 / 1.72 / 1.65, 8192 x 1024 -> 50257
+// 2.69 / 2.40 / 2.56 / 2.56; fp32 4096 x 1024 -> 32000 4.32 / 3.88 / 3.66 / 3.63.
+constexpr int64_t LOSS_PIECE_BYTES = 512ll << 20;
 
 }  // namespace
+
+// products of less time together than this are one launch
+constexpr float BOTH_US = 60.f;
 
 LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   LossPlan p = {};
@@ -694,6 +852,8 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   const uint64_t in_row = 2 * (uint64_t)(f32 ? row_of<3>(a.in_features) : row_of<1>(a.in_features));
   p.pack_x = f32 || !direct(a.x, a.ldx, a.in_features);
   p.pack_w = f32 || !direct(a.w, a.ldw, a.in_features);
+  p.few = !backward && a.rows <= SKINNY_ROWS && p.pack_w;
+  if (p.few) p.pack_x = p.pack_w = false;
   // pieces of a multiple of 256 classes, all alike but the last
   int64_t most = a.classes;
   const int64_t each = f32 ? 8 : 2;
@@ -701,7 +861,7 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   if (p.pack_w) most = std::min(most, LOSS_PIECE_BYTES / (int64_t)in_row);
   const int64_t pieces = (a.classes + std::max<int64_t>(256, most) - 1) / std::max<int64_t>(256, most);
   p.piece = pieces == 1 ? a.classes : (int)(((a.classes + pieces - 1) / pieces + 255) / 256 * 256);
-  p.wave = shape_of(a.rows, p.piece, a.in_features, f32, 1).wave;
+  p.wave = p.few ? 16 : shape_of(a.rows, p.piece, a.in_features, f32, 1).wave;
   p.columns = (a.classes + p.wave - 1) / p.wave;
   p.ds_row = f32 ? row_of<3>(p.piece) : row_of<1>(p.piece);
   uint64_t o = 0;
@@ -726,13 +886,26 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
     p.off_ds = take(rows * p.ds_row * 2);
     if (a.dx && p.piece < a.classes) p.off_acc = take(rows * up8(a.in_features) * 4);
     if (a.dbias) p.off_bias = take((uint64_t)2 * ceil_div(a.rows, 2 * p.wave) * p.piece * 4);
-    uint64_t parts = 0;
-    auto product = [&](ProductShape& s, int64_t M, int64_t N, int64_t K) {
-      s = shape_of(M, N, K, f32);
-      if (s.parts > 1) parts = std::max(parts, (uint64_t)s.parts * M * up8(N) * 4);
-    };
-    if (a.dx) product(p.dx, a.rows, a.in_features, p.piece);
-    if (a.dw) product(p.dw, p.piece, a.in_features, a.rows);
+    auto floats = [](const ProductShape& s, int64_t M, int64_t N) { return s.parts > 1 ? s.parts * M * up8(N) : 0; };
+    const int64_t in = a.in_features;
+    p.dx = shape_of(a.rows, in, p.piece, f32);
+    p.dw = shape_of(p.piece, in, a.rows, f32);
+    // Neither product fills the card: both in one launch, with the tiles that suit the two together best.  (The same ones where only one
+    // is asked for: a gradient's bits are the same beside the others and alone.)
+    if (p.dx.wave < 128 && p.dw.wave < 128 && p.dx.us + p.dw.us < BOTH_US) {
+      p.both = a.dx && a.dw;
+      float least = 0.f;
+      for (int w : {64, 32}) {
+        const ProductShape dx = shape_of(a.rows, in, p.piece, f32, 32, w), dw = shape_of(p.piece, in, a.rows, f32, 32, w);
+        if (least != 0.f && dx.us + dw.us >= least) continue;
+        least = dx.us + dw.us;
+        p.dx = dx;
+        p.dw = dw;
+      }
+    }
+    p.dx_parts = a.dx ? floats(p.dx, a.rows, in) : 0;
+    const int64_t dw_parts = a.dw ? floats(p.dw, p.piece, in) : 0;
+    const uint64_t parts = 4 * (uint64_t)(p.both ? p.dx_parts + dw_parts : std::max(p.dx_parts, dw_parts));
     if (parts) p.off_parts = take(parts);
   }
   p.bytes = o;

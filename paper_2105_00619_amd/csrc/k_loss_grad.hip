@@ -47,16 +47,13 @@ template <class O, bool DW> __device__ __forceinline__ void finish(const Grad& g
   store8<O>((O*)g.out + row * g.ldo + col, n, v);
 }
 
-// O: type of the result; T: of the planes
+// One block's tile of a product.  O: type of the result; T: of the planes
 template <class O, class T, int W, bool DW>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8)))
-grad_kernel(Grad a) {
+__device__ __forceinline__ void tile(const Grad& a, uint32_t block, unsigned char* smem) {
   constexpr int PL = sizeof(O) == 4 ? 3 : 1;
   typedef Tile<T, PL, W, DW, true> G;
-  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   // neighbouring tiles on one XCD: each of the eight takes a run of them, eight rows of tiles at a time
   const int total = a.tiles_m * a.tiles_n * a.parts;
-  const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
   const int per = (total + 7) / 8, id = (block & 7) * per + (block >> 3);
   if ((int)(block >> 3) >= per || id >= total) return;
   const int tiles = a.tiles_m * a.tiles_n, part = id / tiles, t = id - part * tiles;
@@ -105,12 +102,17 @@ grad_kernel(Grad a) {
   }
 }
 
-// the parts' sums, added in order
-template <class O, bool DW>
-__global__ void __launch_bounds__(256) grad_join_kernel(Grad a) {
+template <class O, class T, int W, bool DW>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 128 ? 1 : 2, W == 128 ? 1 : 8))) grad_kernel(Grad a) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  tile<O, T, W, DW>(a, blockIdx.y * gridDim.x + blockIdx.x, smem);
+}
+
+// the parts' sums, added in order: block `block` of `blocks`
+template <class O, bool DW> __device__ __forceinline__ void join_parts(const Grad& a, int block, int blocks) {
   const int c8 = (a.N + 7) / 8;
   const int64_t n = a.M * c8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) {
     const int64_t r = i / c8;
     const int c = (int)(i - r * c8) * 8;
     const Before before = before_of<DW>(a, r, c);
@@ -124,6 +126,28 @@ __global__ void __launch_bounds__(256) grad_join_kernel(Grad a) {
     }
     finish<O, DW>(a, r, c, v, min(8, a.N - c), before);
   }
+}
+template <class O, bool DW> __global__ void __launch_bounds__(256) grad_join_kernel(Grad a) { join_parts<O, DW>(a, blockIdx.x, gridDim.x); }
+
+// Both products and the sums for dbias in one launch, where neither product fills the card: they read the same ds and nothing of each other.
+// 128 x 512 -> 1000 in bf16: 11.5 us as two launches, 7.6 as one.
+struct Both {
+  Grad dw, dx;
+  uint32_t dw_blocks, dx_blocks;   // of the products; then those of dbias
+  const float* bias_sums; int bias_rows; float* dbias;
+  int dw_joins, dx_joins;          // blocks that add up parts
+};
+template <class O, class T, int W>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 8))) both_kernel(Both b) {
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+  const uint32_t block = blockIdx.x;
+  if (block < b.dw_blocks) tile<O, T, W, true>(b.dw, block, smem);
+  else if (block < b.dw_blocks + b.dx_blocks) tile<O, T, W, false>(b.dx, block - b.dw_blocks, smem);
+  else column_sums(b.bias_sums, b.bias_rows, (int)b.dw.M, b.dbias, block - b.dw_blocks - b.dx_blocks, reinterpret_cast<float(*)[17]>(smem));
+}
+template <class O> __global__ void __launch_bounds__(256) both_join_kernel(Both b) {
+  if ((int)blockIdx.x < b.dw_joins) join_parts<O, true>(b.dw, blockIdx.x, b.dw_joins);
+  else join_parts<O, false>(b.dx, blockIdx.x - b.dw_joins, b.dx_joins);
 }
 
 template <class O, class T, int W, bool DW> void run_w(hipStream_t st, Grad& a) {
@@ -145,26 +169,59 @@ template <class O, class T, bool DW> void run(hipStream_t st, Grad& a, const Pro
   else run_w<O, T, 32, DW>(st, a);
 }
 
+template <class O, class T, int W> void run_both(hipStream_t st, Both& b) {
+  constexpr int PL = sizeof(O) == 4 ? 3 : 1, LDS = Tile<T, PL, W, true, true>::LDS;
+  static_assert(LDS == Tile<T, PL, W, false, true>::LDS, "both products' slots are alike");
+  auto blocks = [](Grad& g) {
+    g.tiles_m = ceil_div(g.M, 2 * W);
+    g.tiles_n = ceil_div(g.N, 2 * W);
+    return (uint32_t)((g.tiles_m * g.tiles_n * g.parts + 7) / 8 * 8);
+  };
+  auto joins = [](const Grad& g) { return g.parts > 1 ? grid_of(g.M * ((g.N + 7) / 8)) : 0; };
+  b.dw_blocks = blocks(b.dw);
+  b.dx_blocks = blocks(b.dx);
+  auto k = both_kernel<O, T, W>;
+  if (LDS > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  OSEQ_LAUNCH(k, dim3(b.dw_blocks + b.dx_blocks + (b.dbias ? ceil_div(b.dw.M, 16) : 0)), dim3(256), LDS, st, b);
+  b.dw_joins = joins(b.dw);
+  b.dx_joins = joins(b.dx);
+  if (b.dw_joins + b.dx_joins) OSEQ_LAUNCH(both_join_kernel<O>, dim3(b.dw_joins + b.dx_joins), dim3(256), 0, st, b);
+}
+
 template <class O, class T> void piece_of(const optorch_softmax_loss_t& a, const LossPiece& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
+  Both b = {};
   Grad g = {};
   g.a = p.ds; g.lda = (int)p.ds_row;
-  g.partial = p.parts;
   g.info = (const float4*)p.info;
   g.scale = p.scale;
   g.unscale = 1.f / loss_scale_of(a.precision);
   if (a.dx) {
     g.b = p.w; g.ldb = p.ldw;
     g.M = a.rows; g.N = a.in_features; g.K = p.count;
+    g.partial = p.parts;
     g.acc = p.acc; g.start = p.start; g.end = p.end;
     g.out = a.dx; g.ldo = a.lddx;
-    run<O, T, false>(st, g, p.dx);
+    b.dx = g;
+    if (!p.both) run<O, T, false>(st, g, p.dx);
   }
   if (a.dw) {
     g.b = p.xs; g.ldb = p.ldxs;
     g.M = p.count; g.N = a.in_features; g.K = (int)a.rows;
+    g.partial = p.both ? p.parts + p.dx_parts : p.parts;
     g.out = (O*)a.dw + p.first * a.lddw; g.ldo = a.lddw;
-    run<O, T, true>(st, g, p.dw);
+    b.dw = g;
+    if (!p.both) run<O, T, true>(st, g, p.dw);
+  }
+  if (p.both) {
+    for (Grad* q : {&b.dx, &b.dw}) {
+      q->cut = parts_of(q->K, q == &b.dx ? p.dx.parts : p.dw.parts);
+      q->parts = q->cut.count;
+    }
+    b.bias_sums = p.bias_sums; b.bias_rows = p.bias_rows; b.dbias = a.dbias ? a.dbias + p.first : nullptr;
+    if (p.dx.wave == 64) run_both<O, T, 64>(st, b); else run_both<O, T, 32>(st, b);
+  } else if (a.dbias) {
+    OSEQ_LAUNCH(dbias_kernel, dim3(ceil_div(p.count, 16)), dim3(256), 0, st, p.bias_sums, p.bias_rows, p.count, a.dbias + p.first);
   }
 }
 

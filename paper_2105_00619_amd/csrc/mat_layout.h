@@ -95,10 +95,86 @@ template <int PL, class T> __device__ __forceinline__ void store_planes8(T* row,
   }
 }
 
-// dbias[c] = sum of the row blocks' sums: sixteen threads a column
-__global__ void __launch_bounds__(256) dbias_kernel(const float* __restrict__ sums, int blocks, int cols, float* __restrict__ out) {
-  __shared__ float part[16][17];
-  const int cl = threadIdx.x & 15, t = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
+// ---- operands of 16 x 16 MFMAs straight from memory
+typedef __attribute__((ext_vector_type(4))) float v4f;
+__device__ __forceinline__ v4f mma16(Op<bf16_t>::V a, Op<bf16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ v4f mma16(Op<f16_t>::V a, Op<f16_t>::V b, v4f c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// Eight values of a row as loaded, those that the eight places from k on have before `end`.  Not SINGLE (at least eight
+// values before `end`): at the end they are the row's last eight, those that an earlier group has taken as zeros: the same
+// ones in either operand. ODD: 16-bit values off the boundaries of 32 bits, from the 32-bit words that hold them (16-byte
+// loads at such addresses: 9705 x 2687 -> 37 in bf16 92 us, so 49).
+enum Loads { WIDE, ODD, SINGLE };
+template <class S> struct Raw8 { Chunk c[sizeof(S) / 2]; };
+template <class S, Loads L> __device__ __forceinline__ Raw8<S> raw8(const S* row, int k, int end) {
+  Raw8<S> r;
+  if (L != SINGLE) {
+    const S* p = row + min(k, end - 8);
+    if constexpr (L == ODD) {
+      const uint32_t half = (uint32_t)(uintptr_t)p & 2u;
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p) - half);
+      struct Words { uint32_t v[4]; } const w = *reinterpret_cast<const Words*>(q);
+      const uint32_t last = q[half ? 4 : 3];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.c[0][i] = __builtin_amdgcn_alignbit(i < 3 ? w.v[i + 1] : last, w.v[i], half * 8);
+    } else {
+      r = __builtin_bit_cast(Raw8<S>, *reinterpret_cast<const Loose<S, 8>*>(p));
+    }
+    if (k + 8 > end) {
+      Vec<S, 8> v = __builtin_bit_cast(Vec<S, 8>, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.v[e] = end - 8 + e < k ? from_f32<S>(0.f) : v.v[e];
+      r = __builtin_bit_cast(Raw8<S>, v);
+    }
+  } else {
+    Vec<S, 8> v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v.v[e] = k + e < end ? row[k + e] : from_f32<S>(0.f);
+    r = __builtin_bit_cast(Raw8<S>, v);
+  }
+  return r;
+}
+// ... as MFMA operands, values as planes_of has them: with its cases only where there is a value beyond the largest bf16 (a
+// NaN makes all of its planes NaN here; what counts is the first)
+template <class S, class T> __device__ __forceinline__ void planes8(const Raw8<S>& r, typename Op<T>::V (&p)[sizeof(S) == 4 ? 3 : 1]) {
+  if constexpr (sizeof(S) == 2) {
+    p[0] = __builtin_bit_cast(typename Op<T>::V, r.c[0]);
+  } else {
+    const Vec<float, 8> v = __builtin_bit_cast(Vec<float, 8>, r);
+    float x[8], most = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = v.v[e];
+      most = fmaxf(most, fabsf(x[e]));
+    }
+    if (__builtin_expect(most > 3.3895314e38f, 0)) {
+      Vec<bf16_t, 8> q[3];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        bf16_t t[3];
+        planes_of(x[e], t);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) q[k].v[e] = t[k];
+      }
+#pragma unroll
+      for (int k = 0; k < 3; ++k) p[k] = __builtin_bit_cast(typename Op<T>::V, q[k]);
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const Vec<bf16_t, 8> q = round_vec<bf16_t, 8>(x);
+      p[k] = __builtin_bit_cast(typename Op<T>::V, q);
+      if (k < 2) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] -= (float)q.v[e];
+      }
+    }
+  }
+}
+
+// out[c] = sum of the row blocks' sums: sixteen threads a column, sixteen columns a block; part: LDS, 16 x 17
+__device__ __forceinline__ void column_sums(const float* __restrict__ sums, int blocks, int cols, float* __restrict__ out, int block, float (*part)[17]) {
+  const int cl = threadIdx.x & 15, t = threadIdx.x >> 4, c = block * 16 + cl;
   float s = 0.f;
   if (c < cols) {
     float q[4] = {0.f, 0.f, 0.f, 0.f};  // (four loads on their way)
@@ -118,6 +194,10 @@ __global__ void __launch_bounds__(256) dbias_kernel(const float* __restrict__ su
     for (int k = 0; k < 16; ++k) s += part[k][cl];
     out[c] = s;
   }
+}
+__global__ void __launch_bounds__(256) dbias_kernel(const float* __restrict__ sums, int blocks, int cols, float* __restrict__ out) {
+  __shared__ float part[16][17];
+  column_sums(sums, blocks, cols, out, blockIdx.x, part);
 }
 
 // What sums that are not finite have to become, two bits a value (1: NaN, 2: infinity, 3: -infinity, 0: as summed), eight
@@ -163,12 +243,13 @@ bool direct(const void* p, int64_t ld, int cols) { return aligned16(p) && ld % 8
 // bf16 and fp32, with all tiles and 1 to 32 parts: the choice is within 10 % of the best of them.  (By filling the CUs
 // alone, 1024 x 1024 x 1024 in bf16 took 14.3 us in two parts, 8.3 in one, and 432 x 13952 x 2968 79 us as 64 x 64 tiles,
 // 56 as 128 x 128 in four parts; in fp32 636 and 383.)
-ProductShape shape_of(int64_t M, int64_t N, int64_t K, bool f32, int64_t most_parts = 32) {
+ProductShape shape_of(int64_t M, int64_t N, int64_t K, bool f32, int64_t most_parts = 32, int only = 0) {
   constexpr int CUS = 256;
-  ProductShape best = {32, 1};
+  ProductShape best = {32, 1, 0.f};
   double least = 1e300;
   const int64_t steps = f32 ? (K + 15) / 16 : (K + 63) / 64, most = std::max<int64_t>(1, std::min<int64_t>(most_parts, std::min(steps / 4, (K + 63) / 64)));
   for (int w : {128, 64, 32}) {
+    if (only && w != only) continue;
     const int64_t tiles = (int64_t)ceil_div(M, 2 * w) * ceil_div(N, 2 * w);
     const double step = w == 128 ? (f32 ? 2.0 : 1.65) : w == 64 ? (f32 ? 0.65 : 0.6) : 0.3;
     const double ends = w == 128 ? 8.0 : w == 64 ? 4.0 : 3.5;
@@ -179,7 +260,7 @@ ProductShape shape_of(int64_t M, int64_t N, int64_t K, bool f32, int64_t most_pa
       const double busy = up <= 1 || share == 1 ? std::max(1., up) : 0.82 * 0.5 * (load + up);  // blocks a CU makes, as if one by one
       double us = std::max(1., busy) * each * step + ends * std::ceil(up / share);
       if (parts > 1) us += 3.0 + 0.3 * parts + (double)M * N * (4 * parts + (f32 ? 12 : 6)) / 6e6;
-      if (us < least) { least = us; best = {w, (int)parts}; }
+      if (us < least) { least = us; best = {w, (int)parts, (float)us}; }
     }
   }
   return best;

@@ -37,8 +37,8 @@ inline bool same_place(const Place& a, const Place& b) {
   return a.at == b.at && (a.pitch == b.pitch || a.rows <= 1) && a.width == b.width;
 }
 
-// How a product M x N over K is cut: block tiles of 2 * wave x 2 * wave, the reduction in `parts`
-struct ProductShape { int wave, parts; };
+// How a product M x N over K is cut: block tiles of 2 * wave x 2 * wave, the reduction in `parts`; what it is estimated to take
+struct ProductShape { int wave, parts; float us; };
 
 // What a linear layer's call does with its workspace: where each piece begins, and how the products run
 struct LinearPlan {
@@ -62,12 +62,15 @@ void launch_norm_backward(const optorch_layer_norm_t& a, const NormPlan& p);
 // What a loss' call does with its workspace.  The classes are taken in pieces (of whole tiles): forward only where their weights
 // are laid out anew, backward as many as keep a piece of ds within LOSS_PIECE_BYTES.
 struct LossPlan {
+  bool few;             // forward: operands straight from memory
   bool pack_x, pack_w;
   int wave;             // the logits' tiles: 2 * wave x 2 * wave; a row's sums are kept for every `wave` classes
   int columns;          // how many of those
   int piece;            // classes of a piece
   int64_t ds_row;       // places of a row of ds
   ProductShape dx, dw;
+  bool both;            // dx and dw in one launch, with the same tiles
+  int64_t dx_parts;     // floats of dx' parts in front of dw's, in one launch
   uint64_t off_x, off_w, off_sums, off_totals, off_picked;     // operands; [columns][rows] (maximum, sum), sums of logits; targets' logits
   uint64_t off_index, off_target, off_start, off_flag;         // a teacher's entries in order of their classes
   uint64_t off_info, off_scale, off_xs, off_ds, off_acc, off_parts, off_bias;
@@ -87,6 +90,8 @@ struct LossPiece {
   float* acc; float* parts;        // dx summed over the pieces; parts of a reduction
   bool start, end;                 // whether it is the first and the last piece
   ProductShape dx, dw;
+  bool both; int64_t dx_parts;     // in one launch, the parts of dw behind these of dx
+  const float* bias_sums; int bias_rows;  // sums of ds for dbias, of the piece's classes
 };
 void launch_loss_piece(const optorch_softmax_loss_t& a, const LossPiece& p);
 // what ds is multiplied by while it is held: its largest values, of up to 2, stay in the type's range, and the smallest ones that

@@ -260,8 +260,8 @@ def test_distillation_of_one_entry_is_cross_entropy():
         assert torch.equal(p, q)
 
 
-# sizes that take more than one piece of the classes: ds beyond 256 MB; weights that are laid out anew beyond 256 MB
-@pytest.mark.parametrize("name,rows,cin,classes", [("bf16", 20000, 24, 9001), ("fp32", 8200, 17, 5003), ("fp32", 5, 1030, 40009), ("bf16", 7, 1031, 140000), ("fp16", 30011, 8, 4999)])
+# sizes that take more than one piece of the classes: ds beyond 512 MB; weights that are laid out anew beyond 512 MB
+@pytest.mark.parametrize("name,rows,cin,classes", [("bf16", 30000, 24, 9601), ("fp32", 8200, 17, 9003), ("fp32", 70, 1030, 70009), ("bf16", 71, 1031, 280000), ("fp16", 50011, 8, 5999)])
 def test_pieces_of_the_classes(name, rows, cin, classes):
     from paper_2105_00619_amd import binding as B
     torch = _t()
