@@ -602,9 +602,9 @@ def _int32(name, v):
 
 def _check_matrix(name, t, rows, cols, like):
     """A rows x cols matrix of like's type and device whose rows lie one behind the other (any distance)."""
-    if tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError("%s: expected a %d x %d matrix, got %s" % (name, rows, cols, tuple(t.shape)))
-    if t.dtype != like.dtype or t.device != like.device:
+    if t is not like and (t.dtype != like.dtype or t.device != like.device):
         raise TypeError("%s: expected %s on %s, got %s on %s" % (name, like.dtype, like.device, t.dtype, t.device))
     if cols > 1 and t.stride(1) != 1:
         raise ValueError("%s: the elements of a row must lie next to each other" % name)
@@ -636,7 +636,7 @@ def _linear_args(x, activation, rows, cin, cout):
 
 def _matrix_call(torch, fn, a, device, workspace=None):
     """fn(a) on device's current stream; workspace(a): the bytes it needs."""
-    if torch.cuda.current_device() != device.index:
+    if torch._C._cuda_getDevice() != device.index:  # (torch.cuda.current_device() asks whether there is one first: 0.5 us)
         with torch.cuda.device(device):
             return _matrix_call(torch, fn, a, device, workspace)
     if workspace is not None:
@@ -756,10 +756,8 @@ def layer_norm_forward(x, weight=None, bias=None, *, eps=1e-5, save_stats=False,
         _check_matrix("out", out, rows, cols, x)
     a.y, a.ldy = out.data_ptr(), _ld(out)
     if save_stats:
-        stats = torch.empty((2, rows), dtype=torch.float32, device=x.device)
-        mean, rstd = stats[0], stats[1]
-        a.mean = stats.data_ptr()
-        a.rstd = a.mean + 4 * rows if rows else a.mean
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device).unbind()
+        a.mean, a.rstd = mean.data_ptr(), rstd.data_ptr()
     _matrix_call(torch, load_library().optorch_layer_norm_forward, a, x.device)
     return (out, mean, rstd) if save_stats else out
 
@@ -845,10 +843,8 @@ def _teacher(a, x, indices, teacher, temperature):
 
 def _loss_forward(a, x):
     import torch
-    out = torch.empty((2, a.rows), dtype=torch.float32, device=x.device)
-    loss, lse = out[0], out[1]
-    a.loss = out.data_ptr()
-    a.lse = a.loss + 4 * a.rows if a.rows else None
+    loss, lse = torch.empty((2, a.rows), dtype=torch.float32, device=x.device).unbind()
+    a.loss, a.lse = loss.data_ptr(), lse.data_ptr()
     lib = load_library()
     _matrix_call(torch, lib.optorch_softmax_loss_forward, a, x.device, lambda a: lib.optorch_softmax_loss_workspace(C.byref(a), 0))
     return loss, lse

@@ -414,6 +414,137 @@ template <class S, class T> void run_few(hipStream_t st, const Logits& l) {
   run_few_by<S, T, WIDE>(st, l);
 }
 
+// Up to 16 rows of aligned 16-bit operands: the weights are what is read, 16 classes at a time by all wavefronts of a block, 512 values of k
+// each, and the next 16 classes on their way; the rows of x stay in registers as operands.  A block walks its groups of classes, a wavefront in turn
+// adds up a group's sums and goes on with the rows' maxima and sums of exponentials: one of each row for every block.
+// 16 x 2048 -> 65536, 268 MB that no cache holds: 60 us with the join (4.5 TB/s), 73 as tiles of 128 x 128.
+struct Stream { Logits l; int groups; };
+constexpr int STREAM_ROWS = 16, KS = 16;  // (32 rows of 256 values of k: 80 us, as tiles 72)
+template <class T, bool TOP>
+__global__ void __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) stream_logits_kernel(Stream s) {
+  typedef typename Op<T>::V V;
+  const Logits& a = s.l;
+  extern __shared__ float red[];  // [2][wavefront][256]
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const int r16 = lane & 15, kc = (lane >> 4) * 8, k0 = wave * (32 * KS);
+  const V zero = {};
+  V px[KS], pw[2][KS];
+  const T* x = (const T*)a.x + min<int64_t>(r16, a.M - 1) * a.ldx;
+#pragma unroll
+  for (int u = 0; u < KS; ++u) {
+    const int k = k0 + u * 32 + kc;
+    px[u] = k < a.K ? *reinterpret_cast<const V*>(x + k) : zero;
+  }
+  // (past a row's end its first values, taken for zeros)
+  auto fetch = [&](int g, V (&p)[KS]) {
+    const T* w = (const T*)a.w + (int64_t)min(g * 16 + r16, a.N - 1) * a.ldw;
+#pragma unroll
+    for (int u = 0; u < KS; ++u) {
+      const int k = k0 + u * 32 + kc;
+      p[u] = __builtin_nontemporal_load(reinterpret_cast<const V*>(w + (k < a.K ? k : 0)));
+    }
+  };
+  // of a lane's row: what its wavefront has seen
+  float most = -__builtin_inff(), sum = 0.f, all = 0.f;
+  auto group = [&](int g, int turn, const V (&p)[KS]) {
+    v4f acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < KS; ++u) acc = mma16(k0 + u * 32 + kc < a.K ? p[u] : zero, px[u], acc);
+    float* r = red + (turn & 1) * (waves * 256);
+    *reinterpret_cast<v4f*>(r + (wave * 64 + lane) * 4) = acc;
+    __syncthreads();
+    if (turn % waves != wave) return;
+    const int cls = a.first + g * 16 + (lane >> 4) * 4, inside = min(4, a.N - g * 16 - (lane >> 4) * 4);
+    {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int q = 0; q < waves; ++q) {
+        const v4f t = *reinterpret_cast<const v4f*>(r + (q * 64 + lane) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += t[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (a.bias && e < inside) v[e] += a.bias[cls + e];
+        v[e] *= a.per_temperature;
+      }
+      const int row = r16;
+      if (row < a.M) {
+        if (TOP) {
+          const uint16_t* st = a.start + (int64_t)row * (a.columns + 1) + (a.first + g * 16) / 16;
+          for (int t = st[0]; t < st[1]; ++t) {
+            const int at = a.index[row * a.top + t] - cls;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (at == e) a.picked[row * a.top + t] = v[e];
+          }
+        } else {
+          const int at = a.labels[row] - cls;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (at == e && e < inside) a.picked[row] = v[e];
+        }
+      }
+      float top = most;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (e < inside) all += v[e];
+        v[e] = e < inside ? v[e] : -__builtin_inff();
+        top = fmaxf(top, v[e]);
+      }
+      // (an infinity: an infinite sum, above the largest finite maximum, as in a tile)
+      const float above = top == -__builtin_inff() || top == __builtin_inff() ? 0.f : top;
+      float more = sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((most - above) * LOG2E);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) more += __builtin_amdgcn_exp2f((v[e] - above) * LOG2E);
+      sum = more;
+      most = top == __builtin_inff() ? 3.4028235e38f : top;
+    }
+  };
+  int g = blockIdx.x, turn = 0;
+  if (g < s.groups) fetch(g, pw[0]);
+  for (; g < s.groups; g += 2 * gridDim.x, turn += 2) {
+    const int g1 = g + gridDim.x, g2 = g1 + gridDim.x;
+    if (g1 < s.groups) fetch(g1, pw[1]);
+    group(g, turn, pw[0]);
+    if (g1 >= s.groups) break;
+    if (g2 < s.groups) fetch(g2, pw[0]);
+    group(g1, turn + 1, pw[1]);
+  }
+  // the wavefronts' and the lanes' joined: red holds (maximum, sum, all) of each
+  __syncthreads();
+  float* mine = red + (wave * 64 + lane) * 3;
+  mine[0] = most; mine[1] = sum; mine[2] = all;
+  __syncthreads();
+  if (const int row = threadIdx.x; row < a.M) {
+    float top = -__builtin_inff(), total = 0.f, every = 0.f;
+    for (int i = 0; i < waves * 4; ++i) {
+      const float* r = red + ((i >> 2) * 64 + (i & 3) * 16 + row) * 3;
+      const float up = fmaxf(top, r[0]);
+      total = up == -__builtin_inff() ? total + r[1] : total * __builtin_amdgcn_exp2f((top - up) * LOG2E) + r[1] * __builtin_amdgcn_exp2f((r[0] - up) * LOG2E);
+      top = up;
+      every += r[2];
+    }
+    a.sums[(int64_t)blockIdx.x * a.M + row] = make_float2(top, total);
+    if (a.totals) a.totals[(int64_t)blockIdx.x * a.M + row] = every;
+  }
+}
+
+template <class T> void run_stream(hipStream_t st, const Logits& l, int blocks) {
+  const int waves = ceil_div(l.K, 32 * KS);
+  Stream s = {l, ceil_div(l.N, 16)};
+  const size_t lds = (size_t)waves * 2048;
+  if (l.labels) OSEQ_LAUNCH((stream_logits_kernel<T, false>), dim3(blocks), dim3(waves * 64), lds, st, s);
+  else OSEQ_LAUNCH((stream_logits_kernel<T, true>), dim3(blocks), dim3(waves * 64), lds, st, s);
+}
+// Blocks of the kernel above, eight wavefronts on a CU, or 0 where tiles are taken: rows of little less than 2048 or 4096 values.  16 rows, us
+// so / as tiles: 2048 -> 1000 13 / 16, -> 32000 38 / 39, -> 128000 105 / 127; 4096 -> 32000 60 / 64, -> 65536 106 / 127, -> 128000 194 / 179; but
+// 3000 -> 30000 56 / 44, 1024 -> 32000 25 / 20, 256 -> 50000 20 / 16.
+int stream_blocks(int64_t rows, int classes, int k) {
+  const int waves = ceil_div(k, 32 * KS);
+  const bool suits = rows <= STREAM_ROWS && (waves == 4 || waves == 8) && k * 10 >= waves * 32 * KS * 9;
+  return suits ? std::min(ceil_div(classes, 16), 256 * (8 / waves)) : 0;
+}
+
 // ---- a teacher's entries -----------------------------------------------------------------------------------------------
 // Those of a row in order of their classes (then of their places), entries of one class added up in the first of them; softmax of their logits;
 // where the entries of each run of `width` classes begin.  Threads N a row, N a power of two of at least `top`.
@@ -503,7 +634,7 @@ __global__ void __launch_bounds__(N < 256 ? 256 : N) teacher_kernel(Teacher a) {
 struct Join {
   const float2* sums; const float* totals; const float* picked;
   int64_t rows;
-  int columns, log_rows;           // a block's rows: 1 << log_rows
+  int columns, runs, log_rows;     // of the table of a teacher's entries, of the sums; a block's rows: 1 << log_rows
   const int32_t* labels; int classes;
   float smoothing, z_loss;
   int top; const float2* target; const float* flag; const uint16_t* start;
@@ -530,13 +661,13 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
   float m4[AT_ONCE], l4[AT_ONCE];
 #pragma unroll
   for (int q = 0; q < AT_ONCE; ++q) { m4[q] = -__builtin_inff(); l4[q] = 0.f; }
-  for (int c = slot; c < a.columns; c += AT_ONCE * slots) {
+  for (int c = slot; c < a.runs; c += AT_ONCE * slots) {
     float2 t[AT_ONCE];
 #pragma unroll
     for (int q = 0; q < AT_ONCE; ++q) {
       const int at = c + q * slots;
-      t[q] = at < a.columns ? a.sums[(int64_t)at * a.rows + row] : make_float2(-__builtin_inff(), 0.f);
-      if (a.totals && at < a.columns) extra += a.totals[(int64_t)at * a.rows + row];
+      t[q] = at < a.runs ? a.sums[(int64_t)at * a.rows + row] : make_float2(-__builtin_inff(), 0.f);
+      if (a.totals && at < a.runs) extra += a.totals[(int64_t)at * a.rows + row];
     }
 #pragma unroll
     for (int q = 0; q < AT_ONCE; ++q) join(m4[q], l4[q], t[q].x, t[q].y);
@@ -774,16 +905,19 @@ template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t
   l.sums = (float2*)(ws + p.off_sums);
   l.picked = (float*)(ws + p.off_picked);
   if (a.labels && a.label_smoothing != 0.f) l.totals = (float*)(ws + p.off_totals);
-  if (p.few) {
-    l.w = a.w; l.ldw = (int)a.ldw;
-    l.K = a.in_features; l.N = a.classes;
+  l.w = a.w; l.ldw = (int)a.ldw;
+  l.N = a.classes;
+  if (p.stream) {
+    if constexpr (PL == 1) run_stream<T>(st, l, p.stream);
+  } else if (p.few) {
+    l.K = a.in_features;
     run_few<S, T>(st, l);
   } else {
     each_piece<S, T, PL>(a, p, l, [&](int, int) { run_logits<S, T, false>(st, l, p.wave); });
   }
   Join j = {};
   j.sums = l.sums; j.totals = l.totals; j.picked = l.picked;
-  j.rows = a.rows; j.columns = p.columns;
+  j.rows = a.rows; j.columns = p.columns; j.runs = p.stream ? p.stream : p.columns;
   // (few rows: a block each)
   while (a.rows > SKINNY_ROWS && (1 << j.log_rows) < JOIN_ROWS) ++j.log_rows;
   j.labels = a.labels; j.classes = a.classes;
@@ -854,6 +988,7 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   p.pack_w = f32 || !direct(a.w, a.ldw, a.in_features);
   p.few = !backward && a.rows <= SKINNY_ROWS && p.pack_w;
   if (p.few) p.pack_x = p.pack_w = false;
+  if (!backward && !p.pack_x && !p.pack_w && !p.few) p.stream = stream_blocks(a.rows, a.classes, a.in_features);
   // pieces of a multiple of 256 classes, all alike but the last
   int64_t most = a.classes;
   const int64_t each = f32 ? 8 : 2;
@@ -861,7 +996,7 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   if (p.pack_w) most = std::min(most, LOSS_PIECE_BYTES / (int64_t)in_row);
   const int64_t pieces = (a.classes + std::max<int64_t>(256, most) - 1) / std::max<int64_t>(256, most);
   p.piece = pieces == 1 ? a.classes : (int)(((a.classes + pieces - 1) / pieces + 255) / 256 * 256);
-  p.wave = p.few ? 16 : shape_of(a.rows, p.piece, a.in_features, f32, 1).wave;
+  p.wave = p.few || p.stream ? 16 : shape_of(a.rows, p.piece, a.in_features, f32, 1).wave;
   p.columns = (a.classes + p.wave - 1) / p.wave;
   p.ds_row = f32 ? row_of<3>(p.piece) : row_of<1>(p.piece);
   uint64_t o = 0;
@@ -876,8 +1011,9 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
     p.off_flag = take(rows * 4);
   }
   if (!backward) {
-    p.off_sums = take(rows * p.columns * 8);
-    if (!teacher && a.label_smoothing != 0.f) p.off_totals = take(rows * p.columns * 4);
+    const uint64_t runs = p.stream ? p.stream : p.columns;
+    p.off_sums = take(rows * runs * 8);
+    if (!teacher && a.label_smoothing != 0.f) p.off_totals = take(rows * runs * 4);
     p.off_picked = take(rows * (teacher ? a.top : 1) * 4);
   } else {
     p.off_info = take(rows * 16);

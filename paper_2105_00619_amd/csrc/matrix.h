@@ -63,6 +63,7 @@ void launch_norm_backward(const optorch_layer_norm_t& a, const NormPlan& p);
 // are laid out anew, backward as many as keep a piece of ds within LOSS_PIECE_BYTES.
 struct LossPlan {
   bool few;             // forward: operands straight from memory
+  int stream;           // forward: blocks that walk the classes, each with a row's sums of its own, or 0
   bool pack_x, pack_w;
   int wave;             // the logits' tiles: 2 * wave x 2 * wave; a row's sums are kept for every `wave` classes
   int columns;          // how many of those

@@ -121,7 +121,8 @@ class Reference:
 # (rows, in, classes): single values, one row, one class, odd sizes, the edges of tiles and of the runs of columns that a row's sums are kept for, many
 # classes with few rows and many rows with few classes
 SIZES = [(1, 1, 1), (1, 8, 2), (3, 5, 7), (2, 64, 1000), (17, 33, 65), (64, 64, 64), (65, 72, 129), (130, 200, 300), (257, 128, 513), (33, 520, 4099),
-         (300, 40, 1031), (5, 1024, 20000), (1000, 24, 10), (520, 256, 2050)]
+         (300, 40, 1031), (5, 1024, 20000), (1000, 24, 10), (520, 256, 2050),
+         (1, 2048, 5), (16, 2040, 3333), (7, 1968, 20011), (13, 4096, 900)]
 
 
 def _operands(rows, cin, classes, name, seed=None):
