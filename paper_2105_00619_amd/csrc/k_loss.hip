@@ -13,6 +13,29 @@ namespace {
 
 constexpr float LOG2E = 1.4426950408889634f;
 
+// ---- operands laid out anew --------------------------------------------------------------------------------------------
+// Columns are filled up to whole blocks (block_of) with zeros.  With `info`, rows times their power of two.
+struct Layout { const void* src; int64_t ld, rows; int cols; void* dst; const float4* info; const float* scale; };
+template <class S, class T, int PL> __device__ __forceinline__ void lay_out_rows(const Layout& a, int block, int blocks) {
+  const int c8 = (a.cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
+  const int64_t n = a.rows * c8;
+  const float largest = a.info ? *a.scale : 1.f;
+  for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) {
+    const int64_t r = i / c8;
+    const int c = (int)(i - r * c8) * 8;
+    float v[8];
+    load8<S>((const S*)a.src + r * a.ld + c, max(0, min(8, a.cols - c)), v);
+    if (a.info) {
+      const float4 row = a.info[r];
+      const float f = row.w / largest;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = row.z == 0.f ? 0.f : v[e] * f;
+    }
+    store_planes8<PL, T>((T*)a.dst + r * c8 * (8 * span_of(PL)), c, v);
+  }
+}
+
+// ---- logits -------------------------------------------------------------------------------------------------------------
 struct Logits {
   const void *x, *w; int ldx, ldw;  // operands, mat_core.h
   int64_t M;
@@ -31,6 +54,7 @@ struct Logits {
   float spread, hit, scale;         // label_smoothing / classes; 1 - label_smoothing; what ds is held times
   void* ds; int64_t ds_row;
   float* bias_sums;
+  Layout xs; int xs_blocks;         // blocks behind the tiles' lay out x for dw, or 0
 };
 
 // What the backward pass knows of a row, four floats: its lse; what p and the target are multiplied by (the second is 0 in a row that is
@@ -79,6 +103,11 @@ logits_kernel(Logits a) {
   const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
   // neighbouring tiles on one XCD: each of the eight takes a run of them, eight rows of tiles at a time
   const int per = (total + 7) / 8, id = (block & 7) * per + (block >> 3);
+  if (GRAD && (int)(block >> 3) >= per) {
+    const int copy = (int)block - per * 8;
+    if (copy < a.xs_blocks) lay_out_rows<S, T, PL>(a.xs, copy, a.xs_blocks);
+    return;
+  }
   if ((int)(block >> 3) >= per || id >= total) return;
   const int band = id / (8 * a.tiles_n), rows_in = min(8, a.tiles_m - band * 8), u = id - band * 8 * a.tiles_n;
   const int tn = u / rows_in, tm = band * 8 + u - tn * rows_in;
@@ -557,12 +586,16 @@ struct Teacher {
   int32_t* index; float2* target; uint16_t* start; float* flag;
 };
 
+// the threads of a row (a wavefront's own accesses to LDS are in order)
+template <int N> __device__ __forceinline__ void row_sync() {
+  if (N <= 64) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); else __syncthreads();
+}
 template <int N, class F> __device__ __forceinline__ float over_row(float v, float* lds, int t, F&& f) {
   for (int o = N / 2; o > 0; o >>= 1) {
     lds[t] = v;
-    __syncthreads();
+    row_sync<N>();
     v = f(v, lds[t ^ o]);
-    __syncthreads();
+    row_sync<N>();
   }
   return v;
 }
@@ -594,15 +627,15 @@ __global__ void __launch_bounds__(N < 256 ? 256 : N) teacher_kernel(Teacher a) {
   for (int run = 2; run <= N; run *= 2)
     for (int o = run / 2; o > 0; o >>= 1) {
       keys[r][t] = key;
-      __syncthreads();
+      row_sync<N>();
       const uint32_t other = keys[r][t ^ o];
       const bool least = ((t & o) == 0) == ((t & run) == 0);
       key = least ? min(key, other) : max(key, other);
-      __syncthreads();
+      row_sync<N>();
     }
   keys[r][t] = key;
   values[r][t] = log_q;
-  __syncthreads();
+  row_sync<N>();
   const bool real = wanted < a.rows;
   if (real && t < a.top && key != 0xffffffffu) {
     const uint32_t mine = key >> 10;
@@ -736,7 +769,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
 // dw, where a power of two costs no bits.  (All of it in ds would leave fp16's range, all of it in x round every value a second time: dw
 // of 4096 x 2048 -> 65536 with rows that weigh differently was 2.9e-3 off in bf16, so 2.3e-3.)  Where dloss is the same for all rows, a
 // mean's, m is 1, and the value that counts most, -1 at a label that the network does not know, is exact.
-// One block, eight rows a thread on their way at once.
+// One block, eight rows a thread on their way at once: 4 us for 4096 rows.
 struct Rows {
   const float *dloss, *lse, *flag;
   const int32_t* labels;
@@ -745,16 +778,15 @@ struct Rows {
   float z_loss, per_temperature;
   float4* info; float* scale;
 };
-__global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
-  __shared__ float part[1024];
+template <int THREADS> __device__ __forceinline__ void rows_of(const Rows& a, float* part) {
   const float nan = __builtin_nanf("");
   // f(row, whether it is used, whether its target cannot be, lse, factor of p, f, whole factor)
   auto each_row = [&](auto f) {
-    for (int64_t base = threadIdx.x; base < a.rows; base += 8192) {
+    for (int64_t base = threadIdx.x; base < a.rows; base += 8 * THREADS) {
       float target[8], lse[8], g[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int64_t r = min(base + i * 1024, a.rows - 1);
+        const int64_t r = min(base + i * THREADS, a.rows - 1);
         if (a.labels) {
           const int y = a.labels[r];
           target[i] = y < 0 ? 0.f : y >= a.classes ? nan : 1.f;
@@ -766,9 +798,9 @@ __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        if (base + i * 1024 >= a.rows) break;
+        if (base + i * THREADS >= a.rows) break;
         const float p = a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * lse[i] : 1.f, top = fmaxf(1.f, fabsf(p));
-        f(base + i * 1024, target[i] != 0.f, target[i] != target[i], lse[i], p, top, g[i] * a.per_temperature * top);
+        f(base + i * THREADS, target[i] != 0.f, target[i] != target[i], lse[i], p, top, g[i] * a.per_temperature * top);
       }
     }
   };
@@ -778,7 +810,7 @@ __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
   });
   part[threadIdx.x] = most;
   __syncthreads();
-  for (int o = 512; o > 0; o >>= 1) {
+  for (int o = THREADS / 2; o > 0; o >>= 1) {
     if ((int)threadIdx.x < o) part[threadIdx.x] = fmaxf(part[threadIdx.x], part[threadIdx.x + o]);
     __syncthreads();
   }
@@ -798,34 +830,22 @@ __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
   });
 }
 
-// ---- operands laid out anew --------------------------------------------------------------------------------------------
-// Columns are filled up to whole blocks (block_of) with zeros.  With `info`, rows times their power of two.
-struct Layout { const void* src; int64_t ld, rows; int cols; void* dst; const float4* info; const float* scale; };
-template <class S, class T, int PL>
-__global__ void __launch_bounds__(256) layout_kernel(Layout a) {
-  const int c8 = (a.cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
-  const int64_t n = a.rows * c8;
-  const float largest = a.info ? *a.scale : 1.f;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / c8;
-    const int c = (int)(i - r * c8) * 8;
-    float v[8];
-    load8<S>((const S*)a.src + r * a.ld + c, max(0, min(8, a.cols - c)), v);
-    if (a.info) {
-      const float4 row = a.info[r];
-      const float f = row.w / largest;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = row.z == 0.f ? 0.f : v[e] * f;
-    }
-    store_planes8<PL, T>((T*)a.dst + r * c8 * (8 * span_of(PL)), c, v);
-  }
+__global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
+  __shared__ float part[1024];
+  rows_of<1024>(a, part);
 }
 
-template <class S, class T, int PL>
-void lay_out(hipStream_t st, const void* src, int64_t ld, int64_t rows, int cols, void* dst, const float4* info = nullptr, const float* scale = nullptr) {
-  Layout l = {src, ld, rows, cols, dst, info, scale};
-  OSEQ_LAUNCH((layout_kernel<S, T, PL>), dim3(grid_of(rows * ((cols + 7) / 8))), dim3(256), 0, st, l);
+// What a call begins with, in one launch: operands that are laid out anew, and (the first block, where there is one) the rows' values
+struct Prepare { Layout x, w; int x_blocks, w_blocks; Rows rows; int row_blocks; };
+template <class S, class T, int PL> __global__ void __launch_bounds__(256) prepare_kernel(Prepare p) {
+  __shared__ float part[256];
+  int block = blockIdx.x;
+  if (block < p.row_blocks) { rows_of<256>(p.rows, part); return; }
+  block -= p.row_blocks;
+  if (block < p.x_blocks) lay_out_rows<S, T, PL>(p.x, block, p.x_blocks);
+  else lay_out_rows<S, T, PL>(p.w, block - p.x_blocks, p.w_blocks);
 }
+int layout_blocks(int64_t rows, int cols) { return grid_of(rows * ((cols + 7) / 8)); }
 
 template <class S, class T, int W, bool TOP, bool GRAD> void run_logits_w(hipStream_t st, Logits& l) {
   typedef Tile<T, sizeof(S) == 4 ? 3 : 1, W, false, false> G;
@@ -835,7 +855,7 @@ template <class S, class T, int W, bool TOP, bool GRAD> void run_logits_w(hipStr
   auto k = logits_kernel<S, T, W, TOP, GRAD>;
   // (more LDS than a launch gets unasked; set again on every launch: which devices know it is not ours to remember)
   if (G::LDS > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
-  OSEQ_LAUNCH(k, grid_of_blocks(per * 8), dim3(256), G::LDS, st, l);
+  OSEQ_LAUNCH(k, grid_of_blocks(per * 8 + l.xs_blocks), dim3(256), G::LDS, st, l);
 }
 template <class S, class T, bool GRAD> void run_logits(hipStream_t st, Logits& l, int wave) {
   if (l.labels) {
@@ -855,21 +875,30 @@ template <class S> void run_teacher(hipStream_t st, const Teacher& t) {
   else OSEQ_LAUNCH((teacher_kernel<S, 1024>), grid_of_blocks(t.rows), dim3(1024), 0, st, t);
 }
 
-// what both directions begin with
-template <class S, class T, int PL> Logits begin(const optorch_softmax_loss_t& a, const LossPlan& p) {
+// The weights of the piece from class `first` on as operands: as they lie, or where they are laid out
+template <class S, int PL> void weights_of(const optorch_softmax_loss_t& a, const LossPlan& p, int first, Logits& l) {
+  l.w = p.pack_w ? (const void*)((char*)a.workspace + p.off_w) : (const void*)((const S*)a.w + first * a.ldw);
+  l.ldw = p.pack_w ? row_of<PL>(a.in_features) : (int)a.ldw;
+  l.first = first;
+  l.N = std::min(p.piece, a.classes - first);
+}
+template <class S> Layout weights_anew(const optorch_softmax_loss_t& a, const LossPlan& p, const Logits& l) {
+  return {(const S*)a.w + l.first * a.ldw, a.ldw, l.N, a.in_features, (char*)a.workspace + p.off_w, nullptr, nullptr};
+}
+
+// What both directions begin with: a teacher's entries in order, the rows' values (backward), operands laid out anew
+template <class S, class T, int PL> Logits begin(const optorch_softmax_loss_t& a, const LossPlan& p, Rows* rows) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
   Logits l = {};
-  l.x = a.x; l.ldx = (int)a.ldx;
-  if (p.pack_x) {
-    lay_out<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_x);
-    l.x = ws + p.off_x; l.ldx = row_of<PL>(a.in_features);
-  }
+  l.x = p.pack_x ? ws + p.off_x : a.x;
+  l.ldx = p.pack_x ? row_of<PL>(a.in_features) : (int)a.ldx;
   l.M = a.rows; l.K = (int)up8(a.in_features);  // (up to the zeros behind a row)
   l.bias = a.bias;
   l.per_temperature = a.labels ? 1.f : 1.f / a.temperature;
   l.labels = a.labels;
   l.columns = p.columns;
+  weights_of<S, PL>(a, p, 0, l);
   if (!a.labels) {
     Teacher t = {a.indices, a.ldi, a.teacher, a.ldt, a.rows, a.top, a.classes, p.wave, p.columns, l.per_temperature,
                  (int32_t*)(ws + p.off_index), (float2*)(ws + p.off_target), (uint16_t*)(ws + p.off_start), (float*)(ws + p.off_flag)};
@@ -879,41 +908,50 @@ template <class S, class T, int PL> Logits begin(const optorch_softmax_loss_t& a
     l.top = a.top;
     l.index = t.index; l.target = t.target; l.start = t.start;
   }
+  if (rows) {
+    *rows = {a.dloss, a.lse, (const float*)(ws + p.off_flag), a.labels, a.rows, a.classes, a.labels ? a.z_loss : 0.f, l.per_temperature,
+             (float4*)(ws + p.off_info), (float*)(ws + p.off_scale)};
+  }
+  Prepare q = {};
+  if (p.pack_x) { q.x = {a.x, a.ldx, a.rows, a.in_features, ws + p.off_x, nullptr, nullptr}; q.x_blocks = layout_blocks(a.rows, a.in_features); }
+  if (p.pack_w) { q.w = weights_anew<S>(a, p, l); q.w_blocks = layout_blocks(l.N, a.in_features); }
+  if (q.x_blocks + q.w_blocks) {
+    if (rows) { q.rows = *rows; q.row_blocks = 1; }
+    OSEQ_LAUNCH((prepare_kernel<S, T, PL>), dim3(q.row_blocks + q.x_blocks + q.w_blocks), dim3(256), 0, st, q);
+  } else if (rows) {
+    OSEQ_LAUNCH(rows_kernel, dim3(1), dim3(1024), 0, st, *rows);
+  }
   return l;
 }
 
-// f(first class, classes) for each piece, its weights in l
+// f() for each piece, its weights in l
 template <class S, class T, int PL, class F> void each_piece(const optorch_softmax_loss_t& a, const LossPlan& p, Logits& l, F&& f) {
-  char* ws = (char*)a.workspace;
   for (int v = 0; v < a.classes; v += p.piece) {
-    const int n = std::min(p.piece, a.classes - v);
-    const S* w = (const S*)a.w + v * a.ldw;
-    l.w = w; l.ldw = (int)a.ldw;
-    if (p.pack_w) {
-      lay_out<S, T, PL>((hipStream_t)a.hip_stream, w, a.ldw, n, a.in_features, ws + p.off_w);
-      l.w = ws + p.off_w; l.ldw = row_of<PL>(a.in_features);
+    weights_of<S, PL>(a, p, v, l);
+    if (v && p.pack_w) {
+      Prepare q = {};
+      q.w = weights_anew<S>(a, p, l);
+      q.w_blocks = layout_blocks(l.N, a.in_features);
+      OSEQ_LAUNCH((prepare_kernel<S, T, PL>), dim3(q.w_blocks), dim3(256), 0, (hipStream_t)a.hip_stream, q);
     }
-    l.first = v; l.N = n;
-    f(v, n);
+    f();
   }
 }
 
 template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t& a, const LossPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
-  Logits l = begin<S, T, PL>(a, p);
+  Logits l = begin<S, T, PL>(a, p, nullptr);
   l.sums = (float2*)(ws + p.off_sums);
   l.picked = (float*)(ws + p.off_picked);
   if (a.labels && a.label_smoothing != 0.f) l.totals = (float*)(ws + p.off_totals);
-  l.w = a.w; l.ldw = (int)a.ldw;
-  l.N = a.classes;
   if (p.stream) {
     if constexpr (PL == 1) run_stream<T>(st, l, p.stream);
   } else if (p.few) {
     l.K = a.in_features;
     run_few<S, T>(st, l);
   } else {
-    each_piece<S, T, PL>(a, p, l, [&](int, int) { run_logits<S, T, false>(st, l, p.wave); });
+    each_piece<S, T, PL>(a, p, l, [&] { run_logits<S, T, false>(st, l, p.wave); });
   }
   Join j = {};
   j.sums = l.sums; j.totals = l.totals; j.picked = l.picked;
@@ -931,12 +969,15 @@ template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t
 template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_t& a, const LossPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
   char* ws = (char*)a.workspace;
-  Logits l = begin<S, T, PL>(a, p);
-  float4* info = (float4*)(ws + p.off_info);
-  float* scale = (float*)(ws + p.off_scale);
-  Rows r = {a.dloss, a.lse, (const float*)(ws + p.off_flag), a.labels, a.rows, a.classes, a.labels ? a.z_loss : 0.f, l.per_temperature, info, scale};
-  OSEQ_LAUNCH(rows_kernel, dim3(1), dim3(1024), 0, st, r);
-  if (a.dw) lay_out<S, T, PL>(st, a.x, a.ldx, a.rows, a.in_features, ws + p.off_xs, info, scale);
+  Rows rows;
+  Logits l = begin<S, T, PL>(a, p, &rows);
+  float4* info = rows.info;
+  float* scale = rows.scale;
+  // (x for dw beside the first piece's tiles, which need nothing of it: 4096 x 2048 -> 100 in fp16 8.5 us less)
+  if (a.dw) {
+    l.xs = {a.x, a.ldx, a.rows, a.in_features, ws + p.off_xs, info, scale};
+    l.xs_blocks = std::min(grid_of(a.rows * ((a.in_features + 7) / 8)), 1024);
+  }
   l.info = info;
   l.spread = a.labels ? a.label_smoothing / (float)a.classes : 0.f;
   l.hit = 1.f - a.label_smoothing;
@@ -950,12 +991,13 @@ template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_
   g.acc = (float*)(ws + p.off_acc); g.parts = (float*)(ws + p.off_parts);
   g.dx = p.dx; g.dw = p.dw;
   g.both = p.both; g.dx_parts = p.dx_parts;
-  each_piece<S, T, PL>(a, p, l, [&](int v, int n) {
+  each_piece<S, T, PL>(a, p, l, [&] {
     run_logits<S, T, true>(st, l, p.wave);
+    l.xs_blocks = 0;
     g.bias_sums = l.bias_sums; g.bias_rows = 2 * l.tiles_m;
     g.w = l.w; g.ldw = l.ldw;
-    g.first = v; g.count = n;
-    g.start = v == 0; g.end = v + n == a.classes;
+    g.first = l.first; g.count = l.N;
+    g.start = l.first == 0; g.end = l.first + l.N == a.classes;
     launch_loss_piece(a, g);
   });
 }
@@ -997,6 +1039,9 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   const int64_t pieces = (a.classes + std::max<int64_t>(256, most) - 1) / std::max<int64_t>(256, most);
   p.piece = pieces == 1 ? a.classes : (int)(((a.classes + pieces - 1) / pieces + 255) / 256 * 256);
   p.wave = p.few || p.stream ? 16 : shape_of(a.rows, p.piece, a.in_features, f32, 1).wave;
+  // (a tile's end costs more where ds leaves it than the estimate has: tiles of 256 / 128, us in bf16 4096 x 256 -> 8192 119 / 110, 8192 x
+  // 512 -> 4096 155 / 153, 4096 x 1024 -> 32000 765 / 773; fp32 414 / 361, 643 / 589, 3708 / 3717)
+  if (backward && p.wave == 128 && a.in_features <= 640) p.wave = 64;
   p.columns = (a.classes + p.wave - 1) / p.wave;
   p.ds_row = f32 ? row_of<3>(p.piece) : row_of<1>(p.piece);
   uint64_t o = 0;
