@@ -115,7 +115,7 @@ int optorch_layer_norm_backward(const optorch_layer_norm_t* a);
  *   indices, teacher  q = softmax(teacher / temperature) over the row's `top` entries; the probabilities of entries of one class add
  *                     up.  Entries with a negative index or a logit of -infinity are unused; a row without any other is left out.  An
  *                     index not below `classes` makes the row's loss and gradients NaN, and so does a logit that is NaN or infinite.
- * Rows left out have a loss of zero and no gradient, whatever their x is.  `precision` is the type of x, w, dx and dw; everything
+ * Rows left out have a loss of zero and no gradient, whatever their x is (no gradient: those with a dloss of zero as well).  `precision` is the type of x, w, dx and dw; everything
  * else is fp32.  Products are summed in fp32 (fp32 operands as three bf16 planes, sums that are not finite come out as NaN). */
 typedef struct {
   int32_t precision, teacher_precision;

@@ -680,7 +680,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
   __shared__ float2 part[JOIN_THREADS];
   __shared__ float more[JOIN_THREADS];
   const int rows = 1 << a.log_rows, rl = threadIdx.x & (rows - 1), slot = threadIdx.x >> a.log_rows, slots = JOIN_THREADS >> a.log_rows;
-  const int64_t wanted = (int64_t)blockIdx.x * rows + rl, row = min(wanted, a.rows - 1);
+  const int64_t wanted = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * rows + rl, row = min(wanted, a.rows - 1);
   float most = -__builtin_inff(), sum = 0.f, extra = 0.f;
   auto join = [](float& m, float& l, float m2, float l2) {
     // (a maximum that is NaN has a sum that is; one of -infinity a sum of zero)
@@ -769,7 +769,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
 // dw, where a power of two costs no bits.  (All of it in ds would leave fp16's range, all of it in x round every value a second time: dw
 // of 4096 x 2048 -> 65536 with rows that weigh differently was 2.9e-3 off in bf16, so 2.3e-3.)  Where dloss is the same for all rows, a
 // mean's, m is 1, and the value that counts most, -1 at a label that the network does not know, is exact.
-// One block, eight rows a thread on their way at once: 4 us for 4096 rows.
+// Up to 8192 rows one block (4 us for 4096 rows); more rows two launches of up to 256 blocks, the largest factors of the blocks first.
 struct Rows {
   const float *dloss, *lse, *flag;
   const int32_t* labels;
@@ -777,46 +777,57 @@ struct Rows {
   int classes;
   float z_loss, per_temperature;
   float4* info; float* scale;
+  float* largest; int blocks;   // of the blocks, or null and 1
 };
-template <int THREADS> __device__ __forceinline__ void rows_of(const Rows& a, float* part) {
+// f(row, whether it is used, whether its target cannot be, lse, factor of p, f, whole factor) for the rows of a block, eight a thread on their way
+// at once
+template <int THREADS, class F> __device__ __forceinline__ void each_row(const Rows& a, int block, F&& f) {
   const float nan = __builtin_nanf("");
-  // f(row, whether it is used, whether its target cannot be, lse, factor of p, f, whole factor)
-  auto each_row = [&](auto f) {
-    for (int64_t base = threadIdx.x; base < a.rows; base += 8 * THREADS) {
-      float target[8], lse[8], g[8];
+  for (int64_t base = (int64_t)block * 8 * THREADS + threadIdx.x; base < a.rows; base += (int64_t)a.blocks * 8 * THREADS) {
+    float target[8], lse[8], g[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t r = min(base + i * THREADS, a.rows - 1);
-        if (a.labels) {
-          const int y = a.labels[r];
-          target[i] = y < 0 ? 0.f : y >= a.classes ? nan : 1.f;
-        } else {
-          target[i] = a.flag[r];
-        }
-        lse[i] = a.lse[r];
-        g[i] = a.dloss[r];
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = min(base + i * THREADS, a.rows - 1);
+      if (a.labels) {
+        const int y = a.labels[r];
+        target[i] = y < 0 ? 0.f : y >= a.classes ? nan : 1.f;
+      } else {
+        target[i] = a.flag[r];
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (base + i * THREADS >= a.rows) break;
-        const float p = a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * lse[i] : 1.f, top = fmaxf(1.f, fabsf(p));
-        f(base + i * THREADS, target[i] != 0.f, target[i] != target[i], lse[i], p, top, g[i] * a.per_temperature * top);
-      }
+      lse[i] = a.lse[r];
+      g[i] = a.dloss[r];
     }
-  };
-  float most = 0.f;
-  each_row([&](int64_t, bool used, bool, float, float, float, float g) {
-    if (used && finite(g)) most = fmaxf(most, fabsf(g));
-  });
-  part[threadIdx.x] = most;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (base + i * THREADS >= a.rows) break;
+      const float p = a.z_loss != 0.f ? 1.f + 2.f * a.z_loss * lse[i] : 1.f, top = fmaxf(1.f, fabsf(p));
+      f(base + i * THREADS, target[i] != 0.f, target[i] != target[i], lse[i], p, top, g[i] * a.per_temperature * top);
+    }
+  }
+}
+// the largest of a block's values, in every thread
+template <int THREADS> __device__ __forceinline__ float block_max(float v, float* part) {
+  part[threadIdx.x] = v;
   __syncthreads();
   for (int o = THREADS / 2; o > 0; o >>= 1) {
     if ((int)threadIdx.x < o) part[threadIdx.x] = fmaxf(part[threadIdx.x], part[threadIdx.x + o]);
     __syncthreads();
   }
-  const float c = part[0] == 0.f ? 1.f : part[0];
-  if (threadIdx.x == 0) *a.scale = c;
-  each_row([&](int64_t r, bool used, bool wrong, float lse, float p, float f, float g) {
+  return part[0];
+}
+template <int THREADS> __device__ __forceinline__ float largest_of(const Rows& a, int block, float* part) {
+  float most = 0.f;
+  each_row<THREADS>(a, block, [&](int64_t, bool used, bool, float, float, float, float g) {
+    if (used && finite(g)) most = fmaxf(most, fabsf(g));
+  });
+  return block_max<THREADS>(most, part);
+}
+template <int THREADS> __device__ __forceinline__ void rows_of(const Rows& a, int block, float* part) {
+  const float nan = __builtin_nanf("");
+  float c = a.largest ? block_max<THREADS>((int)threadIdx.x < a.blocks ? a.largest[threadIdx.x] : 0.f, part) : largest_of<THREADS>(a, 0, part);
+  if (c == 0.f) c = 1.f;
+  if (block == 0 && threadIdx.x == 0) *a.scale = c;
+  each_row<THREADS>(a, block, [&](int64_t r, bool used, bool wrong, float lse, float p, float f, float g) {
     float m = g / c, power = 1.f;
     if (finite(m) && m != 0.f) {
       int e;
@@ -829,10 +840,26 @@ template <int THREADS> __device__ __forceinline__ void rows_of(const Rows& a, fl
     a.info[r] = used ? make_float4(lse, wrong ? nan : p / f * m, wrong ? nan : m / f, c * power) : make_float4(0.f, 0.f, 0.f, 0.f);
   });
 }
-
 __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
   __shared__ float part[1024];
-  rows_of<1024>(a, part);
+  rows_of<1024>(a, blockIdx.x, part);
+}
+__global__ void __launch_bounds__(1024) largest_kernel(Rows a) {
+  __shared__ float part[1024];
+  const float c = largest_of<1024>(a, blockIdx.x, part);
+  if (threadIdx.x == 0) a.largest[blockIdx.x] = c;
+}
+constexpr int ROWS_AT_ONCE = 8192, ROW_BLOCKS = 256;
+
+// sums of 64 rows each
+__global__ void __launch_bounds__(256) fold_kernel(const float* sums, int64_t rows, int cols, float* out) {
+  const int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x, g = i / cols;
+  if (g * 64 >= rows) return;
+  const float* p = sums + g * 64 * cols + (i - g * cols);
+  const int n = (int)min<int64_t>(64, rows - g * 64);
+  float s = 0.f;
+  for (int r = 0; r < n; ++r) s += p[(int64_t)r * cols];
+  out[i] = s;
 }
 
 // What a call begins with, in one launch: operands that are laid out anew, and (the first block, where there is one) the rows' values
@@ -840,7 +867,7 @@ struct Prepare { Layout x, w; int x_blocks, w_blocks; Rows rows; int row_blocks;
 template <class S, class T, int PL> __global__ void __launch_bounds__(256) prepare_kernel(Prepare p) {
   __shared__ float part[256];
   int block = blockIdx.x;
-  if (block < p.row_blocks) { rows_of<256>(p.rows, part); return; }
+  if (block < p.row_blocks) { rows_of<256>(p.rows, 0, part); return; }
   block -= p.row_blocks;
   if (block < p.x_blocks) lay_out_rows<S, T, PL>(p.x, block, p.x_blocks);
   else lay_out_rows<S, T, PL>(p.w, block - p.x_blocks, p.w_blocks);
@@ -910,15 +937,22 @@ template <class S, class T, int PL> Logits begin(const optorch_softmax_loss_t& a
   }
   if (rows) {
     *rows = {a.dloss, a.lse, (const float*)(ws + p.off_flag), a.labels, a.rows, a.classes, a.labels ? a.z_loss : 0.f, l.per_temperature,
-             (float4*)(ws + p.off_info), (float*)(ws + p.off_scale)};
+             (float4*)(ws + p.off_info), (float*)(ws + p.off_scale), nullptr, 1};
+    if (a.rows > ROWS_AT_ONCE) {
+      rows->largest = rows->scale + 64;
+      rows->blocks = (int)std::min<int64_t>((a.rows + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE, ROW_BLOCKS);
+      OSEQ_LAUNCH(largest_kernel, dim3(rows->blocks), dim3(1024), 0, st, *rows);
+      OSEQ_LAUNCH(rows_kernel, dim3(rows->blocks), dim3(1024), 0, st, *rows);
+    }
   }
+  const bool wait = rows && !rows->largest;  // rows whose values are still to be made
   Prepare q = {};
   if (p.pack_x) { q.x = {a.x, a.ldx, a.rows, a.in_features, ws + p.off_x, nullptr, nullptr}; q.x_blocks = layout_blocks(a.rows, a.in_features); }
   if (p.pack_w) { q.w = weights_anew<S>(a, p, l); q.w_blocks = layout_blocks(l.N, a.in_features); }
   if (q.x_blocks + q.w_blocks) {
-    if (rows) { q.rows = *rows; q.row_blocks = 1; }
+    if (wait) { q.rows = *rows; q.row_blocks = 1; }
     OSEQ_LAUNCH((prepare_kernel<S, T, PL>), dim3(q.row_blocks + q.x_blocks + q.w_blocks), dim3(256), 0, st, q);
-  } else if (rows) {
+  } else if (wait) {
     OSEQ_LAUNCH(rows_kernel, dim3(1), dim3(1024), 0, st, *rows);
   }
   return l;
@@ -963,8 +997,11 @@ template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t
   j.top = a.top; j.target = l.target; j.start = l.start;
   j.flag = (const float*)(ws + p.off_flag);
   j.loss = a.loss; j.lse = a.lse;
-  OSEQ_LAUNCH(loss_join_kernel, dim3(ceil_div(a.rows, 1 << j.log_rows)), dim3(JOIN_THREADS), 0, st, j);
+  OSEQ_LAUNCH(loss_join_kernel, grid_of_blocks(ceil_div(a.rows, 1 << j.log_rows)), dim3(JOIN_THREADS), 0, st, j);
 }
+
+// rows of sums for dbias from which on they are added up 64 at a time first
+constexpr int FOLD_FROM = 2048;
 
 template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_t& a, const LossPlan& p) {
   hipStream_t st = (hipStream_t)a.hip_stream;
@@ -995,6 +1032,12 @@ template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_
     run_logits<S, T, true>(st, l, p.wave);
     l.xs_blocks = 0;
     g.bias_sums = l.bias_sums; g.bias_rows = 2 * l.tiles_m;
+    if (a.dbias && g.bias_rows > FOLD_FROM) {
+      const int64_t folded = ((int64_t)g.bias_rows + 63) / 64;
+      float* out = l.bias_sums + (int64_t)g.bias_rows * l.N;
+      OSEQ_LAUNCH(fold_kernel, grid_of_blocks((folded * l.N + 255) / 256), dim3(256), 0, st, (const float*)l.bias_sums, (int64_t)g.bias_rows, l.N, out);
+      g.bias_sums = out; g.bias_rows = (int)folded;
+    }
     g.w = l.w; g.ldw = l.ldw;
     g.first = l.first; g.count = l.N;
     g.start = l.first == 0; g.end = l.first + l.N == a.classes;
@@ -1062,11 +1105,12 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
     p.off_picked = take(rows * (teacher ? a.top : 1) * 4);
   } else {
     p.off_info = take(rows * 16);
-    p.off_scale = take(4);
+    p.off_scale = take(4 * (64 + ROW_BLOCKS));
     if (a.dw) p.off_xs = take(rows * in_row);
     p.off_ds = take(rows * p.ds_row * 2);
     if (a.dx && p.piece < a.classes) p.off_acc = take(rows * up8(a.in_features) * 4);
-    if (a.dbias) p.off_bias = take((uint64_t)2 * ceil_div(a.rows, 2 * p.wave) * p.piece * 4);
+    const uint64_t bias_rows = 2 * (uint64_t)ceil_div(a.rows, 2 * p.wave);
+    if (a.dbias) p.off_bias = take((bias_rows + (bias_rows > FOLD_FROM ? (bias_rows + 63) / 64 : 0)) * p.piece * 4);
     auto floats = [](const ProductShape& s, int64_t M, int64_t N) { return s.parts > 1 ? s.parts * M * up8(N) : 0; };
     const int64_t in = a.in_features;
     p.dx = shape_of(a.rows, in, p.piece, f32);

@@ -122,7 +122,7 @@ class Reference:
 # classes with few rows and many rows with few classes
 SIZES = [(1, 1, 1), (1, 8, 2), (3, 5, 7), (2, 64, 1000), (17, 33, 65), (64, 64, 64), (65, 72, 129), (130, 200, 300), (257, 128, 513), (33, 520, 4099),
          (300, 40, 1031), (5, 1024, 20000), (1000, 24, 10), (520, 256, 2050),
-         (1, 2048, 5), (16, 2040, 3333), (7, 1968, 20011), (13, 4096, 900)]
+         (1, 2048, 5), (16, 2040, 3333), (7, 1968, 20011), (13, 4096, 900), (300, 800, 50001), (2300, 712, 7001)]
 
 
 def _operands(rows, cin, classes, name, seed=None):
@@ -261,8 +261,10 @@ def test_distillation_of_one_entry_is_cross_entropy():
         assert torch.equal(p, q)
 
 
-# sizes that take more than one piece of the classes: ds beyond 512 MB; weights that are laid out anew beyond 512 MB
-@pytest.mark.parametrize("name,rows,cin,classes", [("bf16", 30000, 24, 9601), ("fp32", 8200, 17, 9003), ("fp32", 70, 1030, 70009), ("bf16", 71, 1031, 280000), ("fp16", 50011, 8, 5999)])
+# sizes that take more than one piece of the classes: ds beyond 512 MB; weights that are laid out anew beyond 512 MB; the last with tiles of 256 x 256 in
+# all three products
+@pytest.mark.parametrize("name,rows,cin,classes", [("bf16", 30000, 24, 9601), ("fp32", 8200, 17, 9003), ("fp32", 70, 1030, 70009), ("bf16", 71, 1031, 280000), ("fp16", 50011, 8, 5999),
+                                                   ("bf16", 16400, 712, 17001)])
 def test_pieces_of_the_classes(name, rows, cin, classes):
     from paper_2105_00619_amd import binding as B
     torch = _t()
@@ -292,6 +294,27 @@ def test_pieces_of_the_classes(name, rows, cin, classes):
     _within(loss, ref.loss, ref.loss_tol + more, "loss")
     ref.ds_logit += 20 * U
     got = B.distillation_backward(dloss, x, w, idx, t, lse, bias, temperature=2.0)
+    for what, g, (r, tol) in zip(("dx", "dw", "dbias"), got, ref.gradients(lse, dloss)):
+        _within(g, r, tol, what)
+
+
+@pytest.mark.parametrize("name,rows", [("bf16", 8193), ("fp32", 70001), ("fp16", 300007)])
+def test_many_rows_of_few_classes(name, rows):
+    """Rows' factors from more than one block, sums for dbias of more than 2048 rows of tiles."""
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    dt = _dt(name)
+    x, w = _randn(rows, 20, seed=1).to(dt), _randn(11, 20, seed=2, scale=0.4).to(dt)
+    bias = _randn(11, seed=3).float()
+    labels = torch.randint(-1, 11, (rows,), generator=torch.Generator().manual_seed(4), dtype=torch.int32).cuda()
+    target, used = _entropy_target(labels, 11, 0.0)
+    ref = Reference(name, x, w, bias, target, used)
+    loss, lse = B.cross_entropy_forward(x, w, labels, bias)
+    _within(lse, ref.lse, ref.lse_tol, "lse")
+    _within(loss, ref.loss, ref.loss_tol, "loss")
+    dloss = (_rand(rows, seed=5) + 0.1).float()
+    dloss[rows - 1] = 40.0
+    got = B.cross_entropy_backward(dloss, x, w, labels, lse, bias)
     for what, g, (r, tol) in zip(("dx", "dw", "dbias"), got, ref.gradients(lse, dloss)):
         _within(g, r, tol, what)
 
