@@ -193,7 +193,10 @@ logits_kernel(Logits a) {
         asm volatile("" ::: "memory");
       }
       float all = 0.f;
-      if (a.totals) {
+      if (a.totals && inside == W) {
+#pragma unroll
+        for (int n = 0; n < NV; ++n) all += v[n];
+      } else if (a.totals) {
 #pragma unroll
         for (int n = 0; n < NV; ++n) all += class_of(n) < inside ? v[n] : 0.f;
       }
@@ -305,69 +308,89 @@ logits_kernel(Logits a) {
 
 // ---- few rows ----------------------------------------------------------------------------------------------------------
 // Up to 64 rows whose weights would have to be laid out anew (fp32, or off the alignment of 16 bytes): straight from memory into 16 x 16
-// MFMAs, as the layers do it, 16 classes of all rows a block, its wavefronts (4 to 16) sharing the reduction.  The forward pass alone;
-// a row's sums are of runs of 16 classes.  16 x 2048 -> 65536 in fp32: 890 us by way of planes in memory, so 130.
+// MFMAs, as the layers do it, 64, 32 or 16 classes of up to 16, 32 or 64 rows a block (what is read of x, and split into planes, serves all of
+// them), its wavefronts (4 to 16) sharing the reduction.  The forward pass alone; a row's sums are of runs of 16 classes.
+// 16 x 2048 -> 65536 in fp32: 890 us by way of planes in memory.
 constexpr int SKINNY_ROWS = 64;
 template <class S, class T, int MB, Loads L, bool TOP>
 __global__ void __launch_bounds__(1024) few_logits_kernel(Logits a, int k_wave) {
-  constexpr int PL = sizeof(S) == 4 ? 3 : 1, U = PL == 3 ? (MB == 4 ? 1 : 2) : L == SINGLE ? 1 : MB == 4 || L == ODD ? 4 : 8;
+  constexpr int PL = sizeof(S) == 4 ? 3 : 1, CB = 4 / MB, U = PL == 3 || L == SINGLE ? 1 : L == ODD ? 2 : 4;
   typedef typename Op<T>::V V;
-  extern __shared__ float red[];  // [wavefront][MB][256]
+  extern __shared__ float red[];  // [wavefront][CB][MB][256]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 16;
-  if (first >= a.N) return;
+  const int64_t block0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (16 * CB);
+  if (block0 >= a.N) return;
   const int r16 = lane & 15, kc = (lane >> 4) * 8;
   const int k0 = wave * k_wave, k1 = min(a.K, k0 + k_wave);
-  const S* one = (const S*)a.w + min(first + r16, (int64_t)a.N - 1) * a.ldw;
-  const S* many[MB];
+  const S *one[CB], *many[MB];
+#pragma unroll
+  for (int c = 0; c < CB; ++c) one[c] = (const S*)a.w + min(block0 + c * 16 + r16, (int64_t)a.N - 1) * a.ldw;
 #pragma unroll
   for (int m = 0; m < MB; ++m) many[m] = (const S*)a.x + min<int64_t>(m * 16 + r16, a.M - 1) * a.ldx;
-  v4f acc[MB], rest[PL == 3 ? MB : 1];
+  v4f acc[CB][MB], rest[CB][MB];
 #pragma unroll
-  for (int m = 0; m < MB; ++m) {
-    acc[m] = v4f{0.f, 0.f, 0.f, 0.f};
-    if constexpr (PL == 3) rest[m] = acc[m];
-  }
+  for (int c = 0; c < CB; ++c)
+#pragma unroll
+    for (int m = 0; m < MB; ++m) acc[c][m] = rest[c][m] = v4f{0.f, 0.f, 0.f, 0.f};
   for (int k = k0; k < k1; k += 32 * U) {
-    Raw8<S> ro[U], rm[U][MB];
+    Raw8<S> ro[U][CB], rm[U][MB];
 #pragma unroll
-    for (int u = 0; u < U; ++u) ro[u] = raw8<S, L>(one, k + u * 32 + kc, k1);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int c = 0; c < CB; ++c) ro[u][c] = raw8<S, L>(one[c], k + u * 32 + kc, k1);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int m = 0; m < MB; ++m) rm[u][m] = raw8<S, L>(many[m], k + u * 32 + kc, k1);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      V po[PL], pm[PL];
-      planes8<S, T>(ro[u], po);
-#pragma unroll
-      for (int m = 0; m < MB; ++m) {
-        planes8<S, T>(rm[u][m], pm);
+      auto add = [&](int c, int m, const V (&po)[PL], const V (&pm)[PL]) {
 #pragma unroll
         for (int i = PL - 1; i >= 0; --i)
 #pragma unroll
           for (int j = PL - 1 - i; j >= 0; --j) {
-            v4f& sum = i + j ? rest[PL == 3 ? m : 0] : acc[m];
+            v4f& sum = i + j ? rest[c][m] : acc[c][m];
             sum = mma16(po[i], pm[j], sum);
           }
+      };
+      V po[PL], pm[CB == 1 ? 1 : MB][PL];  // (one block of classes: the rows' planes in turn)
+      if constexpr (CB == 1) {
+        planes8<S, T>(ro[u][0], po);
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          planes8<S, T>(rm[u][m], pm[0]);
+          add(0, m, po, pm[0]);
+        }
+      } else {
+#pragma unroll
+        for (int m = 0; m < MB; ++m) planes8<S, T>(rm[u][m], pm[m]);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+          planes8<S, T>(ro[u][c], po);
+#pragma unroll
+          for (int m = 0; m < MB; ++m) add(c, m, po, pm[m]);
+        }
       }
     }
   }
 #pragma unroll
-  for (int m = 0; m < MB; ++m) {
-    if constexpr (PL == 3) {
+  for (int c = 0; c < CB; ++c)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[m][e] += finite(acc[m][e]) ? rest[m][e] : 0.f;
+    for (int m = 0; m < MB; ++m) {
+      if constexpr (PL == 3) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[c][m][e] += finite(acc[c][m][e]) ? rest[c][m][e] : 0.f;
+      }
+      *reinterpret_cast<v4f*>(red + (((wave * CB + c) * MB + m) * 64 + lane) * 4) = acc[c][m];
     }
-    *reinterpret_cast<v4f*>(red + ((wave * MB + m) * 64 + lane) * 4) = acc[m];
-  }
   __syncthreads();
   // a wavefront has 16 rows, four threads each with four of the classes
-  const int i = threadIdx.x, row = (i >> 6) * 16 + (i & 15), c = (i & 63) >> 4;
-  if (i >= MB * 64) return;
+  const int i = threadIdx.x, row = (i >> 6) % MB * 16 + (i & 15), c = (i & 63) >> 4;
+  const int64_t first = block0 + (i >> 6) / MB * 16;
+  if (i >= CB * MB * 64 || first >= a.N) return;
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   for (int q = 0; q < waves; ++q) {
-    const v4f t = *reinterpret_cast<const v4f*>(red + (q * MB * 64 + i) * 4);
+    const v4f t = *reinterpret_cast<const v4f*>(red + (q * CB * MB * 64 + i) * 4);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] += t[e];
   }
@@ -422,12 +445,12 @@ __global__ void __launch_bounds__(1024) few_logits_kernel(Logits a, int k_wave) 
 
 template <class S, class T, int MB, Loads L> void run_few_of(hipStream_t st, const Logits& l) {
   // wavefronts of at least 256 values of k each, more of them where there are few blocks
-  const int blocks = ceil_div(l.N, 16), most = blocks >= 1024 ? 4 : blocks >= 256 ? 8 : 16;
+  const int blocks = ceil_div(l.N, 64 / MB), most = blocks >= 1024 ? 4 : blocks >= 256 ? 8 : 16;
   int waves = 4;
   while (waves < most && waves * 512 <= l.K) waves *= 2;
   const int k_wave = (ceil_div(l.K, waves) + 31) & ~31;
-  if (l.labels) OSEQ_LAUNCH((few_logits_kernel<S, T, MB, L, false>), grid_of_blocks(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, l, k_wave);
-  else OSEQ_LAUNCH((few_logits_kernel<S, T, MB, L, true>), grid_of_blocks(blocks), dim3(waves * 64), (size_t)waves * MB * 1024, st, l, k_wave);
+  if (l.labels) OSEQ_LAUNCH((few_logits_kernel<S, T, MB, L, false>), grid_of_blocks(blocks), dim3(waves * 64), (size_t)waves * 4096, st, l, k_wave);
+  else OSEQ_LAUNCH((few_logits_kernel<S, T, MB, L, true>), grid_of_blocks(blocks), dim3(waves * 64), (size_t)waves * 4096, st, l, k_wave);
 }
 template <class S, class T, Loads L> void run_few_by(hipStream_t st, const Logits& l) {
   if (l.M <= 16) run_few_of<S, T, 1, L>(st, l);

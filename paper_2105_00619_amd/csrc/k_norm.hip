@@ -11,44 +11,61 @@ namespace oseq {
 
 namespace {
 
-// Two sums over the G threads of a row (G a power of two; rows of more than a wavefront: `lds` holds two floats a wavefront, a
-// place of its own for every other call)
-template <int G> __device__ __forceinline__ void row_sums(float& a, float& b, float* lds) {
-  a = lanes_sum<(G < 64 ? G : 64)>(a);
-  b = lanes_sum<(G < 64 ? G : 64)>(b);
-  if constexpr (G > 64) {
-    constexpr int WAVES = G / 64;
-    const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) { lds[2 * wave] = a; lds[2 * wave + 1] = b; }
-    __syncthreads();
+// Two sums over the threads of a row: G lanes (a power of two up to 64), or with G = 0 the whole block of up to MAX threads.  `lds` holds two
+// floats a wavefront, a place of its own for every other call, zeros for wavefronts that the block does not have (row_sums_begin): all are
+// read at once, where a loop over those that there are waits for each (16384 x 4096 forward 52 us, so 46).
+template <int MAX> struct RowSums { float2 part[2][MAX / 64]; };
+template <int G, int MAX> __device__ __forceinline__ void row_sums_begin(RowSums<MAX>& lds) {
+  const int i = threadIdx.x % (MAX / 64), waves = blockDim.x >> 6;
+  if (G == 0 && threadIdx.x < 2 * (MAX / 64) && i >= waves) lds.part[threadIdx.x / (MAX / 64)][i] = make_float2(0.f, 0.f);
+}
+template <int G, int MAX> __device__ __forceinline__ void row_sums(float& a, float& b, RowSums<MAX>& lds, int turn) {
+  a = lanes_sum<(G ? G : 64)>(a);
+  b = lanes_sum<(G ? G : 64)>(b);
+  if constexpr (G == 0) {
+    if ((threadIdx.x & 63) == 0) lds.part[turn][threadIdx.x >> 6] = make_float2(a, b);
+    // (not __syncthreads, which waits for the next row's loads and the last one's stores)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     a = b = 0.f;
-    const float* p = lds + wave / WAVES * (2 * WAVES);
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) { a += p[2 * w]; b += p[2 * w + 1]; }
+    for (int w = 0; w < MAX / 64; ++w) {
+      const float2 t = lds.part[turn][w];
+      a += t.x;
+      b += t.y;
+    }
   }
 }
 
-constexpr int threads_of(int lanes) { return lanes < 256 ? 256 : lanes; }
-
-// Eight neighbouring values as they were loaded, n of them inside, zeros beside them.  ONCE: past the caches, 16-bit values.  (As vectors
-// of words: as an array of values the loads of 16384 x 4096 took 55 us forward, so 47.)
+// A thread's eight neighbouring values of a row of `cols`: from column `at` on, the first `skip` of them another thread's (the last threads have
+// the row's last eight; all eight skipped: nothing of the row).  So no load depends on a branch: one that does waits for the loads before it, and
+// rows that do not end with a wavefront took half as long again (15249 x 2304 backward 103 us, 2560 columns 74).
+struct Piece { int at, skip; };
+__device__ __forceinline__ Piece piece_of(int column, int cols) {
+  const int at = max(0, min(column, cols - 8));
+  return {at, min(8, column - at)};
+}
+// ... as they were loaded; rows of fewer than eight values end with zeros.  ONCE: past the caches, 16-bit values.  (As vectors of words: as an
+// array of values the loads of 16384 x 4096 took 55 us forward, so 47.)
 template <class S> struct Raw { Vec<S, 8> v; };
 template <int BYTES> struct Loose16;
 template <> struct Loose16<2> { typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t V; };
 template <> struct Loose16<4> { typedef __attribute__((ext_vector_type(4), aligned(4))) uint32_t V; };
-template <class S, bool ONCE> __device__ __forceinline__ void ask(const S* p, int n, Raw<S>& r) {
+// SHORT: there may be fewer than eight columns.
+template <class S, bool ONCE, bool SHORT> __device__ __forceinline__ void ask(const S* row, const Piece& p, int cols, Raw<S>& r) {
   typedef typename Loose16<sizeof(S)>::V V;
-  if (n == 8) {
+  if (!SHORT || cols >= 8) {
     V c[sizeof(S) / 2];
 #pragma unroll
     for (int i = 0; i < (int)sizeof(S) / 2; ++i) {
-      const V* q = reinterpret_cast<const V*>(p) + i;
+      const V* q = reinterpret_cast<const V*>(row + p.at) + i;
       c[i] = ONCE ? __builtin_nontemporal_load(q) : *q;
     }
     __builtin_memcpy(&r, c, sizeof(r));
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r.v.v[e] = e < n ? p[e] : from_f32<S>(0.f);
+    for (int e = 0; e < 8; ++e) r.v.v[e] = e < cols ? row[e] : from_f32<S>(0.f);
   }
 }
 template <class S> __device__ __forceinline__ void take(const Raw<S>& r, float (&v)[8]) {
@@ -65,6 +82,26 @@ struct NormForward {
   int64_t rows; int cols;
 };
 
+// Whether any thread of the wavefront has less than eight values of its own; the others' wavefronts need no selects (as many as half of what
+// else a forward pass has to do)
+__device__ __forceinline__ bool any_cut(bool cut) { return __ballot(cut) != 0; }
+// what is not the thread's own, or not there: zero
+__device__ __forceinline__ void own(const Piece& p, int cols, float (&v)[8]) {
+  asm volatile("");  // (a branch, not selects)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e >= p.skip && e < cols ? v[e] : 0.f;
+}
+template <bool SHORT, class T> __device__ __forceinline__ void put(T* row, const Piece& p, int cols, const float (&v)[8]) {
+  if (p.skip == 0 && (!SHORT || cols >= 8)) {
+    store8<T>(row + p.at, 8, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e >= p.skip && e < cols) row[p.at + e] = from_f32<T>(v[e]);
+    asm volatile("");  // (or the two ways share their last stores, and the other one is no longer of 16 bytes)
+  }
+}
+
 template <int N> __device__ __forceinline__ void vector_of(const float* p, int c, int n, float other, float (&v)[N]) {
   if (p) load8<float>(p + c, n, v);
 #pragma unroll
@@ -72,30 +109,34 @@ template <int N> __device__ __forceinline__ void vector_of(const float* p, int c
 }
 
 // Mean and variance from the deviations from a first mean: the mean that was rounded in its sum is off, and the deviations, which
-// are exact, say by how much.  G threads have a row, 8 C values each, in pieces that lie side by side for neighbouring threads; a block walks its rows, weight and bias
+// are exact, say by how much.  G threads have a row (0: a block of up to MAX threads), 8 C values each, in pieces that lie side by side for
+// neighbouring threads; a block walks its rows, weight and bias
 // in registers, the next row on its way.
-template <class S, int G, int C>
-__global__ void __launch_bounds__(threads_of(G)) norm_forward_kernel(NormForward a) {
-  constexpr int ROWS = threads_of(G) / G;
-  __shared__ float lds[2][2 * 16];
-  const int t = threadIdx.x % G, r = threadIdx.x / G;
+template <class S, int G, int MAX, int C>
+__global__ void __launch_bounds__(MAX) norm_forward_kernel(NormForward a) {
+  constexpr int ROWS = G ? MAX / G : 1;
+  __shared__ RowSums<MAX> lds;
+  row_sums_begin<G, MAX>(lds);
+  const int lanes = G ? G : blockDim.x, t = G ? threadIdx.x % lanes : threadIdx.x, r = G ? threadIdx.x / lanes : 0;
   float w[C][8], b[C][8];
-  int inside[C];
+  Piece piece[C];
 #pragma unroll
   for (int j = 0; j < C; ++j) {
-    const int c = (j * G + t) * 8;
-    inside[j] = min(8, max(0, a.cols - c));
-    vector_of(a.weight, c, inside[j], 1.f, w[j]);
-    vector_of(a.bias, c, inside[j], 0.f, b[j]);
+    piece[j] = piece_of((j * lanes + t) * 8, a.cols);
+    vector_of(a.weight, piece[j].at, min(8, a.cols), 1.f, w[j]);
+    vector_of(a.bias, piece[j].at, min(8, a.cols), 0.f, b[j]);
   }
   const float n = 1.f / (float)a.cols;
-  const bool whole = a.cols == G * C * 8;
+  bool cut = a.cols < 8;
+#pragma unroll
+  for (int j = 0; j < C; ++j) cut |= piece[j].skip > 0;
+  cut = any_cut(cut);
   const int64_t step = (int64_t)gridDim.x * ROWS;
   Raw<S> next[C];
   auto fetch = [&](int64_t first) {
     const S* x = (const S*)a.x + min(first + r, a.rows - 1) * a.ldx;
 #pragma unroll
-    for (int j = 0; j < C; ++j) ask<S, false>(x + (j * G + t) * 8, inside[j], next[j]);
+    for (int j = 0; j < C; ++j) ask<S, false, G == 8>(x, piece[j], a.cols, next[j]);
   };
   int64_t first = (int64_t)blockIdx.x * ROWS;
   if (first < a.rows) fetch(first);
@@ -105,23 +146,27 @@ __global__ void __launch_bounds__(threads_of(G)) norm_forward_kernel(NormForward
 #pragma unroll
     for (int j = 0; j < C; ++j) {
       take<S>(next[j], v[j]);
+      if (cut) own(piece[j], a.cols, v[j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += v[j][e];
     }
     if (first + step < a.rows) fetch(first + step);
-    row_sums<G>(sum, square, lds[0]);
+    asm volatile("" ::: "memory");  // (the loads go out here)
+    row_sums<G, MAX>(sum, square, lds, 0);
     const float mean = sum * n;
     sum = square = 0.f;
 #pragma unroll
-    for (int j = 0; j < C; ++j)
+    for (int j = 0; j < C; ++j) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[j][e] -= mean;
+      if (cut) own(piece[j], a.cols, v[j]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        v[j][e] -= mean;
-        if (!whole) v[j][e] = e < inside[j] ? v[j][e] : 0.f;
         sum += v[j][e];
         square = __fmaf_rn(v[j][e], v[j][e], square);
       }
-    row_sums<G>(sum, square, lds[1]);
+    }
+    row_sums<G, MAX>(sum, square, lds, 1);
     const float off = sum * n, rstd = 1.f / sqrtf(fmaxf(square * n - off * off, 0.f) + a.eps);
     const int64_t row = first + r;
     if (row >= a.rows) continue;
@@ -130,7 +175,7 @@ __global__ void __launch_bounds__(threads_of(G)) norm_forward_kernel(NormForward
     for (int j = 0; j < C; ++j) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[j][e] = __fmaf_rn((v[j][e] - off) * rstd, w[j][e], b[j][e]);
-      if (inside[j] > 0) store8<S>((S*)a.y + row * a.ldy + (j * G + t) * 8, inside[j], v[j]);
+      put<G == 8>((S*)a.y + row * a.ldy, piece[j], a.cols, v[j]);
     }
   }
 }
@@ -138,7 +183,7 @@ __global__ void __launch_bounds__(threads_of(G)) norm_forward_kernel(NormForward
 // Rows of more than 16384 columns: a block each, which reads it for every sum (the second and third time from the caches)
 template <class S>
 __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormForward a) {
-  __shared__ float lds[2][2 * 16];
+  __shared__ RowSums<1024> lds;
   const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (row >= a.rows) return;
   const S* x = (const S*)a.x + row * a.ldx;
@@ -154,7 +199,7 @@ __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormForward a) 
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum += v[e];
   });
-  row_sums<1024>(sum, square, lds[0]);
+  row_sums<0, 1024>(sum, square, lds, 0);
   const float n = 1.f / (float)a.cols, first = sum * n;
   sum = square = 0.f;
   each8([&](int, int k, float (&v)[8]) {
@@ -165,7 +210,7 @@ __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormForward a) 
       square = __fmaf_rn(d, d, square);
     }
   });
-  row_sums<1024>(sum, square, lds[1]);
+  row_sums<0, 1024>(sum, square, lds, 1);
   const float off = sum * n, rstd = 1.f / sqrtf(fmaxf(square * n - off * off, 0.f) + a.eps);
   if (threadIdx.x == 0 && a.mean) { a.mean[row] = first + off; a.rstd[row] = rstd; }
   each8([&](int c, int k, float (&v)[8]) {
@@ -189,25 +234,29 @@ struct NormBackward {
 };
 
 // A block walks its rows, the next one's values on their way; a thread keeps the same columns of all of them, and their sums for dweight and dbias in
-// registers.  dy is zero beside the matrix, so nothing else has to be left out.  Without SUMS it
+// registers.  dy is taken for zero where a value is not the thread's own, so nothing else has to be left out.  Without SUMS it
 // makes dx alone.
-template <class S, int G, int C, bool SUMS, bool ONCE>
-__global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackward a) {
-  constexpr int ROWS = threads_of(G) / G;
-  __shared__ float lds[2][2 * 16];
+template <class S, int G, int MAX, int C, bool SUMS, bool ONCE>
+__global__ void __launch_bounds__(MAX) norm_backward_kernel(NormBackward a) {
+  constexpr int ROWS = G ? MAX / G : 1;
+  __shared__ RowSums<MAX> lds;
+  row_sums_begin<G, MAX>(lds);
   __shared__ float part[ROWS > 1 && SUMS ? 2 : 1][ROWS > 1 && SUMS ? ROWS : 1][ROWS > 1 && SUMS ? G * 8 * C : 1];
-  const int t = threadIdx.x % G, r = threadIdx.x / G;
+  const int lanes = G ? G : blockDim.x, t = G ? threadIdx.x % lanes : threadIdx.x, r = G ? threadIdx.x / lanes : 0;
   float w[C][8], dw[C][8], db[C][8];
-  int inside[C];
+  Piece piece[C];
 #pragma unroll
   for (int j = 0; j < C; ++j) {
-    const int c = (j * G + t) * 8;
-    inside[j] = min(8, max(0, a.cols - c));
-    vector_of(a.weight, c, inside[j], 1.f, w[j]);
+    piece[j] = piece_of((j * lanes + t) * 8, a.cols);
+    vector_of(a.weight, piece[j].at, min(8, a.cols), 1.f, w[j]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) dw[j][e] = db[j][e] = 0.f;
   }
   const float n = 1.f / (float)a.cols;
+  bool cut = a.cols < 8;
+#pragma unroll
+  for (int j = 0; j < C; ++j) cut |= piece[j].skip > 0;
+  cut = any_cut(cut);
   const int64_t step = (int64_t)gridDim.x * ROWS;
   const bool add = a.residual && a.dx, stats = a.dx || a.dweight;
   Raw<S> nx[C] = {}, ny[C], nr[C];
@@ -217,10 +266,9 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
     const S *x = (const S*)a.x + row * a.ldx, *dy = (const S*)a.dy + row * a.lddy, *res = (const S*)a.residual + row * a.ldr;
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      const int c = (j * G + t) * 8;
-      if (stats) ask<S, ONCE>(x + c, inside[j], nx[j]);
-      ask<S, ONCE>(dy + c, first + r < a.rows ? inside[j] : 0, ny[j]);
-      if (add) ask<S, ONCE>(res + c, inside[j], nr[j]);
+      if (stats) ask<S, ONCE, G == 8>(x, piece[j], a.cols, nx[j]);
+      ask<S, ONCE, G == 8>(dy, piece[j], a.cols, ny[j]);
+      if (add) ask<S, ONCE, G == 8>(res, piece[j], a.cols, nr[j]);
     }
     if (stats) {
       mean = a.mean[row];
@@ -235,11 +283,13 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
     const bool real = row < a.rows;
     float h[C][8], u[C][8], su = 0.f, suh = 0.f;
     const float rs = rstd;
+    const bool all = !cut && first + ROWS <= a.rows;
     Raw<S> res[C];
 #pragma unroll
     for (int j = 0; j < C; ++j) {
       take<S>(nx[j], h[j]);
       take<S>(ny[j], u[j]);
+      if (!all) own(real ? piece[j] : Piece{0, 8}, a.cols, u[j]);
       if (add) res[j] = nr[j];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -254,8 +304,9 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
       }
     }
     if (first + step < a.rows) fetch(first + step);
+    asm volatile("" ::: "memory");  // (the loads go out here)
     if (!a.dx) continue;
-    row_sums<G>(su, suh, lds[turn]);
+    row_sums<G, MAX>(su, suh, lds, turn);
     su *= n;
     suh *= n;
     if (!real) continue;
@@ -268,7 +319,7 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
         u[j][e] = __fmaf_rn(-h[j][e], suh, u[j][e] - su);
         u[j][e] = add ? __fmaf_rn(rs, u[j][e], more[e]) : rs * u[j][e];
       }
-      if (inside[j] > 0) store8<S>((S*)a.dx + row * a.lddx + (j * G + t) * 8, inside[j], u[j]);
+      put<G == 8>((S*)a.dx + row * a.lddx, piece[j], a.cols, u[j]);
     }
   }
   if (!SUMS || (!a.dweight && !a.dbias)) return;
@@ -278,11 +329,13 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
     for (int j = 0; j < C; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        part[0][r][(j * G + t) * 8 + e] = dw[j][e];
-        part[1][r][(j * G + t) * 8 + e] = db[j][e];
+        if (e >= piece[j].skip) {
+          part[0][r][piece[j].at + e] = dw[j][e];
+          part[1][r][piece[j].at + e] = db[j][e];
+        }
       }
     __syncthreads();
-    for (int c = threadIdx.x; c < a.cols; c += threads_of(G)) {
+    for (int c = threadIdx.x; c < a.cols; c += MAX) {
       float s = 0.f, b = 0.f;
 #pragma unroll
       for (int q = 0; q < ROWS; ++q) { s += part[0][q][c]; b += part[1][q][c]; }
@@ -292,9 +345,8 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
   } else {
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      if (inside[j] <= 0) break;
-      if (dweight) store8<float>(dweight + (j * G + t) * 8, inside[j], dw[j]);
-      if (dbias) store8<float>(dbias + (j * G + t) * 8, inside[j], db[j]);
+      if (dweight) put<G == 8>(dweight, piece[j], a.cols, dw[j]);
+      if (dbias) put<G == 8>(dbias, piece[j], a.cols, db[j]);
     }
   }
 }
@@ -302,7 +354,7 @@ __global__ void __launch_bounds__(threads_of(G)) norm_backward_kernel(NormBackwa
 // Rows of more than 16384 columns: dx as above, a block for each row
 template <class S>
 __global__ void __launch_bounds__(1024) norm_dx_long_kernel(NormBackward a) {
-  __shared__ float lds[2 * 16];
+  __shared__ RowSums<1024> lds;
   const int64_t row = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
   if (row >= a.rows) return;
   const float mean = a.mean[row], rstd = a.rstd[row], n = 1.f / (float)a.cols;
@@ -326,7 +378,7 @@ __global__ void __launch_bounds__(1024) norm_dx_long_kernel(NormBackward a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) { su += u[e]; suh = __fmaf_rn(u[e], h[e], suh); }
   });
-  row_sums<1024>(su, suh, lds);
+  row_sums<0, 1024>(su, suh, lds, 0);
   su *= n;
   suh *= n;
   each8([&](int c, int k, float (&h)[8], float (&u)[8]) {
@@ -404,32 +456,40 @@ __global__ void __launch_bounds__(256) norm_clear_kernel(float* a, float* b, int
   if (b) b[i] = 0.f;
 }
 
-// Blocks of 256 threads (of more threads as many fewer)
-constexpr int FORWARD_BLOCKS = 2048, BACKWARD_BLOCKS = 1024;
+// Blocks that walk the rows: as many as are on the card together, by their registers 32 wavefronts on a CU forward and 16 backward (a few
+// more take as long again: 15249 x 2348 backward in 819 blocks of five wavefronts 154 us).
+constexpr int FORWARD_WAVES = 32, BACKWARD_WAVES = 16;
+int blocks_of(int threads, int waves) { return 256 * std::max(1, waves / (threads / 64)); }
 // Whether a gradient's matrices are read past the caches: where they are larger than the last of those holds (256 MB), which else still has them
 // from whatever made them.  bf16, past the caches / through them: 16384 x 4096 91 / 102 us, 8192 x 8192 88 / 103; 65536 x 512 49 / 45, 7003 x 1777 34 / 28.
 bool once(const optorch_layer_norm_t& a) { return a.rows * (int64_t)a.cols * 2 * (a.residual ? 4 : 3) > (384ll << 20); }
 
-// The threads of a row, eight values each (or 16 of 1024 threads); 0 where it does not fit
+// The threads of a row: a power of two of lanes up to 64 (512 columns), as many wavefronts as it takes up to 8192 columns, eight values each, or
+// 16 of 1024 threads; 0: rows longer than that.  (Powers of two there too: 15249 x 2348 in bf16 backward 115 us, so 78.)
 int lanes_of(int cols) {
+  if (cols > 16384) return 0;
+  if (cols > 8192) return 1024;
+  if (cols > 512) return ceil_div(cols, 512) * 64;
   int g = 8;
-  while (g < 1024 && g * 8 < cols) g *= 2;
-  return cols <= 16384 ? g : 0;
+  while (g * 8 < cols) g *= 2;
+  return g;
 }
-// f(threads of a row, eights of values that each has)
+int threads_of(int lanes) { return std::max(lanes, lanes > 64 ? 0 : 256); }
+// f(lanes of a row or 0, most threads of a block, eights of values that each has)
 template <class F> void with_lanes(int cols, F&& f) {
-  switch (lanes_of(cols)) {
-    case 8: f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{}); break;
-    case 16: f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{}); break;
-    case 32: f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{}); break;
-    case 64: f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{}); break;
-    case 128: f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{}); break;
-    case 256: f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{}); break;
-    case 512: f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{}); break;
-    default:
-      if (cols <= 8192) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
-      else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
-  }
+  const int lanes = lanes_of(cols);
+  auto go = [&](auto g, auto most, auto c) { f(g, most, c); };
+  typedef std::integral_constant<int, 0> Block;
+  typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, 256> T256;
+  if (lanes == 8) go(std::integral_constant<int, 8>{}, T256{}, One{});
+  else if (lanes == 16) go(std::integral_constant<int, 16>{}, T256{}, One{});
+  else if (lanes == 32) go(std::integral_constant<int, 32>{}, T256{}, One{});
+  else if (lanes == 64) go(std::integral_constant<int, 64>{}, T256{}, One{});
+  else if (lanes <= 256) go(Block{}, T256{}, One{});
+  else if (lanes <= 512) go(Block{}, std::integral_constant<int, 512>{}, One{});
+  else if (cols <= 8192) go(Block{}, std::integral_constant<int, 1024>{}, One{});
+  else go(Block{}, std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
 }
 
 template <class S> void forward_of(const optorch_layer_norm_t& a) {
@@ -439,11 +499,9 @@ template <class S> void forward_of(const optorch_layer_norm_t& a) {
     OSEQ_LAUNCH(norm_forward_long_kernel<S>, grid_of_blocks(a.rows), dim3(1024), 0, st, f);
     return;
   }
-  with_lanes(a.cols, [&](auto g, auto c) {
-    constexpr int G = g, C = c;
-    const dim3 grid(std::min(ceil_div(a.rows, threads_of(G) / G), FORWARD_BLOCKS * 256 / threads_of(G))), block(threads_of(G));
-    OSEQ_LAUNCH((norm_forward_kernel<S, G, C>), grid, block, 0, st, f);
-  });
+  const int lanes = lanes_of(a.cols), threads = threads_of(lanes);
+  const dim3 grid((unsigned)std::min<int64_t>((a.rows + threads / lanes - 1) / (threads / lanes), blocks_of(threads, FORWARD_WAVES))), block(threads);
+  with_lanes(a.cols, [&](auto g, auto most, auto c) { OSEQ_LAUNCH((norm_forward_kernel<S, g, most, c>), grid, block, 0, st, f); });
 }
 
 template <class S> void backward_of(const optorch_layer_norm_t& a, const NormPlan& p) {
@@ -461,16 +519,16 @@ template <class S> void backward_of(const optorch_layer_norm_t& a, const NormPla
   if (!p.lanes) {
     if (a.dx) OSEQ_LAUNCH(norm_dx_long_kernel<S>, grid_of_blocks(a.rows), dim3(1024), 0, st, b);
   } else if (a.dx || !apart) {
-    with_lanes(a.cols, [&](auto g, auto c) {
-      constexpr int G = g, C = c;
-      const dim3 grid(apart ? (int)std::min<int64_t>(a.rows, 256) : p.blocks), block(threads_of(G));
+    const dim3 grid(apart ? (unsigned)std::min<int64_t>(a.rows, 256) : p.blocks), block(threads_of(p.lanes));
+    with_lanes(a.cols, [&](auto g, auto most, auto c) {
+      constexpr int G = g, MAX = most, C = c;
       if constexpr (sizeof(S) == 2) {
         if (once(a)) {
-          OSEQ_LAUNCH((norm_backward_kernel<S, G, C, C == 1, true>), grid, block, 0, st, b);
+          OSEQ_LAUNCH((norm_backward_kernel<S, G, MAX, C, C == 1, true>), grid, block, 0, st, b);
           return;
         }
       }
-      OSEQ_LAUNCH((norm_backward_kernel<S, G, C, C == 1, false>), grid, block, 0, st, b);
+      OSEQ_LAUNCH((norm_backward_kernel<S, G, MAX, C, C == 1, false>), grid, block, 0, st, b);
     });
   }
   if (apart && sums) OSEQ_LAUNCH(norm_sums_long_kernel<S>, dim3(ceil_div(a.cols, 256), p.blocks), dim3(256), 0, st, b, (int64_t)ceil_div(a.rows, p.blocks));
@@ -485,7 +543,8 @@ NormPlan plan_norm_backward(const optorch_layer_norm_t& a) {
   p.lanes = lanes_of(a.cols);
   if (p.lanes && a.cols <= 8192) {
     const int threads = threads_of(p.lanes), rows = threads / p.lanes;
-    p.blocks = (int)std::min<int64_t>((a.rows + rows - 1) / rows, BACKWARD_BLOCKS * 256 / threads);
+    p.blocks = (int)std::min<int64_t>((a.rows + rows - 1) / rows, blocks_of(threads, BACKWARD_WAVES));
+    if (p.blocks <= 4) p.blocks = 1;  // (four turns of one block: no second launch to join them)
   } else {
     p.blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, 2048 / ((a.cols + 255) / 256)));
   }

@@ -64,7 +64,7 @@ def _untouched(buf, before, rows, cols, pad, shift):
 
 # (rows, cols): single values, one row, one column, odd sizes, the ends of each kind of block and their neighbours, rows longer than a block keeps
 SIZES = [(1, 1), (5, 1), (1, 8), (3, 5), (2, 17), (33, 128), (70, 129), (257, 256), (64, 264), (31, 512), (5, 1000), (9, 1024), (9, 1031), (5, 2048),
-         (1030, 2049), (1, 4096), (7, 4097), (3, 8192), (5, 8200), (2, 16384), (3, 16385), (37, 20000), (2, 40001), (20011, 24), (2100, 640)]
+         (1030, 2049), (1, 4096), (7, 4097), (3, 8192), (5, 8200), (2, 16384), (3, 16385), (37, 20000), (2, 40001), (20011, 24), (2100, 640), (300, 2348), (4, 600)]
 
 
 def _case(rows, cols, name):
