@@ -44,7 +44,13 @@ template <class O, bool DW> __device__ __forceinline__ void finish(const Grad& g
   const float f = (DW ? *g.scale : g.info[row].w) * g.unscale;
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] *= f;
-  store8<O>((O*)g.out + row * g.ldo + col, n, v);
+  O* out = (O*)g.out + row * g.ldo + col;
+  if (n == 8) {
+    store8<O>(out, 8, v);
+  } else {
+    store8<O>(out, n, v);
+    asm volatile("");  // (or the two ways share their last stores, and the other one is no longer of 16 bytes)
+  }
 }
 
 // One block's tile of a product.  O: type of the result; T: of the planes
