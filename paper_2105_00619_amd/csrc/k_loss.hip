@@ -69,7 +69,8 @@ __device__ __forceinline__ void halves(float v, float& a, float& b) {
 __device__ __forceinline__ float halves_max(float v) { float a, b; halves(v, a, b); return fmaxf(a, b); }
 __device__ __forceinline__ float halves_sum(float v) { float a, b; halves(v, a, b); return a + b; }
 
-// exp(k' (v - from)), k = k' log2(e).  16 bits: one multiply-add, off by the rounding of k from besides (2^-24 |k from| of the result).
+// exp(k' (v - from)), k = k' log2(e).  16 bits: one multiply-add, and what counts as `from` is k from as rounded, a power of two's exponent: the
+// rows' sums are kept beside that and joined with it.
 template <bool FULL> __device__ __forceinline__ float exp_above(float v, float from, float k) {
   return __builtin_amdgcn_exp2f(FULL ? (v - from) * k : __fmaf_rn(v, k, -from * k));
 }
@@ -221,16 +222,18 @@ logits_kernel(Logits a) {
       if (a.totals) all = halves_sum(all) * a.per_temperature;
       if (!half && real) {
         const int64_t at = (int64_t)column * a.M + row;
-        a.sums[at] = make_float2(infinite ? 3.4028235e38f : most * a.per_temperature, sum);
+        a.sums[at] = make_float2(infinite ? 3.4028235e38f : most * (FULL ? a.per_temperature : k), sum);
         if (a.totals) a.totals[at] = all;
       }
     } else {
+      // (16 bits: what rounding lse log2(e) leaves goes into the row's factor of p)
       const float lse = FULL ? info[j].x : info[j].x * LOG2E, spread = a.spread * info[j].z;
+      const float factor_p = FULL ? info[j].y : info[j].y * __fmaf_rn(__fmaf_rn(info[j].x, LOG2E, -lse), -0.69314718f, 1.f);
       const bool used = real && info[j].z != 0.f;
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
         const float p = __builtin_amdgcn_exp2f(FULL ? (v[n] * a.per_temperature - lse) * LOG2E : __fmaf_rn(v[n], k, -lse));
-        v[n] = __fmaf_rn(p, info[j].y, -spread);
+        v[n] = __fmaf_rn(p, factor_p, -spread);
       }
       if (inside < W) {
 #pragma unroll
@@ -689,6 +692,7 @@ __global__ void __launch_bounds__(N < 256 ? 256 : N) teacher_kernel(Teacher a) {
 // ---- forward: a row's sums joined --------------------------------------------------------------------------------------
 struct Join {
   const float2* sums; const float* totals; const float* picked;
+  bool exponents;                  // the maxima are exponents of two
   int64_t rows;
   int columns, runs, log_rows;     // of the table of a teacher's entries, of the sums; a block's rows: 1 << log_rows
   const int32_t* labels; int classes;
@@ -705,10 +709,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
   const int rows = 1 << a.log_rows, rl = threadIdx.x & (rows - 1), slot = threadIdx.x >> a.log_rows, slots = JOIN_THREADS >> a.log_rows;
   const int64_t wanted = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * rows + rl, row = min(wanted, a.rows - 1);
   float most = -__builtin_inff(), sum = 0.f, extra = 0.f;
-  auto join = [](float& m, float& l, float m2, float l2) {
+  const float unit = a.exponents ? 1.f : LOG2E;
+  auto join = [&](float& m, float& l, float m2, float l2) {
     // (a maximum that is NaN has a sum that is; one of -infinity a sum of zero)
     const float top = fmaxf(m, m2);
-    if (top != -__builtin_inff()) l = l * __builtin_amdgcn_exp2f((m - top) * LOG2E) + l2 * __builtin_amdgcn_exp2f((m2 - top) * LOG2E);
+    if (top != -__builtin_inff()) l = l * __builtin_amdgcn_exp2f((m - top) * unit) + l2 * __builtin_amdgcn_exp2f((m2 - top) * unit);
     else l += l2;
     m = top;
   };
@@ -769,7 +774,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
     }
   }
   if (slot || wanted >= a.rows) return;
-  const float lse = all.x + logf(all.y);
+  // (an exponent of two: one product in 64 bits, so that log(2) is not rounded a second time, and -infinity stays what it is)
+  const float lse = a.exponents ? (float)((double)(all.x + log2f(all.y)) * 0.6931471805599453) : all.x + logf(all.y);
   float loss;
   if (teacher) {
     const float flag = a.flag[row];
@@ -1011,6 +1017,7 @@ template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t
     each_piece<S, T, PL>(a, p, l, [&] { run_logits<S, T, false>(st, l, p.wave); });
   }
   Join j = {};
+  j.exponents = PL == 1 && !p.few && !p.stream;
   j.sums = l.sums; j.totals = l.totals; j.picked = l.picked;
   j.rows = a.rows; j.columns = p.columns; j.runs = p.stream ? p.stream : p.columns;
   // (few rows: a block each)
