@@ -3,6 +3,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include <string.h>
 
 #include <string>
 
@@ -50,7 +51,10 @@ inline int check_workspace(const void* p, uint64_t given, uint64_t bytes) {
 // What a call writes against everything that it reads or writes besides
 struct Operands {
   static constexpr int MOST = 16;
-  struct Named { const char* name; Place p; bool written; } list[MOST];
+  struct Named {
+    const char* name; Place p; bool written;
+    bool is(const char* n) const { return strcmp(name, n) == 0; }
+  } list[MOST];
   int n = 0;
   void add(const char* name, const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes, bool written) {
     if (p && rows > 0 && cols > 0) list[n++] = Named{name, place_in(p, rows, cols, ld, bytes), written};

@@ -64,8 +64,8 @@ static int norm_overlaps(const optorch_layer_norm_t* a, bool backward, uint64_t 
     o.vector("dbias", a->dbias, cols, 4, true);
     o.vector("workspace", workspace_bytes ? a->workspace : nullptr, (int64_t)workspace_bytes, 1, true);
   }
-  return o.apart([&](const Operands::Named& p, const Operands::Named& q) {
-    return backward && p.p.at == (uintptr_t)a->residual && q.p.at == (uintptr_t)a->dx && same_place(p.p, q.p);
+  return o.apart([](const Operands::Named& p, const Operands::Named& q) {
+    return p.is("residual") && q.is("dx") && same_place(p.p, q.p);
   });
 }
 

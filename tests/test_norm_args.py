@@ -54,6 +54,14 @@ def test_refusals(kw, backward, word):
     assert word in lib.optorch_matrix_last_error().decode()
 
 
+@pytest.mark.parametrize("name", ["dy", "x"])
+def test_only_the_residual_may_lie_where_dx_does(name):
+    """... and what is read beside it may not, wherever the residual is."""
+    lib = B.load_library()
+    assert lib.optorch_layer_norm_backward(C.byref(_norm(**{name: 5 << 24, "residual": 5 << 24}))) == E_INVALID
+    assert "%s and dx overlap" % name in lib.optorch_matrix_last_error().decode()
+
+
 def test_null_arguments_and_a_short_workspace():
     lib = B.load_library()
     assert lib.optorch_layer_norm_forward(None) == E_INVALID and lib.optorch_layer_norm_backward(None) == E_INVALID
