@@ -70,8 +70,8 @@ static int linear_overlaps(const optorch_linear_t* a, bool backward, uint64_t wo
     o.add("dbias", a->dbias, 1, out, out, 4, true);
   }
   o.add("workspace", workspace_bytes ? a->workspace : nullptr, 1, (int64_t)workspace_bytes, (int64_t)workspace_bytes, 1, true);
-  return o.apart([&](const Operands::Named& p, const Operands::Named& q) {
-    return !backward && p.p.at == (uintptr_t)a->residual && q.p.at == (uintptr_t)a->y && same_place(p.p, q.p);
+  return o.apart([](const Operands::Named& p, const Operands::Named& q) {
+    return p.is("residual") && q.is("y") && same_place(p.p, q.p);
   });
 }
 

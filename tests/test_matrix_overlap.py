@@ -72,6 +72,16 @@ def test_linear_buffers_that_overlap(backward, written, other):
     assert lib.optorch_linear_forward(C.byref(a)) == B.E_INVALID and "overlap" in lib.optorch_matrix_last_error().decode()
 
 
+def test_x_where_the_residual_and_y_are():
+    """The residual may lie where y does, x may not: y's tiles would be written while others read x."""
+    a = _apart()
+    a.out_features = a.ldw = a.ldr = a.ldy = a.ldz = IN
+    a.residual = a.y = a.x
+    lib = B.load_library()
+    assert lib.optorch_linear_forward(C.byref(a)) == B.E_INVALID
+    assert "x and y overlap" in lib.optorch_matrix_last_error().decode()
+
+
 def test_flat_vectors_that_overlap():
     f = getattr(B.load_library(), "_ZN4oseq21ortho_vectors_overlapEPK13optorch_orthoPKviS4_i")
     f.argtypes, f.restype = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32], C.c_bool
