@@ -123,7 +123,7 @@ typedef struct {
   int32_t in_features, classes;       /* 1 .. 2^22 - 8, leading dimensions too; fp32: 1 .. 2^20 - 16 */
   const void* x; int64_t ldx;         /* rows x in */
   const void* w; int64_t ldw;         /* classes x in */
-  const float* bias;                  /* classes, or NULL; -infinity leaves a class out */
+  const float* bias;                  /* classes, or NULL; -infinity leaves a class out (with label_smoothing: losses of infinity) */
   const int32_t* labels;              /* rows, or NULL: a teacher */
   const int32_t* indices; int64_t ldi;/* rows x top */
   const void* teacher; int64_t ldt;   /* rows x top */

@@ -886,7 +886,8 @@ def _loss_backward(a, dloss, x, lse, bias, need, dx, dw, dbias):
 def cross_entropy_forward(x, w, labels, bias=None, *, label_smoothing=0.0, z_loss=0.0):
     """(loss, lse), float32 [rows] each: with s = x w^T + bias, lse = log(sum(exp(s))) and loss = lse - (target . s) + z_loss lse^2 for
     every row, where target is 1 at the row's label, or 1 - label_smoothing there and label_smoothing / classes everywhere.  x [rows, in]
-    and w [classes, in] in fp32, bf16 or fp16, labels int32 [rows], bias float32 [classes] (-infinity leaves a class out).  A
+    and w [classes, in] in fp32, bf16 or fp16, labels int32 [rows], bias float32 [classes] (-infinity leaves a class out; with label_smoothing losses are then
+    infinite).  A
     negative label leaves the row out: its loss is zero; a label not below `classes` makes it NaN.  The logits are never held.  Nothing
     is recorded for autograd: the gradients are `cross_entropy_backward`'s."""
     a = _loss_args(x, w, bias)

@@ -41,9 +41,10 @@ template <class O, bool DW> __device__ __forceinline__ void finish(const Grad& g
     store_f32<float, 8>(g.acc + row * ((g.N + 7) & ~7) + col, v);
     return;
   }
-  const float f = (DW ? *g.scale : g.info[row].w) * g.unscale;
+  const float4 known = DW ? make_float4(0.f, 0.f, 1.f, *g.scale) : g.info[row];
+  const float f = known.w * g.unscale;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] *= f;
+  for (int e = 0; e < 8; ++e) v[e] = known.z == 0.f ? 0.f : v[e] * f;  // (a row that is left out: weights that are not finite say nothing of it)
   O* out = (O*)g.out + row * g.ldo + col;
   if (n == 8) {
     store8<O>(out, 8, v);

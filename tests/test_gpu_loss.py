@@ -439,6 +439,41 @@ def test_a_sure_student_and_large_logits():
     assert torch.equal(dx, 400 * (torch.eye(64, device="cuda") - torch.eye(64, device="cuda").roll(1, 1)))
 
 
+@pytest.mark.parametrize("rows", [40, 300])
+@pytest.mark.parametrize("name", DTYPES)
+def test_left_out_rows_keep_no_gradient_where_weights_are_not_finite(name, rows):
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    dt = _dt(name)
+    x, w = _randn(rows, 72, seed=1).to(dt), _randn(200, 72, seed=2, scale=0.2).to(dt)
+    w[5, 3], w[170, 70] = math.nan, math.inf
+    labels = torch.arange(rows, dtype=torch.int32, device="cuda") % 150
+    labels[[3, 17]] = -1
+    dloss = torch.ones(rows, device="cuda")
+    dloss[30] = 0
+    loss, lse = B.cross_entropy_forward(x, w, labels)
+    assert not bool(loss[[3, 17]].any()) and not bool(torch.isfinite(loss[4]))
+    dx = B.cross_entropy_backward(dloss, x, w, labels, lse, need=("dx",))[0]
+    assert not bool(dx[[3, 17, 30]].any()) and bool(torch.isnan(dx[4]).any())
+
+
+@pytest.mark.parametrize("name", DTYPES)
+def test_smoothing_over_a_class_that_is_left_out(name):
+    """Its share of the target is a logit of -infinity: an infinite loss, and gradients that are those of the formula."""
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    dt = _dt(name)
+    x, w = _randn(70, 72, seed=1).to(dt), _randn(40, 72, seed=2, scale=0.2).to(dt)
+    bias = torch.zeros(40, device="cuda")
+    bias[39] = -math.inf
+    labels = torch.arange(70, dtype=torch.int32, device="cuda") % 39
+    loss, lse = B.cross_entropy_forward(x, w, labels, bias, label_smoothing=0.1)
+    assert bool((loss == math.inf).all()) and bool(torch.isfinite(lse).all())
+    db = B.cross_entropy_backward(torch.ones(70, device="cuda"), x, w, labels, lse, bias, label_smoothing=0.1, need=("dbias",))[2]
+    # 70 equal terms of a fortieth of 0.1, each off by its rounding and its product's, and a sum's 70 roundings
+    assert abs(float(db[39]) + 70 * 0.1 / 40) <= 73 * U * 70 * 0.1 / 40
+
+
 @pytest.mark.parametrize("name", DTYPES)
 def test_factors_of_rows_that_are_far_apart(name):
     """dloss from 1e-6 to 1: every row's dx as exact as the others', dw as exact as its largest terms."""
