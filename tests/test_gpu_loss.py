@@ -439,6 +439,40 @@ def test_a_sure_student_and_large_logits():
     assert torch.equal(dx, 400 * (torch.eye(64, device="cuda") - torch.eye(64, device="cuda").roll(1, 1)))
 
 
+def test_python_checks_name_what_is_wrong():
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    x, w, labels = torch.zeros(6, 8, device="cuda"), torch.zeros(5, 8, device="cuda"), torch.zeros(6, dtype=torch.int32, device="cuda")
+    rows = torch.zeros(6, device="cuda")
+    idx, t = torch.zeros(6, 2, dtype=torch.int32, device="cuda"), torch.zeros(6, 2, device="cuda")
+    fails = [
+        (ValueError, "GPU", lambda: B.cross_entropy_forward(x.cpu(), w, labels)),
+        (TypeError, "labels", lambda: B.cross_entropy_forward(x, w, labels.long())),
+        (TypeError, "labels", lambda: B.cross_entropy_forward(x, w, labels.cpu())),
+        (ValueError, "labels", lambda: B.cross_entropy_forward(x, w, labels[:5])),
+        (ValueError, "labels", lambda: B.cross_entropy_forward(x, w, labels.repeat(2)[::2])),
+        (TypeError, "w", lambda: B.cross_entropy_forward(x, w.half(), labels)),
+        (ValueError, "w", lambda: B.cross_entropy_forward(x, w[:, :7], labels)),
+        (ValueError, "bias", lambda: B.cross_entropy_forward(x, w, labels, rows)),
+        (B.OptorchError, "label_smoothing", lambda: B.cross_entropy_forward(x, w, labels, label_smoothing=1.5)),
+        (ValueError, "dloss", lambda: B.cross_entropy_backward(rows[:5], x, w, labels, rows)),
+        (ValueError, "lse", lambda: B.cross_entropy_backward(rows, x, w, labels, rows.repeat(2)[::2])),
+        (ValueError, "need", lambda: B.cross_entropy_backward(rows, x, w, labels, rows, need=("dy",))),
+        (ValueError, "need", lambda: B.cross_entropy_backward(rows, x, w, labels, rows, need=())),
+        (ValueError, "dw: given", lambda: B.cross_entropy_backward(rows, x, w, labels, rows, need=("dx",), dw=w)),
+        (B.OptorchError, "overlap", lambda: B.cross_entropy_backward(rows, x, w, labels, rows, dw=w)),
+        (TypeError, "indices", lambda: B.distillation_forward(x, w, idx.long(), t)),
+        (ValueError, "indices", lambda: B.distillation_forward(x, w, idx, t[:, :1])),
+        (ValueError, "next to each other", lambda: B.distillation_forward(x, w, idx.t().contiguous().t(), t)),
+        (B.OptorchError, "temperature", lambda: B.distillation_forward(x, w, idx, t, temperature=0.0)),
+        (B.OptorchError, "top", lambda: B.distillation_forward(x, w, idx.repeat(1, 513), t.repeat(1, 513))),
+    ]
+    for i, (kind, word, call) in enumerate(fails):
+        with pytest.raises(kind, match=word):
+            call()
+            pytest.fail("call %d was taken" % i)
+
+
 @pytest.mark.parametrize("rows", [40, 300])
 @pytest.mark.parametrize("name", DTYPES)
 def test_left_out_rows_keep_no_gradient_where_weights_are_not_finite(name, rows):
