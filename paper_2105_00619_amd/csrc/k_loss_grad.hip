@@ -137,7 +137,7 @@ template <class O, bool DW> __device__ __forceinline__ void join_parts(const Gra
 template <class O, bool DW> __global__ void __launch_bounds__(256) grad_join_kernel(Grad a) { join_parts<O, DW>(a, blockIdx.x, gridDim.x); }
 
 // Both products and the sums for dbias in one launch, where neither product fills the card: they read the same ds and nothing of each other.
-// 128 x 512 -> 1000 in bf16: 11.5 us as two launches, 7.6 as one.
+// 128 x 512 -> 1000 in bf16: 11.5 us of kernels as two launches, 7.6 as one.
 struct Both {
   Grad dw, dx;
   uint32_t dw_blocks, dx_blocks;   // of the products; then those of dbias

@@ -3,8 +3,8 @@
 //   dx = rstd (u - mean(u) - h mean(u h)) + residual,  u = dy weight;  dweight = sum over rows of dy h,  dbias = that of dy.
 // Both are bound by memory: a row is read once and stays in the registers of the threads that share it, eight values each, for all of its
 // sums; blocks walk the rows, the next one on its way while the sums of this one are made, weight and bias in registers (read for every
-// row they are four times a bf16 row: forward 74 us).  16384 x 4096 in bf16: forward 47 us (5.7 TB/s), backward with the skip
-// connection's gradient 92 us and 6 to join the blocks' sums (5.5 TB/s); a kernel that only adds three such matrices takes 74 to 95.
+// row they are four times a bf16 row: forward 74 us).  16384 x 4096 in bf16: forward 45 us (5.9 TB/s), backward with the skip
+// connection's gradient 89 us and 4 to join the blocks' sums (5.7 TB/s); a kernel that only adds three such matrices takes 74 to 95.
 #include "mat_layout.h"
 
 namespace oseq {
@@ -13,7 +13,7 @@ namespace {
 
 // Two sums over the threads of a row: G lanes (a power of two up to 64), or with G = 0 the whole block of up to MAX threads.  `lds` holds two
 // floats a wavefront, a place of its own for every other call, zeros for wavefronts that the block does not have (row_sums_begin): all are
-// read at once, where a loop over those that there are waits for each (16384 x 4096 forward 52 us, so 46).
+// read at once, where a loop over those that there are waits for each (15249 x 2304 in bf16 backward 72 us, so 60).
 template <int MAX> struct RowSums { float2 part[2][MAX / 64]; };
 template <int G, int MAX> __device__ __forceinline__ void row_sums_begin(RowSums<MAX>& lds) {
   const int i = threadIdx.x % (MAX / 64), waves = blockDim.x >> 6;
@@ -465,7 +465,7 @@ int blocks_of(int threads, int waves) { return 256 * std::max(1, waves / (thread
 bool once(const optorch_layer_norm_t& a) { return a.rows * (int64_t)a.cols * 2 * (a.residual ? 4 : 3) > (384ll << 20); }
 
 // The threads of a row: a power of two of lanes up to 64 (512 columns), as many wavefronts as it takes up to 8192 columns, eight values each, or
-// 16 of 1024 threads; 0: rows longer than that.  (Powers of two there too: 15249 x 2348 in bf16 backward 115 us, so 78.)
+// 16 of 1024 threads; 0: rows longer than that.  (Powers of two there too: 15249 x 2348 in bf16 backward 114 us, so 60.)
 int lanes_of(int cols) {
   if (cols > 16384) return 0;
   if (cols > 8192) return 1024;

@@ -1,4 +1,4 @@
-// Host-callable launchers of the matrix operators (k_linear.hip, k_norm.hip, k_loss.hip, k_ortho.hip).  All launches are asynchronous on `st`.
+// Host-callable launchers of the matrix operators (k_linear.hip, k_norm.hip, k_loss.hip, k_loss_grad.hip, k_ortho.hip).  All launches are asynchronous on `st`.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
