@@ -618,13 +618,18 @@ struct Teacher {
 template <int N> __device__ __forceinline__ void row_sync() {
   if (N <= 64) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); else __syncthreads();
 }
+// thread t ^ o's value: by LDS from another wavefront (all by LDS, with a wait or barrier for each: ten entries of 128 rows 5.9 us, so 4.4)
+template <int N, class V> __device__ __forceinline__ V across(V v, V* lds, int t, int o) {
+  if (o < 64) return __shfl_xor(v, o);
+  lds[t] = v;
+  row_sync<N>();
+  v = lds[t ^ o];
+  row_sync<N>();
+  return v;
+}
 template <int N, class F> __device__ __forceinline__ float over_row(float v, float* lds, int t, F&& f) {
-  for (int o = N / 2; o > 0; o >>= 1) {
-    lds[t] = v;
-    row_sync<N>();
-    v = f(v, lds[t ^ o]);
-    row_sync<N>();
-  }
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1) v = f(v, across<N>(v, lds, t, o));
   return v;
 }
 
@@ -652,14 +657,13 @@ __global__ void __launch_bounds__(N < 256 ? 256 : N) teacher_kernel(Teacher a) {
   const float log_q = v - most - logf(sum);
   uint32_t key = valid && !wrong ? (uint32_t)c << 10 | t : 0xffffffffu;
   // bitonic: pairs of keys at a distance of `o` in runs of `run`
+#pragma unroll
   for (int run = 2; run <= N; run *= 2)
+#pragma unroll
     for (int o = run / 2; o > 0; o >>= 1) {
-      keys[r][t] = key;
-      row_sync<N>();
-      const uint32_t other = keys[r][t ^ o];
+      const uint32_t other = across<N>(key, keys[r], t, o);
       const bool least = ((t & o) == 0) == ((t & run) == 0);
       key = least ? min(key, other) : max(key, other);
-      row_sync<N>();
     }
   keys[r][t] = key;
   values[r][t] = log_q;
@@ -838,13 +842,13 @@ template <int THREADS, class F> __device__ __forceinline__ void each_row(const R
 }
 // the largest of a block's values, in every thread
 template <int THREADS> __device__ __forceinline__ float block_max(float v, float* part) {
-  part[threadIdx.x] = v;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
   __syncthreads();
-  for (int o = THREADS / 2; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) part[threadIdx.x] = fmaxf(part[threadIdx.x], part[threadIdx.x + o]);
-    __syncthreads();
-  }
-  return part[0];
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) v = fmaxf(v, part[w]);
+  return v;
 }
 template <int THREADS> __device__ __forceinline__ float largest_of(const Rows& a, int block, float* part) {
   float most = 0.f;
@@ -872,11 +876,11 @@ template <int THREADS> __device__ __forceinline__ void rows_of(const Rows& a, in
   });
 }
 __global__ void __launch_bounds__(1024) rows_kernel(Rows a) {
-  __shared__ float part[1024];
+  __shared__ float part[16];
   rows_of<1024>(a, blockIdx.x, part);
 }
 __global__ void __launch_bounds__(1024) largest_kernel(Rows a) {
-  __shared__ float part[1024];
+  __shared__ float part[16];
   const float c = largest_of<1024>(a, blockIdx.x, part);
   if (threadIdx.x == 0) a.largest[blockIdx.x] = c;
 }
@@ -896,7 +900,7 @@ __global__ void __launch_bounds__(256) fold_kernel(const float* sums, int64_t ro
 // What a call begins with, in one launch: operands that are laid out anew, and (the first block, where there is one) the rows' values
 struct Prepare { Layout x, w; int x_blocks, w_blocks; Rows rows; int row_blocks; };
 template <class S, class T, int PL> __global__ void __launch_bounds__(256) prepare_kernel(Prepare p) {
-  __shared__ float part[256];
+  __shared__ float part[4];
   int block = blockIdx.x;
   if (block < p.row_blocks) { rows_of<256>(p.rows, 0, part); return; }
   block -= p.row_blocks;
