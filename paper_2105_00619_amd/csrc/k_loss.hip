@@ -16,19 +16,19 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 
 // ---- operands laid out anew --------------------------------------------------------------------------------------------
-// Columns are filled up to whole blocks (block_of) with zeros.  With `info`, rows times their power of two.
-struct Layout { const void* src; int64_t ld, rows; int cols; void* dst; const float4* info; const float* scale; };
+// Columns are filled up to whole blocks (block_of) with zeros.  With `info`, rows times their power of two; `twice`: all rows once more behind them.
+struct Layout { const void* src; int64_t ld, rows; int cols; void* dst; const float4* info; const float* scale; bool twice; };
 template <class S, class T, int PL> __device__ __forceinline__ void lay_out_rows(const Layout& a, int block, int blocks) {
   const int c8 = (a.cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
-  const int64_t n = a.rows * c8;
+  const int64_t n = a.rows * c8 * (a.twice ? 2 : 1);
   const float largest = a.info ? *a.scale : 1.f;
   for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) {
-    const int64_t r = i / c8;
+    const int64_t r = i / c8, from = r < a.rows ? r : r - a.rows;
     const int c = (int)(i - r * c8) * 8;
     float v[8];
-    load8<S>((const S*)a.src + r * a.ld + c, max(0, min(8, a.cols - c)), v);
+    load8<S>((const S*)a.src + from * a.ld + c, max(0, min(8, a.cols - c)), v);
     if (a.info) {
-      const float4 row = a.info[r];
+      const float4 row = a.info[from];
       const float f = row.w / largest;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = row.z == 0.f ? 0.f : v[e] * f;
@@ -55,6 +55,7 @@ struct Logits {
   const float4* info;
   float spread, hit, scale;         // label_smoothing / classes; 1 - label_smoothing; what ds is held times
   void* ds; int64_t ds_row;
+  int64_t low;                      // rows of ds behind which its low parts go, or 0: it has none
   float* bias_sums;
   Layout xs; int xs_blocks;         // blocks behind the tiles' lay out x for dw, or 0
 };
@@ -265,36 +266,45 @@ logits_kernel(Logits a) {
         for (int n = 0; n < NV; ++n) sums[n] = __fmaf_rn(v[n], factor, sums[n]);
       }
       // out: rows of places, 16 bytes a lane; the columns up to whole blocks (block_of) are zeros already
-#pragma unroll
-      for (int n = 0; n < NV; n += 4) {
-        const int c = class_of(n);
-        float q[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[e] = v[n + e] * a.scale;
-        if constexpr (PL == 1) {
-          *reinterpret_cast<Vec<T, 4>*>(out + sl * PITCH + c) = round_vec<T, 4>(q);
-        } else {
-          // (values within 2, or NaN, which then is in every plane: no cases)
-#pragma unroll
-          for (int p = 0; p < 3; ++p) {
-            const Vec<T, 4> t = round_vec<T, 4>(q);
-            *reinterpret_cast<Vec<T, 4>*>(out + sl * PITCH + place_of<PL>(c, p)) = t;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) q[e] -= (float)t.v[e];
-          }
-        }
-      }
-      asm volatile("" ::: "memory");
       constexpr int LANES = W * span_of(PL) / 8, AT_ONCE = 64 / LANES > 0 ? 64 / LANES : 1;  // lanes of a row, rows at once
       const int padded = ((a.N + block_of(PL) - 1) / block_of(PL) * block_of(PL) - n0 - c0) * span_of(PL);
-      T* ds = (T*)a.ds + m0 * a.ds_row + place_of<PL>(n0 + c0);
+      constexpr int COPIES = PL == 1 && W < 128 ? 2 : 1;
+      for (int copy = 0; copy < COPIES && (copy == 0 || a.low); ++copy) {
 #pragma unroll
-      for (int q = 0; q < 32 / AT_ONCE; ++q) {
-        const int o = q * AT_ONCE + lane / LANES, p = lane % LANES * 8, to = wn * W + j * 32 + o;
-        const Chunk t = *reinterpret_cast<const Chunk*>(out + o * PITCH + p);
-        if (to < rows && p < padded && !(PL == 3 && p % 64 >= 48)) *reinterpret_cast<Chunk*>(ds + to * a.ds_row + p) = t;
+        for (int n = 0; n < NV; n += 4) {
+          const int c = class_of(n);
+          float q[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) q[e] = v[n + e] * a.scale;
+          if constexpr (PL == 1) {
+            Vec<T, 4> t = round_vec<T, 4>(q);
+            if (COPIES > 1 && copy) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) q[e] -= to_f32(t.v[e]);
+              t = round_vec<T, 4>(q);
+            }
+            *reinterpret_cast<Vec<T, 4>*>(out + sl * PITCH + c) = t;
+          } else {
+            // (values within 2, or NaN, which then is in every plane: no cases)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+              const Vec<T, 4> t = round_vec<T, 4>(q);
+              *reinterpret_cast<Vec<T, 4>*>(out + sl * PITCH + place_of<PL>(c, p)) = t;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) q[e] -= (float)t.v[e];
+            }
+          }
+        }
+        asm volatile("" ::: "memory");
+        T* ds = (T*)a.ds + (m0 + copy * a.low) * a.ds_row + place_of<PL>(n0 + c0);
+#pragma unroll
+        for (int q = 0; q < 32 / AT_ONCE; ++q) {
+          const int o = q * AT_ONCE + lane / LANES, p = lane % LANES * 8, to = wn * W + j * 32 + o;
+          const Chunk t = *reinterpret_cast<const Chunk*>(out + o * PITCH + p);
+          if (to < rows && p < padded && !(PL == 3 && p % 64 >= 48)) *reinterpret_cast<Chunk*>(ds + to * a.ds_row + p) = t;
+        }
+        asm volatile("" ::: "memory");
       }
-      asm volatile("" ::: "memory");
     }
   });
   if constexpr (GRAD) {
@@ -1048,14 +1058,15 @@ template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_
   float* scale = rows.scale;
   // (x for dw beside the first piece's tiles, which need nothing of it: 4096 x 2048 -> 100 in fp16 8.5 us less)
   if (a.dw) {
-    l.xs = {a.x, a.ldx, a.rows, a.in_features, ws + p.off_xs, info, scale};
-    l.xs_blocks = std::min(grid_of(a.rows * ((a.in_features + 7) / 8)), 1024);
+    l.xs = {a.x, a.ldx, a.rows, a.in_features, ws + p.off_xs, info, scale, p.copies > 1};
+    l.xs_blocks = std::min(grid_of(a.rows * p.copies * ((a.in_features + 7) / 8)), 1024);
   }
   l.info = info;
   l.spread = a.labels ? a.label_smoothing / (float)a.classes : 0.f;
   l.hit = 1.f - a.label_smoothing;
   l.scale = loss_scale_of(a.precision);
   l.ds = ws + p.off_ds; l.ds_row = p.ds_row;
+  l.low = p.copies > 1 ? a.rows : 0;
   l.bias_sums = a.dbias ? (float*)(ws + p.off_bias) : nullptr;
   LossPiece g = {};
   g.ds = l.ds; g.ds_row = p.ds_row;
@@ -1063,7 +1074,7 @@ template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_
   g.info = info; g.scale = scale;
   g.acc = (float*)(ws + p.off_acc); g.parts = (float*)(ws + p.off_parts);
   g.dx = p.dx; g.dw = p.dw;
-  g.both = p.both; g.dx_parts = p.dx_parts;
+  g.copies = p.copies; g.both = p.both; g.dx_parts = p.dx_parts;
   each_piece<S, T, PL>(a, p, l, [&] {
     run_logits<S, T, true>(st, l, p.wave);
     l.xs_blocks = 0;
@@ -1113,7 +1124,7 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   if (!backward && !p.pack_x && !p.pack_w && !p.few) p.stream = stream_blocks(a.rows, a.classes, a.in_features);
   // pieces of a multiple of 256 classes, all alike but the last
   int64_t most = a.classes;
-  const int64_t each = f32 ? 8 : 2;
+  const int64_t each = f32 ? 8 : a.rows <= SKINNY_ROWS ? 4 : 2;
   if (backward) most = std::min(most, LOSS_PIECE_BYTES / (each * a.rows));
   if (p.pack_w) most = std::min(most, LOSS_PIECE_BYTES / (int64_t)in_row);
   const int64_t pieces = (a.classes + std::max<int64_t>(256, most) - 1) / std::max<int64_t>(256, most);
@@ -1124,6 +1135,10 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   if (backward && p.wave == 128 && a.in_features <= 640) p.wave = 64;
   p.columns = (a.classes + p.wave - 1) / p.wave;
   p.ds_row = f32 ? row_of<3>(p.piece) : row_of<1>(p.piece);
+  // Few rows: ds in two parts, the low ones as further rows of its products, which the weights bound: each value's rounding would be in all of
+  // its row of dx, and few rows do not even it out.  2 x 247 -> 10496 in fp16: dx 3.1e-4 off in one part, 2.2e-4 in two, as with fp32 and one rounding.
+  // In us one part / two: that 25 / 28; bf16 16 x 512 -> 1000 17.5 / 19.7, 16 x 2048 -> 65536 258 / 269, 64 x 2048 -> 32000 114 / 128.
+  p.copies = backward && !f32 && a.rows <= SKINNY_ROWS && p.wave < 128 ? 2 : 1;
   uint64_t o = 0;
   auto take = [&](uint64_t n) { const uint64_t at = o; o = up256(o + n); return at; };
   const uint64_t rows = a.rows;
@@ -1143,30 +1158,30 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   } else {
     p.off_info = take(rows * 16);
     p.off_scale = take(4 * (64 + ROW_BLOCKS));
-    if (a.dw) p.off_xs = take(rows * in_row);
-    p.off_ds = take(rows * p.ds_row * 2);
+    if (a.dw) p.off_xs = take(rows * p.copies * in_row);
+    p.off_ds = take(rows * p.copies * p.ds_row * 2);
     if (a.dx && p.piece < a.classes) p.off_acc = take(rows * up8(a.in_features) * 4);
     const uint64_t bias_rows = 2 * (uint64_t)ceil_div(a.rows, 2 * p.wave);
     if (a.dbias) p.off_bias = take((bias_rows + (bias_rows > FOLD_FROM ? (bias_rows + 63) / 64 : 0)) * p.piece * 4);
-    auto floats = [](const ProductShape& s, int64_t M, int64_t N) { return s.parts > 1 ? s.parts * M * up8(N) : 0; };
-    const int64_t in = a.in_features;
-    p.dx = shape_of(a.rows, in, p.piece, f32);
-    p.dw = shape_of(p.piece, in, a.rows, f32);
+    auto floats = [](const ProductShape& s, int copies, int64_t M, int64_t N) { return s.parts * copies > 1 ? s.parts * M * up8(N) : 0; };
+    const int64_t in = a.in_features, rows2 = a.rows * p.copies;
+    p.dx = shape_of(rows2, in, p.piece, f32);
+    p.dw = shape_of(p.piece, in, rows2, f32);
     // Neither product fills the card: both in one launch, with the tiles that suit the two together best.  (The same ones where only one
     // is asked for: a gradient's bits are the same beside the others and alone.)
     if (p.dx.wave < 128 && p.dw.wave < 128 && p.dx.us + p.dw.us < BOTH_US) {
       p.both = a.dx && a.dw;
       float least = 0.f;
       for (int w : {64, 32}) {
-        const ProductShape dx = shape_of(a.rows, in, p.piece, f32, 32, w), dw = shape_of(p.piece, in, a.rows, f32, 32, w);
+        const ProductShape dx = shape_of(rows2, in, p.piece, f32, 32, w), dw = shape_of(p.piece, in, rows2, f32, 32, w);
         if (least != 0.f && dx.us + dw.us >= least) continue;
         least = dx.us + dw.us;
         p.dx = dx;
         p.dw = dw;
       }
     }
-    p.dx_parts = a.dx ? floats(p.dx, a.rows, in) : 0;
-    const int64_t dw_parts = a.dw ? floats(p.dw, p.piece, in) : 0;
+    p.dx_parts = a.dx ? floats(p.dx, p.copies, rows2, in) : 0;
+    const int64_t dw_parts = a.dw ? floats(p.dw, 1, p.piece, in) : 0;
     const uint64_t parts = 4 * (uint64_t)(p.both ? p.dx_parts + dw_parts : std::max(p.dx_parts, dw_parts));
     if (parts) p.off_parts = take(parts);
   }

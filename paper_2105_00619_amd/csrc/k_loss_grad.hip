@@ -14,8 +14,9 @@ struct Grad {
   int64_t M;
   int N, K;
   int tiles_m, tiles_n, parts;
+  int copies;         // rows of the result that are added up, M / copies apart
   Parts cut;          // of K, in `parts`
-  float* partial;     // parts > 1: [parts][M][up8(N)] sums
+  float* partial;     // with more than one of either: [parts][M][up8(N)] sums
   float* acc;         // dx: [M][up8(N)], the sums of the pieces before this one, unless `start`; the sums with it, unless `end`
   bool start, end;
   const float4* info; // dx: the rows' factors
@@ -73,9 +74,9 @@ __device__ __forceinline__ void tile(const Grad& a, uint32_t block, unsigned cha
   const Operand<T> oa = {(const T*)a.a + (DW ? (int64_t)k0 * a.lda + place_of<PL>(m0) : m0 * a.lda + place_of<PL>(k0)), a.lda, rows};
   const Operand<T> ob = {(const T*)a.b + (int64_t)k0 * a.ldb + place_of<PL>(n0), a.ldb, cols};
   const int n8 = (a.N + 7) & ~7;
-  auto ask = [&](int r, int c, int) { return a.parts > 1 ? Before{} : before_of<DW>(a, m0 + r, n0 + c); };
+  auto ask = [&](int r, int c, int) { return a.parts * a.copies > 1 ? Before{} : before_of<DW>(a, m0 + r, n0 + c); };
   auto emit = [&](int r, int c, float (&v)[8], int n, const Before& before) {
-    if (a.parts > 1) store_f32<float, 8>(a.partial + ((int64_t)part * a.M + m0 + r) * n8 + n0 + c, v);
+    if (a.parts * a.copies > 1) store_f32<float, 8>(a.partial + ((int64_t)part * a.M + m0 + r) * n8 + n0 + c, v);
     else finish<O, DW>(a, m0 + r, n0 + c, v, n, before);
   };
   typename G::Acc acc;
@@ -115,17 +116,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(W == 1
   tile<O, T, W, DW>(a, blockIdx.y * gridDim.x + blockIdx.x, smem);
 }
 
-// the parts' sums, added in order: block `block` of `blocks`
+// the parts' sums and the copies', added in order: block `block` of `blocks`
 template <class O, bool DW> __device__ __forceinline__ void join_parts(const Grad& a, int block, int blocks) {
   const int c8 = (a.N + 7) / 8;
-  const int64_t n = a.M * c8;
+  const int64_t n = a.M / a.copies * c8;
   for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < n; i += (int64_t)blocks * 256) {
     const int64_t r = i / c8;
     const int c = (int)(i - r * c8) * 8;
     const Before before = before_of<DW>(a, r, c);
     float v[8];
     load_f32<float, 8>(a.partial + i * 8, v);
-    for (int p = 1; p < a.parts; ++p) {
+    for (int p = 1; p < a.parts * a.copies; ++p) {
       float t[8];
       load_f32<float, 8>(a.partial + ((int64_t)p * n + i) * 8, t);
 #pragma unroll
@@ -166,7 +167,7 @@ template <class O, class T, int W, bool DW> void run_w(hipStream_t st, Grad& a) 
   // (more LDS than a launch gets unasked; set again on every launch: which devices know it is not ours to remember)
   if (G::LDS > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
   OSEQ_LAUNCH(k, grid_of_blocks((int64_t)per * 8), dim3(256), G::LDS, st, a);
-  if (a.parts > 1) OSEQ_LAUNCH((grad_join_kernel<O, DW>), dim3(grid_of(a.M * ((a.N + 7) / 8))), dim3(256), 0, st, a);
+  if (a.parts * a.copies > 1) OSEQ_LAUNCH((grad_join_kernel<O, DW>), dim3(grid_of(a.M / a.copies * ((a.N + 7) / 8))), dim3(256), 0, st, a);
 }
 template <class O, class T, bool DW> void run(hipStream_t st, Grad& a, const ProductShape& s) {
   a.cut = parts_of(a.K, s.parts);
@@ -184,7 +185,7 @@ template <class O, class T, int W> void run_both(hipStream_t st, Both& b) {
     g.tiles_n = ceil_div(g.N, 2 * W);
     return (uint32_t)((g.tiles_m * g.tiles_n * g.parts + 7) / 8 * 8);
   };
-  auto joins = [](const Grad& g) { return g.parts > 1 ? grid_of(g.M * ((g.N + 7) / 8)) : 0; };
+  auto joins = [](const Grad& g) { return g.parts * g.copies > 1 ? grid_of(g.M / g.copies * ((g.N + 7) / 8)) : 0; };
   b.dw_blocks = blocks(b.dw);
   b.dx_blocks = blocks(b.dx);
   auto k = both_kernel<O, T, W>;
@@ -205,7 +206,8 @@ template <class O, class T> void piece_of(const optorch_softmax_loss_t& a, const
   g.unscale = 1.f / loss_scale_of(a.precision);
   if (a.dx) {
     g.b = p.w; g.ldb = p.ldw;
-    g.M = a.rows; g.N = a.in_features; g.K = p.count;
+    g.M = a.rows * p.copies; g.N = a.in_features; g.K = p.count;
+    g.copies = p.copies;
     g.partial = p.parts;
     g.acc = p.acc; g.start = p.start; g.end = p.end;
     g.out = a.dx; g.ldo = a.lddx;
@@ -214,7 +216,8 @@ template <class O, class T> void piece_of(const optorch_softmax_loss_t& a, const
   }
   if (a.dw) {
     g.b = p.xs; g.ldb = p.ldxs;
-    g.M = p.count; g.N = a.in_features; g.K = (int)a.rows;
+    g.M = p.count; g.N = a.in_features; g.K = (int)(a.rows * p.copies);
+    g.copies = 1;
     g.partial = p.both ? p.parts + p.dx_parts : p.parts;
     g.out = (O*)a.dw + p.first * a.lddw; g.ldo = a.lddw;
     b.dw = g;

@@ -69,6 +69,7 @@ struct LossPlan {
   int columns;          // how many of those
   int piece;            // classes of a piece
   int64_t ds_row;       // places of a row of ds
+  int copies;           // 2: the low parts of ds are rows behind its own, and x is there twice for dw; or 1
   ProductShape dx, dw;
   bool both;            // dx and dw in one launch, with the same tiles
   int64_t dx_parts;     // floats of dx' parts in front of dw's, in one launch
@@ -86,6 +87,7 @@ struct LossPiece {
   const void *ds, *w, *xs;         // operands, with the distances of their rows
   int64_t ds_row; int ldw, ldxs;
   int first, count;                // the piece's classes
+  int copies;                      // 2: rows of ds for the low parts behind its own, and of xs; or 1
   const void* info;                // a row's factor of dx: the fourth of four floats
   const float* scale;              // the factor of dw
   float* acc; float* parts;        // dx summed over the pieces; parts of a reduction

@@ -104,14 +104,16 @@ class Reference:
         near = torch.where(p > 0, U * (3 * (self.s - k).abs() + (0 if name == "fp32" else 2 * (self.s.abs() + k.abs()))), torch.zeros_like(p))
         ds = g * (a * p - self.target)
         exact = g.abs() * (a.abs() * p * (self.ds_logit + near + 8 * U) + 4 * U * (self.target + a.abs() * p))
-        held = exact + e * ds.abs() + (g.abs() * f * 2.0 ** -38 if name == "fp16" else 0)
+        # ds in the storage type; up to 64 rows in two parts of it, the second what the first one leaves
+        copies = 2 if name != "fp32" and self.x.shape[0] <= 64 else 1
+        held = exact + e ** copies * ds.abs() + (g.abs() * f * 2.0 ** -38 if name == "fp16" else 0)
         largest = float((g.abs() * f).max())
         x, w = self.x, self.w
         out_floor = 2.0 ** -25 if name == "fp16" else 2.0 ** -134
         dx, dw = _mm(ds, w), _mm(ds.T, x)
         dx_fp32 = _mm(held, w.abs()) + (_adds(w.shape[0], name) + 40) * U23 * _mm(ds.abs(), w.abs())
         xe = (2.0 ** -25 * (largest / g.abs().clamp_min(1e-300)).clamp_max(1e30) if name == "fp16" else torch.zeros_like(g)) + torch.zeros_like(x)
-        dw_fp32 = _mm(held.T, x.abs() + xe) + _mm(ds.abs().T, xe) + (_adds(x.shape[0], name) + 40) * U23 * _mm(ds.abs().T, x.abs())
+        dw_fp32 = _mm(held.T, x.abs() + xe) + _mm(ds.abs().T, xe) + (_adds(copies * x.shape[0], name) + 40) * U23 * _mm(ds.abs().T, x.abs())
         eo = torch.finfo(dt).eps / 2
         db_tol = exact.sum(0) + (80 + x.shape[0] / 16) * U * ds.abs().sum(0)
         return (dx, dx_fp32 + eo * (dx.abs() + dx_fp32) + out_floor), (dw, dw_fp32 + eo * (dw.abs() + dw_fp32) + out_floor), (ds.sum(0), db_tol)
