@@ -150,9 +150,9 @@ int optorch_softmax_loss_forward(const optorch_softmax_loss_t* a);
 
 /* ds = dloss (p - q), with labels dloss ((1 + 2 z_loss lse) p - target), with a teacher over the temperature;
  *   dx = ds w,  dw = ds^T x,  dbias = column sums of ds.
- * p is made from the logits, made again, and the given lse.  In 16-bit precision ds, over its row's dloss, is rounded to the storage
- * type for the two products (dx and dw: as much again as their own rounding; not with up to 64 rows); dbias sums it unrounded.  With rows = 0, dw and dbias
- * are zero. */
+ * p is made from the logits, made again, and the given lse.  In 16-bit precision ds, over its row's dloss, is held as two values of the storage
+ * type for the two products, which keeps 16 (bf16) or 22 (fp16) of its bits, so that dx and dw are rounded once; dbias sums it
+ * unrounded.  With rows = 0, dw and dbias are zero. */
 int optorch_softmax_loss_backward(const optorch_softmax_loss_t* a);
 
 /* ---- orthogonalised updates ------------------------------------------------------------------------ */

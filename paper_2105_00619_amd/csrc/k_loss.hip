@@ -2,10 +2,10 @@
 //   loss = sum over classes of q (log q - s) + lse(s),   ds = p - q,   p = exp(s - lse).
 // The logits are made tile by tile (mat_core.h) and never leave the block that makes them: forward it keeps of each row the maximum of its
 // columns, the sum of their exponentials above it and the targets' logits, which a second kernel joins; backward it turns them into ds, in
-// the storage type and for a piece of the classes at a time, which the gradients' products read (k_loss_grad.hip).  What a row's target is at some of its
+// planes of the storage type (two of 16 bits) and for a piece of the classes at a time, which the gradients' products read (k_loss_grad.hip).  What a row's target is at some of its
 // columns is put into the tile on its way through LDS, where the row's values lie side by side.
 // Large calls are bound by the matrix cores: 8192 x 4096 -> 128000 in bf16 6.26 ms forward (1370 TFLOP/s, matrix cores busy 75 % of the kernel) and
-// 20.0 ms backward (three such products, 1290 TFLOP/s); few rows by memory (the weights at 4.8 TB/s), small calls by their launches.
+// 35.3 ms backward (five such products, two each for dx and dw, 1220 TFLOP/s); few rows by memory (the weights at 4.8 TB/s), small calls by their launches.
 #include "mat_layout.h"
 #include "parts.h"
 
@@ -16,7 +16,8 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 
 // ---- operands laid out anew --------------------------------------------------------------------------------------------
-// Columns are filled up to whole blocks (block_of) with zeros.  With `info`, rows times their power of two; `twice`: all rows once more behind them.
+// Columns are filled up to whole blocks (block_of) with zeros.  With `info`, rows times their power of two; `twice`: all rows once more behind them,
+// for the second plane of ds, over what that is held larger by.
 struct Layout { const void* src; int64_t ld, rows; int cols; void* dst; const float4* info; const float* scale; bool twice; };
 template <class S, class T, int PL> __device__ __forceinline__ void lay_out_rows(const Layout& a, int block, int blocks) {
   const int c8 = (a.cols + block_of(PL) - 1) / block_of(PL) * (block_of(PL) / 8);
@@ -29,7 +30,7 @@ template <class S, class T, int PL> __device__ __forceinline__ void lay_out_rows
     load8<S>((const S*)a.src + from * a.ld + c, max(0, min(8, a.cols - c)), v);
     if (a.info) {
       const float4 row = a.info[from];
-      const float f = row.w / largest;
+      const float f = row.w / largest * (r < a.rows ? 1.f : Tile<T, PL, 32, false, false>::BETWEEN);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = row.z == 0.f ? 0.f : v[e] * f;
     }
@@ -55,7 +56,7 @@ struct Logits {
   const float4* info;
   float spread, hit, scale;         // label_smoothing / classes; 1 - label_smoothing; what ds is held times
   void* ds; int64_t ds_row;
-  int64_t low;                      // rows of ds behind which its low parts go, or 0: it has none
+  int64_t low;                      // 16 bits: rows of ds behind which its second plane goes
   float* bias_sums;
   Layout xs; int xs_blocks;         // blocks behind the tiles' lay out x for dw, or 0
 };
@@ -268,8 +269,9 @@ logits_kernel(Logits a) {
       // out: rows of places, 16 bytes a lane; the columns up to whole blocks (block_of) are zeros already
       constexpr int LANES = W * span_of(PL) / 8, AT_ONCE = 64 / LANES > 0 ? 64 / LANES : 1;  // lanes of a row, rows at once
       const int padded = ((a.N + block_of(PL) - 1) / block_of(PL) * block_of(PL) - n0 - c0) * span_of(PL);
-      constexpr int COPIES = PL == 1 && W < 128 ? 2 : 1;
-      for (int copy = 0; copy < COPIES && (copy == 0 || a.low); ++copy) {
+      // 16 bits: two planes, ds rounded and what that leaves, in fp16 2048 times larger (mat_core.h); an infinity is in the first one alone
+      constexpr int PLANES = PL == 1 ? 2 : 1;
+      for (int plane = 0; plane < PLANES; ++plane) {
 #pragma unroll
         for (int n = 0; n < NV; n += 4) {
           const int c = class_of(n);
@@ -278,9 +280,12 @@ logits_kernel(Logits a) {
           for (int e = 0; e < 4; ++e) q[e] = v[n + e] * a.scale;
           if constexpr (PL == 1) {
             Vec<T, 4> t = round_vec<T, 4>(q);
-            if (COPIES > 1 && copy) {
+            if (plane) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) q[e] -= to_f32(t.v[e]);
+              for (int e = 0; e < 4; ++e) {
+                const float rest = q[e] - to_f32(t.v[e]);
+                q[e] = finite(rest) ? rest * (1.f / G::BETWEEN) : 0.f;
+              }
               t = round_vec<T, 4>(q);
             }
             *reinterpret_cast<Vec<T, 4>*>(out + sl * PITCH + c) = t;
@@ -296,7 +301,7 @@ logits_kernel(Logits a) {
           }
         }
         asm volatile("" ::: "memory");
-        T* ds = (T*)a.ds + (m0 + copy * a.low) * a.ds_row + place_of<PL>(n0 + c0);
+        T* ds = (T*)a.ds + (m0 + plane * a.low) * a.ds_row + place_of<PL>(n0 + c0);
 #pragma unroll
         for (int q = 0; q < 32 / AT_ONCE; ++q) {
           const int o = q * AT_ONCE + lane / LANES, p = lane % LANES * 8, to = wn * W + j * 32 + o;
@@ -1066,10 +1071,10 @@ template <class S, class T, int PL> void backward_of(const optorch_softmax_loss_
   l.hit = 1.f - a.label_smoothing;
   l.scale = loss_scale_of(a.precision);
   l.ds = ws + p.off_ds; l.ds_row = p.ds_row;
-  l.low = p.copies > 1 ? a.rows : 0;
+  l.low = a.rows;
   l.bias_sums = a.dbias ? (float*)(ws + p.off_bias) : nullptr;
   LossPiece g = {};
-  g.ds = l.ds; g.ds_row = p.ds_row;
+  g.ds = l.ds; g.ds_row = p.ds_row; g.second = PL == 1 && p.copies == 1 ? a.rows * p.ds_row : 0;
   g.xs = ws + p.off_xs; g.ldxs = row_of<PL>(a.in_features);
   g.info = info; g.scale = scale;
   g.acc = (float*)(ws + p.off_acc); g.parts = (float*)(ws + p.off_parts);
@@ -1102,15 +1107,15 @@ template <class S> void clear_of(const optorch_softmax_loss_t& a) {
   if (a.dbias) OSEQ_LAUNCH(loss_clear_kernel<float>, dim3(grid_of(a.classes)), dim3(256), 0, st, a.dbias, (int64_t)1, a.classes, (int64_t)a.classes);
 }
 
-// A piece of ds (and of weights that are laid out anew) takes at most about this.  In ms with 64 / 256 / 512 / 1024 MB: 8192 x 4096 -> 128000 in
-// bf16 21.4 / 19.9 / 19.8 / 19.8, 4096 x 2048 -> 65536 2.95 / 2.78 / 2.74 / 2.73, 16384 x 512 -> 32000 2.15 / 1.90 / 1.72 / 1.65, 8192 x 1024 -> 50257
-// 2.69 / 2.40 / 2.56 / 2.56; fp32 4096 x 1024 -> 32000 4.32 / 3.88 / 3.66 / 3.63.
-constexpr int64_t LOSS_PIECE_BYTES = 512ll << 20;
+// A piece of ds (and of weights that are laid out anew) takes at most about this; more of it would be faster, and the caller's memory.  In ms with
+// 300 / 600 / 1200 MB: 8192 x 4096 -> 128000 in bf16 38.8 / 35.3 / 34.4, 4096 x 2048 -> 65536 4.71 / 4.62 / 4.60, 16384 x 512 -> 32000 3.25 / 3.19 / 2.91,
+// 8192 x 1024 -> 50257 4.99 / 4.73 / 4.54; fp32 4096 x 1024 -> 32000 3.92 / 3.70 / 3.67.
+constexpr int64_t LOSS_PIECE_BYTES = 600ll << 20;
 
 }  // namespace
 
-// Products of less time together than this are one launch.  The whole call, us as two launches / as one: bf16 128 x 512 -> 1000 21 / 18, 512 x 1024 ->
-// 8000 53 / 50, 1024 x 1024 -> 8000 75 / 72, 1000 x 768 -> 20000 124 / 124; fp16 700 x 333 -> 9000 53 / 45; fp32 300 x 512 -> 8000 84 / 77.
+// Products of less time together than this are one launch.  The whole call, us as two launches / as one: fp16 128 x 512 -> 1000 27.8 / 23.3,
+// 700 x 333 -> 9000 78 / 65; bf16 512 x 1024 -> 8000 76.6 / 73.4, 1000 x 768 -> 20000 208 / 208; fp32 300 x 512 -> 8000 84 / 77.
 constexpr float BOTH_US = 60.f;
 
 LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
@@ -1124,21 +1129,22 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
   if (!backward && !p.pack_x && !p.pack_w && !p.few) p.stream = stream_blocks(a.rows, a.classes, a.in_features);
   // pieces of a multiple of 256 classes, all alike but the last
   int64_t most = a.classes;
-  const int64_t each = f32 ? 8 : a.rows <= SKINNY_ROWS ? 4 : 2;
+  const int64_t each = f32 ? 8 : 4;
   if (backward) most = std::min(most, LOSS_PIECE_BYTES / (each * a.rows));
   if (p.pack_w) most = std::min(most, LOSS_PIECE_BYTES / (int64_t)in_row);
   const int64_t pieces = (a.classes + std::max<int64_t>(256, most) - 1) / std::max<int64_t>(256, most);
   p.piece = pieces == 1 ? a.classes : (int)(((a.classes + pieces - 1) / pieces + 255) / 256 * 256);
   p.wave = p.few || p.stream ? 16 : shape_of(a.rows, p.piece, a.in_features, f32, 1).wave;
-  // (a tile's end costs more where ds leaves it than the estimate has: tiles of 256 / 128, us in bf16 4096 x 256 -> 8192 119 / 110, 8192 x
-  // 512 -> 4096 155 / 153, 4096 x 1024 -> 32000 765 / 773; fp32 414 / 361, 643 / 589, 3708 / 3717)
+  // (a tile's end costs more where ds leaves it than the estimate has: tiles of 256 / 128, us in bf16 4096 x 256 -> 8192 161 / 147, 8192 x
+  // 512 -> 4096 238 / 231, 4096 x 1024 -> 32000 1250 / 1289; fp32 414 / 361, 643 / 589, 3708 / 3757)
   if (backward && p.wave == 128 && a.in_features <= 640) p.wave = 64;
   p.columns = (a.classes + p.wave - 1) / p.wave;
   p.ds_row = f32 ? row_of<3>(p.piece) : row_of<1>(p.piece);
-  // Few rows: ds in two parts, the low ones as further rows of its products, which the weights bound: each value's rounding would be in all of
-  // its row of dx, and few rows do not even it out.  2 x 247 -> 10496 in fp16: dx 3.1e-4 off in one part, 2.2e-4 in two, as with fp32 and one rounding.
-  // In us one part / two: that 25 / 28; bf16 16 x 512 -> 1000 17.5 / 19.7, 16 x 2048 -> 65536 258 / 269, 64 x 2048 -> 32000 114 / 128.
-  p.copies = backward && !f32 && a.rows <= SKINNY_ROWS && p.wave < 128 ? 2 : 1;
+  // 16 bits: ds rounded to one plane adds as much as the results' own rounding (dx and dw in bf16 2.3e-3 off, so 1.7e-3; fp16 2.9e-4, 2.1e-4), so
+  // it has two, and the products twice as much to do (8192 x 4096 -> 128000 in bf16 20.0 ms with one, 4096 x 256 -> 8192 106 us, so 35.3 and 147).  Few
+  // rows: the second plane as further rows of them, which the weights bound.  In us as the second half of the reduction / as rows: bf16
+  // 64 x 2048 -> 32000 156 / 131, 16 x 2048 -> 65536 333 / 266, 16 x 512 -> 1000 21 / 21.
+  p.copies = backward && !f32 && a.rows <= SKINNY_ROWS ? 2 : 1;
   uint64_t o = 0;
   auto take = [&](uint64_t n) { const uint64_t at = o; o = up256(o + n); return at; };
   const uint64_t rows = a.rows;
@@ -1159,7 +1165,7 @@ LossPlan plan_loss(const optorch_softmax_loss_t& a, bool backward) {
     p.off_info = take(rows * 16);
     p.off_scale = take(4 * (64 + ROW_BLOCKS));
     if (a.dw) p.off_xs = take(rows * p.copies * in_row);
-    p.off_ds = take(rows * p.copies * p.ds_row * 2);
+    p.off_ds = take(rows * p.ds_row * (f32 ? 2 : 4));
     if (a.dx && p.piece < a.classes) p.off_acc = take(rows * up8(a.in_features) * 4);
     const uint64_t bias_rows = 2 * (uint64_t)ceil_div(a.rows, 2 * p.wave);
     if (a.dbias) p.off_bias = take((bias_rows + (bias_rows > FOLD_FROM ? (bias_rows + 63) / 64 : 0)) * p.piece * 4);

@@ -69,7 +69,7 @@ struct LossPlan {
   int columns;          // how many of those
   int piece;            // classes of a piece
   int64_t ds_row;       // places of a row of ds
-  int copies;           // 2: the low parts of ds are rows behind its own, and x is there twice for dw; or 1
+  int copies;           // 2: the second plane of ds is rows of the products behind the first one's, and x is there twice for dw; or 1
   ProductShape dx, dw;
   bool both;            // dx and dw in one launch, with the same tiles
   int64_t dx_parts;     // floats of dx' parts in front of dw's, in one launch
@@ -85,9 +85,10 @@ void launch_loss_backward(const optorch_softmax_loss_t& a, const LossPlan& p);
 // The two products of a loss' gradient for a piece of the classes (k_loss_grad.hip)
 struct LossPiece {
   const void *ds, *w, *xs;         // operands, with the distances of their rows
-  int64_t ds_row; int ldw, ldxs;
+  int64_t ds_row, second;          // second: values from the first plane of ds to the second, or 0
+  int ldw, ldxs;
   int first, count;                // the piece's classes
-  int copies;                      // 2: rows of ds for the low parts behind its own, and of xs; or 1
+  int copies;                      // 2: the second plane of ds is rows behind the first one's, and xs has as many; or 1
   const void* info;                // a row's factor of dx: the fourth of four floats
   const float* scale;              // the factor of dw
   float* acc; float* parts;        // dx summed over the pieces; parts of a reduction
