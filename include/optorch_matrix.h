@@ -152,7 +152,7 @@ int optorch_softmax_loss_forward(const optorch_softmax_loss_t* a);
  *   dx = ds w,  dw = ds^T x,  dbias = column sums of ds.
  * p is made from the logits, made again, and the given lse.  In 16-bit precision ds, over its row's dloss, is held as two values of the storage
  * type for the two products, which keeps 16 (bf16) or 22 (fp16) of its bits, so that dx and dw are rounded once; dbias sums it
- * unrounded.  With rows = 0, dw and dbias are zero. */
+ * unrounded.  (fp16, dw: what a row's dloss is below 2^-11 of the largest one's is taken off its x, whose smallest step is 2^-24.)  With rows = 0, dw and dbias are zero. */
 int optorch_softmax_loss_backward(const optorch_softmax_loss_t* a);
 
 /* ---- orthogonalised updates ------------------------------------------------------------------------ */

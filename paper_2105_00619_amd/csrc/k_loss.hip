@@ -816,9 +816,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
 // ---- backward: what a row's values are multiplied by ----------------------------------------------------------------------
 // A row's dloss / temperature (times f = max(1, 1 + 2 z_loss lse), which keeps the rest within 2) is c m 2^e, c the largest of the rows', m
 // in (1/2, 1] and e <= 0.  ds is held as m (p (1 + 2 z_loss lse) - target) / f, and what is left is the factor of dx afterwards and of x in
-// dw, where a power of two costs no bits.  (All of it in ds would leave fp16's range, all of it in x round every value a second time: dw
-// of 4096 x 2048 -> 65536 with rows that weigh differently was 2.9e-3 off in bf16, so 2.3e-3.)  Where dloss is the same for all rows, a
-// mean's, m is 1, and the value that counts most, -1 at a label that the network does not know, is exact.
+// dw, where a power of two costs no bits in bf16 and fp32.  (All of it in x would round every value of x a second time.)  In fp16 x has few
+// steps below 1, and two planes of ds more than they need: values of 2^-38 keep eleven bits.  So the first 2^11 of a row's 2^e are ds', and x
+// begins to lose bits only in rows below that (values of 0.1: with 1e-5 of the largest row's dloss 1.1e-2 of what they add to dw, all of it in x,
+// so none).  Where dloss is the same for all rows, a mean's, m is 1, and the value that counts most, -1 at a label that the network does not know, is exact.
 // Up to 8192 rows one block (4 us for 4096 rows); more rows two launches of up to 256 blocks, the largest factors of the blocks first.
 struct Rows {
   const float *dloss, *lse, *flag;
@@ -826,6 +827,7 @@ struct Rows {
   int64_t rows;
   int classes;
   float z_loss, per_temperature;
+  int in_ds;                    // of a row's 2^e, the powers of two that ds takes
   float4* info; float* scale;
   float* largest; int blocks;   // of the blocks, or null and 1
 };
@@ -884,8 +886,9 @@ template <int THREADS> __device__ __forceinline__ void rows_of(const Rows& a, in
       frexpf(m, &e);  // |m| in [2^(e - 1), 2^e)
       if (fabsf(m) == ldexpf(0.5f, e)) --e;
       e = max(e, -120);
-      power = ldexpf(1.f, e);
-      m = ldexpf(m, -e);
+      const int held = min(-e, a.in_ds);
+      power = ldexpf(1.f, e + held);
+      m = ldexpf(m, -e - held);
     }
     a.info[r] = used ? make_float4(lse, wrong ? nan : p / f * m, wrong ? nan : m / f, c * power) : make_float4(0.f, 0.f, 0.f, 0.f);
   });
@@ -987,7 +990,7 @@ template <class S, class T, int PL> Logits begin(const optorch_softmax_loss_t& a
   }
   if (rows) {
     *rows = {a.dloss, a.lse, (const float*)(ws + p.off_flag), a.labels, a.rows, a.classes, a.labels ? a.z_loss : 0.f, l.per_temperature,
-             (float4*)(ws + p.off_info), (float*)(ws + p.off_scale), nullptr, 1};
+             a.precision == OPTORCH_FP16 ? 11 : 0, (float4*)(ws + p.off_info), (float*)(ws + p.off_scale), nullptr, 1};
     if (a.rows > ROWS_AT_ONCE) {
       rows->largest = rows->scale + 64;
       rows->blocks = (int)std::min<int64_t>((a.rows + ROWS_AT_ONCE - 1) / ROWS_AT_ONCE, ROW_BLOCKS);

@@ -69,3 +69,32 @@ def test_gradients_are_rounded_once(rows, cin, classes, name):
     got = B.distillation_backward(dloss, x, w, idx, t, lse, temperature=2.0)
     for what, g, (r, tol) in zip(("dx", "dw"), got, _gradients(ref, lse, dloss)):
         _within(g, r, tol, what)
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("rows", [40, 300])
+def test_classes_that_only_rows_of_small_factors_reach(rows, name):
+    """One row weighs 256, the others 1e-4 to 1e-5 of that, and its softmax is nothing but its own two classes: what the others' classes
+    get is as exact as if that row were not there.  fp16: the first 2^11 of a row's distance from the largest are ds', which has the bits to spare; beyond
+    that x is held smaller, whose smallest step is 2^-24."""
+    from paper_2105_00619_amd import binding as B
+    torch = _t()
+    dt = _dt(name)
+    x, w = _randn(rows, 72, seed=rows, scale=0.1), _randn(64, 72, seed=rows + 1, scale=0.3)
+    x[:, 71], x[0] = 0.0, 0.0
+    x[0, 71], w[:, 71], w[0, 71] = 1.0, 0.0, 60.0
+    x, w = x.to(dt), w.to(dt)
+    labels = (2 + torch.arange(rows, device="cuda") % 62).int()
+    labels[0] = 1
+    dloss = (256 * 10 ** (-4 - _rand(rows, seed=rows + 2))).float()
+    dloss[0] = 256.0
+    target, used = _entropy_target(labels, 64, 0.0)
+    ref = Reference(name, x, w, None, target, used)
+    lse = B.cross_entropy_forward(x, w, labels)[1]
+    got = B.cross_entropy_backward(dloss, x, w, labels, lse)
+    x_floor = 2.0 ** -25 * (256 / dloss.double() * 2.0 ** -11).clamp_min(1)[:, None] if name == "fp16" else 0.0
+    for what, g, (r, tol) in zip(("dx", "dw"), got, _gradients(ref, lse, dloss, 0.0 if name != "fp16" else x_floor)):
+        _within(g, r, tol, what)
+    # the norms too: of a correct rounding of the classes beyond the first two
+    dw = _mm((dloss.double()[:, None] * (torch.exp(ref.s - lse.double()[:, None]) - target)).T, ref.x)[2:]
+    assert float((got[1][2:].double() - dw).norm()) <= torch.finfo(dt).eps / 2 * float(dw.norm())
