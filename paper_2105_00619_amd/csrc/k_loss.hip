@@ -73,11 +73,11 @@ __device__ __forceinline__ void halves(float v, float& a, float& b) {
 __device__ __forceinline__ float halves_max(float v) { float a, b; halves(v, a, b); return fmaxf(a, b); }
 __device__ __forceinline__ float halves_sum(float v) { float a, b; halves(v, a, b); return a + b; }
 
-// exp(k' (v - from)), k = k' log2(e).  16 bits: one multiply-add, and what counts as `from` is k from as rounded, a power of two's exponent: the
-// rows' sums are kept beside that and joined with it.
-template <bool FULL> __device__ __forceinline__ float exp_above(float v, float from, float k) {
-  return __builtin_amdgcn_exp2f(FULL ? (v - from) * k : __fmaf_rn(v, k, -from * k));
-}
+// In 16 bits exp(k' (v - from)) is one multiply-add, 2^(k v - r), r = k from as rounded, k = k' log2(e): off by a factor that is the same for all v
+// and is made up for.  That goes where rounding k from costs 2^-13 at most.  (A mask's logits, of 1e10 or a type's lowest value, are beyond: rounding
+// k from alone would make exp of them 2^100, or k from infinite.)  Farther ones have `from` taken off first, a row of them beside others that stay as
+// they are: a row's bits are its own.
+__device__ __forceinline__ bool far_off(float exponent) { return !(fabsf(exponent) <= 4096.f); }
 
 // An accumulator's value.  256 x 256 tiles have all of their accumulation registers full: as an ordinary copy the compiler moves them out at
 // once where the block's paths part, and spills.  It does not see into the instruction, so what lies between a tile's last MFMA and
@@ -216,29 +216,41 @@ logits_kernel(Logits a) {
       // (nothing but -infinity: a sum of zero; an infinity: an infinite sum, above the largest finite maximum)
       const bool infinite = most == __builtin_inff();
       const float above = infinite || most == -__builtin_inff() ? 0.f : most;
+      const bool far = FULL || far_off(above * k);
+      const float from = far ? above : 0.f, r2 = far ? 0.f : above * k;
+      if (FULL || __any(far)) {
+#pragma unroll
+        for (int n = 0; n < NV; ++n) v[n] -= from;
+      }
       float sum = 0.f, sum2 = 0.f;
 #pragma unroll
       for (int n = 0; n < NV; n += 2) {
-        sum += exp_above<FULL>(v[n], above, k);
-        sum2 += exp_above<FULL>(v[n + 1], above, k);
+        sum += __builtin_amdgcn_exp2f(FULL ? v[n] * k : __fmaf_rn(v[n], k, -r2));
+        sum2 += __builtin_amdgcn_exp2f(FULL ? v[n + 1] * k : __fmaf_rn(v[n + 1], k, -r2));
       }
-      sum = halves_sum(sum + sum2);
+      sum += sum2;
+      if (!FULL) sum *= __builtin_amdgcn_exp2f(__fmaf_rn(from - above, k, r2));
+      sum = halves_sum(sum);
       if (a.totals) all = halves_sum(all) * a.per_temperature;
       if (!half && real) {
         const int64_t at = (int64_t)column * a.M + row;
-        a.sums[at] = make_float2(infinite ? 3.4028235e38f : most * (FULL ? a.per_temperature : k), sum);
+        a.sums[at] = make_float2(infinite ? 3.4028235e38f : most * a.per_temperature, sum);
         if (a.totals) a.totals[at] = all;
       }
     } else {
       // (16 bits: what rounding lse log2(e) leaves goes into the row's factor of p)
-      const float lse = FULL ? info[j].x : info[j].x * LOG2E, spread = a.spread * info[j].z;
-      const float factor_p = FULL ? info[j].y : info[j].y * __fmaf_rn(__fmaf_rn(info[j].x, LOG2E, -lse), -0.69314718f, 1.f);
+      const float lse = info[j].x, lse2 = lse * LOG2E, spread = a.spread * info[j].z;
       const bool used = real && info[j].z != 0.f;
+      const bool far = FULL || far_off(lse2);
+      const float kp = far ? LOG2E : k, r2 = far ? 0.f : lse2;
+      const float factor_p = far ? info[j].y : info[j].y * __fmaf_rn(__fmaf_rn(lse, LOG2E, -lse2), -0.69314718f, 1.f);
+      if (FULL || __any(far)) {
 #pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        const float p = __builtin_amdgcn_exp2f(FULL ? (v[n] * a.per_temperature - lse) * LOG2E : __fmaf_rn(v[n], k, -lse));
-        v[n] = __fmaf_rn(p, factor_p, -spread);
+        for (int n = 0; n < NV; ++n) v[n] = far ? v[n] * a.per_temperature - lse : v[n];
       }
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+        v[n] = __fmaf_rn(__builtin_amdgcn_exp2f(FULL ? v[n] * kp : __fmaf_rn(v[n], kp, -r2)), factor_p, -spread);
       if (inside < W) {
 #pragma unroll
         for (int n = 0; n < NV; ++n) v[n] = class_of(n) < inside ? v[n] : 0.f;
@@ -451,7 +463,7 @@ __global__ void __launch_bounds__(1024) few_logits_kernel(Logits a, int k_wave) 
   const float above = infinite || most == -__builtin_inff() ? 0.f : most;
   float sum = 0.f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) sum += exp_above<true>(v[e], above, LOG2E);
+  for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((v[e] - above) * LOG2E);
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
   all += __shfl_xor(all, 16);
@@ -713,7 +725,6 @@ __global__ void __launch_bounds__(N < 256 ? 256 : N) teacher_kernel(Teacher a) {
 // ---- forward: a row's sums joined --------------------------------------------------------------------------------------
 struct Join {
   const float2* sums; const float* totals; const float* picked;
-  bool exponents;                  // the maxima are exponents of two
   int64_t rows;
   int columns, runs, log_rows;     // of the table of a teacher's entries, of the sums; a block's rows: 1 << log_rows
   const int32_t* labels; int classes;
@@ -730,11 +741,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
   const int rows = 1 << a.log_rows, rl = threadIdx.x & (rows - 1), slot = threadIdx.x >> a.log_rows, slots = JOIN_THREADS >> a.log_rows;
   const int64_t wanted = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * rows + rl, row = min(wanted, a.rows - 1);
   float most = -__builtin_inff(), sum = 0.f, extra = 0.f;
-  const float unit = a.exponents ? 1.f : LOG2E;
   auto join = [&](float& m, float& l, float m2, float l2) {
     // (a maximum that is NaN has a sum that is; one of -infinity a sum of zero)
     const float top = fmaxf(m, m2);
-    if (top != -__builtin_inff()) l = l * __builtin_amdgcn_exp2f((m - top) * unit) + l2 * __builtin_amdgcn_exp2f((m2 - top) * unit);
+    if (top != -__builtin_inff()) l = l * __builtin_amdgcn_exp2f((m - top) * LOG2E) + l2 * __builtin_amdgcn_exp2f((m2 - top) * LOG2E);
     else l += l2;
     m = top;
   };
@@ -795,8 +805,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
     }
   }
   if (slot || wanted >= a.rows) return;
-  // (an exponent of two: one product in 64 bits, so that log(2) is not rounded a second time, and -infinity stays what it is)
-  const float lse = a.exponents ? (float)((double)(all.x + log2f(all.y)) * 0.6931471805599453) : all.x + logf(all.y);
+  const float lse = all.x + logf(all.y);
   float loss;
   if (teacher) {
     const float flag = a.flag[row];
@@ -1041,7 +1050,6 @@ template <class S, class T, int PL> void forward_of(const optorch_softmax_loss_t
     each_piece<S, T, PL>(a, p, l, [&] { run_logits<S, T, false>(st, l, p.wave); });
   }
   Join j = {};
-  j.exponents = PL == 1 && !p.few && !p.stream;
   j.sums = l.sums; j.totals = l.totals; j.picked = l.picked;
   j.rows = a.rows; j.columns = p.columns; j.runs = p.stream ? p.stream : p.columns;
   // (few rows: a block each)
