@@ -811,12 +811,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
     const float flag = a.flag[row];
     loss = flag == 0.f ? 0.f : flag != flag ? flag : part[rl].x + lse * part[rl].y;
   } else {
+    // (terms of a factor of zero are none: a logit or lse that is infinite would make NaN of them)
     const int y = a.labels[row];
-    loss = lse;
-    if (y >= a.classes) loss = __builtin_nanf("");
-    else if (y >= 0) loss = lse - (1.f - a.smoothing) * a.picked[row] + a.z_loss * lse * lse;
-    else loss = 0.f;
-    if (a.totals && y >= 0) loss -= a.smoothing * (total / (float)a.classes);
+    loss = y < 0 ? 0.f : y >= a.classes ? __builtin_nanf("") : lse;
+    if (y >= 0 && y < a.classes) {
+      if (a.smoothing < 1.f) loss -= (1.f - a.smoothing) * a.picked[row];
+      if (a.z_loss > 0.f) loss += a.z_loss * lse * lse;
+      if (a.totals) loss -= a.smoothing * (total / (float)a.classes);
+    }
   }
   a.loss[row] = loss;
   a.lse[row] = lse;
