@@ -630,8 +630,8 @@ int stream_blocks(int64_t rows, int classes, int k) {
 }
 
 // ---- a teacher's entries -----------------------------------------------------------------------------------------------
-// Those of a row in order of their classes (then of their places), entries of one class added up in the first of them; softmax of their logits;
-// where the entries of each run of `width` classes begin.  Threads N a row, N a power of two of at least `top`.
+// Those of a row in order of their classes (then of their places), entries of one class added up in the first of them; softmax of their logits, whose
+// distance from the row's largest is what is divided by the temperature: the logits themselves may be a type's lowest and largest values; where the entries of each run of `width` classes begin.  Threads N a row, N a power of two of at least `top`.
 struct Teacher {
   const int32_t* indices; int64_t ldi;
   const void* logits; int64_t ldt;
@@ -671,17 +671,17 @@ __global__ void __launch_bounds__(N < 256 ? 256 : N) teacher_kernel(Teacher a) {
   float v = -__builtin_inff();
   if (t < a.top) {
     c = a.indices[row * a.ldi + t];
-    if (c >= 0) v = to_f32(((const S*)a.logits)[row * a.ldt + t]) * a.per_temperature;
+    if (c >= 0) v = to_f32(((const S*)a.logits)[row * a.ldt + t]);
   }
   const bool valid = c >= 0 && v != -__builtin_inff(), wrong = valid && (c >= a.classes || !(fabsf(v) <= 3.4028235e38f));
   if (!valid) v = -__builtin_inff();
   auto most_of = [](float p, float q) { return fmaxf(p, q); };
   auto sum_of = [](float p, float q) { return p + q; };
   const float most = over_row<N>(v, values[r], t, most_of);
-  const float e = valid ? __builtin_amdgcn_exp2f((v - most) * LOG2E) : 0.f;
+  const float d = (v - most) * a.per_temperature, e = valid ? __builtin_amdgcn_exp2f(d * LOG2E) : 0.f;
   const float sum = over_row<N>(e, values[r], t, sum_of);
   const float any_wrong = over_row<N>(wrong ? 1.f : 0.f, values[r], t, most_of);
-  const float log_q = v - most - logf(sum);
+  const float log_q = d - logf(sum);
   uint32_t key = valid && !wrong ? (uint32_t)c << 10 | t : 0xffffffffu;
   // bitonic: pairs of keys at a distance of `o` in runs of `run`
 #pragma unroll
