@@ -102,6 +102,9 @@ template <bool SHORT, class T> __device__ __forceinline__ void put(T* row, const
   }
 }
 
+// (a NaN stays one, which fmaxf makes a zero of: rstd of a row that is not finite)
+__device__ __forceinline__ float not_below_zero(float v) { return v < 0.f ? 0.f : v; }
+
 template <int N> __device__ __forceinline__ void vector_of(const float* p, int c, int n, float other, float (&v)[N]) {
   if (p) load8<float>(p + c, n, v);
 #pragma unroll
@@ -167,7 +170,7 @@ __global__ void __launch_bounds__(MAX) norm_forward_kernel(NormForward a) {
       }
     }
     row_sums<G, MAX>(sum, square, lds, 1);
-    const float off = sum * n, rstd = 1.f / sqrtf(fmaxf(square * n - off * off, 0.f) + a.eps);
+    const float off = sum * n, rstd = 1.f / sqrtf(not_below_zero(square * n - off * off) + a.eps);
     const int64_t row = first + r;
     if (row >= a.rows) continue;
     if (t == 0 && a.mean) { a.mean[row] = mean + off; a.rstd[row] = rstd; }
@@ -211,7 +214,7 @@ __global__ void __launch_bounds__(1024) norm_forward_long_kernel(NormForward a) 
     }
   });
   row_sums<0, 1024>(sum, square, lds, 1);
-  const float off = sum * n, rstd = 1.f / sqrtf(fmaxf(square * n - off * off, 0.f) + a.eps);
+  const float off = sum * n, rstd = 1.f / sqrtf(not_below_zero(square * n - off * off) + a.eps);
   if (threadIdx.x == 0 && a.mean) { a.mean[row] = first + off; a.rstd[row] = rstd; }
   each8([&](int c, int k, float (&v)[8]) {
     float w[8], b[8];
