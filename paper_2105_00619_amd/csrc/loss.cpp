@@ -116,4 +116,10 @@ void loss_shape(const optorch_softmax_loss_t* a, bool backward, int32_t out[4]) 
   out[2] = 2000 * p.dx.wave + p.dx.parts;
   out[3] = 2000 * p.dw.wave + p.dw.parts;
 }
+// ... and which kernel makes the forward pass' logits: 0 tiles, 1 weights straight from memory, otherwise the blocks that stream them
+int32_t loss_path(const optorch_softmax_loss_t* a);
+int32_t loss_path(const optorch_softmax_loss_t* a) {
+  const LossPlan p = plan_loss(*a, false);
+  return p.few ? 1 : p.stream;
+}
 }  // namespace oseq
