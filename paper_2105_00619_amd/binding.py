@@ -837,7 +837,7 @@ def _teacher(a, x, indices, teacher, temperature):
             a.rows, tuple(indices.shape), tuple(teacher.shape)))
     if a.rows and indices.shape[1] > 1 and (indices.stride(1) != 1 or teacher.stride(1) != 1):
         raise ValueError("indices and teacher: the elements of a row must lie next to each other")
-    a.teacher_precision, a.top, a.temperature = _precision(teacher.dtype), indices.shape[1], temperature
+    a.teacher_precision, a.top, a.temperature = _precision(teacher.dtype), _int32("top", indices.shape[1]), temperature
     a.indices, a.ldi, a.teacher, a.ldt = indices.data_ptr(), _ld(indices), teacher.data_ptr(), _ld(teacher)
 
 
