@@ -428,15 +428,6 @@ struct Tile {
     });
   }
 
-  // 32 rows of a wavefront's sums to its part of LDS
-  __device__ static __forceinline__ void put_rows(float* area, const v16f (&acc)[MI], int lane) {
-#pragma unroll
-    for (int j = 0; j < MI; ++j)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) area[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * EPITCH + j * 32 + (lane & 31)] = acc[j][e];
-    asm volatile("" ::: "memory");
-  }
-
  private:
   // Sums times BETWEEN, each where it lies.  (As ordinary multiplications the compiler moves all of a 256 x 256 tile's out of the
   // accumulation registers at once and spills, in the loop too.)  It does not see into the block, so what an MFMA and a use of its result
@@ -449,6 +440,14 @@ struct Tile {
       acc[n / 16 / MI][n / 16 % MI][n % 16] = x;
     });
     asm volatile("s_nop 7");
+  }
+  // 32 rows of a wavefront's sums to its part of LDS
+  __device__ static __forceinline__ void put_rows(float* area, const v16f (&acc)[MI], int lane) {
+#pragma unroll
+    for (int j = 0; j < MI; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) area[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * EPITCH + j * 32 + (lane & 31)] = acc[j][e];
+    asm volatile("" ::: "memory");
   }
 };
 
