@@ -97,7 +97,7 @@ typedef struct {
 int64_t optorch_layer_norm_workspace(const optorch_layer_norm_t* a);
 
 /* mean and variance of every row (over its cols values), rstd = 1 / sqrt(variance + eps), y = (x - mean) rstd weight + bias.
- * The squares of a row's deviations have to stay in fp32's range. */
+ * A row's sum and the squares of its deviations have to stay in fp32's range; mean, rstd and y of a row with a NaN or an infinity are not finite. */
 int optorch_layer_norm_forward(const optorch_layer_norm_t* a);
 
 /* With h = (x - mean) rstd and u = dy weight, means over a row:

@@ -4,7 +4,7 @@
 // columns, the sum of their exponentials above it and the targets' logits, which a second kernel joins; backward it turns them into ds, in
 // planes of the storage type (two of 16 bits) and for a piece of the classes at a time, which the gradients' products read (k_loss_grad.hip).  What a row's target is at some of its
 // columns is put into the tile on its way through LDS, where the row's values lie side by side.
-// Large calls are bound by the matrix cores: 8192 x 4096 -> 128000 in bf16 6.26 ms forward (1370 TFLOP/s, matrix cores busy 75 % of the kernel) and
+// Large calls are bound by the matrix cores: 8192 x 4096 -> 128000 in bf16 6.33 ms forward (1360 TFLOP/s, matrix cores busy 75 % of the kernel) and
 // 35.3 ms backward (five such products, two each for dx and dw, 1220 TFLOP/s); few rows by memory (the weights at 4.8 TB/s), small calls by their launches.
 #include "mat_layout.h"
 #include "parts.h"
@@ -501,7 +501,7 @@ template <class S, class T> void run_few(hipStream_t st, const Logits& l) {
 // Up to 16 rows of aligned 16-bit operands: the weights are what is read, 16 classes at a time by all wavefronts of a block, 512 values of k
 // each, and the next 16 classes on their way; the rows of x stay in registers as operands.  A block walks its groups of classes, a wavefront in turn
 // adds up a group's sums and goes on with the rows' maxima and sums of exponentials: one of each row for every block.
-// 16 x 2048 -> 65536, 268 MB that no cache holds: 56 us and 5 for the join (4.8 TB/s), 73 as tiles of 128 x 128.
+// 16 x 2048 -> 65536, ten such matrices of 268 MB in turn, which no cache holds: 55 us and 5 for the join (4.8 TB/s); a call 62, as tiles 73.
 struct Stream { Logits l; int groups; };
 constexpr int STREAM_ROWS = 16, KS = 16;  // (32 rows of 256 values of k: 80 us, as tiles 72)
 template <class T, bool TOP>
@@ -620,9 +620,11 @@ template <class T> void run_stream(hipStream_t st, const Logits& l, int blocks) 
   if (l.labels) OSEQ_LAUNCH((stream_logits_kernel<T, false>), dim3(blocks), dim3(waves * 64), lds, st, s);
   else OSEQ_LAUNCH((stream_logits_kernel<T, true>), dim3(blocks), dim3(waves * 64), lds, st, s);
 }
-// Blocks of the kernel above, eight wavefronts on a CU, or 0 where tiles are taken: rows of little less than 2048 or 4096 values.  16 rows, us
-// so / as tiles: 2048 -> 1000 13 / 16, -> 32000 38 / 39, -> 128000 105 / 127; 4096 -> 32000 60 / 64, -> 65536 106 / 127, -> 128000 194 / 179; but
-// 3000 -> 30000 56 / 44, 1024 -> 32000 25 / 20, 256 -> 50000 20 / 16.
+// Blocks of the kernel above, eight wavefronts on a CU, or 0 where tiles are taken: rows of little less than 2048 or 4096 values.  A call of 16 rows, the
+// weights in no cache, us so / as tiles: 2048 -> 1000 13 / 20, -> 32000 39 / 39, -> 65536 62 / 73, -> 96000 84 / 88, -> 128000 107 / 104, -> 160000 128 / 154; 4096 -> 1000
+// 20 / 32, -> 32000 63 / 67, -> 65536 108 / 128, -> 96000 154 / 151, -> 128000 199 / 190, -> 160000 245 / 249: tiles are ahead by 5 % where they fill the card evenly.
+// (Weights that the last-level cache still has, 2048 -> 32000: 37 / 27.)  Other widths leave wavefronts without work: 3000 -> 30000 56 / 44, 1024 -> 32000 25 / 20,
+// 256 -> 50000 20 / 16.
 int stream_blocks(int64_t rows, int classes, int k) {
   const int waves = ceil_div(k, 32 * KS);
   const bool suits = rows <= STREAM_ROWS && (waves == 4 || waves == 8) && k * 10 >= waves * 32 * KS * 9;
@@ -831,7 +833,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) loss_join_kernel(Join a) {
 // steps below 1, and two planes of ds more than they need: values of 2^-38 keep eleven bits.  So the first 2^11 of a row's 2^e are ds', and x
 // begins to lose bits only in rows below that (values of 0.1: with 1e-5 of the largest row's dloss 1.1e-2 of what they add to dw, all of it in x,
 // so none).  Where dloss is the same for all rows, a mean's, m is 1, and the value that counts most, -1 at a label that the network does not know, is exact.
-// Up to 8192 rows one block (4 us for 4096 rows); more rows two launches of up to 256 blocks, the largest factors of the blocks first.
+// Up to 8192 rows one block (7 us for 4096 rows, 14 for 8192; two launches take a call of 2048 to 8192 rows 1.5 us longer); more rows two launches of
+// up to 256 blocks, the largest factors of the blocks first.
 struct Rows {
   const float *dloss, *lse, *flag;
   const int32_t* labels;
